@@ -484,6 +484,140 @@ int psd_table_body(void* user, const int32_t* tokens, const int32_t* mask, int32
                    void* hidden_bf16, void* cuda_stream);
 
 /*
+ * ---- Around the step: attention of the drafts, upkeep of the prefix's cache, confidences from logits ----
+ *
+ * The verification pass runs the body on B*D drafts that differ only in their active block: the D drafts
+ * of a sequence share its prefix (prompt and finished blocks), whose keys and values are cached once per
+ * sequence.  (Sec. 3.2 Stage 3: the prefix's cache can be shared by the drafts.)  A NODE is one draft of
+ * one sequence, n = b*D + d; a token of the batch is t = n*M + i.  Query heads h share key head
+ * h / (Hq / Hkv).  With M = 1 the same calls serve token-by-token decoding of B*D continuations.
+ */
+#define PSD_BF16 0
+#define PSD_FP16 1
+#define PSD_FP32 2 /* psd_confidence_logits only */
+
+/* Element strides of a cache [outer, token, head, Dh]; the innermost stride is 1. */
+typedef struct psd_kv_strides_t {
+    int64_t outer; /* sequence (prefix cache) or node (a draft's own keys); 0 shares one among all */
+    int64_t token; /* > 0 */
+    int64_t head;  /* 0 shares one among all heads */
+} psd_kv_strides_t;
+
+/* Shapes of psd_draft_attention and psd_prefix_weights (which reads the fields marked *). */
+typedef struct psd_attention_t {
+    int32_t B, D, M;     /* * sequences, drafts per sequence, query tokens per draft; all >= 1               */
+    int32_t Hq, Hkv, Dh; /* * heads, key heads (Hq a multiple of Hkv, Hq/Hkv <= 128), 8 <= Dh <= 128, Dh % 8 == 0 */
+    int32_t P;           /* * token capacity of the prefix cache, >= 0                                        */
+    int32_t S;           /* capacity of a draft's own keys, >= 0                                              */
+    int32_t dtype;       /* * PSD_BF16 or PSD_FP16: q, caches and out                                         */
+    int32_t causal;      /* own keys: 0 every row sees all own_len keys of its node; 1 query i sees own key s
+                            iff s <= own_len - M + i (its node's last M own keys are the queries' own)      */
+    float scale;         /* * > 0, finite                                                                     */
+    int32_t reserved;    /* 0 */
+    int64_t q_token, q_head;     /* * element strides of q [B*D*M, Hq, Dh]                                    */
+    int64_t out_token, out_head; /* element strides of out                                                    */
+    psd_kv_strides_t kp, vp;     /* * (kp) prefix caches [B, P, Hkv, Dh]                                      */
+    psd_kv_strides_t ko, vo;     /* own keys and values [B*D, S, Hkv, Dh]                                     */
+} psd_attention_t;
+
+/* Bytes of scratch psd_draft_attention needs (0 = bad sizes; the smallest value for good ones is 256). */
+size_t psd_attention_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P,
+                                     int32_t S);
+
+/*
+ * psd_draft_attention — attention of all drafts' tokens over the shared prefix, read once for all of a
+ * sequence's drafts, and over each draft's own keys.
+ * For token t = (b, d, i) and head h, over the keys K_j = prefix keys j < prefix_len[b] of sequence b and
+ * own keys of node (b, d) that `causal` lets it see:
+ *   s_j = scale * q[t,h] . K_j,   lse[t,h] = ln sum_j exp(s_j),   out[t,h] = sum_j exp(s_j - lse) V_j.
+ * A row without keys gives out = 0 and lse = -inf.  Scores, softmax statistics and sums are fp32, the
+ * weights are rounded to the inputs' type before they multiply V, out is rounded once at the end.
+ *   prefix_len [B] int32, device, or NULL for P everywhere;  own_len [B*D] int32, device, or NULL for S;
+ *   values outside [0, P] ([0, S]) are clamped.  What lies past a length is never used, whatever it holds, and
+ *   a draft's outputs never depend on another draft's keys.  P = 0 (S = 0): the pointers may be NULL.
+ *   q, k_*, v_*, out 16-byte aligned, their strides multiples of 8 elements (PSD_ERR_ALIGN otherwise)
+ *   lse [B*D*M, Hq] fp32 or NULL;  workspace 256-byte aligned, >= psd_attention_workspace_bytes
+ *   status_dev NULL, or the status word (PSD_ERR_TIMEOUT: outputs invalid)
+ */
+int psd_draft_attention(const void* q, const void* k_prefix, const void* v_prefix, const int32_t* prefix_len,
+                        const void* k_own, const void* v_own, const int32_t* own_len, const psd_attention_t* a,
+                        void* out, float* lse, void* workspace, size_t workspace_bytes, int32_t* status_dev,
+                        void* cuda_stream);
+
+/* Bytes of scratch psd_prefix_weights needs (0 = bad sizes). */
+size_t psd_weights_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P);
+
+/*
+ * psd_prefix_weights — the attention weight that every prefix key has drawn, summed over the rows that read it:
+ *   acc_out[b,h,j] = beta * acc_in[b,h,j] + sum over t of sequence b and heads g of key head h of
+ *                    exp(scale * q[t,g] . K_j - lse[t,g])          for j < prefix_len[b],  0 for j >= prefix_len[b].
+ * lse [B*D*M, Hq] fp32 is psd_draft_attention's (a row with lse = -inf, which saw no keys, adds nothing).
+ *   acc_in, acc_out [B, Hkv, P] fp32; acc_in NULL counts as 0 and may be acc_out itself.  P >= 1.
+ * The sum's order is fixed: equal inputs give equal bits.  Other arguments as for psd_draft_attention.
+ */
+int psd_prefix_weights(const void* q, const void* k_prefix, const int32_t* prefix_len, const float* lse,
+                       const psd_attention_t* a, float beta, const float* acc_in, float* acc_out, void* workspace,
+                       size_t workspace_bytes, int32_t* status_dev, void* cuda_stream);
+
+/* Shapes of psd_prefix_evict. */
+typedef struct psd_evict_t {
+    int32_t B, Hkv, Dh;       /* as above                                                                    */
+    int32_t P;                /* capacity of the cache, >= 1                                                 */
+    int32_t keep;             /* keys to keep per sequence and key head, >= 1                                 */
+    int32_t n_sink, n_recent; /* always keep the first n_sink and the last n_recent; both >= 0, sum <= keep   */
+    int32_t dtype;            /* PSD_BF16 or PSD_FP16 */
+    psd_kv_strides_t k, v;    /* [B, P, Hkv, Dh] */
+    psd_kv_strides_t k_out, v_out; /* [B, keep, Hkv, Dh], not overlapping k and v; no stride 0 */
+} psd_evict_t;
+
+/*
+ * psd_prefix_evict — cuts the cache to `keep` keys per sequence and key head: the first n_sink, the last n_recent and,
+ * of the others, those with the highest score (equal scores: lower position first; NaN below every number), packed
+ * in order of position.
+ *   scores [B, Hkv, P] fp32 (psd_prefix_weights' acc_out);  prefix_len as above
+ *   index      [B, Hkv, keep] int32 out: kept positions ascending, then -1
+ *   scores_out [B, Hkv, keep] fp32 out or NULL: their scores, then 0;  len_out [B] int32 out or NULL: min(prefix_len, keep)
+ *   k_out, v_out: kept keys and values; slots past len_out are left untouched.
+ */
+int psd_prefix_evict(const float* scores, const void* k, const void* v, const int32_t* prefix_len, const psd_evict_t* e,
+                     void* k_out, void* v_out, int32_t* index, float* scores_out, int32_t* len_out, void* cuda_stream);
+
+/* Edits of psd_confidence_logits; pointers are device pointers, each may be NULL (that edit is then not made). */
+typedef struct psd_logits_edit_t {
+    const int32_t* history;      /* [B, history_cap] tokens of the text so far; ids outside [0, V) are ignored     */
+    const int32_t* history_len;  /* [B], clamped to [0, history_cap]; NULL = history_cap                           */
+    const int32_t* draft_tokens; /* [B*D, M] tokens of the drafts: where draft_mask is 0 they count as text of      */
+    const int32_t* draft_mask;   /* [B*D, M] their own draft (both or neither)                                    */
+    const float* bias;           /* [bias_rows, V] fp32                                                           */
+    const uint32_t* allow;       /* [allow_rows, ceil(V/32)]: bit v%32 of word v/32 set = token v may be chosen     */
+    int32_t history_cap;         /* >= 0 */
+    int32_t bias_rows;           /* divides B*D*M: row r uses bias row r / (B*D*M / bias_rows)                      */
+    int32_t allow_rows;          /* likewise                                                                       */
+    float repetition;            /* > 0, finite; 1 = none */
+    float presence, frequency;   /* finite; 0 = none */
+    int32_t reserved;            /* 0 */
+} psd_logits_edit_t;
+
+/* Bytes of scratch psd_confidence_logits needs (0 = bad sizes). */
+size_t psd_logits_workspace_bytes(int32_t n_rows, int32_t V);
+
+/*
+ * psd_confidence_logits — psd_confidence for bodies that hand out logits, with penalties for repeated tokens, biases
+ * and grammar masks.  For row r = (b, d, i) and token v with c = how often v occurs in the text of (b, d), in fp32, each
+ * operation rounded on its own:
+ *   c > 0:  x = l > 0 ? l / repetition : l * repetition;  x = x - (frequency * c + presence);   else x = l
+ *   x = x + bias;   tokens whose allow bit is 0 drop out, whatever their logit holds.
+ * out_token, out_conf, out_lse are those of psd_confidence over x.  A row in which no token is left (or all that are left
+ * have x = -inf) gives token -1, confidence 0 and lse -inf; it is not counted as non-finite, and its token must not be
+ * committed.  A NaN or +inf among the tokens left gives confidence NaN and is counted in status_dev.
+ *   logits [B*D*M, V] bf16, fp16 or fp32 (dtype), rows row_stride >= V elements apart, aligned to their element
+ *   edit: HOST pointer, NULL = no edits;  workspace >= psd_logits_workspace_bytes(B*D*M, V), 256-byte aligned
+ */
+int psd_confidence_logits(const void* logits, int32_t dtype, int64_t row_stride, int32_t B, int32_t D, int32_t M, int32_t V,
+                          const psd_logits_edit_t* edit, int32_t* out_token, float* out_conf, float* out_lse,
+                          void* workspace, size_t workspace_bytes, int32_t* status_dev, void* cuda_stream);
+
+/*
  * Which kernel psd_confidence uses.  Process-wide; returns the previous value, or PSD_ERR_SHAPE for
  * an unknown value.
  *   0  (default) the tcgen05/TMA kernels, chosen by size: pairs of CTAs on one tile of 256 rows

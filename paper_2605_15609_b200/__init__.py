@@ -13,6 +13,8 @@ from .binding import (ACCEPT_AGREE_AND_CONF, ACCEPT_AGREE_AND_POLICY, ACCEPT_AGR
                       psd_step_host_bytes, psd_step_host_block, host_step_buffers, psd_verify_accept, psd_workspace_bytes, status_string, psd_decode_blocks, psd_decode_scratch_bytes,
                       table_body_address, table_body_user, psd_table_body, PsdDag, psd_dag_init,
                       psd_build_drafts_dag, psd_verify_accept_dag, psd_step_dag, PsdDecodeStats, PsdTableBody, ORDER_TWO_PASSES,
-                      ORDER_ONE_PASS)
+                      ORDER_ONE_PASS, PSD_BF16, PSD_FP16, PSD_FP32, PsdAttention, PsdEvict, PsdKvStrides, PsdLogitsEdit,
+                      psd_attention_workspace_bytes, psd_draft_attention, psd_weights_workspace_bytes, psd_prefix_weights,
+                      psd_prefix_evict, psd_logits_workspace_bytes, psd_confidence_logits)
 
 __all__ = [n for n in dir() if not n.startswith("_")]

@@ -53,6 +53,32 @@ class PsdTableBody(ctypes.Structure):
     _fields_ = [("table_bf16", _vp), ("B", _i32), ("H", _i32)]
 
 
+class PsdKvStrides(ctypes.Structure):
+    """psd_kv_strides_t"""
+    _fields_ = [("outer", _i64), ("token", _i64), ("head", _i64)]
+
+
+class PsdAttention(ctypes.Structure):
+    """psd_attention_t"""
+    _fields_ = [*[(n, _i32) for n in ("B", "D", "M", "Hq", "Hkv", "Dh", "P", "S", "dtype", "causal")],
+                ("scale", _f32), ("reserved", _i32),
+                *[(n, _i64) for n in ("q_token", "q_head", "out_token", "out_head")],
+                *[(n, PsdKvStrides) for n in ("kp", "vp", "ko", "vo")]]
+
+
+class PsdEvict(ctypes.Structure):
+    """psd_evict_t"""
+    _fields_ = [*[(n, _i32) for n in ("B", "Hkv", "Dh", "P", "keep", "n_sink", "n_recent", "dtype")],
+                *[(n, PsdKvStrides) for n in ("k", "v", "k_out", "v_out")]]
+
+
+class PsdLogitsEdit(ctypes.Structure):
+    """psd_logits_edit_t"""
+    _fields_ = [*[(n, _vp) for n in ("history", "history_len", "draft_tokens", "draft_mask", "bias", "allow")],
+                *[(n, _i32) for n in ("history_cap", "bias_rows", "allow_rows")],
+                *[(n, _f32) for n in ("repetition", "presence", "frequency")], ("reserved", _i32)]
+
+
 # psd_body_fn
 BODY_FN = ctypes.CFUNCTYPE(ctypes.c_int, _vp, _vp, _vp, _i32, _i32, _vp, _vp)
 ORDER_TWO_PASSES, ORDER_ONE_PASS = 0, 1
@@ -123,6 +149,23 @@ def _load() -> ctypes.CDLL:
                                       _vp, _sz, _vp, _sz, _vp, _vp, _vp, _vp, ctypes.POINTER(PsdDecodeStats), _vp]
     lib.psd_table_body.restype = ctypes.c_int
     lib.psd_table_body.argtypes = [_vp, _vp, _vp, _i32, _i32, _vp, _vp]
+    lib.psd_attention_workspace_bytes.restype = _sz
+    lib.psd_attention_workspace_bytes.argtypes = [_i32] * 8
+    lib.psd_draft_attention.restype = ctypes.c_int
+    lib.psd_draft_attention.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.POINTER(PsdAttention), _vp, _vp, _vp,
+                                        _sz, _vp, _vp]
+    lib.psd_weights_workspace_bytes.restype = _sz
+    lib.psd_weights_workspace_bytes.argtypes = [_i32] * 7
+    lib.psd_prefix_weights.restype = ctypes.c_int
+    lib.psd_prefix_weights.argtypes = [_vp, _vp, _vp, _vp, ctypes.POINTER(PsdAttention), _f32, _vp, _vp, _vp, _sz, _vp,
+                                       _vp]
+    lib.psd_prefix_evict.restype = ctypes.c_int
+    lib.psd_prefix_evict.argtypes = [_vp, _vp, _vp, _vp, ctypes.POINTER(PsdEvict), _vp, _vp, _vp, _vp, _vp, _vp]
+    lib.psd_logits_workspace_bytes.restype = _sz
+    lib.psd_logits_workspace_bytes.argtypes = [_i32, _i32]
+    lib.psd_confidence_logits.restype = ctypes.c_int
+    lib.psd_confidence_logits.argtypes = [_vp, _i32, _i64, _i32, _i32, _i32, _i32, ctypes.POINTER(PsdLogitsEdit), _vp,
+                                          _vp, _vp, _vp, _sz, _vp, _vp]
     lib.psd_set_confidence_impl.restype = ctypes.c_int
     lib.psd_set_confidence_impl.argtypes = [ctypes.c_int]
     lib.psd_set_tuning.restype = ctypes.c_int
@@ -478,3 +521,163 @@ def psd_verify_accept_dag(tokV, confV, sigma, draft_tokens, draft_mask, p: PsdPo
     _check(LIB.psd_verify_accept_dag(_ptr(tokV), _ptr(confV), _ptr(sigma), _ptr(draft_tokens), _ptr(draft_mask), B, M,
                                      p, ctypes.byref(g), _ptr(tokens), _ptr(mask), _ptr(k_star), _ptr(n_spec_accepted),
                                      _ptr(n_committed), _ptr(accepted), _stream(stream)), "psd_verify_accept_dag")
+
+
+# ---- around the step: attention of the drafts, the prefix's cache, confidences from logits -------------------------
+
+PSD_BF16, PSD_FP16, PSD_FP32 = 0, 1, 2
+_DTYPES = {torch.bfloat16: PSD_BF16, torch.float16: PSD_FP16, torch.float32: PSD_FP32}
+
+
+def _dtype(*tensors):
+    """The one element type of the tensors that are given (a type the library does not know becomes -1, which
+    the call refuses)."""
+    dt = tensors[0].dtype
+    for t in tensors[1:]:
+        if t is not None and t.dtype != dt:
+            raise ValueError(f"psd binding: tensors of one call differ in type ({dt} and {t.dtype})")
+    return _DTYPES.get(dt, -1)
+
+
+def _want(t, shape, dtype, name):
+    """A dense tensor of this shape and type, or None."""
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != shape):
+        raise ValueError(f"psd binding: {name} must be {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def _want_n(t, n, dtype, name):
+    """A dense tensor of n elements of this type, whatever its shape, or None."""
+    if t is not None and (t.dtype != dtype or t.numel() != n):
+        raise ValueError(f"psd binding: {name} must be {dtype} with {n} elements, got {t.dtype} {tuple(t.shape)}")
+    return _ptr(t)
+
+
+def _tokens_strides(t, name):
+    """(token, head) strides of [N, M, H, Dh] whose first two dimensions are one run of tokens."""
+    N, M, H, Dh = t.shape
+    sn, sm, sh, sd = t.stride()
+    if (sd != 1 and Dh > 1) or (N > 1 and M > 1 and sn != M * sm):
+        raise ValueError(f"psd binding: {name} needs a dense last dimension and nodes M tokens apart")
+    return (sm if M > 1 else sn if N > 1 else H * Dh), (sh if H > 1 else Dh)
+
+
+def _kv_strides(t, name):
+    if t is None:
+        return PsdKvStrides(0, 8, 0)
+    so, st, sh, sd = t.stride()
+    if sd != 1 and t.shape[3] > 1:
+        raise ValueError(f"psd binding: {name} needs a dense last dimension")
+    # the stride of a dimension of one is never walked: 0 (shared) or the smallest the library takes
+    return PsdKvStrides(so if t.shape[0] > 1 else 0, st if t.shape[1] > 1 else 8, sh if t.shape[2] > 1 else 0)
+
+
+def _data(t):
+    return t.data_ptr() if t is not None and t.numel() else None
+
+
+def _attention(q, k_prefix, scale, causal=False, out=None, v_prefix=None, k_own=None, v_own=None):
+    N, M, Hq, Dh = q.shape
+    B, P, Hkv, dk = k_prefix.shape
+    if B < 1 or N % B or dk != Dh:
+        raise ValueError("psd binding: q [B*D, M, Hq, Dh] and k_prefix [B, P, Hkv, Dh] do not belong together")
+    S = 0
+    for a, b in ((v_prefix, k_prefix), (v_own, k_own), (out, q)):
+        if a is not None and a.shape != b.shape:
+            raise ValueError("psd binding: keys and values, and out and q, have one shape")
+    if (k_own is None) != (v_own is None):
+        raise ValueError("psd binding: k_own and v_own come together")
+    if k_own is not None:
+        S = k_own.shape[1]
+        if tuple(k_own.shape) != (N, S, Hkv, Dh):
+            raise ValueError("psd binding: k_own is [B*D, S, Hkv, Dh]")
+    qt, qh = _tokens_strides(q, "q")
+    ot, oh = _tokens_strides(out, "out") if out is not None else (0, 0)
+    return PsdAttention(B, N // B, M, Hq, Hkv, Dh, P, S, _dtype(q, k_prefix, v_prefix, k_own, v_own, out),
+                        1 if causal else 0, float(Dh) ** -0.5 if scale is None else scale, 0, qt, qh, ot, oh,
+                        _kv_strides(k_prefix, "k_prefix"), _kv_strides(v_prefix, "v_prefix"),
+                        _kv_strides(k_own, "k_own"), _kv_strides(v_own, "v_own"))
+
+
+def psd_attention_workspace_bytes(B, D, M, Hq, Hkv, Dh, P, S) -> int:
+    return int(LIB.psd_attention_workspace_bytes(B, D, M, Hq, Hkv, Dh, P, S))
+
+
+def psd_draft_attention(q, k_prefix, v_prefix, out, lse=None, k_own=None, v_own=None, prefix_len=None, own_len=None,
+                        scale=None, causal=False, workspace=None, status=None, stream=None):
+    """q [B*D, M, Hq, Dh] over the prefix caches [B, P, Hkv, Dh] and each node's own keys [B*D, S, Hkv, Dh] -> out
+    (like q) and lse [B*D, M, Hq].  Strided tensors are taken as they are; ``scale`` defaults to 1/sqrt(Dh)."""
+    a = _attention(q, k_prefix, scale, causal, out, v_prefix, k_own, v_own)
+    _check(LIB.psd_draft_attention(q.data_ptr(), _data(k_prefix), _data(v_prefix),
+                                   _want(prefix_len, (a.B,), torch.int32, "prefix_len"), _data(k_own), _data(v_own),
+                                   _want(own_len, (a.B * a.D,), torch.int32, "own_len"), a, out.data_ptr(),
+                                   _want(lse, (a.B * a.D, a.M, a.Hq), torch.float32, "lse"), _ptr(workspace),
+                                   workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                                   _ptr(status), _stream(stream)), "psd_draft_attention")
+
+
+def psd_weights_workspace_bytes(B, D, M, Hq, Hkv, Dh, P) -> int:
+    return int(LIB.psd_weights_workspace_bytes(B, D, M, Hq, Hkv, Dh, P))
+
+
+def psd_prefix_weights(q, k_prefix, lse, acc_out, acc_in=None, beta=1.0, prefix_len=None, scale=None, workspace=None,
+                       status=None, stream=None):
+    """acc_out [B, Hkv, P] = beta * acc_in + the attention weight each prefix key draws from the rows of ``q`` (``lse``
+    [B*D, M, Hq] as psd_draft_attention wrote it).  acc_in may be acc_out."""
+    a = _attention(q, k_prefix, scale)
+    sums = (a.B, a.Hkv, a.P)
+    _check(LIB.psd_prefix_weights(q.data_ptr(), _data(k_prefix), _want(prefix_len, (a.B,), torch.int32, "prefix_len"),
+                                  _want(lse, (a.B * a.D, a.M, a.Hq), torch.float32, "lse"), a, beta,
+                                  _want(acc_in, sums, torch.float32, "acc_in"),
+                                  _want(acc_out, sums, torch.float32, "acc_out"), _ptr(workspace),
+                                  workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                                  _ptr(status), _stream(stream)), "psd_prefix_weights")
+
+
+def psd_prefix_evict(scores, k, v, k_out, v_out, index, scores_out=None, len_out=None, prefix_len=None, n_sink=0,
+                     n_recent=0, stream=None):
+    """Keep index.shape[2] keys per sequence and key head of the caches k, v [B, P, Hkv, Dh]: packed into k_out, v_out
+    [B, keep, Hkv, Dh], their positions into index [B, Hkv, keep]."""
+    B, P, Hkv, Dh = k.shape
+    keep = index.shape[-1]
+    if v.shape != k.shape or tuple(k_out.shape) != (B, keep, Hkv, Dh) or v_out.shape != k_out.shape:
+        raise ValueError("psd binding: k, v are [B, P, Hkv, Dh], k_out, v_out [B, keep, Hkv, Dh]")
+    e = PsdEvict(B, Hkv, Dh, P, keep, n_sink, n_recent, _dtype(k, v, k_out, v_out), _kv_strides(k, "k"),
+                 _kv_strides(v, "v"), _kv_strides(k_out, "k_out"), _kv_strides(v_out, "v_out"))
+    _check(LIB.psd_prefix_evict(_want(scores, (B, Hkv, P), torch.float32, "scores"), k.data_ptr(), v.data_ptr(),
+                                _want(prefix_len, (B,), torch.int32, "prefix_len"), e, k_out.data_ptr(), v_out.data_ptr(),
+                                _want(index, (B, Hkv, keep), torch.int32, "index"),
+                                _want(scores_out, (B, Hkv, keep), torch.float32, "scores_out"),
+                                _want(len_out, (B,), torch.int32, "len_out"), _stream(stream)), "psd_prefix_evict")
+
+
+def psd_logits_workspace_bytes(n_rows: int, V: int) -> int:
+    return int(LIB.psd_logits_workspace_bytes(n_rows, V))
+
+
+def psd_confidence_logits(logits, out_token, out_conf, out_lse=None, B=None, D=1, M=1, history=None, history_len=None,
+                          draft_tokens=None, draft_mask=None, repetition=1.0, presence=0.0, frequency=0.0, bias=None,
+                          allow=None, workspace=None, status=None, stream=None):
+    """Token, confidence and lse of every row of ``logits`` [B*D*M, V] after the edits: penalties for tokens of
+    ``history`` [B, T] (the first history_len[b]) and of a draft's filled slots, ``bias`` [V] or [rows, V], ``allow``
+    [rows, ceil(V/32)] int32 bit masks (a row of bias or allow serves R / rows consecutive rows)."""
+    R, V = logits.shape
+    if B is None:
+        B = R // (D * M)
+    if B * D * M != R or (logits.stride(1) != 1 and V > 1):
+        raise ValueError("psd binding: logits [B*D*M, V] needs a dense last dimension")
+    T, words = (history.shape[1] if history is not None else 0), (V + 31) // 32
+    bias_rows = 1 if bias is None or bias.dim() == 1 else bias.shape[0]
+    allow_rows = 1 if allow is None else allow.shape[0]
+    e = PsdLogitsEdit(_want(history, (B, T), torch.int32, "history") if T else None,
+                      _want(history_len, (B,), torch.int32, "history_len"),
+                      _want_n(draft_tokens, R, torch.int32, "draft_tokens"), _want_n(draft_mask, R, torch.int32, "draft_mask"),
+                      _want(bias, (V,) if bias is not None and bias.dim() == 1 else (bias_rows, V), torch.float32, "bias"),
+                      _want(allow, (allow_rows, words), torch.int32, "allow"), T, bias_rows, allow_rows, repetition,
+                      presence, frequency, 0)
+    _check(LIB.psd_confidence_logits(logits.data_ptr(), _dtype(logits), logits.stride(0) if R > 1 else V, B, D, M, V, e,
+                                     _want_n(out_token, R, torch.int32, "out_token"),
+                                     _want_n(out_conf, R, torch.float32, "out_conf"),
+                                     _want_n(out_lse, R, torch.float32, "out_lse"), _ptr(workspace),
+                                     workspace.numel() * workspace.element_size() if workspace is not None else 0,
+                                     _ptr(status), _stream(stream)), "psd_confidence_logits")
