@@ -1,90 +1,296 @@
-// Attention weight drawn by every prefix key, summed over the rows that read it.
+// Attention weight drawn by every prefix key, summed over the rows that read it:
+//   sum_r exp(scale * q_r . K_j - lse_r)  =  sum_r 2^(c * q_r . K_j - lse_r log2 e),   c = scale * log2 e.
 //
-// One thread per key: the key stays in registers, the queries of the key head pass by in shared memory (every thread
-// reads the same query element), and the thread adds exp2(s * scale * log2 e - lse * log2 e) of its own column of scores.
-// No reduction between threads and a fixed order of the sum.
-#include "ops_internal.cuh"
-#include "tc_common.cuh"
+// The scores are computed transposed, S^T = K Q^T: a tile of 128 keys is the M side of tcgen05.mma and 128 query rows are
+// the N side, so a thread of the epilogue (one TMEM lane) owns one KEY and walks the query rows as columns.  The sum over
+// rows is then a running sum in a register: no reduction between threads, no atomics, a fixed order.  A CTA keeps two key
+// tiles in shared memory and streams the query rows of their key head past both (each query tile is fetched once per 256
+// keys), so K is read once and nothing but the sums is written.
+//
+// Warps 0-3 and 4-7 take the two key tiles, warp 8 loads, warp 9 issues the products.  Accumulators are double-buffered per
+// key tile (4 x 128 TMEM columns).  One exponential per score is what bounds the kernel (16 per clock and SM against 8192
+// multiply-adds): see ex2_some.
+#include "attn_tc.cuh"
 
 namespace psd {
 namespace {
 
-constexpr int kKeys = 128, kRows = 8;
+constexpr int kKeysPerCta = 256;
+constexpr int kQStages = 4;
+constexpr int kWThreads = 320;
+constexpr int kMaxSplits = 16;
 
-template <typename T> __device__ __forceinline__ float to_f(T x);
-template <> __device__ __forceinline__ float to_f(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <> __device__ __forceinline__ float to_f(__half x) { return __half2float(x); }
+struct WeightsArgs {
+    const int32_t* prefix_len;
+    const float *lse, *acc_in;
+    float *acc_out, *part;          // part: [splits][B * Hkv][P] when splits > 1
+    int32_t* status_dev;
+    int T, G, Hq, Hkv, Dh, P;       // T: tokens per sequence (D * M)
+    int tq, n_qt, key_ctas, splits; // tokens per query tile, query tiles, CTAs along the keys, splits of the query tiles
+    int k_outer, k_head;            // 0: that dimension of the cache is shared
+    float c, beta;
+    int bf16;
+    long long wait_limit;
+};
 
-template <typename T, int DHP>
-__global__ void __launch_bounds__(kKeys) weights_kernel(const T* __restrict__ q, const T* __restrict__ k,
-                                                        const int32_t* __restrict__ prefix_len, const float* __restrict__ lse,
-                                                        const psd_attention_t a, float beta, const float* acc_in, float* acc_out) {
-    __shared__ float4 qs[kRows][DHP / 4];
-    __shared__ float ls[kRows];
-    const int b = blockIdx.y / a.Hkv, h = blockIdx.y % a.Hkv, G = a.Hq / a.Hkv;
-    const int L = prefix_len ? min(max(prefix_len[b], 0), a.P) : a.P;
-    const int j = blockIdx.x * kKeys + threadIdx.x;
-    float kr[DHP];
-#pragma unroll
-    for (int d = 0; d < DHP; ++d)
-        kr[d] = j < L && d < a.Dh ? to_f(k[b * a.kp.outer + j * a.kp.token + h * a.kp.head + d]) : 0.f;
-    float sum = 0.f;
-    const int n = a.D * a.M * G;
-    if (blockIdx.x * kKeys < L) {
-        for (int r0 = 0; r0 < n; r0 += kRows) {
-            __syncthreads();
-            for (int i = threadIdx.x; i < kRows * DHP; i += kKeys) {
-                const int r = r0 + i / DHP, d = i % DHP;
-                float x = 0.f;
-                if (r < n && d < a.Dh)
-                    x = to_f(q[((int64_t)b * a.D * a.M + r / G) * a.q_token + (int64_t)(h * G + r % G) * a.q_head + d]);
-                reinterpret_cast<float*>(qs[i / DHP])[d] = x;
+template <int SLABS>
+__global__ void __launch_bounds__(kWThreads, 1)
+weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_q, const WeightsArgs a) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    constexpr int TILE = SLABS * kSlabBytes;
+    unsigned char* k_tiles = smem;                                   // [2][TILE]
+    unsigned char* q_tiles = smem + 2 * TILE;                        // [kQStages][TILE]
+    float* lse_buf = reinterpret_cast<float*>(smem + (2 + kQStages) * TILE);       // [8 warps][2][128]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(lse_buf + 8 * 2 * 128);
+    uint64_t *k_full = bars, *q_full = bars + 1, *q_empty = q_full + kQStages, *s_full = q_empty + kQStages /* [2][2] */,
+             *s_empty = s_full + 4, *drain = s_empty + 4;
+    uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int kc = blockIdx.x % a.key_ctas;
+    const int rest = blockIdx.x / a.key_ctas, split = rest % a.splits, bh = rest / a.splits;
+    const int b = bh / a.Hkv, h = bh % a.Hkv;
+    const int key0 = kc * kKeysPerCta;
+
+    if (threadIdx.x == 0) {
+        mbar_init(k_full, 1);
+        for (int s = 0; s < kQStages; ++s) { mbar_init(&q_full[s], 1); mbar_init(&q_empty[s], 1); }
+        for (int s = 0; s < 4; ++s) { mbar_init(&s_full[s], 1); mbar_init(&s_empty[s], 4); }
+        mbar_init(drain, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8 && lane == 0) { tma_prefetch_desc(&map_k); tma_prefetch_desc(&map_q); }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_holder;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    const WaitCtx wc = {abort_flag, a.status_dev, a.wait_limit, 0u};
+    const int L = a.prefix_len ? min(max(a.prefix_len[b], 0), a.P) : a.P;
+    // query tiles of this split; none when no key of this CTA is inside the prefix
+    const int q_lo = key0 < L ? (int)((long long)a.n_qt * split / a.splits) : 0;
+    const int q_hi = key0 < L ? (int)((long long)a.n_qt * (split + 1) / a.splits) : 0;
+    const int n_it = q_hi - q_lo;
+    const int n_kt = L - key0 > 128 ? 2 : 1;      // key tiles that hold keys
+
+    if (warp == 8) {
+        if (lane == 0 && n_it > 0) {
+            mbar_arrive_expect_tx(k_full, n_kt * TILE);
+            for (int t = 0; t < n_kt; ++t)
+                for (int s = 0; s < SLABS; ++s)
+                    tma_load_4d(k_tiles + t * TILE + s * kSlabBytes, &map_k, k_full, s * kSlabElems, h * a.k_head, key0 + t * 128, b * a.k_outer);
+            const uint32_t q_bytes = (uint32_t)(SLABS * a.tq * a.G * 128);
+            int it = 0;
+            bool ok = true;
+            for (; it < n_it; ++it) {
+                const int s = it % kQStages;
+                if (!mbar_wait(&q_empty[s], ((it / kQStages) & 1) ^ 1, wc)) { ok = false; break; }
+                mbar_arrive_expect_tx(&q_full[s], q_bytes);
+                for (int c = 0; c < SLABS; ++c)
+                    tma_load_3d(q_tiles + s * TILE + c * kSlabBytes, &map_q, &q_full[s], c * kSlabElems, h * a.G, b * a.T + (q_lo + it) * a.tq);
             }
-            if (threadIdx.x < kRows) {
-                const int r = r0 + threadIdx.x;
-                const float l = r < n ? lse[((int64_t)b * a.D * a.M + r / G) * a.Hq + h * G + r % G] : -INFINITY;
-                ls[threadIdx.x] = l == -INFINITY ? INFINITY : l;
-            }
-            __syncthreads();
-            for (int r = 0; r < kRows; ++r) {
-                float s = 0.f;
-#pragma unroll
-                for (int d = 0; d < DHP / 4; ++d) {
-                    const float4 x = qs[r][d];
-                    s = fmaf(x.x, kr[4 * d], s); s = fmaf(x.y, kr[4 * d + 1], s);
-                    s = fmaf(x.z, kr[4 * d + 2], s); s = fmaf(x.w, kr[4 * d + 3], s);
+            if (!ok) {
+                // giving up: no copy may be in flight when the CTA exits
+                long long t0 = clock64();
+                while (!mbar_try_wait(k_full, 0) && clock64() - t0 < WAIT_LIMIT_CYCLES) {}
+                for (int i = it > kQStages ? it - kQStages : 0; i < it; ++i) {
+                    t0 = clock64();
+                    while (!mbar_try_wait(&q_full[i % kQStages], (i / kQStages) & 1) && clock64() - t0 < WAIT_LIMIT_CYCLES) {}
                 }
-                sum += ex2((s * a.scale - ls[r]) * 1.4426950408889634f);
             }
         }
+    } else if (warp == 9) {
+        if (lane == 0 && n_it > 0) {
+            const uint32_t idesc = umma_idesc16(128, a.bf16, false);
+            const int k_steps = (a.Dh + 15) / 16;
+            bool ok = mbar_wait(k_full, 0, wc);
+            for (int it = 0; ok && it < n_it; ++it) {
+                const int s = it % kQStages;
+                if (!mbar_wait(&q_full[s], (it / kQStages) & 1, wc)) { ok = false; break; }
+                const int buf = it & 1;
+                for (int t = 0; t < n_kt; ++t) {
+                    if (!mbar_wait(&s_empty[t * 2 + buf], ((it >> 1) & 1) ^ 1, wc)) { ok = false; break; }
+                    tc_fence_after();
+                    for (int k = 0; k < k_steps; ++k) {
+                        const uint32_t off = (uint32_t)((k / 4) * kSlabBytes), in = (uint64_t)((k % 4) * 2);
+                        umma_f16(tmem + (t * 2 + buf) * 128, umma_smem_desc(smem_u32(k_tiles + t * TILE) + off) + in,
+                                 umma_smem_desc(smem_u32(q_tiles + s * TILE) + off) + in, idesc, k != 0);
+                    }
+                    umma_commit(&s_full[t * 2 + buf]);
+                }
+                if (ok) umma_commit(&q_empty[s]);
+            }
+            if (!ok) {
+                umma_commit(drain);
+                const long long t0 = clock64();
+                while (!mbar_try_wait(drain, 0) && clock64() - t0 < WAIT_LIMIT_CYCLES) {}
+            }
+        }
+    } else {
+        const int t = warp >> 2, quarter = warp & 3;
+        const int key = key0 + t * 128 + quarter * 32 + lane;
+        float* lb = lse_buf + warp * 256;
+        const int RT = a.tq * a.G;                        // rows of a query tile
+        f32x2 sum[2] = {0ull, 0ull};
+        const f32x2 cc = pack2(a.c, a.c);
+        bool ok = true;
+        // -lse * log2 e of this lane's four columns of tile `it`; -inf marks a column that adds nothing
+        auto fetch_lse = [&](int it, float (&v)[4]) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int c = lane * 4 + u, tok = (q_lo + it) * a.tq + c / a.G;
+                const float l = c < RT && tok < a.T ? a.lse[((int64_t)b * a.T + tok) * a.Hq + h * a.G + c % a.G] : -INFINITY;
+                v[u] = l == -INFINITY ? -INFINITY : -l * kLog2e;
+            }
+        };
+        float nl[4];
+        if (t < n_kt && n_it > 0) fetch_lse(0, nl);
+        for (int it = 0; t < n_kt && it < n_it; ++it) {
+            const int buf = it & 1;
+            float* lt = lb + buf * 128;
+            *reinterpret_cast<float4*>(lt + lane * 4) = make_float4(nl[0], nl[1], nl[2], nl[3]);
+            const bool all = __all_sync(0xffffffffu, nl[0] > -INFINITY && nl[1] > -INFINITY && nl[2] > -INFINITY && nl[3] > -INFINITY);
+            if (it + 1 < n_it) fetch_lse(it + 1, nl);
+            __syncwarp();
+            if (!mbar_wait(&s_full[t * 2 + buf], (it >> 1) & 1, wc)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((t * 2 + buf) * 128);
+#pragma unroll
+            for (int c = 0; c < 128; c += 32) {
+                uint32_t r[32];
+                tmem_ld32(at + c, r);
+                tmem_wait_ld(r);
+                if (c == 96) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&s_empty[t * 2 + buf]);
+                }
+#pragma unroll
+                for (int j = 0; j < 32; j += 4) {
+                    const float4 l = *reinterpret_cast<const float4*>(lt + c + j);
+                    float x[4];
+                    unpack2(fma2(pack2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), cc, pack2(l.x, l.y)), x[0], x[1]);
+                    unpack2(fma2(pack2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])), cc, pack2(l.z, l.w)), x[2], x[3]);
+                    if (!all) {      // absent columns hold whatever the tile held there
+                        x[0] = l.x > -INFINITY || l.x != l.x ? x[0] : -INFINITY;
+                        x[1] = l.y > -INFINITY || l.y != l.y ? x[1] : -INFINITY;
+                        x[2] = l.z > -INFINITY || l.z != l.z ? x[2] : -INFINITY;
+                        x[3] = l.w > -INFINITY || l.w != l.w ? x[3] : -INFINITY;
+                    }
+                    sum[0] = add2(sum[0], pack2(ex2(x[0]), ex2(x[1])));
+                    sum[1] = add2(sum[1], pack2(ex2(x[2]), ex2(x[3])));
+                }
+            }
+        }
+        if (ok && key < a.P) {
+            float s0, s1, s2, s3;
+            unpack2(sum[0], s0, s1);
+            unpack2(sum[1], s2, s3);
+            const float total = (s0 + s1) + (s2 + s3);
+            const int64_t o = (int64_t)bh * a.P + key;
+            if (a.splits > 1)
+                a.part[(int64_t)split * (gridDim.x / a.key_ctas / a.splits) * a.P + o] = total;
+            else
+                a.acc_out[o] = key < L ? (a.acc_in ? a.beta * a.acc_in[o] : 0.f) + total : 0.f;
+        }
     }
-    if (j < a.P) {
-        const int64_t o = (int64_t)blockIdx.y * a.P + j;
-        acc_out[o] = j < L ? (acc_in ? beta * acc_in[o] : 0.f) + sum : 0.f;
+    tc_fence_before();
+    __syncthreads();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (warp == 9) {
+        __syncwarp();
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
 }
 
-template <typename T>
-void run(const void* q, const void* k, const int32_t* prefix_len, const float* lse, const psd_attention_t& a, float beta,
-         const float* acc_in, float* acc_out, cudaStream_t st) {
-    const dim3 grid((a.P + kKeys - 1) / kKeys, a.B * a.Hkv);
-    if (a.Dh <= 64)
-        weights_kernel<T, 64><<<grid, kKeys, 0, st>>>((const T*)q, (const T*)k, prefix_len, lse, a, beta, acc_in, acc_out);
-    else
-        weights_kernel<T, 128><<<grid, kKeys, 0, st>>>((const T*)q, (const T*)k, prefix_len, lse, a, beta, acc_in, acc_out);
+// Adds the splits' sums in order.
+__global__ void __launch_bounds__(256) weights_join_kernel(const WeightsArgs a, int64_t n) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int64_t o = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (o >= n) return;
+    const int j = (int)(o % a.P), b = (int)(o / a.P) / a.Hkv;
+    const int L = a.prefix_len ? min(max(a.prefix_len[b], 0), a.P) : a.P;
+    float s = 0.f;
+    for (int i = 0; i < a.splits; ++i) s += a.part[(int64_t)i * n + o];
+    a.acc_out[o] = j < L ? (a.acc_in ? a.beta * a.acc_in[o] : 0.f) + s : 0.f;
+}
+
+struct WeightsPlan { int tq, n_qt, key_ctas, splits; };
+
+// Splits of the query rows: only when the key tiles alone leave SMs idle.
+WeightsPlan plan_weights(int B, int D, int M, int Hq, int Hkv, int P) {
+    WeightsPlan p;
+    p.tq = 128 / (Hq / Hkv);
+    const int64_t T = (int64_t)D * M;
+    p.n_qt = (int)((T + p.tq - 1) / p.tq);
+    p.key_ctas = (P + kKeysPerCta - 1) / kKeysPerCta;
+    const int64_t ctas = (int64_t)B * Hkv * p.key_ctas;
+    int64_t s = sm_count() / ctas;
+    if (s > kMaxSplits) s = kMaxSplits;
+    if (s > p.n_qt) s = p.n_qt;
+    p.splits = s < 1 ? 1 : (int)s;
+    return p;
+}
+
+template <int SLABS>
+int launch_w(const CUtensorMap& mk, const CUtensorMap& mq, const WeightsArgs& a, int64_t grid, cudaStream_t st) {
+    constexpr int smem = (2 + kQStages) * SLABS * kSlabBytes + 8 * 2 * 128 * 4 + 1024 + 256;
+    static_assert(smem <= 227 * 1024, "shared memory of the weights kernel");
+    static std::atomic<unsigned long long> set{0};
+    if (!ensure_dynamic_smem(weights_tc_kernel<SLABS>, smem, set)) return PSD_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kWThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, weights_tc_kernel<SLABS>, mk, mq, a);
+    count_launch();
+    if (e != cudaSuccess) return PSD_ERR_CUDA;
+    if (a.splits > 1) {
+        const int64_t n = grid / a.splits / a.key_ctas * a.P;
+        cfg.gridDim = dim3((unsigned)((n + 255) / 256));
+        cfg.blockDim = dim3(256);
+        cfg.dynamicSmemBytes = 0;
+        e = cudaLaunchKernelEx(&cfg, weights_join_kernel, a, n);
+        count_launch();
+    }
+    return e == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
 }
 
 }  // namespace
 
-size_t prefix_weights_workspace(int, int, int, int, int, int, int) { return 256; }
+size_t prefix_weights_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
+    const WeightsPlan p = plan_weights(B, D, M, Hq, Hkv, P);
+    return p.splits > 1 ? ((size_t)p.splits * B * Hkv * P * 4 + 255) / 256 * 256 : 256;
+}
 
 int launch_prefix_weights(const void* q, const void* k_prefix, const int32_t* prefix_len, const float* lse,
-                          const psd_attention_t& a, float beta, const float* acc_in, float* acc_out, void*, int32_t*,
-                          cudaStream_t st) {
-    if (a.dtype == PSD_BF16) run<__nv_bfloat16>(q, k_prefix, prefix_len, lse, a, beta, acc_in, acc_out, st);
-    else run<__half>(q, k_prefix, prefix_len, lse, a, beta, acc_in, acc_out, st);
-    count_launch();
-    return cudaGetLastError() == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
+                          const psd_attention_t& a, float beta, const float* acc_in, float* acc_out, void* workspace,
+                          int32_t* status_dev, cudaStream_t st) {
+    const WeightsPlan p = plan_weights(a.B, a.D, a.M, a.Hq, a.Hkv, a.P);
+    const int64_t grid = (int64_t)p.key_ctas * p.splits * a.B * a.Hkv;
+    if (grid > INT32_MAX) return PSD_ERR_SHAPE;
+    CUtensorMap mk, mq;
+    if (!make_cache_map(&mk, k_prefix, a.dtype, a.kp, a.B, a.P, a.Hkv, a.Dh, 128) || !make_query_map(&mq, q, a, p.tq))
+        return PSD_ERR_CUDA;
+    WeightsArgs w = {prefix_len, lse, acc_in, acc_out, reinterpret_cast<float*>(workspace), status_dev, a.D * a.M, a.Hq / a.Hkv, a.Hq,
+                     a.Hkv, a.Dh, a.P, p.tq, p.n_qt, p.key_ctas, p.splits, a.kp.outer ? 1 : 0, a.kp.head ? 1 : 0,
+                     a.scale * kLog2e, beta, a.dtype == PSD_BF16 ? 1 : 0, wait_limit_cycles()};
+    return a.Dh <= 64 ? launch_w<1>(mk, mq, w, grid, st) : launch_w<2>(mk, mq, w, grid, st);
 }
 
 }  // namespace psd
