@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libpsd_b200.so")
 LIB_DEBUG = os.path.join(PKG, "libpsd_b200_debug.so")   # the same sources compiled with -DPSD_DEBUG
 SOURCES = ["psd_api.cu", "confidence_tc.cu", "confidence_tc2.cu", "confidence_simt.cu", "combine.cu", "policy.cu",
-           "confidence_static.cu", "decode_loop.cu", "dag.cu", "compact.cu", "ops_api.cu", "draft_attention.cu",
+           "confidence_static.cu", "decode_loop.cu", "dag.cu", "compact.cu", "ops_api.cu", "draft_attention.cu", "prefix_attention.cu",
            "prefix_weights.cu", "prefix_evict.cu", "confidence_logits.cu"]
 EXTRA_SOURCES: list[str] = []
 NVCC_FLAGS = [*os.environ.get("PSD_NVCC_EXTRA", "").split(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

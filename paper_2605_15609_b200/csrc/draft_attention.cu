@@ -5,14 +5,12 @@
 // every tile each, and join their maxima, sums and outputs at the end.  Products are m16n8k16 tensor instructions with
 // fp32 accumulation; K and V tiles are double-buffered by asynchronous copies that fill what lies past a length (or past
 // Dh) with zeros, so nothing that was never written is multiplied, and a CTA only ever reads its own draft's keys.
-#include "ops_internal.cuh"
-#include "tc_common.cuh"
+#include "attn_tc.cuh"
+#include "prefix_attention.cuh"
 
 namespace psd {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kKeys = 64;        // keys per tile
 constexpr int kThreads = 128;
 
@@ -61,6 +59,10 @@ struct OwnArgs {
     float* lse;
     psd_attention_t a;
     int row_blocks;      // CTAs per (node, key head)
+    // partial results over the prefix (prefix_attention.cu), or NULL: this kernel walks the prefix's keys itself
+    const float *po, *pl;
+    int splits, dhp;
+    int64_t rows;
 };
 
 template <typename T, int DHP, int WM>
@@ -77,8 +79,10 @@ __global__ void __launch_bounds__(kThreads) draft_attention_kernel(const OwnArgs
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wm = warp / WK, wk = warp % WK;
     const int r0 = rb * 16 * WM + wm * 16 + (lane >> 2);       // this thread's rows: r0 and r0 + 8
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int Lp = a.P == 0 ? 0 : p.prefix_len ? min(max(p.prefix_len[b], 0), a.P) : a.P;
+    // With partial results the kernel before this one is the prefix's, which has itself waited for whatever wrote the
+    // inputs; only its results are waited for, below.
+    if (!p.po) asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int Lp = a.P == 0 || p.po ? 0 : p.prefix_len ? min(max(p.prefix_len[b], 0), a.P) : a.P;
     const int Lo = a.S == 0 ? 0 : p.own_len ? min(max(p.own_len[node], 0), a.S) : a.S;
 
     // query fragments straight from global memory
@@ -253,11 +257,37 @@ __global__ void __launch_bounds__(kThreads) draft_attention_kernel(const OwnArgs
             }
         }
     }
+    if (p.po) asm volatile("griddepcontrol.wait;" ::: "memory");
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         if (!live[u]) continue;
         const int r = r0 + 8 * u, i = r / G, g = r % G;
         const int64_t t = (int64_t)node * a.M + i;
+        if (p.po) {
+            // join the prefix's partial results, in order: out = (2^(m-T) o + sum_i 2^(z_i-T) O_i) / (2^(m-T) l + sum_i 2^(z_i-T))
+            const int64_t at = t * a.Hq + h * G + g;
+            float T2 = m[u];
+            for (int x = 0; x < p.splits; ++x) T2 = fmaxf(T2, p.pl[x * p.rows + at]);
+            const float f = m[u] == -INFINITY ? 1.f : ex2(m[u] - T2);
+            l[u] *= f;
+#pragma unroll
+            for (int n = 0; n < NO; ++n) { o[n][2 * u] *= f; o[n][2 * u + 1] *= f; }
+            for (int x = 0; x < p.splits; ++x) {
+                const float z = p.pl[x * p.rows + at];
+                if (z == -INFINITY) continue;                    // the split held no key: its output was not written
+                const float w = ex2(z - T2);
+                const float* po = p.po + (x * p.rows + at) * p.dhp + (lane & 3) * 2;
+                l[u] += w;
+#pragma unroll
+                for (int n = 0; n < NO; ++n) {
+                    if (n * 8 >= a.Dh) break;
+                    const float2 y = *reinterpret_cast<const float2*>(po + n * 8);
+                    o[n][2 * u] = fmaf(w, y.x, o[n][2 * u]);
+                    o[n][2 * u + 1] = fmaf(w, y.y, o[n][2 * u + 1]);
+                }
+            }
+            m[u] = T2;
+        }
         const bool none = m[u] == -INFINITY && l[u] == 0.f;
         const float inv = none ? 0.f : 1.f / l[u];
         T* out = reinterpret_cast<T*>(p.out) + t * a.out_token + (int64_t)(h * G + g) * a.out_head;
@@ -304,12 +334,27 @@ int launch_dh(OwnArgs& p, cudaStream_t st) {
 
 }  // namespace
 
-size_t draft_attention_workspace(int, int, int, int, int, int, int, int) { return 256; }
+size_t draft_attention_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
+    if (P == 0) return 256;
+    const PrefixPlan p = plan_prefix(B, D, M, Hq, Hkv, Dh, P);
+    return ((size_t)B * D * M * Hq * p.splits * (p.dhp + 1) * 4 + 255) / 256 * 256;
+}
 
 int launch_draft_attention(const void* q, const void* k_prefix, const void* v_prefix, const int32_t* prefix_len,
                            const void* k_own, const void* v_own, const int32_t* own_len, const psd_attention_t& a,
-                           void* out, float* lse, void*, int32_t*, cudaStream_t st) {
-    OwnArgs p = {q, k_prefix, v_prefix, k_own, v_own, prefix_len, own_len, out, lse, a, 0};
+                           void* out, float* lse, void* workspace, int32_t* status_dev, cudaStream_t st) {
+    OwnArgs p = {q, k_prefix, v_prefix, k_own, v_own, prefix_len, own_len, out, lse, a, 0, nullptr, nullptr, 0, 0, 0};
+    if (a.P > 0) {
+        const PrefixPlan plan = plan_prefix(a.B, a.D, a.M, a.Hq, a.Hkv, a.Dh, a.P);
+        p.rows = (int64_t)a.B * a.D * a.M * a.Hq;
+        float* po = reinterpret_cast<float*>(workspace);
+        float* pl = po + p.rows * plan.splits * plan.dhp;
+        if (const int e = launch_prefix_attention(q, k_prefix, v_prefix, prefix_len, a, plan, po, pl, status_dev, st)) return e;
+        p.po = po;
+        p.pl = pl;
+        p.splits = plan.splits;
+        p.dhp = plan.dhp;
+    }
     if (a.dtype == PSD_BF16) return a.Dh <= 64 ? launch_dh<__nv_bfloat16, 64>(p, st) : launch_dh<__nv_bfloat16, 128>(p, st);
     return a.Dh <= 64 ? launch_dh<__half, 64>(p, st) : launch_dh<__half, 128>(p, st);
 }

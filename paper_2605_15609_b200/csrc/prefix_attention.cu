@@ -1,0 +1,414 @@
+// Attention of query tiles over the shared prefix, on tcgen05: partial outputs and log-sum-exps, joined with the drafts'
+// own keys by draft_attention_kernel.
+//
+// All query rows of a sequence that share a key head (tokens of all its drafts times the heads of the group) are cut into
+// tiles of up to 128 rows; a CTA runs two STREAMS, each with its own tile S of scores (128 rows x 128 keys) and output O
+// in tensor memory (4 x 128 columns: all of it).  With two or more tiles the streams take two query tiles over the same
+// keys, so every K and V tile in shared memory serves 256 rows; with one tile they take the two halves of the CTA's
+// keys.  One warp loads K and V tiles by TMA into a ring, one issues the products, and four warps per stream do the
+// softmax: a thread owns a row (TMEM lane), so maxima and sums need no other thread.  While one stream's softmax runs, the
+// tensor cores work on the other stream:
+//   .. PV0(j) S0(j+1) | PV1(j) S1(j+1) | PV0(j+1) ..      (S0(j+1) overwrites the scores whose weights PV0(j) just read)
+// The weights P overwrite the scores in tensor memory as packed 16-bit pairs and are the A operand of PV.
+//
+// The running maximum is only raised, and O rescaled, when a row's maximum grew by more than 2^8: weights may then be as
+// large as 2^8, which costs no accuracy in a floating type, and rescaling O (reading and writing 128 x Dh of tensor
+// memory) becomes rare.
+//
+// Keys past the prefix's end are masked in the scores, and their V rows are zeroed in shared memory before the product,
+// since 0 * NaN would spoil a row.
+#include "attn_tc.cuh"
+#include "prefix_attention.cuh"
+
+namespace psd {
+namespace {
+
+constexpr int kPThreads = 384;              // warps 0-3, 4-7: softmax of stream 0, 1; 8: TMA; 9: MMA; 10, 11 idle
+constexpr float kRaise = 8.0f;              // growth of a row's maximum (log2) that triggers a rescale
+
+template <int SLABS> struct Ring { static constexpr int N = SLABS == 2 ? 5 : 8; };
+
+struct PrefixArgs {
+    const int32_t* prefix_len;
+    float* po;                 // [splits][R * Hq][DHP] normalised outputs
+    float* pl;                 // [splits][R * Hq] log2-sum-exp2
+    int32_t* status_dev;
+    int64_t rows;              // R * Hq
+    int T, G, Hq, Hkv, Dh, P;
+    int tq, n_qt, units, splits;   // tokens per tile, tiles per (sequence, key head), CTAs along them, splits written
+    int k_outer, k_head, v_outer, v_head;
+    float c;                   // scale * log2 e
+    int bf16;
+    long long wait_limit;
+};
+
+__device__ __forceinline__ uint32_t pack16(float lo, float hi, bool bf16) {
+    uint32_t r;
+    if (bf16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+template <int SLABS, bool BF16>
+__global__ void __launch_bounds__(kPThreads, 1)
+prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                        const __grid_constant__ CUtensorMap map_v, const PrefixArgs a) {
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    constexpr int TILE = SLABS * kSlabBytes, NS = Ring<SLABS>::N, DHP = SLABS * 64;
+    unsigned char* q_tiles = smem;                                   // [2][TILE]
+    unsigned char* ring = smem + 2 * TILE;                           // [NS][TILE]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(ring + NS * TILE);
+    uint64_t *q_full = bars, *full = bars + 1, *empty = full + NS, *s_full = empty + NS /* [2] */, *p_ready = s_full + 2,
+             *o_done = p_ready + 2, *drain = o_done + 2;
+    uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const bool shared_keys = a.n_qt > 1;          // two query tiles over the same keys
+    const int unit = blockIdx.x % a.units;
+    const int rest = blockIdx.x / a.units;
+    const int n_cs = shared_keys ? a.splits : a.splits / 2;          // CTAs along the keys
+    const int cs = rest % n_cs, bh = rest / n_cs;
+    const int b = bh / a.Hkv, h = bh % a.Hkv;
+    const int qt0 = shared_keys ? unit * 2 : 0;
+    const int n_streams = shared_keys ? min(2, a.n_qt - qt0) : 2;
+
+    if (threadIdx.x == 0) {
+        mbar_init(q_full, 1);
+        for (int s = 0; s < NS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&s_full[s], 1); mbar_init(&p_ready[s], 4); mbar_init(&o_done[s], 1); }
+        mbar_init(drain, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8 && lane == 0) { tma_prefetch_desc(&map_q); tma_prefetch_desc(&map_k); tma_prefetch_desc(&map_v); }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_holder;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    const WaitCtx wc = {abort_flag, a.status_dev, a.wait_limit, 0u};
+    const int L = a.prefix_len ? min(max(a.prefix_len[b], 0), a.P) : a.P;
+    const int tiles = (L + 127) / 128;
+    // key tiles [t0, t0 + nt) of each stream: split s of a.splits even shares
+    int t0[2], nt[2], sp[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        sp[s] = shared_keys ? cs : cs * 2 + s;
+        t0[s] = (int)((long long)tiles * sp[s] / a.splits);
+        nt[s] = s < n_streams ? (int)((long long)tiles * (sp[s] + 1) / a.splits) - t0[s] : 0;
+    }
+    const int most = max(nt[0], nt[1]);
+    const int n_q = shared_keys ? n_streams : 1;                     // query tiles of this CTA
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        if (warp == 8 && lane == 0 && most > 0) {
+            // ---------------------------------------------------------------- loader
+            mbar_arrive_expect_tx(q_full, (uint32_t)(n_q * SLABS * a.tq * a.G * 128));
+            for (int t = 0; t < n_q; ++t)
+                for (int c = 0; c < SLABS; ++c)
+                    tma_load_3d(q_tiles + t * TILE + c * kSlabBytes, &map_q, q_full, c * kSlabElems, h * a.G, b * a.T + (qt0 + t) * a.tq);
+            int item = 0;
+            bool ok = true;
+            auto load = [&](bool is_v, int tile) {
+                const int s = item % NS;
+                if (!mbar_wait(&empty[s], ((item / NS) & 1) ^ 1, wc)) { ok = false; return; }
+                mbar_arrive_expect_tx(&full[s], TILE);
+                for (int c = 0; c < SLABS; ++c) {
+                    if (is_v) tma_load_4d(ring + s * TILE + c * kSlabBytes, &map_v, &full[s], c * kSlabElems, h * a.v_head, tile * 128, b * a.v_outer);
+                    else tma_load_4d(ring + s * TILE + c * kSlabBytes, &map_k, &full[s], c * kSlabElems, h * a.k_head, tile * 128, b * a.k_outer);
+                }
+                ++item;
+            };
+            const int ns = shared_keys ? 1 : 2;     // shared: stream 0's list serves both
+            for (int s = 0; ok && s < ns; ++s)
+                if (nt[s] > 0) load(false, t0[s]);
+            for (int j = 0; ok && j < most; ++j)
+                for (int s = 0; ok && s < ns; ++s) {
+                    if (j < nt[s]) load(true, t0[s] + j);
+                    if (ok && j + 1 < nt[s]) load(false, t0[s] + j + 1);
+                }
+            if (!ok) {
+                // giving up: no copy may be in flight when the CTA exits
+                long long c0 = clock64();
+                while (!mbar_try_wait(q_full, 0) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
+                for (int i = item > NS ? item - NS : 0; i < item; ++i) {
+                    c0 = clock64();
+                    while (!mbar_try_wait(&full[i % NS], (i / NS) & 1) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
+                }
+            }
+        } else if (warp == 9 && lane == 0 && most > 0) {
+            // ---------------------------------------------------------------- products
+            const uint32_t id_s = umma_idesc16(128, BF16, false);
+            const uint32_t id_o = umma_idesc16((a.Dh + 15) / 16 * 16, BF16, true);
+            const int k_steps = (a.Dh + 15) / 16;
+            auto wait_item = [&](int item) { const bool r = mbar_wait(&full[item % NS], (item / NS) & 1, wc); tc_fence_after(); return r; };
+            auto scores = [&](int s, int item) {
+                const unsigned char* q = q_tiles + (shared_keys ? s : 0) * TILE;
+                const unsigned char* k = ring + (item % NS) * TILE;
+                for (int i = 0; i < k_steps; ++i) {
+                    const uint32_t off = (uint32_t)((i / 4) * kSlabBytes);
+                    umma_f16(tmem + s * 128, umma_smem_desc(smem_u32(q) + off) + (uint64_t)((i % 4) * 2),
+                             umma_smem_desc(smem_u32(k) + off) + (uint64_t)((i % 4) * 2), id_s, i != 0);
+                }
+                umma_commit(&s_full[s]);
+            };
+            int next = 0;      // ring items in the loader's order
+            bool ok = mbar_wait(q_full, 0, wc);
+            if (ok && shared_keys) {
+                const int k = next++;
+                ok = wait_item(k);
+                if (ok) {
+                    for (int s = 0; s < n_streams; ++s) scores(s, k);
+                    umma_commit(&empty[k % NS]);
+                }
+            } else {
+                for (int s = 0; ok && s < 2; ++s) {
+                    if (nt[s] == 0) continue;
+                    const int k = next++;
+                    if (!(ok = wait_item(k))) break;
+                    scores(s, k);
+                    umma_commit(&empty[k % NS]);
+                }
+            }
+            for (int j = 0; ok && j < most; ++j) {
+                int v = 0, k = 0;
+                for (int s = 0; ok && s < n_streams; ++s) {
+                    if (j >= nt[s]) continue;
+                    const bool first = !shared_keys || s == 0, last = !shared_keys || s == n_streams - 1;
+                    if (first) { v = next++; k = j + 1 < nt[s] ? next++ : -1; }
+                    if (!(ok = mbar_wait(&p_ready[s], j & 1, wc)) || !(ok = wait_item(v))) break;
+                    // keys of this tile in steps of 16 (the last tile may hold fewer)
+                    const int left = L - (t0[s] + j) * 128, steps = left >= 128 ? 8 : (left + 15) / 16;
+                    const uint64_t vd = umma_smem_desc_mn(smem_u32(ring + (v % NS) * TILE), kSlabBytes);
+                    for (int i = 0; i < steps; ++i)
+                        umma_f16_ts(tmem + 256 + s * 128, tmem + s * 128 + i * 8, vd + (uint64_t)(i * (2048 >> 4)), id_o, (j | i) != 0);
+                    umma_commit(&o_done[s]);
+                    if (last) umma_commit(&empty[v % NS]);
+                    if (k >= 0) {
+                        if (!(ok = wait_item(k))) break;
+                        scores(s, k);
+                        if (last) umma_commit(&empty[k % NS]);
+                    }
+                }
+            }
+            if (!ok) {
+                umma_commit(drain);
+                const long long c0 = clock64();
+                while (!mbar_try_wait(drain, 0) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
+            }
+        }
+        __syncwarp();
+    } else {
+        // -------------------------------------------------------------------- softmax of stream s, row = lane
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        const int s = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const uint32_t t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
+        const f32x2 cc = pack2(a.c, a.c);
+        float m = 0.f, l = 0.f;          // reference maximum (scaled by c) and sum relative to it
+        bool ok = true;
+        const int n = nt[s];
+        // the ring items of this stream's V tiles, for the zeroing of the last one
+        for (int j = 0; j < n; ++j) {
+            if (!mbar_wait_warp(&s_full[s], j & 1, wc)) { ok = false; break; }
+            tc_fence_after();
+            uint32_t r[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, r[c]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_wait_ld(r[c]);
+            const int left = L - (t0[s] + j) * 128;
+            if (left < 128) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (c * 32 + i >= left) r[c][i] = 0xff800000u;
+            }
+            float mx[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                mx[c] = __uint_as_float(r[c][0]);
+#pragma unroll
+                for (int i = 1; i < 31; i += 2) mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(r[c][i])), __uint_as_float(r[c][i + 1]));
+                mx[c] = fmaxf(mx[c], __uint_as_float(r[c][31]));
+            }
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.c;
+            if (j == 0) {
+                m = top == -INFINITY ? 0.f : top;
+            } else if (__any_sync(0xffffffffu, top > m + kRaise)) {
+                // rare: raise the reference and rescale what has been summed (PV of the tile before must be done)
+                const float mn = top > m + kRaise ? top : m;
+                const float f = ex2(m - mn);
+                m = mn;
+                l *= f;
+                if (!mbar_wait_warp(&o_done[s], (j - 1) & 1, wc)) { ok = false; break; }
+                tc_fence_after();
+                for (int c = 0; c < a.Dh; c += 8) {
+                    uint32_t o[8];
+                    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                                 : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7])
+                                 : "r"(t_o + c));
+                    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                                 : "+r"(o[0]), "+r"(o[1]), "+r"(o[2]), "+r"(o[3]), "+r"(o[4]), "+r"(o[5]), "+r"(o[6]), "+r"(o[7]) :: "memory");
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                                 ::"r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]), "r"(t_o + c)
+                                 : "memory");
+                }
+                tmem_wait_st();
+            }
+            const f32x2 nm = pack2(-m, -m);
+            f32x2 acc = pack2(0.f, 0.f);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t p[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float x, y;
+                    unpack2(fma2(pack2(__uint_as_float(r[c][2 * i]), __uint_as_float(r[c][2 * i + 1])), cc, nm), x, y);
+                    x = ex2(x);
+                    y = ex2(y);
+                    acc = add2(acc, pack2(x, y));
+                    p[i] = pack16(x, y, BF16);
+                }
+                tmem_st16(t_s + c * 16, p);
+            }
+            float l0, l1;
+            unpack2(acc, l0, l1);
+            l += l0 + l1;
+            tmem_wait_st();
+            if (left < 128 && (s == 0 || !shared_keys)) {
+                // V rows past the end that the product's last step of 16 keys reads: zero, whatever the cache holds there
+                int item;
+                if (shared_keys) item = 1 + 2 * j;
+                else {
+                    // items before this V: the first K tiles of both streams, then per round V and next K of each stream
+                    item = (nt[0] > 0) + (nt[1] > 0);
+                    for (int q = 0; q < j; ++q)
+                        for (int u = 0; u < 2; ++u) item += (q < nt[u]) + (q + 1 < nt[u]);
+                    if (s == 1) item += (j < nt[0]) + (j + 1 < nt[0]);
+                }
+                if (!mbar_wait_warp(&full[item % NS], (item / NS) & 1, wc)) { ok = false; break; }
+                const int stop = (left + 15) / 16 * 16;
+                unsigned char* v = ring + (item % NS) * TILE;
+                for (int x = left * 8 * SLABS + row; x < stop * 8 * SLABS; x += 128) {
+                    const int key = x / (8 * SLABS), ch = x % (8 * SLABS);
+                    *reinterpret_cast<uint4*>(v + (ch / 8) * kSlabBytes + key * 128 + (ch % 8) * 16) = make_uint4(0, 0, 0, 0);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&p_ready[s]);
+        }
+        if (ok && s < n_streams) {
+            const int64_t tok0 = (int64_t)b * a.T + (int64_t)(qt0 + (shared_keys ? s : 0)) * a.tq;
+            const int64_t tok = tok0 + row / a.G;
+            const bool live = row < a.tq * a.G && tok < (int64_t)(b + 1) * a.T;
+            const int64_t at = (int64_t)sp[s] * a.rows + tok * a.Hq + h * a.G + row % a.G;
+            if (n > 0) {
+                ok = mbar_wait_warp(&o_done[s], (n - 1) & 1, wc);
+                tc_fence_after();
+                if (ok) {
+                    const float inv = 1.0f / l;
+                    float* o = a.po + at * DHP;
+#pragma unroll 1
+                    for (int c = 0; c < DHP; c += 32) {
+                        if (c >= a.Dh) break;
+                        uint32_t x[32];
+                        tmem_ld32(t_o + c, x);
+                        tmem_wait_ld(x);
+                        if (live) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 8)
+                                asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(o + c + i),
+                                             "f"(__uint_as_float(x[i]) * inv), "f"(__uint_as_float(x[i + 1]) * inv),
+                                             "f"(__uint_as_float(x[i + 2]) * inv), "f"(__uint_as_float(x[i + 3]) * inv),
+                                             "f"(__uint_as_float(x[i + 4]) * inv), "f"(__uint_as_float(x[i + 5]) * inv),
+                                             "f"(__uint_as_float(x[i + 6]) * inv), "f"(__uint_as_float(x[i + 7]) * inv) : "memory");
+                        }
+                    }
+                }
+            }
+            if (live && ok) a.pl[at] = n > 0 ? m + log2f(l) : -INFINITY;
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (warp == 9) {
+        __syncwarp();
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+template <int SLABS, bool BF16>
+int launch_p(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const PrefixArgs& a, int64_t grid, cudaStream_t st) {
+    constexpr int smem = (2 + Ring<SLABS>::N) * SLABS * kSlabBytes + 1024 + 256;
+    static_assert(smem <= 227 * 1024, "shared memory of the prefix kernel");
+    static std::atomic<unsigned long long> set{0};
+    if (!ensure_dynamic_smem(prefix_attention_kernel<SLABS, BF16>, smem, set)) return PSD_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kPThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, prefix_attention_kernel<SLABS, BF16>, mq, mk, mv, a);
+    count_launch();
+    return e == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
+}
+
+}  // namespace
+
+// How the prefix's keys are split.  A CTA takes two query tiles (or the only one twice, over two ranges of keys); when
+// (sequence, key head, tile pair) alone leaves SMs idle the keys are split, down to kMinTiles tiles of 128 keys per split.
+PrefixPlan plan_prefix(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
+    constexpr int kMinTiles = 2;
+    PrefixPlan p = {};
+    p.tq = 128 / (Hq / Hkv);
+    p.n_qt = (int)(((int64_t)D * M + p.tq - 1) / p.tq);
+    p.units = p.n_qt > 1 ? (p.n_qt + 1) / 2 : 1;
+    const int tiles = (P + 127) / 128;
+    const int64_t ctas = (int64_t)B * Hkv * p.units;
+    int64_t s = sm_count() / ctas;
+    const int per = p.n_qt > 1 ? 1 : 2;                 // splits a CTA writes
+    if (s * per > tiles / kMinTiles) s = tiles / kMinTiles / per;
+    if (s < 1) s = 1;
+    p.splits = (int)s * per;
+    p.dhp = Dh <= 64 ? 64 : 128;
+    return p;
+}
+
+int launch_prefix_attention(const void* q, const void* k, const void* v, const int32_t* prefix_len, const psd_attention_t& a,
+                            const PrefixPlan& p, float* po, float* pl, int32_t* status_dev, cudaStream_t st) {
+    CUtensorMap mq, mk, mv;
+    if (!make_query_map(&mq, q, a, p.tq) || !make_cache_map(&mk, k, a.dtype, a.kp, a.B, a.P, a.Hkv, a.Dh, 128) ||
+        !make_cache_map(&mv, v, a.dtype, a.vp, a.B, a.P, a.Hkv, a.Dh, 128))
+        return PSD_ERR_CUDA;
+    const int64_t grid = (int64_t)a.B * a.Hkv * p.units * (p.n_qt > 1 ? p.splits : p.splits / 2);
+    if (grid > INT32_MAX) return PSD_ERR_SHAPE;
+    const bool bf16 = a.dtype == PSD_BF16;
+    PrefixArgs x = {prefix_len, po, pl, status_dev, (int64_t)a.B * a.D * a.M * a.Hq, a.D * a.M, a.Hq / a.Hkv, a.Hq, a.Hkv, a.Dh, a.P,
+                    p.tq, p.n_qt, p.units, p.splits, a.kp.outer ? 1 : 0, a.kp.head ? 1 : 0, a.vp.outer ? 1 : 0, a.vp.head ? 1 : 0,
+                    a.scale * kLog2e, bf16 ? 1 : 0, wait_limit_cycles()};
+    if (p.dhp == 64) return bf16 ? launch_p<1, true>(mq, mk, mv, x, grid, st) : launch_p<1, false>(mq, mk, mv, x, grid, st);
+    return bf16 ? launch_p<2, true>(mq, mk, mv, x, grid, st) : launch_p<2, false>(mq, mk, mv, x, grid, st);
+}
+
+}  // namespace psd

@@ -1,0 +1,21 @@
+// The prefix part of the drafts' attention (prefix_attention.cu), called by draft_attention.cu.
+#pragma once
+#include "psd_internal.cuh"
+
+namespace psd {
+
+struct PrefixPlan {
+    int tq;        // tokens per query tile (tq * Hq/Hkv <= 128 rows)
+    int n_qt;      // query tiles per sequence and key head
+    int units;     // CTAs along the query tiles
+    int splits;    // partial results per row
+    int dhp;       // floats per partial output row: 64 or 128
+};
+PrefixPlan plan_prefix(int B, int D, int M, int Hq, int Hkv, int Dh, int P);
+
+// Partial results of every row over its sequence's prefix: po [splits][rows][dhp] normalised outputs (not written where
+// the split holds no key), pl [splits][rows] base-2 log-sum-exps (-inf there); row = token * Hq + head.
+int launch_prefix_attention(const void* q, const void* k, const void* v, const int32_t* prefix_len, const psd_attention_t& a,
+                            const PrefixPlan& p, float* po, float* pl, int32_t* status_dev, cudaStream_t st);
+
+}  // namespace psd

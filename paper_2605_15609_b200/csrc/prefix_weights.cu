@@ -160,7 +160,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             const bool all = __all_sync(0xffffffffu, nl[0] > -INFINITY && nl[1] > -INFINITY && nl[2] > -INFINITY && nl[3] > -INFINITY);
             if (it + 1 < n_it) fetch_lse(it + 1, nl);
             __syncwarp();
-            if (!mbar_wait(&s_full[t * 2 + buf], (it >> 1) & 1, wc)) { ok = false; break; }
+            if (!mbar_wait_warp(&s_full[t * 2 + buf], (it >> 1) & 1, wc)) { ok = false; break; }
             tc_fence_after();
             const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((t * 2 + buf) * 128);
 #pragma unroll
