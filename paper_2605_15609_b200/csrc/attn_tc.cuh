@@ -30,6 +30,15 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, c
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, w));
 }
 
+// One lane of a converged warp.  The issuing warps run their loops with all lanes and let the elected one issue: addresses
+// and descriptors then stay in uniform registers.  (With the whole loop under `if (lane == 0)` every operand of every
+// tcgen05.mma is moved there first: eight products took 900 cycles to issue instead of 512 to run.)
+__device__ __forceinline__ bool elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+
 // ---- tcgen05 --------------------------------------------------------------------------------------
 // Instruction descriptor, kind::f16: fp32 accumulator, M = 128, N = n; A and B of one 16-bit type; b_mn: B is stored
 // with its N dimension contiguous (as a tile of V is: keys down, head dimension along).

@@ -64,7 +64,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const bool shared_keys = a.n_qt > 1;          // two query tiles over the same keys
     const int unit = blockIdx.x % a.units;
     const int rest = blockIdx.x / a.units;
@@ -90,51 +90,54 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_holder;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_holder, 0);
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     const WaitCtx wc = {abort_flag, a.status_dev, a.wait_limit, 0u};
     const int L = a.prefix_len ? min(max(a.prefix_len[b], 0), a.P) : a.P;
     const int tiles = (L + 127) / 128;
     // key tiles [t0, t0 + nt) of each stream: split s of a.splits even shares
-    int t0[2], nt[2], sp[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        sp[s] = shared_keys ? cs : cs * 2 + s;
-        t0[s] = (int)((long long)tiles * sp[s] / a.splits);
-        nt[s] = s < n_streams ? (int)((long long)tiles * (sp[s] + 1) / a.splits) - t0[s] : 0;
-    }
-    const int most = max(nt[0], nt[1]);
+    auto share = [&](int x) { return (int)((long long)tiles * x / a.splits); };
+    const int sp0 = shared_keys ? cs : cs * 2, sp1 = shared_keys ? cs : cs * 2 + 1;
+    const int t00 = share(sp0), t01 = share(sp1);
+    const int nt0 = share(sp0 + 1) - t00, nt1 = n_streams > 1 ? share(sp1 + 1) - t01 : 0;
+    const int most = max(nt0, nt1);
     const int n_q = shared_keys ? n_streams : 1;                     // query tiles of this CTA
 
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-        if (warp == 8 && lane == 0 && most > 0) {
+        if (warp == 8 && most > 0) {
             // ---------------------------------------------------------------- loader
-            mbar_arrive_expect_tx(q_full, (uint32_t)(n_q * SLABS * a.tq * a.G * 128));
-            for (int t = 0; t < n_q; ++t)
-                for (int c = 0; c < SLABS; ++c)
-                    tma_load_3d(q_tiles + t * TILE + c * kSlabBytes, &map_q, q_full, c * kSlabElems, h * a.G, b * a.T + (qt0 + t) * a.tq);
+            const bool leader = elect_one();
+            if (leader) {
+                mbar_arrive_expect_tx(q_full, (uint32_t)(n_q * SLABS * a.tq * a.G * 128));
+                for (int t = 0; t < n_q; ++t)
+                    for (int c = 0; c < SLABS; ++c)
+                        tma_load_3d(q_tiles + t * TILE + c * kSlabBytes, &map_q, q_full, c * kSlabElems, h * a.G, b * a.T + (qt0 + t) * a.tq);
+            }
             int item = 0;
             bool ok = true;
-            auto load = [&](bool is_v, int tile) {
+            auto load = [&](const CUtensorMap* map, int head, int outer, int tile) {
                 const int s = item % NS;
-                if (!mbar_wait(&empty[s], ((item / NS) & 1) ^ 1, wc)) { ok = false; return; }
-                mbar_arrive_expect_tx(&full[s], TILE);
-                for (int c = 0; c < SLABS; ++c) {
-                    if (is_v) tma_load_4d(ring + s * TILE + c * kSlabBytes, &map_v, &full[s], c * kSlabElems, h * a.v_head, tile * 128, b * a.v_outer);
-                    else tma_load_4d(ring + s * TILE + c * kSlabBytes, &map_k, &full[s], c * kSlabElems, h * a.k_head, tile * 128, b * a.k_outer);
+                if (!mbar_wait_warp(&empty[s], ((item / NS) & 1) ^ 1, wc)) { ok = false; return; }
+                if (leader) {
+                    mbar_arrive_expect_tx(&full[s], TILE);
+#pragma unroll
+                    for (int c = 0; c < SLABS; ++c)
+                        tma_load_4d(ring + s * TILE + c * kSlabBytes, map, &full[s], c * kSlabElems, head, tile * 128, outer);
                 }
                 ++item;
             };
-            const int ns = shared_keys ? 1 : 2;     // shared: stream 0's list serves both
-            for (int s = 0; ok && s < ns; ++s)
-                if (nt[s] > 0) load(false, t0[s]);
-            for (int j = 0; ok && j < most; ++j)
-                for (int s = 0; ok && s < ns; ++s) {
-                    if (j < nt[s]) load(true, t0[s] + j);
-                    if (ok && j + 1 < nt[s]) load(false, t0[s] + j + 1);
-                }
+            const int kh = h * a.k_head, ko = b * a.k_outer, vh = h * a.v_head, vo = b * a.v_outer;
+            const int na = nt0, nb = shared_keys ? 0 : nt1;     // shared: stream 0's list serves both
+            if (na > 0) load(&map_k, kh, ko, t00);
+            if (ok && nb > 0) load(&map_k, kh, ko, t01);
+            for (int j = 0; ok && j < most; ++j) {
+                if (j < na) load(&map_v, vh, vo, t00 + j);
+                if (ok && j + 1 < na) load(&map_k, kh, ko, t00 + j + 1);
+                if (ok && j < nb) load(&map_v, vh, vo, t01 + j);
+                if (ok && j + 1 < nb) load(&map_k, kh, ko, t01 + j + 1);
+            }
             if (!ok) {
                 // giving up: no copy may be in flight when the CTA exits
                 long long c0 = clock64();
@@ -144,63 +147,88 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                     while (!mbar_try_wait(&full[i % NS], (i / NS) & 1) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
                 }
             }
-        } else if (warp == 9 && lane == 0 && most > 0) {
+        } else if (warp == 9 && most > 0) {
             // ---------------------------------------------------------------- products
+            const bool leader = elect_one();
             const uint32_t id_s = umma_idesc16(128, BF16, false);
             const uint32_t id_o = umma_idesc16((a.Dh + 15) / 16 * 16, BF16, true);
             const int k_steps = (a.Dh + 15) / 16;
-            auto wait_item = [&](int item) { const bool r = mbar_wait(&full[item % NS], (item / NS) & 1, wc); tc_fence_after(); return r; };
-            auto scores = [&](int s, int item) {
-                const unsigned char* q = q_tiles + (shared_keys ? s : 0) * TILE;
-                const unsigned char* k = ring + (item % NS) * TILE;
-                for (int i = 0; i < k_steps; ++i) {
-                    const uint32_t off = (uint32_t)((i / 4) * kSlabBytes);
-                    umma_f16(tmem + s * 128, umma_smem_desc(smem_u32(q) + off) + (uint64_t)((i % 4) * 2),
-                             umma_smem_desc(smem_u32(k) + off) + (uint64_t)((i % 4) * 2), id_s, i != 0);
-                }
-                umma_commit(&s_full[s]);
+            const uint64_t dq = umma_smem_desc(smem_u32(q_tiles)), dk = umma_smem_desc(smem_u32(ring));
+            const uint64_t dv = umma_smem_desc_mn(smem_u32(ring), kSlabBytes);
+            int kslot = 0, vslot = 0;             // ring slots of the K and V tiles at hand
+            int next = 0, nround = 0;             // next ring item: slot and parity of its round
+            auto take = [&](int& slot, uint32_t& parity) {
+                slot = next; parity = nround;
+                if (++next == NS) { next = 0; nround ^= 1; }
             };
-            int next = 0;      // ring items in the loader's order
-            bool ok = mbar_wait(q_full, 0, wc);
-            if (ok && shared_keys) {
-                const int k = next++;
-                ok = wait_item(k);
-                if (ok) {
-                    for (int s = 0; s < n_streams; ++s) scores(s, k);
-                    umma_commit(&empty[k % NS]);
+            auto wait_item = [&](int slot, uint32_t parity) {
+                const bool r = mbar_wait_warp(&full[slot], parity, wc);
+                tc_fence_after();
+                return r;
+            };
+            auto scores = [&](int s, int slot, bool release) {
+                if (leader) {
+                    const uint64_t q = dq + (uint64_t)((shared_keys ? s : 0) * (TILE >> 4)), k = dk + (uint64_t)(slot * (TILE >> 4));
+#pragma unroll
+                    for (int i = 0; i < SLABS * 4; ++i)
+                        if (i < k_steps) {
+                            const uint64_t off = (i / 4) * (kSlabBytes >> 4) + (i % 4) * 2;
+                            umma_f16(tmem + s * 128, q + off, k + off, id_s, i != 0);
+                        }
+                    umma_commit(&s_full[s]);
+                    if (release) umma_commit(&empty[slot]);
                 }
-            } else {
-                for (int s = 0; ok && s < 2; ++s) {
-                    if (nt[s] == 0) continue;
-                    const int k = next++;
-                    if (!(ok = wait_item(k))) break;
-                    scores(s, k);
-                    umma_commit(&empty[k % NS]);
+            };
+            uint32_t kpar = 0, vpar = 0;
+            bool ok = mbar_wait_warp(q_full, 0, wc);
+            if (ok && shared_keys) {
+                take(kslot, kpar);
+                ok = wait_item(kslot, kpar);
+                if (ok) {
+                    scores(0, kslot, n_streams == 1);
+                    if (n_streams > 1) scores(1, kslot, true);
+                }
+            } else if (ok) {
+                if (nt0 > 0) {
+                    take(kslot, kpar);
+                    if ((ok = wait_item(kslot, kpar))) scores(0, kslot, true);
+                }
+                if (ok && nt1 > 0) {
+                    take(kslot, kpar);
+                    if ((ok = wait_item(kslot, kpar))) scores(1, kslot, true);
                 }
             }
             for (int j = 0; ok && j < most; ++j) {
-                int v = 0, k = 0;
-                for (int s = 0; ok && s < n_streams; ++s) {
-                    if (j >= nt[s]) continue;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const int n = s ? nt1 : nt0;
+                    if (!ok || j >= n) continue;
                     const bool first = !shared_keys || s == 0, last = !shared_keys || s == n_streams - 1;
-                    if (first) { v = next++; k = j + 1 < nt[s] ? next++ : -1; }
-                    if (!(ok = mbar_wait(&p_ready[s], j & 1, wc)) || !(ok = wait_item(v))) break;
-                    // keys of this tile in steps of 16 (the last tile may hold fewer)
-                    const int left = L - (t0[s] + j) * 128, steps = left >= 128 ? 8 : (left + 15) / 16;
-                    const uint64_t vd = umma_smem_desc_mn(smem_u32(ring + (v % NS) * TILE), kSlabBytes);
-                    for (int i = 0; i < steps; ++i)
-                        umma_f16_ts(tmem + 256 + s * 128, tmem + s * 128 + i * 8, vd + (uint64_t)(i * (2048 >> 4)), id_o, (j | i) != 0);
-                    umma_commit(&o_done[s]);
-                    if (last) umma_commit(&empty[v % NS]);
-                    if (k >= 0) {
-                        if (!(ok = wait_item(k))) break;
-                        scores(s, k);
-                        if (last) umma_commit(&empty[k % NS]);
+                    const bool more = j + 1 < n;
+                    if (first) {
+                        take(vslot, vpar);
+                        if (more) take(kslot, kpar);
+                    }
+                    if (!(ok = mbar_wait_warp(&p_ready[s], j & 1, wc)) || !(ok = wait_item(vslot, vpar))) continue;
+                    if (leader) {
+                        // keys of this tile in steps of 16 (the last tile may hold fewer)
+                        const int left = L - ((s ? t01 : t00) + j) * 128, steps = left >= 128 ? 8 : (left + 15) / 16;
+                        const uint64_t vd = dv + (uint64_t)(vslot * (TILE >> 4));
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (i < steps)
+                                umma_f16_ts(tmem + 256 + s * 128, tmem + s * 128 + i * 8, vd + (uint64_t)(i * (2048 >> 4)), id_o, (j | i) != 0);
+                        umma_commit(&o_done[s]);
+                        if (last) umma_commit(&empty[vslot]);
+                    }
+                    if (more) {
+                        if (!(ok = wait_item(kslot, kpar))) continue;
+                        scores(s, kslot, last);
                     }
                 }
             }
             if (!ok) {
-                umma_commit(drain);
+                if (leader) umma_commit(drain);
                 const long long c0 = clock64();
                 while (!mbar_try_wait(drain, 0) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
             }
@@ -215,8 +243,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         const f32x2 cc = pack2(a.c, a.c);
         float m = 0.f, l = 0.f;          // reference maximum (scaled by c) and sum relative to it
         bool ok = true;
-        const int n = nt[s];
-        // the ring items of this stream's V tiles, for the zeroing of the last one
+        const int n = s ? nt1 : nt0, first_tile = s ? t01 : t00;
         for (int j = 0; j < n; ++j) {
             if (!mbar_wait_warp(&s_full[s], j & 1, wc)) { ok = false; break; }
             tc_fence_after();
@@ -225,7 +252,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, r[c]);
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_wait_ld(r[c]);
-            const int left = L - (t0[s] + j) * 128;
+            const int left = L - (first_tile + j) * 128;
             if (left < 128) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
@@ -293,10 +320,9 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 if (shared_keys) item = 1 + 2 * j;
                 else {
                     // items before this V: the first K tiles of both streams, then per round V and next K of each stream
-                    item = (nt[0] > 0) + (nt[1] > 0);
-                    for (int q = 0; q < j; ++q)
-                        for (int u = 0; u < 2; ++u) item += (q < nt[u]) + (q + 1 < nt[u]);
-                    if (s == 1) item += (j < nt[0]) + (j + 1 < nt[0]);
+                    item = (nt0 > 0) + (nt1 > 0);
+                    for (int q = 0; q < j; ++q) item += (q < nt0) + (q + 1 < nt0) + (q < nt1) + (q + 1 < nt1);
+                    if (s == 1) item += (j < nt0) + (j + 1 < nt0);
                 }
                 if (!mbar_wait_warp(&full[item % NS], (item / NS) & 1, wc)) { ok = false; break; }
                 const int stop = (left + 15) / 16 * 16;
@@ -315,7 +341,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             const int64_t tok0 = (int64_t)b * a.T + (int64_t)(qt0 + (shared_keys ? s : 0)) * a.tq;
             const int64_t tok = tok0 + row / a.G;
             const bool live = row < a.tq * a.G && tok < (int64_t)(b + 1) * a.T;
-            const int64_t at = (int64_t)sp[s] * a.rows + tok * a.Hq + h * a.G + row % a.G;
+            const int64_t at = (int64_t)(s ? sp1 : sp0) * a.rows + tok * a.Hq + h * a.G + row % a.G;
             if (n > 0) {
                 ok = mbar_wait_warp(&o_done[s], (n - 1) & 1, wc);
                 tc_fence_after();

@@ -48,7 +48,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int kc = blockIdx.x % a.key_ctas;
     const int rest = blockIdx.x / a.key_ctas, split = rest % a.splits, bh = rest / a.splits;
     const int b = bh / a.Hkv, h = bh % a.Hkv;
@@ -70,7 +70,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_holder;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_holder, 0);
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     const WaitCtx wc = {abort_flag, a.status_dev, a.wait_limit, 0u};
@@ -82,20 +82,26 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const int n_kt = L - key0 > 128 ? 2 : 1;      // key tiles that hold keys
 
     if (warp == 8) {
-        if (lane == 0 && n_it > 0) {
-            mbar_arrive_expect_tx(k_full, n_kt * TILE);
-            for (int t = 0; t < n_kt; ++t)
-                for (int s = 0; s < SLABS; ++s)
-                    tma_load_4d(k_tiles + t * TILE + s * kSlabBytes, &map_k, k_full, s * kSlabElems, h * a.k_head, key0 + t * 128, b * a.k_outer);
+        if (n_it > 0) {
+            const bool leader = elect_one();
+            if (leader) {
+                mbar_arrive_expect_tx(k_full, n_kt * TILE);
+                for (int t = 0; t < n_kt; ++t)
+                    for (int s = 0; s < SLABS; ++s)
+                        tma_load_4d(k_tiles + t * TILE + s * kSlabBytes, &map_k, k_full, s * kSlabElems, h * a.k_head, key0 + t * 128, b * a.k_outer);
+            }
             const uint32_t q_bytes = (uint32_t)(SLABS * a.tq * a.G * 128);
             int it = 0;
             bool ok = true;
             for (; it < n_it; ++it) {
                 const int s = it % kQStages;
-                if (!mbar_wait(&q_empty[s], ((it / kQStages) & 1) ^ 1, wc)) { ok = false; break; }
-                mbar_arrive_expect_tx(&q_full[s], q_bytes);
-                for (int c = 0; c < SLABS; ++c)
-                    tma_load_3d(q_tiles + s * TILE + c * kSlabBytes, &map_q, &q_full[s], c * kSlabElems, h * a.G, b * a.T + (q_lo + it) * a.tq);
+                if (!mbar_wait_warp(&q_empty[s], ((it / kQStages) & 1) ^ 1, wc)) { ok = false; break; }
+                if (leader) {
+                    mbar_arrive_expect_tx(&q_full[s], q_bytes);
+#pragma unroll
+                    for (int c = 0; c < SLABS; ++c)
+                        tma_load_3d(q_tiles + s * TILE + c * kSlabBytes, &map_q, &q_full[s], c * kSlabElems, h * a.G, b * a.T + (q_lo + it) * a.tq);
+                }
             }
             if (!ok) {
                 // giving up: no copy may be in flight when the CTA exits
@@ -108,28 +114,35 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             }
         }
     } else if (warp == 9) {
-        if (lane == 0 && n_it > 0) {
+        if (n_it > 0) {
+            const bool leader = elect_one();
             const uint32_t idesc = umma_idesc16(128, a.bf16, false);
             const int k_steps = (a.Dh + 15) / 16;
-            bool ok = mbar_wait(k_full, 0, wc);
+            const uint64_t dk = umma_smem_desc(smem_u32(k_tiles)), dq = umma_smem_desc(smem_u32(q_tiles));
+            bool ok = mbar_wait_warp(k_full, 0, wc);
             for (int it = 0; ok && it < n_it; ++it) {
-                const int s = it % kQStages;
-                if (!mbar_wait(&q_full[s], (it / kQStages) & 1, wc)) { ok = false; break; }
-                const int buf = it & 1;
-                for (int t = 0; t < n_kt; ++t) {
-                    if (!mbar_wait(&s_empty[t * 2 + buf], ((it >> 1) & 1) ^ 1, wc)) { ok = false; break; }
+                const int s = it % kQStages, buf = it & 1;
+                if (!mbar_wait_warp(&q_full[s], (it / kQStages) & 1, wc)) { ok = false; break; }
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    if (!ok || t >= n_kt) continue;
+                    if (!mbar_wait_warp(&s_empty[t * 2 + buf], ((it >> 1) & 1) ^ 1, wc)) { ok = false; continue; }
                     tc_fence_after();
-                    for (int k = 0; k < k_steps; ++k) {
-                        const uint32_t off = (uint32_t)((k / 4) * kSlabBytes), in = (uint64_t)((k % 4) * 2);
-                        umma_f16(tmem + (t * 2 + buf) * 128, umma_smem_desc(smem_u32(k_tiles + t * TILE) + off) + in,
-                                 umma_smem_desc(smem_u32(q_tiles + s * TILE) + off) + in, idesc, k != 0);
+                    if (leader) {
+                        const uint64_t k = dk + (uint64_t)(t * (TILE >> 4)), q = dq + (uint64_t)(s * (TILE >> 4));
+#pragma unroll
+                        for (int i = 0; i < SLABS * 4; ++i)
+                            if (i < k_steps) {
+                                const uint64_t off = (i / 4) * (kSlabBytes >> 4) + (i % 4) * 2;
+                                umma_f16(tmem + (t * 2 + buf) * 128, k + off, q + off, idesc, i != 0);
+                            }
+                        umma_commit(&s_full[t * 2 + buf]);
                     }
-                    umma_commit(&s_full[t * 2 + buf]);
                 }
-                if (ok) umma_commit(&q_empty[s]);
+                if (ok && leader) umma_commit(&q_empty[s]);
             }
             if (!ok) {
-                umma_commit(drain);
+                if (leader) umma_commit(drain);
                 const long long t0 = clock64();
                 while (!mbar_try_wait(drain, 0) && clock64() - t0 < WAIT_LIMIT_CYCLES) {}
             }
