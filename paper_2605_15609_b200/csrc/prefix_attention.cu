@@ -24,6 +24,10 @@ namespace psd {
 namespace {
 
 constexpr int kPThreads = 384;              // warps 0-3, 4-7: softmax of stream 0, 1; 8: TMA; 9: MMA; 10, 11 idle
+#ifndef PSD_POLY
+#define PSD_POLY 3
+#endif
+constexpr int kPolyPairs = PSD_POLY;            // of 8 pairs of scores, those whose exponential is a polynomial
 constexpr float kRaise = 8.0f;              // growth of a row's maximum (log2) that triggers a rescale
 
 template <int SLABS> struct Ring { static constexpr int N = SLABS == 2 ? 5 : 8; };
@@ -60,7 +64,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     unsigned char* ring = smem + 2 * TILE;                           // [NS][TILE]
     uint64_t* bars = reinterpret_cast<uint64_t*>(ring + NS * TILE);
     uint64_t *q_full = bars, *full = bars + 1, *empty = full + NS, *s_full = empty + NS /* [2] */, *p_ready = s_full + 2,
-             *o_done = p_ready + 2, *drain = o_done + 2;
+             *o_done = p_ready + 2 /* [2] */, *drain = o_done + 2;
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
 
@@ -149,81 +153,64 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             }
         } else if (warp == 9 && most > 0) {
             // ---------------------------------------------------------------- products
+            // One warp issues both streams' products in turn: left to themselves (a warp each) the streams fall into step, and
+            // their softmaxes and their products each wait for one another.
             const bool leader = elect_one();
             const uint32_t id_s = umma_idesc16(128, BF16, false);
             const uint32_t id_o = umma_idesc16((a.Dh + 15) / 16 * 16, BF16, true);
             const int k_steps = (a.Dh + 15) / 16;
             const uint64_t dq = umma_smem_desc(smem_u32(q_tiles)), dk = umma_smem_desc(smem_u32(ring));
             const uint64_t dv = umma_smem_desc_mn(smem_u32(ring), kSlabBytes);
-            int kslot = 0, vslot = 0;             // ring slots of the K and V tiles at hand
-            int next = 0, nround = 0;             // next ring item: slot and parity of its round
-            auto take = [&](int& slot, uint32_t& parity) {
-                slot = next; parity = nround;
-                if (++next == NS) { next = 0; nround ^= 1; }
-            };
-            auto wait_item = [&](int slot, uint32_t parity) {
-                const bool r = mbar_wait_warp(&full[slot], parity, wc);
-                tc_fence_after();
-                return r;
-            };
-            auto scores = [&](int s, int slot, bool release) {
-                if (leader) {
-                    const uint64_t q = dq + (uint64_t)((shared_keys ? s : 0) * (TILE >> 4)), k = dk + (uint64_t)(slot * (TILE >> 4));
+            auto wait_item = [&](int item) { return mbar_wait_warp(&full[item % NS], (item / NS) & 1, wc); };
+            auto scores = [&](int s, int item, bool release) {
+                const uint64_t q = dq + (uint64_t)((shared_keys ? s : 0) * (TILE >> 4)), k = dk + (uint64_t)((item % NS) * (TILE >> 4));
 #pragma unroll
-                    for (int i = 0; i < SLABS * 4; ++i)
-                        if (i < k_steps) {
-                            const uint64_t off = (i / 4) * (kSlabBytes >> 4) + (i % 4) * 2;
-                            umma_f16(tmem + s * 128, q + off, k + off, id_s, i != 0);
-                        }
-                    umma_commit(&s_full[s]);
-                    if (release) umma_commit(&empty[slot]);
-                }
+                for (int i = 0; i < SLABS * 4; ++i)
+                    if (i < k_steps) {
+                        const uint64_t off = (i / 4) * (kSlabBytes >> 4) + (i % 4) * 2;
+                        umma_f16(tmem + s * 128, q + off, k + off, id_s, i != 0);
+                    }
+                umma_commit(&s_full[s]);
+                if (release) umma_commit(&empty[item % NS]);
             };
-            uint32_t kpar = 0, vpar = 0;
+            int next = 0;      // ring items, in the loader's order
             bool ok = mbar_wait_warp(q_full, 0, wc);
-            if (ok && shared_keys) {
-                take(kslot, kpar);
-                ok = wait_item(kslot, kpar);
-                if (ok) {
-                    scores(0, kslot, n_streams == 1);
-                    if (n_streams > 1) scores(1, kslot, true);
+            int k_of[2] = {-1, -1};
+            if (nt0 > 0) k_of[0] = next++;
+            if (nt1 > 0) k_of[1] = shared_keys ? 0 : next++;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                if (ok && k_of[s] >= 0 && (ok = wait_item(k_of[s]))) {
+                    tc_fence_after();
+                    if (leader) scores(s, k_of[s], !shared_keys || s == n_streams - 1);
                 }
-            } else if (ok) {
-                if (nt0 > 0) {
-                    take(kslot, kpar);
-                    if ((ok = wait_item(kslot, kpar))) scores(0, kslot, true);
-                }
-                if (ok && nt1 > 0) {
-                    take(kslot, kpar);
-                    if ((ok = wait_item(kslot, kpar))) scores(1, kslot, true);
-                }
-            }
+            int v = 0, k = 0;
             for (int j = 0; ok && j < most; ++j) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     const int n = s ? nt1 : nt0;
                     if (!ok || j >= n) continue;
-                    const bool first = !shared_keys || s == 0, last = !shared_keys || s == n_streams - 1;
-                    const bool more = j + 1 < n;
+                    const bool first = !shared_keys || s == 0, last = !shared_keys || s == n_streams - 1, more = j + 1 < n;
                     if (first) {
-                        take(vslot, vpar);
-                        if (more) take(kslot, kpar);
+                        v = next++;
+                        k = more ? next++ : v;
+                        // the tiles have usually landed long before the weights are ready
+                        if (!(ok = wait_item(v) && wait_item(k))) continue;
                     }
-                    if (!(ok = mbar_wait_warp(&p_ready[s], j & 1, wc)) || !(ok = wait_item(vslot, vpar))) continue;
+                    if (!(ok = mbar_wait_warp(&p_ready[s], j & 1, wc))) continue;
+                    tc_fence_after();
                     if (leader) {
                         // keys of this tile in steps of 16 (the last tile may hold fewer)
                         const int left = L - ((s ? t01 : t00) + j) * 128, steps = left >= 128 ? 8 : (left + 15) / 16;
-                        const uint64_t vd = dv + (uint64_t)(vslot * (TILE >> 4));
+                        const uint64_t vd = dv + (uint64_t)((v % NS) * (TILE >> 4));
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
                             if (i < steps)
                                 umma_f16_ts(tmem + 256 + s * 128, tmem + s * 128 + i * 8, vd + (uint64_t)(i * (2048 >> 4)), id_o, (j | i) != 0);
-                        umma_commit(&o_done[s]);
-                        if (last) umma_commit(&empty[vslot]);
-                    }
-                    if (more) {
-                        if (!(ok = wait_item(kslot, kpar))) continue;
-                        scores(s, kslot, last);
+                        // the scores of the next tile overwrite the weights just read; their commit covers PV as well
+                        if (more) scores(s, k, last);
+                        else umma_commit(&o_done[s]);
+                        if (last) umma_commit(&empty[v % NS]);
                     }
                 }
             }
@@ -248,37 +235,34 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             if (!mbar_wait_warp(&s_full[s], j & 1, wc)) { ok = false; break; }
             tc_fence_after();
             uint32_t r[4][32];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, r[c]);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_wait_ld(r[c]);
+            float mx[4];
             const int left = L - (first_tile + j) * 128;
-            if (left < 128) {
+            tmem_ld32(t_s, r[0]);
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
+            for (int c = 0; c < 4; ++c) {
+                tmem_wait_ld(r[c]);
+                if (c < 3) tmem_ld32(t_s + (c + 1) * 32, r[c + 1]);     // arrives while this chunk's maximum is taken
+                if (left < 128) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
                         if (c * 32 + i >= left) r[c][i] = 0xff800000u;
-            }
-            float mx[4];
+                }
+                auto x = [&](int i) { return __uint_as_float(r[c][i]); };
+                float u = max3(x(0), x(1), x(2)), v = max3(x(3), x(4), x(5));
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                mx[c] = __uint_as_float(r[c][0]);
-#pragma unroll
-                for (int i = 1; i < 31; i += 2) mx[c] = fmaxf(fmaxf(mx[c], __uint_as_float(r[c][i])), __uint_as_float(r[c][i + 1]));
-                mx[c] = fmaxf(mx[c], __uint_as_float(r[c][31]));
+                for (int i = 6; i < 30; i += 4) { u = max3(u, x(i), x(i + 1)); v = max3(v, x(i + 2), x(i + 3)); }
+                mx[c] = max3(fmaxf(u, v), x(30), x(31));
             }
             const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.c;
             if (j == 0) {
                 m = top == -INFINITY ? 0.f : top;
             } else if (__any_sync(0xffffffffu, top > m + kRaise)) {
-                // rare: raise the reference and rescale what has been summed (PV of the tile before must be done)
+                // rare: raise the reference and rescale what has been summed (PV of the tile before is done: these scores were
+                // committed after it)
                 const float mn = top > m + kRaise ? top : m;
                 const float f = ex2(m - mn);
                 m = mn;
                 l *= f;
-                if (!mbar_wait_warp(&o_done[s], (j - 1) & 1, wc)) { ok = false; break; }
-                tc_fence_after();
                 for (int c = 0; c < a.Dh; c += 8) {
                     uint32_t o[8];
                     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -295,27 +279,28 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 tmem_wait_st();
             }
             const f32x2 nm = pack2(-m, -m);
-            f32x2 acc = pack2(0.f, 0.f);
+            f32x2 acc[2] = {0ull, 0ull};
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 uint32_t p[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    float x, y;
-                    unpack2(fma2(pack2(__uint_as_float(r[c][2 * i]), __uint_as_float(r[c][2 * i + 1])), cc, nm), x, y);
-                    x = ex2(x);
-                    y = ex2(y);
-                    acc = add2(acc, pack2(x, y));
-                    p[i] = pack16(x, y, BF16);
+                    const f32x2 x = fma2(pack2(__uint_as_float(r[c][2 * i]), __uint_as_float(r[c][2 * i + 1])), cc, nm);
+                    const f32x2 e = i % 8 < kPolyPairs ? ex2_poly<4, false>(x) : ex2_pair(x);
+                    acc[i & 1] = add2(acc[i & 1], e);
+                    float u, v;
+                    unpack2(e, u, v);
+                    p[i] = pack16(u, v, BF16);
                 }
                 tmem_st16(t_s + c * 16, p);
             }
             float l0, l1;
-            unpack2(acc, l0, l1);
+            unpack2(add2(acc[0], acc[1]), l0, l1);
             l += l0 + l1;
             tmem_wait_st();
-            if (left < 128 && (s == 0 || !shared_keys)) {
-                // V rows past the end that the product's last step of 16 keys reads: zero, whatever the cache holds there
+            if (left < 128) {
+                // V rows past the end that the product's last step of 16 keys reads: zero, whatever the cache holds there (streams
+                // that share the tile both do it: the same zeros)
                 int item;
                 if (shared_keys) item = 1 + 2 * j;
                 else {
@@ -343,7 +328,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             const bool live = row < a.tq * a.G && tok < (int64_t)(b + 1) * a.T;
             const int64_t at = (int64_t)(s ? sp1 : sp0) * a.rows + tok * a.Hq + h * a.G + row % a.G;
             if (n > 0) {
-                ok = mbar_wait_warp(&o_done[s], (n - 1) & 1, wc);
+                ok = mbar_wait_warp(&o_done[s], 0, wc);
                 tc_fence_after();
                 if (ok) {
                     const float inv = 1.0f / l;
