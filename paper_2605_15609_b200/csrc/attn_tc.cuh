@@ -25,9 +25,26 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, u
                  : "memory");
 }
 
-// A bounded wait of a whole warp: every lane gets the same answer, so that warp-wide instructions may follow.
+// A bounded wait of a whole warp: every lane gets the same answer, so that warp-wide instructions may follow.  The loop must
+// not be unrolled: 256 tries in a row at every wait made 137 KB of code out of the prefix attention's kernel, more than the
+// instruction caches hold, and the code between two waits was then fetched from L2 every time.
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, const WaitCtx& w) {
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, w));
+    bool r = mbar_try_wait(bar, parity);
+    if (!r) {
+        const long long t0 = clock64();
+#pragma unroll 1
+        for (int i = 1;; ++i) {
+            r = mbar_try_wait(bar, parity);
+            if (r) break;
+            if (i & 63) continue;
+            if (*w.abort_flag) break;
+            if (clock64() - t0 > w.limit) {
+                raise_abort(w);
+                break;
+            }
+        }
+    }
+    return __all_sync(0xffffffffu, r);
 }
 
 // One lane of a converged warp.  The issuing warps run their loops with all lanes and let the elected one issue: addresses
