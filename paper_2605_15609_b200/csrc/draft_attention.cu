@@ -2,9 +2,14 @@
 //
 // One CTA takes up to 16 * WM rows (query tokens times the heads of one key head) of one draft and walks the keys in
 // tiles of 64 with a running maximum and sum per row; WK = 4 / WM warps share a 16-row block and take 64 / WK keys of
-// every tile each, and join their maxima, sums and outputs at the end.  Products are m16n8k16 tensor instructions with
-// fp32 accumulation; K and V tiles are double-buffered by asynchronous copies that fill what lies past a length (or past
-// Dh) with zeros, so nothing that was never written is multiplied, and a CTA only ever reads its own draft's keys.
+// every tile each.  Products are m16n8k16 tensor instructions with fp32 accumulation: a draft has few keys of its own (a
+// block of 32 or 64), and tiles of 128 keys shared with other drafts would let one draft's NaN reach another's rows.  K and
+// V tiles are double-buffered by asynchronous copies that fill what lies past a length (or past Dh) with zeros, so nothing
+// that was never written is multiplied.
+//
+// What the warps of a row block hold and the partial results over the prefix are then joined row by row, a warp per row
+// and all lanes along Dh: the kernel's time is the traffic of those partial results (4 bytes per output element and split
+// against 2 written), and this order reads and writes whole lines.
 #include "attn_tc.cuh"
 #include "prefix_attention.cuh"
 
@@ -59,11 +64,99 @@ struct OwnArgs {
     float* lse;
     psd_attention_t a;
     int row_blocks;      // CTAs per (node, key head)
+    int stages;          // 1: no more than one tile of keys, 2
     // partial results over the prefix (prefix_attention.cu), or NULL: this kernel walks the prefix's keys itself
     const float *po, *pl;
-    int splits, dhp;
+    int splits;          // <= kMaxPrefixSplits
     int64_t rows;
 };
+
+// Joins the rows warp, warp + 4, .. of a CTA: WK warps' results in shared memory and the splits' in global memory, RB rows
+// and SP splits at a time.  A warp per row, lanes along Dh.
+template <typename T, int DHP, int WK, int RB, int SP>
+__device__ __forceinline__ void join_rows(const OwnArgs& p, const float* so, const float* sm, int row0, int row_end, int node, int h,
+                                          int warp, int lane) {
+    constexpr int E = DHP / 32;                              // elements per lane: 2 or 4
+    constexpr int OLD = DHP + 8;
+    const psd_attention_t& a = p.a;
+    const int G = a.Hq / a.Hkv;
+    const bool in = lane * E < a.Dh;                         // columns past Dh were not written
+    for (int r0 = warp; r0 < row_end; r0 += 4 * RB) {
+        int64_t at[RB], t[RB];
+        float z[RB][2], y[RB][SP][E];                        // log2-sums of splits lane, lane + 32; outputs of SP splits
+        auto fetch = [&](int k, int x0) {
+#pragma unroll
+            for (int u = 0; u < SP; ++u) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) y[k][u][e] = 0.f;
+                if (in && x0 + u < p.splits) {
+                    const float* po = p.po + ((x0 + u) * p.rows + at[k]) * DHP + lane * E;
+                    if (E == 4) *reinterpret_cast<float4*>(y[k][u]) = __ldcs(reinterpret_cast<const float4*>(po));
+                    else *reinterpret_cast<float2*>(y[k][u]) = __ldcs(reinterpret_cast<const float2*>(po));
+                }
+            }
+        };
+        int hh[RB];
+#pragma unroll
+        for (int k = 0; k < RB; ++k) {
+            const int rr = row0 + min(r0 + 4 * k, row_end - 1), i = rr / G;
+            hh[k] = h * G + rr % G;
+            t[k] = (int64_t)node * a.M + i;
+            at[k] = t[k] * a.Hq + hh[k];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) z[k][q] = lane + 32 * q < p.splits ? p.pl[(lane + 32 * q) * p.rows + at[k]] : -INFINITY;
+            fetch(k, 0);
+        }
+#pragma unroll
+        for (int k = 0; k < RB; ++k) {
+            const int r = r0 + 4 * k;
+            if (r >= row_end) break;
+            float top = fmaxf(z[k][0], z[k][1]);
+#pragma unroll
+            for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+            const int r16 = (r / 16) * WK * 16 + r % 16;     // this row in the first of its warps
+#pragma unroll
+            for (int w = 0; w < WK; ++w) top = fmaxf(top, sm[r16 + w * 16]);
+            const float base = top == -INFINITY ? 0.f : top;
+            float acc[E], sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll
+            for (int w = 0; w < WK; ++w) {
+                const float f = ex2(sm[r16 + w * 16] - base);
+                sum = fmaf(f, sm[64 + r16 + w * 16], sum);
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = fmaf(f, so[(r16 + w * 16) * OLD + lane * E + e], acc[e]);
+            }
+#pragma unroll 1
+            for (int x0 = 0; x0 < p.splits; x0 += SP) {
+                if (x0) fetch(k, x0);
+#pragma unroll
+                for (int u = 0; u < SP; ++u) {
+                    const int x = x0 + u;
+                    const float zx = __shfl_sync(0xffffffffu, x < 32 ? z[k][0] : z[k][1], x & 31);
+                    if (x < p.splits && zx != -INFINITY) {
+                        const float wt = ex2(zx - base);
+                        sum += wt;
+#pragma unroll
+                        for (int e = 0; e < E; ++e) acc[e] = fmaf(wt, y[k][u][e], acc[e]);
+                    }
+                }
+            }
+            const bool none = top == -INFINITY && sum == 0.f;
+            const float inv = none ? 0.f : 1.f / sum;
+            if (in) {
+                uint32_t pk[E / 2];
+#pragma unroll
+                for (int e = 0; e < E / 2; ++e) pk[e] = Mma<T>::pack(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+                T* out = reinterpret_cast<T*>(p.out) + t[k] * a.out_token + (int64_t)hh[k] * a.out_head + lane * E;
+                if (E == 4) *reinterpret_cast<uint2*>(out) = make_uint2(pk[0], pk[E / 2 - 1]);
+                else *reinterpret_cast<uint32_t*>(out) = pk[0];
+            }
+            if (p.lse && lane == 0) p.lse[at[k]] = none ? -INFINITY : top * kLn2 + logf(sum);
+        }
+    }
+}
 
 template <typename T, int DHP, int WM>
 __global__ void __launch_bounds__(kThreads) draft_attention_kernel(const OwnArgs p) {
@@ -210,94 +303,29 @@ __global__ void __launch_bounds__(kThreads) draft_attention_kernel(const OwnArgs
         l[u] += __shfl_xor_sync(0xffffffffu, l[u], 1);
         l[u] += __shfl_xor_sync(0xffffffffu, l[u], 2);
     }
-    if (WK > 1) {
-        // join the warps of a row block: maxima and sums first, then the outputs, in warp order
-        float* sm = reinterpret_cast<float*>(smem);             // [4 warps][16] max, then sum
-        float* so = sm + 4 * 16 * 2;                             // [4 warps][16][DHP]
-        const int row = lane >> 2;
-        if ((lane & 3) == 0) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                sm[warp * 16 + row + 8 * u] = m[u];
-                sm[64 + warp * 16 + row + 8 * u] = l[u];
-            }
-        }
-#pragma unroll
-        for (int n = 0; n < NO; ++n)
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-                *reinterpret_cast<float2*>(&so[(warp * 16 + row + 8 * u) * DHP + n * 8 + (lane & 3) * 2]) =
-                    make_float2(o[n][2 * u], o[n][2 * u + 1]);
-        __syncthreads();
-        if (wk != 0) return;
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            float f[WK], mj = -INFINITY;
-#pragma unroll
-            for (int w = 0; w < WK; ++w) mj = fmaxf(mj, sm[(warp + w) * 16 + row + 8 * u]);
-            const float base = mj == -INFINITY ? 0.f : mj;
-            l[u] = 0.f;
-#pragma unroll
-            for (int w = 0; w < WK; ++w) {
-                f[w] = ex2(sm[(warp + w) * 16 + row + 8 * u] - base);
-                l[u] += f[w] * sm[64 + (warp + w) * 16 + row + 8 * u];
-            }
-            m[u] = mj;
-#pragma unroll
-            for (int n = 0; n < NO; ++n) {
-                float x = 0.f, y = 0.f;
-#pragma unroll
-                for (int w = 0; w < WK; ++w) {
-                    const float2 z = *reinterpret_cast<const float2*>(&so[((warp + w) * 16 + row + 8 * u) * DHP + n * 8 + (lane & 3) * 2]);
-                    x += f[w] * z.x;
-                    y += f[w] * z.y;
-                }
-                o[n][2 * u] = x;
-                o[n][2 * u + 1] = y;
-            }
-        }
-    }
-    if (p.po) asm volatile("griddepcontrol.wait;" ::: "memory");
+    // every warp's rows to shared memory (the tiles are no longer needed: the loop ends with a barrier)
+    constexpr int OLD = DHP + 8;                             // padded row: the float2 stores of 8 rows hit different banks
+    float* so = reinterpret_cast<float*>(smem);              // [4 warps][16][OLD]
+    float* sm = so + 4 * 16 * OLD;                           // [4 warps][16] maxima, then sums
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-        if (!live[u]) continue;
-        const int r = r0 + 8 * u, i = r / G, g = r % G;
-        const int64_t t = (int64_t)node * a.M + i;
-        if (p.po) {
-            // join the prefix's partial results, in order: out = (2^(m-T) o + sum_i 2^(z_i-T) O_i) / (2^(m-T) l + sum_i 2^(z_i-T))
-            const int64_t at = t * a.Hq + h * G + g;
-            float T2 = m[u];
-            for (int x = 0; x < p.splits; ++x) T2 = fmaxf(T2, p.pl[x * p.rows + at]);
-            const float f = m[u] == -INFINITY ? 1.f : ex2(m[u] - T2);
-            l[u] *= f;
+        const int r = warp * 16 + (lane >> 2) + 8 * u;
 #pragma unroll
-            for (int n = 0; n < NO; ++n) { o[n][2 * u] *= f; o[n][2 * u + 1] *= f; }
-            for (int x = 0; x < p.splits; ++x) {
-                const float z = p.pl[x * p.rows + at];
-                if (z == -INFINITY) continue;                    // the split held no key: its output was not written
-                const float w = ex2(z - T2);
-                const float* po = p.po + (x * p.rows + at) * p.dhp + (lane & 3) * 2;
-                l[u] += w;
-#pragma unroll
-                for (int n = 0; n < NO; ++n) {
-                    if (n * 8 >= a.Dh) break;
-                    const float2 y = *reinterpret_cast<const float2*>(po + n * 8);
-                    o[n][2 * u] = fmaf(w, y.x, o[n][2 * u]);
-                    o[n][2 * u + 1] = fmaf(w, y.y, o[n][2 * u + 1]);
-                }
-            }
-            m[u] = T2;
+        for (int n = 0; n < NO; ++n)
+            *reinterpret_cast<float2*>(&so[r * OLD + n * 8 + (lane & 3) * 2]) = make_float2(o[n][2 * u], o[n][2 * u + 1]);
+        if ((lane & 3) == 0) {
+            sm[r] = m[u];
+            sm[64 + r] = l[u];
         }
-        const bool none = m[u] == -INFINITY && l[u] == 0.f;
-        const float inv = none ? 0.f : 1.f / l[u];
-        T* out = reinterpret_cast<T*>(p.out) + t * a.out_token + (int64_t)(h * G + g) * a.out_head;
-#pragma unroll
-        for (int n = 0; n < NO; ++n) {
-            const int d = n * 8 + (lane & 3) * 2;
-            if (d < a.Dh) *reinterpret_cast<uint32_t*>(out + d) = Mma<T>::pack(o[n][2 * u] * inv, o[n][2 * u + 1] * inv);
-        }
-        if (p.lse && (lane & 3) == 0) p.lse[t * a.Hq + h * G + g] = none ? -INFINITY : m[u] * kLn2 + logf(l[u]);
     }
+    __syncthreads();
+    if (p.po) asm volatile("griddepcontrol.wait;" ::: "memory");
+    // out = (sum_w 2^(m_w-T) O_w + sum_x 2^(z_x-T) P_x) / (sum_w 2^(m_w-T) l_w + sum_x 2^(z_x-T)), in this order
+    const int row_end = min(16 * WM, rows - rb * 16 * WM);
+    // Few splits: several rows at a time, their loads issued together and before it is known which splits hold keys
+    // (what a split without keys did not write is loaded and dropped).  Many splits: eight splits at a time.
+    if (p.splits <= 2) join_rows<T, DHP, WK, 4, 2>(p, so, sm, rb * 16 * WM, row_end, node, h, warp, lane);
+    else join_rows<T, DHP, WK, 1, 8>(p, so, sm, rb * 16 * WM, row_end, node, h, warp, lane);
 }
 
 template <typename T, int DHP, int WM>
@@ -307,10 +335,12 @@ int launch_rows(OwnArgs& p, cudaStream_t st) {
     p.row_blocks = (rows + 16 * WM - 1) / (16 * WM);
     const int64_t grid = (int64_t)a.B * a.D * a.Hkv * p.row_blocks;
     if (grid > INT32_MAX) return PSD_ERR_SHAPE;
-    constexpr int tile_bytes = 2 * 2 * kKeys * (DHP + 8) * 2, join_bytes = (4 * 16 * 2 + 4 * 16 * DHP) * 4;
-    constexpr int smem = tile_bytes > join_bytes ? tile_bytes : join_bytes;
+    const int64_t tiles = (int64_t)(p.po ? 0 : (a.P + kKeys - 1) / kKeys) + (a.S + kKeys - 1) / kKeys;
+    p.stages = tiles > 1 ? 2 : 1;
+    constexpr int tile_bytes = 2 * kKeys * (DHP + 8) * 2, join_bytes = (4 * 16 * (DHP + 8) + 4 * 16 * 2) * 4;
+    const int smem = p.stages * tile_bytes > join_bytes ? p.stages * tile_bytes : join_bytes;
     static std::atomic<unsigned long long> set{0};
-    if (!ensure_dynamic_smem(draft_attention_kernel<T, DHP, WM>, smem, set)) return PSD_ERR_CUDA;
+    if (!ensure_dynamic_smem(draft_attention_kernel<T, DHP, WM>, 2 * tile_bytes, set)) return PSD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(kThreads);
@@ -325,11 +355,15 @@ int launch_rows(OwnArgs& p, cudaStream_t st) {
     count_launch();
     return e == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
 }
+// Rows per CTA: 64 where that still gives every SM two CTAs, fewer otherwise (then four warps share the keys and the join of
+// a row block).
 template <typename T, int DHP>
 int launch_dh(OwnArgs& p, cudaStream_t st) {
     const int rows = p.a.M * (p.a.Hq / p.a.Hkv);
-    return rows <= 16 ? launch_rows<T, DHP, 1>(p, st) : rows <= 32 ? launch_rows<T, DHP, 2>(p, st)
-                                                                   : launch_rows<T, DHP, 4>(p, st);
+    const int64_t nh = (int64_t)p.a.B * p.a.D * p.a.Hkv, want = 2 * sm_count();
+    if (rows > 32 && nh * ((rows + 63) / 64) >= want) return launch_rows<T, DHP, 4>(p, st);
+    if (rows > 16 && nh * ((rows + 31) / 32) >= want) return launch_rows<T, DHP, 2>(p, st);
+    return launch_rows<T, DHP, 1>(p, st);
 }
 
 }  // namespace
@@ -343,7 +377,7 @@ size_t draft_attention_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, i
 int launch_draft_attention(const void* q, const void* k_prefix, const void* v_prefix, const int32_t* prefix_len,
                            const void* k_own, const void* v_own, const int32_t* own_len, const psd_attention_t& a,
                            void* out, float* lse, void* workspace, int32_t* status_dev, cudaStream_t st) {
-    OwnArgs p = {q, k_prefix, v_prefix, k_own, v_own, prefix_len, own_len, out, lse, a, 0, nullptr, nullptr, 0, 0, 0};
+    OwnArgs p = {q, k_prefix, v_prefix, k_own, v_own, prefix_len, own_len, out, lse, a, 0, 1, nullptr, nullptr, 0, 0};
     if (a.P > 0) {
         const PrefixPlan plan = plan_prefix(a.B, a.D, a.M, a.Hq, a.Hkv, a.Dh, a.P);
         p.rows = (int64_t)a.B * a.D * a.M * a.Hq;
@@ -353,7 +387,6 @@ int launch_draft_attention(const void* q, const void* k_prefix, const void* v_pr
         p.po = po;
         p.pl = pl;
         p.splits = plan.splits;
-        p.dhp = plan.dhp;
     }
     if (a.dtype == PSD_BF16) return a.Dh <= 64 ? launch_dh<__nv_bfloat16, 64>(p, st) : launch_dh<__nv_bfloat16, 128>(p, st);
     return a.Dh <= 64 ? launch_dh<__half, 64>(p, st) : launch_dh<__half, 128>(p, st);

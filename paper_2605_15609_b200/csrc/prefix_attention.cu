@@ -422,6 +422,7 @@ PrefixPlan plan_prefix(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
     int64_t s = sm_count() / ctas;
     const int per = p.n_qt > 1 ? 1 : 2;                 // splits a CTA writes
     if (s * per > tiles / kMinTiles) s = tiles / kMinTiles / per;
+    if (s * per > kMaxPrefixSplits) s = kMaxPrefixSplits / per;
     if (s < 1) s = 1;
     p.splits = (int)s * per;
     p.dhp = Dh <= 64 ? 64 : 128;

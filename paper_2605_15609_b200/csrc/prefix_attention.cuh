@@ -4,6 +4,8 @@
 
 namespace psd {
 
+constexpr int kMaxPrefixSplits = 64;   // two per lane of the warp that joins a row
+
 struct PrefixPlan {
     int tq;        // tokens per query tile (tq * Hq/Hkv <= 128 rows)
     int n_qt;      // query tiles per sequence and key head
