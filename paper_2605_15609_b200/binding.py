@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -152,19 +153,19 @@ def _load() -> ctypes.CDLL:
     lib.psd_attention_workspace_bytes.restype = _sz
     lib.psd_attention_workspace_bytes.argtypes = [_i32] * 8
     lib.psd_draft_attention.restype = ctypes.c_int
-    lib.psd_draft_attention.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.POINTER(PsdAttention), _vp, _vp, _vp,
+    lib.psd_draft_attention.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                         _sz, _vp, _vp]
     lib.psd_weights_workspace_bytes.restype = _sz
     lib.psd_weights_workspace_bytes.argtypes = [_i32] * 7
     lib.psd_prefix_weights.restype = ctypes.c_int
-    lib.psd_prefix_weights.argtypes = [_vp, _vp, _vp, _vp, ctypes.POINTER(PsdAttention), _f32, _vp, _vp, _vp, _sz, _vp,
+    lib.psd_prefix_weights.argtypes = [_vp, _vp, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _sz, _vp,
                                        _vp]
     lib.psd_prefix_evict.restype = ctypes.c_int
-    lib.psd_prefix_evict.argtypes = [_vp, _vp, _vp, _vp, ctypes.POINTER(PsdEvict), _vp, _vp, _vp, _vp, _vp, _vp]
+    lib.psd_prefix_evict.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
     lib.psd_logits_workspace_bytes.restype = _sz
     lib.psd_logits_workspace_bytes.argtypes = [_i32, _i32]
     lib.psd_confidence_logits.restype = ctypes.c_int
-    lib.psd_confidence_logits.argtypes = [_vp, _i32, _i64, _i32, _i32, _i32, _i32, ctypes.POINTER(PsdLogitsEdit), _vp,
+    lib.psd_confidence_logits.argtypes = [_vp, _i32, _i64, _i32, _i32, _i32, _i32, _vp, _vp,
                                           _vp, _vp, _vp, _sz, _vp, _vp]
     lib.psd_set_confidence_impl.restype = ctypes.c_int
     lib.psd_set_confidence_impl.argtypes = [ctypes.c_int]
@@ -524,33 +525,46 @@ def psd_verify_accept_dag(tokV, confV, sigma, draft_tokens, draft_mask, p: PsdPo
 
 
 # ---- around the step: attention of the drafts, the prefix's cache, confidences from logits -------------------------
+#
+# These calls are made many times per forward pass (once per layer), on work that can be a few microseconds long, so their
+# marshalling is kept short: descriptors are packed into bytes in the layout of the C structs (PsdAttention, PsdEvict and
+# PsdLogitsEdit describe the same layouts), and the current stream's handle is asked for without building a Stream object.
 
 PSD_BF16, PSD_FP16, PSD_FP32 = 0, 1, 2
 _DTYPES = {torch.bfloat16: PSD_BF16, torch.float16: PSD_FP16, torch.float32: PSD_FP32}
+_I32, _F32 = torch.int32, torch.float32
+_pack_attention = struct.Struct("=10ifi4q12q").pack
+_pack_evict = struct.Struct("=8i12q").pack
+_pack_edit = struct.Struct("=6Q3i3fi4x").pack
 
 
-def _dtype(*tensors):
-    """The one element type of the tensors that are given (a type the library does not know becomes -1, which
-    the call refuses)."""
-    dt = tensors[0].dtype
-    for t in tensors[1:]:
-        if t is not None and t.dtype != dt:
-            raise ValueError(f"psd binding: tensors of one call differ in type ({dt} and {t.dtype})")
-    return _DTYPES.get(dt, -1)
+def _raw_stream(stream):
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 def _want(t, shape, dtype, name):
-    """A dense tensor of this shape and type, or None."""
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != shape):
-        raise ValueError(f"psd binding: {name} must be {dtype} {shape}, got {t.dtype} {tuple(t.shape)}")
-    return _ptr(t)
+    """Address of a dense tensor of this shape and type, or None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"psd binding: {name} must be dense {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
 
 
 def _want_n(t, n, dtype, name):
-    """A dense tensor of n elements of this type, whatever its shape, or None."""
-    if t is not None and (t.dtype != dtype or t.numel() != n):
-        raise ValueError(f"psd binding: {name} must be {dtype} with {n} elements, got {t.dtype} {tuple(t.shape)}")
-    return _ptr(t)
+    """Address of a dense tensor of n elements of this type, whatever its shape, or None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"psd binding: {name} must be dense {dtype} with {n} elements, got {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _space(t):
+    """(address, bytes) of a workspace."""
+    return (None, 0) if t is None else (_ptr(t), t.numel() * t.element_size())
 
 
 def _tokens_strides(t, name):
@@ -563,40 +577,22 @@ def _tokens_strides(t, name):
 
 
 def _kv_strides(t, name):
+    """(outer, token, head) strides of a cache; that of a dimension of one is never walked: 0 (shared), or the smallest the
+    library takes."""
     if t is None:
-        return PsdKvStrides(0, 8, 0)
+        return 0, 8, 0
+    no, nt, nh, nd = t.shape
     so, st, sh, sd = t.stride()
-    if sd != 1 and t.shape[3] > 1:
+    if sd != 1 and nd > 1:
         raise ValueError(f"psd binding: {name} needs a dense last dimension")
-    # the stride of a dimension of one is never walked: 0 (shared) or the smallest the library takes
-    return PsdKvStrides(so if t.shape[0] > 1 else 0, st if t.shape[1] > 1 else 8, sh if t.shape[2] > 1 else 0)
+    return so if no > 1 else 0, st if nt > 1 else 8, sh if nh > 1 else 0
 
 
-def _data(t):
-    return t.data_ptr() if t is not None and t.numel() else None
-
-
-def _attention(q, k_prefix, scale, causal=False, out=None, v_prefix=None, k_own=None, v_own=None):
-    N, M, Hq, Dh = q.shape
-    B, P, Hkv, dk = k_prefix.shape
-    if B < 1 or N % B or dk != Dh:
-        raise ValueError("psd binding: q [B*D, M, Hq, Dh] and k_prefix [B, P, Hkv, Dh] do not belong together")
-    S = 0
-    for a, b in ((v_prefix, k_prefix), (v_own, k_own), (out, q)):
-        if a is not None and a.shape != b.shape:
-            raise ValueError("psd binding: keys and values, and out and q, have one shape")
-    if (k_own is None) != (v_own is None):
-        raise ValueError("psd binding: k_own and v_own come together")
-    if k_own is not None:
-        S = k_own.shape[1]
-        if tuple(k_own.shape) != (N, S, Hkv, Dh):
-            raise ValueError("psd binding: k_own is [B*D, S, Hkv, Dh]")
-    qt, qh = _tokens_strides(q, "q")
-    ot, oh = _tokens_strides(out, "out") if out is not None else (0, 0)
-    return PsdAttention(B, N // B, M, Hq, Hkv, Dh, P, S, _dtype(q, k_prefix, v_prefix, k_own, v_own, out),
-                        1 if causal else 0, float(Dh) ** -0.5 if scale is None else scale, 0, qt, qh, ot, oh,
-                        _kv_strides(k_prefix, "k_prefix"), _kv_strides(v_prefix, "v_prefix"),
-                        _kv_strides(k_own, "k_own"), _kv_strides(v_own, "v_own"))
+def _one_type(dt, *tensors):
+    for t in tensors:
+        if t is not None and t.dtype is not dt:
+            raise ValueError(f"psd binding: tensors of one call differ in type ({dt} and {t.dtype})")
+    return _DTYPES.get(dt, -1)      # a type the library does not know is refused by the call
 
 
 def psd_attention_workspace_bytes(B, D, M, Hq, Hkv, Dh, P, S) -> int:
@@ -607,13 +603,28 @@ def psd_draft_attention(q, k_prefix, v_prefix, out, lse=None, k_own=None, v_own=
                         scale=None, causal=False, workspace=None, status=None, stream=None):
     """q [B*D, M, Hq, Dh] over the prefix caches [B, P, Hkv, Dh] and each node's own keys [B*D, S, Hkv, Dh] -> out
     (like q) and lse [B*D, M, Hq].  Strided tensors are taken as they are; ``scale`` defaults to 1/sqrt(Dh)."""
-    a = _attention(q, k_prefix, scale, causal, out, v_prefix, k_own, v_own)
-    _check(LIB.psd_draft_attention(q.data_ptr(), _data(k_prefix), _data(v_prefix),
-                                   _want(prefix_len, (a.B,), torch.int32, "prefix_len"), _data(k_own), _data(v_own),
-                                   _want(own_len, (a.B * a.D,), torch.int32, "own_len"), a, out.data_ptr(),
-                                   _want(lse, (a.B * a.D, a.M, a.Hq), torch.float32, "lse"), _ptr(workspace),
-                                   workspace.numel() * workspace.element_size() if workspace is not None else 0,
-                                   _ptr(status), _stream(stream)), "psd_draft_attention")
+    N, M, Hq, Dh = q.shape
+    B, P, Hkv, dk = k_prefix.shape
+    if B < 1 or N % B or dk != Dh:
+        raise ValueError("psd binding: q [B*D, M, Hq, Dh] and k_prefix [B, P, Hkv, Dh] do not belong together")
+    if v_prefix.shape != k_prefix.shape or out.shape != q.shape or (k_own is None) != (v_own is None):
+        raise ValueError("psd binding: keys and values, and out and q, have one shape; k_own and v_own come together")
+    S, ko, vo = 0, None, None
+    if k_own is not None:
+        S = k_own.shape[1]
+        if k_own.shape != (N, S, Hkv, Dh) or v_own.shape != k_own.shape:
+            raise ValueError("psd binding: k_own and v_own are [B*D, S, Hkv, Dh]")
+        ko, vo = k_own.data_ptr() or None, v_own.data_ptr() or None
+    a = _pack_attention(B, N // B, M, Hq, Hkv, Dh, P, S, _one_type(q.dtype, k_prefix, v_prefix, k_own, v_own, out),
+                        1 if causal else 0, Dh ** -0.5 if scale is None else scale, 0, *_tokens_strides(q, "q"),
+                        *_tokens_strides(out, "out"), *_kv_strides(k_prefix, "k_prefix"),
+                        *_kv_strides(v_prefix, "v_prefix"), *_kv_strides(k_own, "k_own"), *_kv_strides(v_own, "v_own"))
+    ws, ws_bytes = _space(workspace)
+    _check(LIB.psd_draft_attention(q.data_ptr(), k_prefix.data_ptr() or None, v_prefix.data_ptr() or None,
+                                   _want(prefix_len, (B,), _I32, "prefix_len"), ko, vo,
+                                   _want(own_len, (N,), _I32, "own_len"), a, out.data_ptr(),
+                                   _want(lse, (N, M, Hq), _F32, "lse"), ws, ws_bytes, _ptr(status),
+                                   _raw_stream(stream)), "psd_draft_attention")
 
 
 def psd_weights_workspace_bytes(B, D, M, Hq, Hkv, Dh, P) -> int:
@@ -624,14 +635,19 @@ def psd_prefix_weights(q, k_prefix, lse, acc_out, acc_in=None, beta=1.0, prefix_
                        status=None, stream=None):
     """acc_out [B, Hkv, P] = beta * acc_in + the attention weight each prefix key draws from the rows of ``q`` (``lse``
     [B*D, M, Hq] as psd_draft_attention wrote it).  acc_in may be acc_out."""
-    a = _attention(q, k_prefix, scale)
-    sums = (a.B, a.Hkv, a.P)
-    _check(LIB.psd_prefix_weights(q.data_ptr(), _data(k_prefix), _want(prefix_len, (a.B,), torch.int32, "prefix_len"),
-                                  _want(lse, (a.B * a.D, a.M, a.Hq), torch.float32, "lse"), a, beta,
-                                  _want(acc_in, sums, torch.float32, "acc_in"),
-                                  _want(acc_out, sums, torch.float32, "acc_out"), _ptr(workspace),
-                                  workspace.numel() * workspace.element_size() if workspace is not None else 0,
-                                  _ptr(status), _stream(stream)), "psd_prefix_weights")
+    N, M, Hq, Dh = q.shape
+    B, P, Hkv, dk = k_prefix.shape
+    if B < 1 or N % B or dk != Dh:
+        raise ValueError("psd binding: q [B*D, M, Hq, Dh] and k_prefix [B, P, Hkv, Dh] do not belong together")
+    a = _pack_attention(B, N // B, M, Hq, Hkv, Dh, P, 0, _one_type(q.dtype, k_prefix), 0,
+                        Dh ** -0.5 if scale is None else scale, 0, *_tokens_strides(q, "q"), 0, 0,
+                        *_kv_strides(k_prefix, "k_prefix"), 0, 0, 0, 0, 0, 0, 0, 0, 0)
+    sums = (B, Hkv, P)
+    ws, ws_bytes = _space(workspace)
+    _check(LIB.psd_prefix_weights(q.data_ptr(), k_prefix.data_ptr() or None, _want(prefix_len, (B,), _I32, "prefix_len"),
+                                  _want(lse, (N, M, Hq), _F32, "lse"), a, beta, _want(acc_in, sums, _F32, "acc_in"),
+                                  _want(acc_out, sums, _F32, "acc_out"), ws, ws_bytes, _ptr(status),
+                                  _raw_stream(stream)), "psd_prefix_weights")
 
 
 def psd_prefix_evict(scores, k, v, k_out, v_out, index, scores_out=None, len_out=None, prefix_len=None, n_sink=0,
@@ -640,15 +656,15 @@ def psd_prefix_evict(scores, k, v, k_out, v_out, index, scores_out=None, len_out
     [B, keep, Hkv, Dh], their positions into index [B, Hkv, keep]."""
     B, P, Hkv, Dh = k.shape
     keep = index.shape[-1]
-    if v.shape != k.shape or tuple(k_out.shape) != (B, keep, Hkv, Dh) or v_out.shape != k_out.shape:
+    if v.shape != k.shape or k_out.shape != (B, keep, Hkv, Dh) or v_out.shape != k_out.shape:
         raise ValueError("psd binding: k, v are [B, P, Hkv, Dh], k_out, v_out [B, keep, Hkv, Dh]")
-    e = PsdEvict(B, Hkv, Dh, P, keep, n_sink, n_recent, _dtype(k, v, k_out, v_out), _kv_strides(k, "k"),
-                 _kv_strides(v, "v"), _kv_strides(k_out, "k_out"), _kv_strides(v_out, "v_out"))
-    _check(LIB.psd_prefix_evict(_want(scores, (B, Hkv, P), torch.float32, "scores"), k.data_ptr(), v.data_ptr(),
-                                _want(prefix_len, (B,), torch.int32, "prefix_len"), e, k_out.data_ptr(), v_out.data_ptr(),
-                                _want(index, (B, Hkv, keep), torch.int32, "index"),
-                                _want(scores_out, (B, Hkv, keep), torch.float32, "scores_out"),
-                                _want(len_out, (B,), torch.int32, "len_out"), _stream(stream)), "psd_prefix_evict")
+    e = _pack_evict(B, Hkv, Dh, P, keep, n_sink, n_recent, _one_type(k.dtype, v, k_out, v_out), *_kv_strides(k, "k"),
+                    *_kv_strides(v, "v"), *_kv_strides(k_out, "k_out"), *_kv_strides(v_out, "v_out"))
+    kept = (B, Hkv, keep)
+    _check(LIB.psd_prefix_evict(_want(scores, (B, Hkv, P), _F32, "scores"), k.data_ptr(), v.data_ptr(),
+                                _want(prefix_len, (B,), _I32, "prefix_len"), e, k_out.data_ptr(), v_out.data_ptr(),
+                                _want(index, kept, _I32, "index"), _want(scores_out, kept, _F32, "scores_out"),
+                                _want(len_out, (B,), _I32, "len_out"), _raw_stream(stream)), "psd_prefix_evict")
 
 
 def psd_logits_workspace_bytes(n_rows: int, V: int) -> int:
@@ -664,20 +680,28 @@ def psd_confidence_logits(logits, out_token, out_conf, out_lse=None, B=None, D=1
     R, V = logits.shape
     if B is None:
         B = R // (D * M)
-    if B * D * M != R or (logits.stride(1) != 1 and V > 1):
+    row, one = logits.stride()
+    if B * D * M != R or (one != 1 and V > 1):
         raise ValueError("psd binding: logits [B*D*M, V] needs a dense last dimension")
-    T, words = (history.shape[1] if history is not None else 0), (V + 31) // 32
-    bias_rows = 1 if bias is None or bias.dim() == 1 else bias.shape[0]
-    allow_rows = 1 if allow is None else allow.shape[0]
-    e = PsdLogitsEdit(_want(history, (B, T), torch.int32, "history") if T else None,
-                      _want(history_len, (B,), torch.int32, "history_len"),
-                      _want_n(draft_tokens, R, torch.int32, "draft_tokens"), _want_n(draft_mask, R, torch.int32, "draft_mask"),
-                      _want(bias, (V,) if bias is not None and bias.dim() == 1 else (bias_rows, V), torch.float32, "bias"),
-                      _want(allow, (allow_rows, words), torch.int32, "allow"), T, bias_rows, allow_rows, repetition,
-                      presence, frequency, 0)
-    _check(LIB.psd_confidence_logits(logits.data_ptr(), _dtype(logits), logits.stride(0) if R > 1 else V, B, D, M, V, e,
-                                     _want_n(out_token, R, torch.int32, "out_token"),
-                                     _want_n(out_conf, R, torch.float32, "out_conf"),
-                                     _want_n(out_lse, R, torch.float32, "out_lse"), _ptr(workspace),
-                                     workspace.numel() * workspace.element_size() if workspace is not None else 0,
-                                     _ptr(status), _stream(stream)), "psd_confidence_logits")
+    T = bias_rows = allow_rows = 0
+    h = hl = dt = dm = bi = al = 0
+    if history is not None:
+        T = history.shape[1]
+        h = _want(history, (B, T), _I32, "history")
+        hl = _want(history_len, (B,), _I32, "history_len") or 0
+    if draft_tokens is not None:
+        dt = _want_n(draft_tokens, R, _I32, "draft_tokens")
+    if draft_mask is not None:
+        dm = _want_n(draft_mask, R, _I32, "draft_mask")
+    if bias is not None:
+        bias_rows = 1 if bias.dim() == 1 else bias.shape[0]
+        bi = _want_n(bias, bias_rows * V, _F32, "bias")
+    if allow is not None:
+        allow_rows = allow.shape[0]
+        al = _want(allow, (allow_rows, (V + 31) // 32), _I32, "allow")
+    e = _pack_edit(h, hl, dt, dm, bi, al, T, bias_rows, allow_rows, repetition, presence, frequency, 0)
+    ws, ws_bytes = _space(workspace)
+    _check(LIB.psd_confidence_logits(logits.data_ptr(), _DTYPES.get(logits.dtype, -1), row if R > 1 else V, B, D, M, V, e,
+                                     _want_n(out_token, R, _I32, "out_token"), _want_n(out_conf, R, _F32, "out_conf"),
+                                     _want_n(out_lse, R, _F32, "out_lse"), ws, ws_bytes, _ptr(status),
+                                     _raw_stream(stream)), "psd_confidence_logits")

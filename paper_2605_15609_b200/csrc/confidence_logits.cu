@@ -6,25 +6,23 @@
 // and writes one (max, sum, lowest argmax) triple per row and chunk; a second kernel merges them.
 //
 // The edits touch few tokens.  The CTA counts the text's tokens of its chunk in shared memory once for all its rows
-// and marks every token that has a count or a bias ("special").  The main loop treats special tokens as absent, like
-// tokens that the grammar forbids; each lane then takes the special tokens of its words one by one, reads the logit
-// again (from L1/L2) and edits it with separately rounded operations.  So the loop that streams the logits has no
-// per-token edit in it, whatever the edits are.
+// and marks every token that has a count or a bias ("special").  Per row, a warp first puts down one bit per column of
+// its own: open = allowed, inside the vocabulary and not special; on the way each lane takes the special tokens of its words
+// one by one, reads the logit and edits it with separately rounded operations.  The loop that streams the logits then
+// knows nothing but those bits, whatever the edits are, and does not load 32 vectors of which no column is open.
 //
 // Differences are taken before the multiplication by log2 e: a row whose maximum is the type's lowest value would
 // overflow a precomputed product, and its rounding would shift every term by the same relative error.
 #include "combine.cuh"
-#include "ops_internal.cuh"
-#include "tc_common.cuh"
+#include "attn_tc.cuh"
 
 namespace psd {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxChunk = 16384;      // tokens per CTA: 64 KB of counts
-constexpr int kMinWarpCols = 512;     // columns a warp takes at least (sets the number of triples per row)
+constexpr int kMinWarpCols = 256;     // columns a warp takes at least (sets the number of triples per row)
 constexpr int kRowsPerCta = 64;
-constexpr float kLog2e = 1.4426950408889634f;
 
 struct Part { float m, s; int32_t a, pad; };
 
@@ -35,6 +33,7 @@ struct LogitsArgs {
     int unit_rows, slices, rows_per_cta;   // rows of one node and one bias row; CTAs they are cut into; rows of each
     int chunk, n_chunks, wpr;              // columns per CTA; CTAs along the vocabulary; warps that share a row
     int rows_per_bias, rows_per_allow, words;
+    int merge_early;                       // the merge's blocks are few: let them become resident at once
     psd_logits_edit_t e;
     Part* part;                            // [rows][n_chunks * wpr]
 };
@@ -78,31 +77,41 @@ __device__ __forceinline__ float rescaled(float s, float m, float M) {
     return m == -INFINITY ? s : s * ex2((m - M) * kLog2e);
 }
 
-// G values of one lane joined to its running maximum and sum; g names the group for the search of the argmax.
-template <int G>
-__device__ __forceinline__ void fold_group(const float (&x)[G], int g, float& m, float& s, int& best) {
-    float gm = x[0];
+// The E values of a lane's vector, -inf where their bit is 0.
+template <int E>
+__device__ __forceinline__ void close_bits(float (&x)[E], uint32_t bits) {
 #pragma unroll
-    for (int j = 1; j < G; ++j) gm = fmaxf(gm, x[j]);
+    for (int j = 0; j < E; ++j) x[j] = bits & (1u << j) ? x[j] : -INFINITY;
+}
+
+// E values joined to a lane's running maximum and sum; g names the vector for the search of the argmax.
+template <int E>
+__device__ __forceinline__ void fold_vector(const float (&x)[E], int g, float& m, float& s, int& best) {
+    float gm = max3(x[0], x[1], x[2]);
+#pragma unroll
+    for (int j = 3; j + 1 < E; j += 2) gm = max3(gm, x[j], x[j + 1]);
+    if (E % 2 == 0) gm = fmaxf(gm, x[E - 1]);
     best = gm > m ? g : best;
     const float mn = fmaxf(m, gm);
     const float base = mn == -INFINITY ? 0.f : mn;
-    float t = s * ex2((m == mn ? 0.f : m - base) * kLog2e);     // m = -inf here means s = 0 (or NaN), factor 0 or 1
-    float acc[2] = {0.f, 0.f};
+    const float f = ex2((m == mn ? 0.f : m - base) * kLog2e);   // m = -inf: s is 0 (or NaN), the factor 0 or 1
+    const f32x2 nb = pack2(-base, -base), k = pack2(kLog2e, kLog2e);
+    f32x2 acc = 0ull;
 #pragma unroll
-    for (int j = 0; j < G; ++j) acc[j & 1] += ex2((x[j] - base) * kLog2e);
-    s = t + (acc[0] + acc[1]);
+    for (int j = 0; j < E; j += 2) acc = add2(acc, ex2_pair(mul2(add2(pack2(x[j], x[j + 1]), nb), k)));
+    float a0, a1;
+    unpack2(acc, a0, a1);
+    s = fmaf(s, f, a0 + a1);
     m = mn;
 }
 
-// VEC: 16-byte loads, lane l takes E neighbouring columns; otherwise (rows not 16-byte aligned) lane l takes columns
-// l, l + 32, .. of a run of 256, one element per load.
-template <typename T, bool VEC>
+template <typename T>
 __global__ void __launch_bounds__(kThreads) logits_kernel(const LogitsArgs a) {
-    constexpr int E = VEC ? Vec<T>::E : 8;     // columns of a lane per step
+    constexpr int E = Vec<T>::E;               // columns of a lane's 16-byte vector
     constexpr int STEP = 32 * E;               // columns of a warp per step
+    constexpr int U = 4;                       // vectors in flight per lane
     extern __shared__ int32_t sh[];
-    int32_t* cnt = sh;                                             // [chunk]
+    int32_t* cnt = sh;                                              // [chunk]
     uint32_t* special = reinterpret_cast<uint32_t*>(sh + a.chunk);  // [chunk / 32]
     const int c = blockIdx.x % a.n_chunks;
     const int us = blockIdx.x / a.n_chunks;
@@ -115,8 +124,11 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const LogitsArgs a) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const bool counts = a.e.history || a.e.draft_tokens;
     const float* bias = a.e.bias ? a.e.bias + (row0 / a.rows_per_bias) * (int64_t)a.V + v0 : nullptr;
+    const int cols = a.chunk / a.wpr;                      // columns of one warp, a multiple of 256
+    uint32_t* open = special + a.chunk / 32 + warp * (cols / 32 + 2) + 1;   // [cols / 32] and a closed word on either side
 
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (a.merge_early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (counts) {
         for (int i = threadIdx.x; i < a.chunk; i += kThreads) cnt[i] = 0;
         __syncthreads();
@@ -124,9 +136,11 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const LogitsArgs a) {
             const int64_t b = node / a.D;
             const int n = a.e.history_len ? min(max(a.e.history_len[b], 0), a.e.history_cap) : a.e.history_cap;
             const int32_t* h = a.e.history + b * a.e.history_cap;
+#pragma unroll 4
             for (int i = threadIdx.x; i < n; i += kThreads) {
-                const unsigned t = (unsigned)h[i] - (unsigned)v0;
-                if (t < (unsigned)vw && h[i] >= 0) atomicAdd(&cnt[t], 1);
+                const int id = h[i];
+                const unsigned t = (unsigned)id - (unsigned)v0;
+                if (t < (unsigned)vw && id >= 0) atomicAdd(&cnt[t], 1);
             }
         }
         if (a.e.draft_tokens) {
@@ -138,84 +152,91 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const LogitsArgs a) {
         }
         __syncthreads();
     }
+#pragma unroll 4
     for (int w = warp; w < a.chunk / 32; w += kWarps) {
         const int i = w * 32 + lane;
         const bool sp = i < vw && ((counts && cnt[i] > 0) || (bias && bias[i] != 0.f));
         const uint32_t bits = __ballot_sync(0xffffffffu, sp);
         if (lane == 0) special[w] = bits;
     }
+    if (lane == 0) open[-1] = open[cols / 32] = 0u;
     __syncthreads();
 
-    const int cols = a.chunk / a.wpr;                      // columns of one warp, a multiple of 512
     const int c0 = (warp % a.wpr) * cols;
+    const int len = max(0, min(cols, vw - c0));            // columns of this warp that exist
     const int n_split = a.n_chunks * a.wpr;
     for (int rr = warp / a.wpr; rr < n_rows; rr += kWarps / a.wpr) {
         const int64_t row = row0 + rr;
-        const T* lg = reinterpret_cast<const T*>(a.logits) + row * a.stride + v0;
-        const uint32_t* allow = a.e.allow ? a.e.allow + (row / a.rows_per_allow) * (int64_t)a.words + v0 / 32 : nullptr;
-        // bits of the 32 columns from column i (a multiple of 32) that the main loop takes
-        auto open_word = [&](int i) -> uint32_t {
-            const int left = vw - i;
-            if (left <= 0) return 0u;
-            uint32_t ok = allow ? allow[i >> 5] : 0xffffffffu;
-            if (left < 32) ok &= (1u << left) - 1u;
-            return ok;
-        };
-        // the E values of step k as the main loop sees them: -inf where absent
-        auto load = [&](int k, float (&x)[E]) {
-            if (VEC) {
-                const int i = c0 + k * STEP + lane * E;
-                const uint32_t w = i < vw ? open_word(i & ~31) & ~special[i >> 5] : 0u;
-                const uint32_t b = w >> (i & 31);
-                if (i + E <= vw) {
-                    const uint4 r = __ldg(reinterpret_cast<const uint4*>(lg + i));
-                    float y[Vec<T>::E];
-                    Vec<T>::unpack(r, y);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) x[j] = (b >> j) & 1u ? y[j < Vec<T>::E ? j : 0] : -INFINITY;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < E; ++j) x[j] = (i + j < vw && ((b >> j) & 1u)) ? Vec<T>::one(lg + i + j) : -INFINITY;
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < E; ++j) {
-                    const int i = c0 + k * STEP + j * 32;
-                    const uint32_t w = i < vw ? open_word(i) & ~special[i >> 5] : 0u;
-                    const float y = i + lane < vw ? Vec<T>::one(lg + i + lane) : 0.f;
-                    x[j] = (w >> lane) & 1u ? y : -INFINITY;
-                }
-            }
-        };
-        float m = -INFINITY, s = 0.f;
-        int best = -1;
-        const int steps = min(cols, max(0, vw - c0) + STEP - 1) / STEP;
-#pragma unroll 4
-        for (int k = 0; k < steps; ++k) {
-            float x[E];
-            load(k, x);
-            fold_group<E>(x, k, m, s, best);
-        }
-        // the special tokens of this warp's columns, in ascending order within a lane
-        float sm = -INFINITY, ss = 0.f;
+        const T* lg = reinterpret_cast<const T*>(a.logits) + row * a.stride + v0 + c0;    // this warp's column 0
+        // Vectors are aligned in memory: with rows that are not, the first one starts `back` columns ahead of column 0.
+        const int back = (int)((reinterpret_cast<uintptr_t>(lg) & 15) / sizeof(T));
+        const uint32_t* allow = a.e.allow ? a.e.allow + (row / a.rows_per_allow) * (int64_t)a.words + (v0 + c0) / 32 : nullptr;
+        float sm = -INFINITY, ss = 0.f;                    // the special tokens of this lane
         int sa = INT32_MAX;
         for (int w = lane; w < cols / 32; w += 32) {
-            const int i = c0 + w * 32;
-            uint32_t bits = i < vw ? special[i >> 5] & open_word(i) : 0u;
+            const int left = len - w * 32;
+            uint32_t ok = 0u;
+            if (left > 0) {
+                ok = allow ? allow[w] : 0xffffffffu;
+                if (left < 32) ok &= (1u << left) - 1u;
+            }
+            const uint32_t sp = special[c0 / 32 + w];
+            open[w] = ok & ~sp;
+            uint32_t bits = ok & sp;
             while (bits) {
-                const int v = i + __ffs(bits) - 1;
+                const int v = w * 32 + __ffs(bits) - 1;
                 bits &= bits - 1;
                 float x = Vec<T>::one(lg + v);
-                const int n = counts ? cnt[v] : 0;
+                const int n = counts ? cnt[c0 + v] : 0;
                 if (n > 0) {
                     x = x > 0.f ? __fdiv_rn(x, a.e.repetition) : __fmul_rn(x, a.e.repetition);
                     x = __fsub_rn(x, __fadd_rn(__fmul_rn(a.e.frequency, (float)n), a.e.presence));
                 }
-                if (bias) x = __fadd_rn(x, bias[v]);
+                if (bias) x = __fadd_rn(x, bias[c0 + v]);
                 const float mn = fmaxf(sm, x);
                 if (x > sm) sa = v;
                 ss = rescaled(ss, sm, mn) + (x == -INFINITY ? 0.f : ex2((x - mn) * kLog2e));
                 sm = mn;
+            }
+        }
+        __syncwarp();
+        // bits of the vector that starts at column i (i >= -back, not a multiple of E when back != 0)
+        auto bits_at = [&](int i) -> uint32_t {
+            const uint32_t* w = open + (i >> 5);
+            if (back == 0) return i < cols ? w[0] >> (i & 31) & ((1u << E) - 1u) : 0u;
+            return i < cols ? __funnelshift_r(w[0], w[1], i & 31) & ((1u << E) - 1u) : 0u;
+        };
+        // first and last column of the row, as columns of this warp: a vector that reaches past them is read piece by piece
+        const int lo = -(v0 + c0), hi = a.V - v0 - c0;
+        auto fetch = [&](int i) -> uint4 {
+            if (i >= lo && i + E <= hi) return __ldg(reinterpret_cast<const uint4*>(lg + i));
+            uint4 r = make_uint4(0, 0, 0, 0);
+            T* piece = reinterpret_cast<T*>(&r);
+#pragma unroll
+            for (int j = 0; j < E; ++j)
+                if (i + j >= lo && i + j < hi) piece[j] = lg[i + j];
+            return r;
+        };
+        float m = -INFINITY, s = 0.f;
+        int best = -1;
+        const int steps = len > 0 ? (len + back + STEP - 1) / STEP : 0;
+        for (int k0 = 0; k0 < steps; k0 += U) {
+            uint32_t bits[U];
+            uint4 raw[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = (k0 + u) * STEP + lane * E - back;
+                bits[u] = k0 + u < steps ? bits_at(i) : 0u;
+                raw[u] = make_uint4(0, 0, 0, 0);
+                if (bits[u]) raw[u] = fetch(i);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (!__any_sync(0xffffffffu, bits[u])) continue;
+                float x[E];
+                Vec<T>::unpack(raw[u], x);
+                close_bits<E>(x, bits[u]);
+                fold_vector<E>(x, k0 + u, m, s, best);
             }
         }
         // the warp's maximum; the lanes that hold it look up its column
@@ -229,21 +250,24 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const LogitsArgs a) {
         if (M > -INFINITY) {
             if (sm == M) at = sa;
             if (m == M) {
+                const int i = best * STEP + lane * E - back;
                 float x[E];
-                load(best, x);
+                Vec<T>::unpack(fetch(i), x);
+                close_bits<E>(x, bits_at(i));
                 int j = E - 1;
 #pragma unroll
                 for (int q = E - 2; q >= 0; --q) j = x[q] == M ? q : j;
-                at = min(at, VEC ? c0 + best * STEP + lane * E + j : c0 + best * STEP + j * 32 + lane);
+                at = min(at, i + j);
             }
         }
         at = __reduce_min_sync(0xffffffffu, at);
         if (lane == 0) {
-            Part p = {M, t, at == INT32_MAX ? INT32_MAX : v0 + at, 0};
+            Part p = {M, t, at == INT32_MAX ? INT32_MAX : v0 + c0 + at, 0};
             a.part[row * n_split + c * a.wpr + warp % a.wpr] = p;
         }
+        __syncwarp();                                      // the row's bits have been read
     }
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (!a.merge_early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
 // One warp per row: the row's triples in a fixed order (lane by lane, then a fixed tree).
@@ -256,6 +280,7 @@ __global__ void __launch_bounds__(kThreads) logits_merge_kernel(const Part* __re
     if (row >= n_rows) return;
     float m = -INFINITY, s = 0.f;
     int at = INT32_MAX;
+#pragma unroll 8
     for (int i = lane; i < n_split; i += 32) {
         const Part p = part[row * n_split + i];
         const float mn = fmaxf(m, p.m);
@@ -291,29 +316,23 @@ void choose_chunk(int64_t units, int rows, int V, int& chunk, int& wpr) {
     while (chunk / wpr > kMinWarpCols && units * ((V + chunk - 1) / chunk) < want) chunk /= 2;
 }
 
+int shared_bytes(int chunk, int wpr) { return chunk * 4 + chunk / 8 + kWarps * (chunk / wpr / 32 + 2) * 4; }
+
 template <typename T>
-int launch(const LogitsArgs& a, int64_t grid, bool vec, cudaStream_t st) {
-    const int smem = a.chunk * 4 + a.chunk / 8;
+int launch(const LogitsArgs& a, int64_t grid, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = shared_bytes(a.chunk, a.wpr);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    static std::atomic<unsigned long long> set_v{0}, set_s{0};
-    constexpr int most = kMaxChunk * 4 + kMaxChunk / 8;
-    cudaError_t e;
-    if (vec) {
-        if (!ensure_dynamic_smem(logits_kernel<T, true>, most, set_v)) return PSD_ERR_CUDA;
-        e = cudaLaunchKernelEx(&cfg, logits_kernel<T, true>, a);
-    } else {
-        if (!ensure_dynamic_smem(logits_kernel<T, false>, most, set_s)) return PSD_ERR_CUDA;
-        e = cudaLaunchKernelEx(&cfg, logits_kernel<T, false>, a);
-    }
+    static std::atomic<unsigned long long> set{0};
+    if (!ensure_dynamic_smem(logits_kernel<T>, shared_bytes(kMaxChunk, 1), set)) return PSD_ERR_CUDA;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, logits_kernel<T>, a);
     count_launch();
     return e == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
 }
@@ -321,7 +340,7 @@ int launch(const LogitsArgs& a, int64_t grid, bool vec, cudaStream_t st) {
 }  // namespace
 
 size_t confidence_logits_workspace(int64_t n_rows, int V) {
-    // a chunk is a multiple of 512 columns and holds at least 512 per warp
+    // a chunk holds at least kMinWarpCols columns per warp
     const int64_t n_split = (V + kMinWarpCols - 1) / kMinWarpCols + kMaxChunk / kMinWarpCols;
     return ((size_t)n_rows * n_split * sizeof(Part) + 255) / 256 * 256;
 }
@@ -351,10 +370,9 @@ int launch_confidence_logits(const void* logits, int dtype, int64_t row_stride, 
     a.part = reinterpret_cast<Part*>(workspace);
     const int64_t grid = units * a.n_chunks;
     if (grid > INT32_MAX) return PSD_ERR_SHAPE;
-    const int esize = dtype == PSD_FP32 ? 4 : 2;
-    const bool vec = reinterpret_cast<uintptr_t>(logits) % 16 == 0 && (row_stride * esize) % 16 == 0;
-    const int rc = dtype == PSD_BF16 ? launch<__nv_bfloat16>(a, grid, vec, st)
-                 : dtype == PSD_FP16 ? launch<__half>(a, grid, vec, st) : launch<float>(a, grid, vec, st);
+    a.merge_early = n_rows <= 8 * kWarps;
+    const int rc = dtype == PSD_BF16 ? launch<__nv_bfloat16>(a, grid, st)
+                 : dtype == PSD_FP16 ? launch<__half>(a, grid, st) : launch<float>(a, grid, st);
     if (rc != PSD_OK) return rc;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((n_rows + kWarps - 1) / kWarps));

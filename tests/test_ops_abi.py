@@ -128,3 +128,15 @@ def test_logits_refusals():
 def test_struct_layouts():
     assert ctypes.sizeof(psd.PsdKvStrides) == 24 and ctypes.sizeof(psd.PsdAttention) == 48 + 32 + 96
     assert ctypes.sizeof(psd.PsdEvict) == 32 + 96 and ctypes.sizeof(psd.PsdLogitsEdit) == 48 + 28 + 4
+
+
+def test_packed_descriptors_are_the_structs():
+    """The bytes the binding packs are those of the C structs."""
+    st = [psd.PsdKvStrides(i, i + 1, i + 2) for i in (100, 200, 300, 400)]
+    flat = [v for s in st for v in (s.outer, s.token, s.head)]
+    head = (1, 2, 3, 4, 5, 6, 7, 8, 1, 1, 0.5, 0, 11, 12, 13, 14)
+    assert bytes(psd.PsdAttention(*head, *st)) == binding._pack_attention(*head, *flat)
+    head = (1, 2, 3, 4, 5, 6, 7, 1)
+    assert bytes(psd.PsdEvict(*head, *st)) == binding._pack_evict(*head, *flat)
+    edit = (1 << 40, 2, 3, 4, 5, 6, 7, 8, 9, 1.5, 0.25, -1.0, 0)
+    assert bytes(psd.PsdLogitsEdit(*edit)) == binding._pack_edit(*edit)
