@@ -1,18 +1,23 @@
 // Token, confidence and log-sum-exp of rows of logits under penalties, biases and grammar masks.
 //
 // One pass over the logits (the only large operand): a CTA takes a few rows that share one text (a draft) and one
-// bias row, and a chunk of the vocabulary; a warp walks a row's columns with a running maximum and sum per lane,
-//     m' = max(m, x),  s' = s * 2^((m - m') log2 e) + sum 2^((x - m') log2 e),
-// and writes one (max, sum, lowest argmax) triple per row and chunk; a second kernel merges them.
+// bias row, and a chunk of the vocabulary; a warp walks a row's columns with a running maximum m and sum s per lane, 32
+// columns at a time, and writes one (max, sum, where) record per row and chunk; a second kernel merges them.
 //
-// The edits touch few tokens.  The CTA counts the text's tokens of its chunk in shared memory once for all its rows
-// and marks every token that has a count or a bias ("special").  Per row, a warp first puts down one bit per column of
-// its own: open = allowed, inside the vocabulary and not special; on the way each lane takes the special tokens of its words
-// one by one, reads the logit and edits it with separately rounded operations.  The loop that streams the logits then
-// knows nothing but those bits, whatever the edits are, and does not load 32 vectors of which no column is open.
+// The edits touch few tokens.  The CTA counts the text's tokens of its chunk in shared memory once for all its rows and
+// lists every token that has a count or a bias ("special"), in order.  Per row, a warp puts down one bit per column of
+// its own: open = allowed, inside the vocabulary and not special; the special tokens are then edited 32 at a time, with
+// separately rounded operations.  The loop that streams the logits knows nothing but the bits, whatever the edits are (a
+// table in shared memory turns the bits of a 16-byte vector into the mask of its words), and does not load a group of
+// vectors of which no column is open.  What bounds it is the instructions per column (about 8) next to the bytes.
 //
-// Differences are taken before the multiplication by log2 e: a row whose maximum is the type's lowest value would
-// overflow a precomputed product, and its rounding would shift every term by the same relative error.
+// Sums are kept relative to 2^r, r = the rounded product m * log2 e, so that a term is one FMA and one exponential,
+// 2^(x log2 e - r), and the rounding of r is the same in every term, the maximum's own included: it cancels in
+// confidence = (the maximum's term) / sum.  Maxima beyond 1e37 (a row of the type's lowest values, infinities) would overflow
+// that product: their terms are 2^((x - m) log2 e).
+//
+// The column of a maximum is looked up only where it counts: a record says which lane's group of 32 columns held the
+// maximum, and the merge searches the one group of each row that won.
 #include "combine.cuh"
 #include "attn_tc.cuh"
 
@@ -21,10 +26,18 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxChunk = 16384;      // tokens per CTA: 64 KB of counts
-constexpr int kMinWarpCols = 256;     // columns a warp takes at least (sets the number of triples per row)
+constexpr int kMinWarpCols = 256;     // columns a warp takes at least (sets the number of records per row)
 constexpr int kRowsPerCta = 64;
+#ifndef PSD_BASE
+#define PSD_BASE 8192
+#endif
+constexpr int kBaseCols = PSD_BASE;
+constexpr int kGuard = 36;            // closed words behind a warp's open bits: a group of 1024 columns may reach past them
+constexpr float kHuge = 1e37f;
 
-struct Part { float m, s; int32_t a, pad; };
+// A warp's record of its columns of a row.  bits == 0: `at` is the column itself (INT32_MAX: none).  Otherwise the maximum is
+// in the group of 32 columns (one lane's vectors) that starts at column `at`, and those with a bit are open.
+struct Part { float m, s; int32_t at; uint32_t bits; };
 
 struct LogitsArgs {
     const void* logits;
@@ -41,7 +54,8 @@ struct LogitsArgs {
 template <typename T> struct Vec;
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int E = 8;
-    static __device__ __forceinline__ void unpack(const uint4& r, float (&x)[8]) {
+    static constexpr uint32_t NEG = 0xff80ff80u;           // two times -inf
+    static __device__ __forceinline__ void unpack(const uint4& r, float* x) {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -53,7 +67,8 @@ template <> struct Vec<__nv_bfloat16> {
 };
 template <> struct Vec<__half> {
     static constexpr int E = 8;
-    static __device__ __forceinline__ void unpack(const uint4& r, float (&x)[8]) {
+    static constexpr uint32_t NEG = 0xfc00fc00u;
+    static __device__ __forceinline__ void unpack(const uint4& r, float* x) {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -66,53 +81,38 @@ template <> struct Vec<__half> {
 };
 template <> struct Vec<float> {
     static constexpr int E = 4;
-    static __device__ __forceinline__ void unpack(const uint4& r, float (&x)[4]) {
+    static constexpr uint32_t NEG = 0xff800000u;
+    static __device__ __forceinline__ void unpack(const uint4& r, float* x) {
         x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
     }
     static __device__ __forceinline__ float one(const float* p) { return *p; }
 };
 
-// A sum relative to maximum m, moved to maximum M >= m (m = -inf: the sum is 0, or NaN from a NaN among the values).
+// Term of x in a sum with maximum m >= x.
+__device__ __forceinline__ float term(float x, float m) {
+    if (fabsf(m) > kHuge) return ex2((x - m) * kLog2e);
+    return ex2(fmaf(x, kLog2e, -__fmul_rn(m, kLog2e)));
+}
+// A sum kept for maximum m, moved to maximum M >= m (m = -inf: the sum is 0, or NaN from a NaN among the values).
 __device__ __forceinline__ float rescaled(float s, float m, float M) {
-    return m == -INFINITY ? s : s * ex2((m - M) * kLog2e);
-}
-
-// The E values of a lane's vector, -inf where their bit is 0.
-template <int E>
-__device__ __forceinline__ void close_bits(float (&x)[E], uint32_t bits) {
-#pragma unroll
-    for (int j = 0; j < E; ++j) x[j] = bits & (1u << j) ? x[j] : -INFINITY;
-}
-
-// E values joined to a lane's running maximum and sum; g names the vector for the search of the argmax.
-template <int E>
-__device__ __forceinline__ void fold_vector(const float (&x)[E], int g, float& m, float& s, int& best) {
-    float gm = max3(x[0], x[1], x[2]);
-#pragma unroll
-    for (int j = 3; j + 1 < E; j += 2) gm = max3(gm, x[j], x[j + 1]);
-    if (E % 2 == 0) gm = fmaxf(gm, x[E - 1]);
-    best = gm > m ? g : best;
-    const float mn = fmaxf(m, gm);
-    const float base = mn == -INFINITY ? 0.f : mn;
-    const float f = ex2((m == mn ? 0.f : m - base) * kLog2e);   // m = -inf: s is 0 (or NaN), the factor 0 or 1
-    const f32x2 nb = pack2(-base, -base), k = pack2(kLog2e, kLog2e);
-    f32x2 acc = 0ull;
-#pragma unroll
-    for (int j = 0; j < E; j += 2) acc = add2(acc, ex2_pair(mul2(add2(pack2(x[j], x[j + 1]), nb), k)));
-    float a0, a1;
-    unpack2(acc, a0, a1);
-    s = fmaf(s, f, a0 + a1);
-    m = mn;
+    if (m == -INFINITY || m == M) return s;
+    if (fabsf(m) > kHuge || fabsf(M) > kHuge) return s * ex2((m - M) * kLog2e);
+    return s * ex2(__fmul_rn(m, kLog2e) - __fmul_rn(M, kLog2e));      // (not contracted: r is the rounded product)
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads) logits_kernel(const LogitsArgs a) {
-    constexpr int E = Vec<T>::E;               // columns of a lane's 16-byte vector
-    constexpr int STEP = 32 * E;               // columns of a warp per step
-    constexpr int U = 4;                       // vectors in flight per lane
-    extern __shared__ int32_t sh[];
-    int32_t* cnt = sh;                                              // [chunk]
-    uint32_t* special = reinterpret_cast<uint32_t*>(sh + a.chunk);  // [chunk / 32]
+__global__ void __launch_bounds__(kThreads, 3) logits_kernel(const LogitsArgs a) {
+    constexpr int E = Vec<T>::E;               // columns of a 16-byte vector
+    constexpr int STEP = 32 * E;               // columns of a warp per vector and lane
+    constexpr int U = 32 / E;                  // vectors of a group: 32 columns per lane, 1024 per warp
+    constexpr int TABLE = 1 << E;
+    extern __shared__ __align__(16) int32_t sh[];
+    uint4* table = reinterpret_cast<uint4*>(sh);                    // [TABLE] masks of a vector's words
+    int32_t* cnt = sh + TABLE * 4;                                  // [chunk] occurrences in the text
+    uint32_t* special = reinterpret_cast<uint32_t*>(cnt + a.chunk);  // [chunk / 32] bits
+    const int words = a.chunk / 32;
+    uint16_t* first = reinterpret_cast<uint16_t*>(special + words);  // [words + 2] special tokens ahead of a word
+    uint16_t* list = first + words + 2;                             // [chunk] special tokens in order
     const int c = blockIdx.x % a.n_chunks;
     const int us = blockIdx.x / a.n_chunks;
     const int slice = us % a.slices;
@@ -125,8 +125,19 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const LogitsArgs a) {
     const bool counts = a.e.history || a.e.draft_tokens;
     const float* bias = a.e.bias ? a.e.bias + (row0 / a.rows_per_bias) * (int64_t)a.V + v0 : nullptr;
     const int cols = a.chunk / a.wpr;                      // columns of one warp, a multiple of 256
-    uint32_t* open = special + a.chunk / 32 + warp * (cols / 32 + 2) + 1;   // [cols / 32] and a closed word on either side
+    // [cols / 32] open bits of this warp's columns, one closed word ahead and kGuard behind
+    uint32_t* open = reinterpret_cast<uint32_t*>(list + a.chunk) + warp * (cols / 32 + 1 + kGuard) + 1;
 
+    if (threadIdx.x < TABLE) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (E == 4) w[i] = threadIdx.x >> i & 1 ? 0xffffffffu : 0u;
+            else w[i] = (threadIdx.x >> (2 * i) & 1 ? 0xffffu : 0u) | (threadIdx.x >> (2 * i + 1) & 1 ? 0xffff0000u : 0u);
+        }
+        table[threadIdx.x] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    for (int i = lane; i < kGuard + 1; i += 32) open[i ? cols / 32 + i - 1 : -1] = 0u;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (a.merge_early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (counts) {
@@ -153,154 +164,229 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const LogitsArgs a) {
         __syncthreads();
     }
 #pragma unroll 4
-    for (int w = warp; w < a.chunk / 32; w += kWarps) {
+    for (int w = warp; w < words; w += kWarps) {
         const int i = w * 32 + lane;
         const bool sp = i < vw && ((counts && cnt[i] > 0) || (bias && bias[i] != 0.f));
         const uint32_t bits = __ballot_sync(0xffffffffu, sp);
         if (lane == 0) special[w] = bits;
     }
-    if (lane == 0) open[-1] = open[cols / 32] = 0u;
+    __syncthreads();
+    if (warp == 0) {
+        int total = 0;
+        for (int w0 = 0; w0 < words; w0 += 32) {
+            const int n = w0 + lane < words ? __popc(special[w0 + lane]) : 0;
+            int run = n;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, run, o);
+                if (lane >= o) run += y;
+            }
+            if (w0 + lane < words) first[w0 + lane] = (uint16_t)(total + run - n);
+            total += __shfl_sync(0xffffffffu, run, 31);
+        }
+        if (lane == 0) first[words] = (uint16_t)total;
+    }
+    __syncthreads();
+    for (int w = threadIdx.x; w < words; w += kThreads) {
+        uint32_t bits = special[w];
+        for (int n = first[w]; bits; ++n) {
+            list[n] = (uint16_t)(w * 32 + __ffs(bits) - 1);
+            bits &= bits - 1;
+        }
+    }
     __syncthreads();
 
     const int c0 = (warp % a.wpr) * cols;
     const int len = max(0, min(cols, vw - c0));            // columns of this warp that exist
     const int n_split = a.n_chunks * a.wpr;
+    const int sp0 = first[c0 / 32], sp1 = first[(c0 + cols) / 32];
     for (int rr = warp / a.wpr; rr < n_rows; rr += kWarps / a.wpr) {
         const int64_t row = row0 + rr;
         const T* lg = reinterpret_cast<const T*>(a.logits) + row * a.stride + v0 + c0;    // this warp's column 0
         // Vectors are aligned in memory: with rows that are not, the first one starts `back` columns ahead of column 0.
         const int back = (int)((reinterpret_cast<uintptr_t>(lg) & 15) / sizeof(T));
         const uint32_t* allow = a.e.allow ? a.e.allow + (row / a.rows_per_allow) * (int64_t)a.words + (v0 + c0) / 32 : nullptr;
-        float sm = -INFINITY, ss = 0.f;                    // the special tokens of this lane
+        if (allow) {
+#pragma unroll 4
+            for (int w = lane; w < cols / 32; w += 32) {
+                const int left = len - w * 32;
+                const uint32_t inside = left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u;
+                open[w] = (left > 0 ? allow[w] : 0u) & inside & ~special[c0 / 32 + w];
+            }
+        } else {
+            for (int w = lane; w < cols / 32; w += 32) {
+                const int left = len - w * 32;
+                open[w] = (left >= 32 ? 0xffffffffu : left > 0 ? (1u << left) - 1u : 0u) & ~special[c0 / 32 + w];
+            }
+        }
+        // the special tokens, ascending within a lane
+        float sm = -INFINITY, ss = 0.f;
         int sa = INT32_MAX;
-        for (int w = lane; w < cols / 32; w += 32) {
-            const int left = len - w * 32;
-            uint32_t ok = 0u;
-            if (left > 0) {
-                ok = allow ? allow[w] : 0xffffffffu;
-                if (left < 32) ok &= (1u << left) - 1u;
+        for (int e = sp0 + lane; e < sp1; e += 32) {
+            const int v = list[e] - c0;
+            float x = Vec<T>::one(lg + v);
+            const int n = counts ? cnt[c0 + v] : 0;
+            if (n > 0) {
+                x = x > 0.f ? __fdiv_rn(x, a.e.repetition) : __fmul_rn(x, a.e.repetition);
+                x = __fsub_rn(x, __fadd_rn(__fmul_rn(a.e.frequency, (float)n), a.e.presence));
             }
-            const uint32_t sp = special[c0 / 32 + w];
-            open[w] = ok & ~sp;
-            uint32_t bits = ok & sp;
-            while (bits) {
-                const int v = w * 32 + __ffs(bits) - 1;
-                bits &= bits - 1;
-                float x = Vec<T>::one(lg + v);
-                const int n = counts ? cnt[c0 + v] : 0;
-                if (n > 0) {
-                    x = x > 0.f ? __fdiv_rn(x, a.e.repetition) : __fmul_rn(x, a.e.repetition);
-                    x = __fsub_rn(x, __fadd_rn(__fmul_rn(a.e.frequency, (float)n), a.e.presence));
-                }
-                if (bias) x = __fadd_rn(x, bias[c0 + v]);
-                const float mn = fmaxf(sm, x);
-                if (x > sm) sa = v;
-                ss = rescaled(ss, sm, mn) + (x == -INFINITY ? 0.f : ex2((x - mn) * kLog2e));
-                sm = mn;
-            }
+            if (bias) x = __fadd_rn(x, bias[c0 + v]);
+            if (allow && !(allow[v >> 5] >> (v & 31) & 1u)) continue;
+            const float mn = fmaxf(sm, x);
+            if (x > sm) sa = v;
+            ss = rescaled(ss, sm, mn) + (x == -INFINITY ? 0.f : term(x, mn));
+            sm = mn;
         }
         __syncwarp();
-        // bits of the vector that starts at column i (i >= -back, not a multiple of E when back != 0)
-        auto bits_at = [&](int i) -> uint32_t {
-            const uint32_t* w = open + (i >> 5);
-            if (back == 0) return i < cols ? w[0] >> (i & 31) & ((1u << E) - 1u) : 0u;
-            return i < cols ? __funnelshift_r(w[0], w[1], i & 31) & ((1u << E) - 1u) : 0u;
-        };
         // first and last column of the row, as columns of this warp: a vector that reaches past them is read piece by piece
         const int lo = -(v0 + c0), hi = a.V - v0 - c0;
-        auto fetch = [&](int i) -> uint4 {
-            if (i >= lo && i + E <= hi) return __ldg(reinterpret_cast<const uint4*>(lg + i));
-            uint4 r = make_uint4(0, 0, 0, 0);
-            T* piece = reinterpret_cast<T*>(&r);
-#pragma unroll
-            for (int j = 0; j < E; ++j)
-                if (i + j >= lo && i + j < hi) piece[j] = lg[i + j];
-            return r;
-        };
+        const int shift = (lane * E - back) & 31;
+        const uint32_t* my_open = open + ((lane * E - back) >> 5);
+        const T* my = lg + lane * E - back;
         float m = -INFINITY, s = 0.f;
         int best = -1;
-        const int steps = len > 0 ? (len + back + STEP - 1) / STEP : 0;
-        for (int k0 = 0; k0 < steps; k0 += U) {
-            uint32_t bits[U];
+        uint32_t best_bits = 0u;
+        const int groups = len > 0 ? (len + back + 1023) / 1024 : 0;
+#pragma unroll 1
+        for (int g = 0; g < groups; ++g) {
+            uint32_t bits = 0u;                            // of this lane's 32 columns
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const uint32_t* w = my_open + g * 32 + u * (STEP / 32);
+                const uint32_t b = back ? __funnelshift_r(w[0], w[1], shift) : w[0] >> shift;
+                bits |= (b & (TABLE - 1)) << (u * E);
+            }
+            if (!__any_sync(0xffffffffu, bits)) continue;
             uint4 raw[U];
+            if (g * 1024 - back >= lo && (g + 1) * 1024 - back <= hi) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) raw[u] = __ldcs(reinterpret_cast<const uint4*>(my + g * 1024 + u * STEP));
+            } else {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int i = g * 1024 + u * STEP + lane * E - back;
+                    raw[u] = make_uint4(0, 0, 0, 0);
+                    if (i >= lo && i + E <= hi) {
+                        raw[u] = __ldcs(reinterpret_cast<const uint4*>(lg + i));
+                    } else {
+                        T* piece = reinterpret_cast<T*>(&raw[u]);
+#pragma unroll
+                        for (int j = 0; j < E; ++j)
+                            if (i + j >= lo && i + j < hi) piece[j] = lg[i + j];
+                    }
+                }
+            }
+            float x[32];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int i = (k0 + u) * STEP + lane * E - back;
-                bits[u] = k0 + u < steps ? bits_at(i) : 0u;
-                raw[u] = make_uint4(0, 0, 0, 0);
-                if (bits[u]) raw[u] = fetch(i);
+                const uint4 k = table[bits >> (u * E) & (TABLE - 1)];
+                constexpr uint32_t N = Vec<T>::NEG;
+                Vec<T>::unpack(make_uint4((raw[u].x & k.x) | (N & ~k.x), (raw[u].y & k.y) | (N & ~k.y),
+                                          (raw[u].z & k.z) | (N & ~k.z), (raw[u].w & k.w) | (N & ~k.w)), x + u * E);
             }
+            float q[4];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (!__any_sync(0xffffffffu, bits[u])) continue;
-                float x[E];
-                Vec<T>::unpack(raw[u], x);
-                close_bits<E>(x, bits[u]);
-                fold_vector<E>(x, k0 + u, m, s, best);
+            for (int i = 0; i < 4; ++i) q[i] = max3(x[i], x[i + 4], x[i + 8]);
+#pragma unroll
+            for (int i = 12; i < 28; i += 8)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) q[k] = max3(q[k], x[i + k], x[i + 4 + k]);
+            const float gm = fmaxf(max3(q[0], x[28], x[29]), max3(max3(q[1], x[30], x[31]), q[2], q[3]));
+            const float mn = fmaxf(m, gm);
+            s = rescaled(s, m, mn);
+            if (gm > m) { best = g; best_bits = bits; }
+            m = mn;
+            f32x2 acc[2] = {0ull, 0ull};
+            if (fabsf(mn) <= kHuge || mn == -INFINITY) {
+                const float r = mn == -INFINITY ? 0.f : __fmul_rn(mn, kLog2e);
+                const f32x2 l2 = pack2(kLog2e, kLog2e), nr = pack2(-r, -r);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[i & 1] = add2(acc[i & 1], ex2_pair(fma2(pack2(x[2 * i], x[2 * i + 1]), l2, nr)));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) acc[0] = add2(acc[0], pack2(ex2((x[i] - mn) * kLog2e), 0.f));
             }
+            float a0, a1;
+            unpack2(add2(acc[0], acc[1]), a0, a1);
+            s += a0 + a1;
         }
-        // the warp's maximum; the lanes that hold it look up its column
-        float M = fmaxf(m, sm);
+        // the warp's maximum and sum
+        float top = fmaxf(m, sm);
 #pragma unroll
-        for (int o = 16; o; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-        float t = rescaled(s, m, M) + rescaled(ss, sm, M);
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        float t = rescaled(s, m, top) + rescaled(ss, sm, top);
 #pragma unroll
         for (int o = 16; o; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-        int at = INT32_MAX;
-        if (M > -INFINITY) {
-            if (sm == M) at = sa;
-            if (m == M) {
-                const int i = best * STEP + lane * E - back;
-                float x[E];
-                Vec<T>::unpack(fetch(i), x);
-                close_bits<E>(x, bits_at(i));
-                int j = E - 1;
-#pragma unroll
-                for (int q = E - 2; q >= 0; --q) j = x[q] == M ? q : j;
-                at = min(at, i + j);
+        const uint32_t in_group = __ballot_sync(0xffffffffu, m == top && best >= 0), in_special = __ballot_sync(0xffffffffu, sm == top && sa != INT32_MAX);
+        Part p = {top, t, INT32_MAX, 0u};
+        if (__popc(in_group) == 1 && in_special == 0u) {
+            // one lane's group holds it: the merge looks the column up if this record wins
+            const int l = __ffs(in_group) - 1;
+            p.at = v0 + c0 + __shfl_sync(0xffffffffu, best, l) * 1024 + l * E - back;
+            p.bits = __shfl_sync(0xffffffffu, best_bits, l);
+        } else if (in_group | in_special) {
+            int at = sm == top ? sa : INT32_MAX;
+            if (m == top && best >= 0) {
+                for (int k = 0; k < 32; ++k) {             // a group's columns ascend with k
+                    const int i = best * 1024 + (k / E) * STEP + lane * E + k % E - back;
+                    if (best_bits >> k & 1u && Vec<T>::one(lg + i) == top) { at = min(at, i); break; }
+                }
             }
+            at = __reduce_min_sync(0xffffffffu, at);
+            p.at = at == INT32_MAX ? INT32_MAX : v0 + c0 + at;
         }
-        at = __reduce_min_sync(0xffffffffu, at);
-        if (lane == 0) {
-            Part p = {M, t, at == INT32_MAX ? INT32_MAX : v0 + c0 + at, 0};
-            a.part[row * n_split + c * a.wpr + warp % a.wpr] = p;
-        }
+        if (lane == 0) a.part[row * n_split + c * a.wpr + warp % a.wpr] = p;
         __syncwarp();                                      // the row's bits have been read
     }
     if (!a.merge_early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
 
-// One warp per row: the row's triples in a fixed order (lane by lane, then a fixed tree).
-__global__ void __launch_bounds__(kThreads) logits_merge_kernel(const Part* __restrict__ part, int64_t n_rows, int n_split,
+// One warp per row: the row's records in a fixed order (lane by lane, then a fixed tree); of equal maxima the first record's.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) logits_merge_kernel(const Part* __restrict__ part, const T* __restrict__ logits,
+                                                                int64_t stride, int64_t n_rows, int n_split,
                                                                 int32_t* __restrict__ out_token, float* __restrict__ out_conf,
                                                                 float* __restrict__ out_lse, int32_t* status_dev) {
+    constexpr int E = Vec<T>::E, STEP = 32 * E;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x & 31;
     const int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
     if (row >= n_rows) return;
     float m = -INFINITY, s = 0.f;
-    int at = INT32_MAX;
+    int from = INT32_MAX;                          // the first record with this maximum
 #pragma unroll 8
     for (int i = lane; i < n_split; i += 32) {
-        const Part p = part[row * n_split + i];
-        const float mn = fmaxf(m, p.m);
-        at = p.m > m ? p.a : p.m == m ? min(at, p.a) : at;
-        s = rescaled(s, m, mn) + rescaled(p.s, p.m, mn);
+        const float2 p = *reinterpret_cast<const float2*>(&part[row * n_split + i]);
+        const float mn = fmaxf(m, p.x);
+        if (p.x > m) from = i;
+        s = rescaled(s, m, mn) + rescaled(p.y, p.x, mn);
         m = mn;
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) {
         const float m2 = __shfl_xor_sync(0xffffffffu, m, o), s2 = __shfl_xor_sync(0xffffffffu, s, o);
-        const int a2 = __shfl_xor_sync(0xffffffffu, at, o);
+        const int f2 = __shfl_xor_sync(0xffffffffu, from, o);
         const float mn = fmaxf(m, m2);
-        at = m2 > m ? a2 : m2 == m ? min(at, a2) : at;
+        from = m2 > m ? f2 : m2 == m ? min(from, f2) : from;
         s = rescaled(s, m, mn) + rescaled(s2, m2, mn);
         m = mn;
     }
+    int token = -1;
+    if (from != INT32_MAX) {
+        const Part p = part[row * n_split + from];
+        token = p.at;
+        if (p.bits) {
+            // lane k looks at the k-th column of the group
+            const int v = p.at + (lane / E) * STEP + lane % E;
+            const bool hit = (p.bits >> lane & 1u) && Vec<T>::one(logits + row * stride + v) == m;
+            const uint32_t hits = __ballot_sync(0xffffffffu, hit);
+            token = __shfl_sync(0xffffffffu, v, hits ? __ffs(hits) - 1 : 0);
+        }
+    }
     if (lane == 0) {
         const bool none = m == -INFINITY;          // nothing left, or only NaN (then s is NaN)
-        const float sum = none && s == 0.f ? 0.f : s;
-        out_token[row] = none || at == INT32_MAX ? -1 : at;
+        const float sum = none ? s : s / term(m, m);
+        out_token[row] = none || token == INT32_MAX ? -1 : token;
         out_conf[row] = none ? sum : 1.0f / sum;
         if (out_lse) out_lse[row] = none ? (sum == 0.f ? -INFINITY : sum) : m + logf(sum);
         if (status_dev && !(isfinite(sum) && m < INFINITY)) count_nonfinite_row(status_dev);
@@ -311,19 +397,22 @@ __global__ void __launch_bounds__(kThreads) logits_merge_kernel(const Part* __re
 // reduction of a row are paid per CTA and per warp), and the grid at least two CTAs per SM.
 void choose_chunk(int64_t units, int rows, int V, int& chunk, int& wpr) {
     wpr = rows >= 8 ? 1 : rows >= 4 ? 2 : rows >= 2 ? 4 : 8;
-    chunk = 4096 * wpr < kMaxChunk ? 4096 * wpr : kMaxChunk;
+    chunk = kBaseCols * wpr < kMaxChunk ? kBaseCols * wpr : kMaxChunk;
     const int64_t want = 2 * (int64_t)sm_count();
     while (chunk / wpr > kMinWarpCols && units * ((V + chunk - 1) / chunk) < want) chunk /= 2;
 }
 
-int shared_bytes(int chunk, int wpr) { return chunk * 4 + chunk / 8 + kWarps * (chunk / wpr / 32 + 2) * 4; }
+int shared_bytes(int chunk, int wpr, int E) {
+    return (16 << E) + chunk * 4 + chunk / 8 + (chunk / 32 + 2) * 2 + chunk * 2 + kWarps * (chunk / wpr / 32 + 1 + kGuard) * 4;
+}
 
 template <typename T>
-int launch(const LogitsArgs& a, int64_t grid, cudaStream_t st) {
+int launch(const LogitsArgs& a, int64_t grid, int64_t n_rows, int32_t* out_token, float* out_conf, float* out_lse, int32_t* status_dev,
+           cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = shared_bytes(a.chunk, a.wpr);
+    cfg.dynamicSmemBytes = shared_bytes(a.chunk, a.wpr, Vec<T>::E);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -331,8 +420,14 @@ int launch(const LogitsArgs& a, int64_t grid, cudaStream_t st) {
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     static std::atomic<unsigned long long> set{0};
-    if (!ensure_dynamic_smem(logits_kernel<T>, shared_bytes(kMaxChunk, 1), set)) return PSD_ERR_CUDA;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, logits_kernel<T>, a);
+    if (!ensure_dynamic_smem(logits_kernel<T>, shared_bytes(kMaxChunk, 1, 8), set)) return PSD_ERR_CUDA;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, logits_kernel<T>, a);
+    count_launch();
+    if (e != cudaSuccess) return PSD_ERR_CUDA;
+    cfg.gridDim = dim3((unsigned)((n_rows + kWarps - 1) / kWarps));
+    cfg.dynamicSmemBytes = 0;
+    e = cudaLaunchKernelEx(&cfg, logits_merge_kernel<T>, (const Part*)a.part, reinterpret_cast<const T*>(a.logits), a.stride, n_rows,
+                           a.n_chunks * a.wpr, out_token, out_conf, out_lse, status_dev);
     count_launch();
     return e == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
 }
@@ -371,22 +466,9 @@ int launch_confidence_logits(const void* logits, int dtype, int64_t row_stride, 
     const int64_t grid = units * a.n_chunks;
     if (grid > INT32_MAX) return PSD_ERR_SHAPE;
     a.merge_early = n_rows <= 8 * kWarps;
-    const int rc = dtype == PSD_BF16 ? launch<__nv_bfloat16>(a, grid, st)
-                 : dtype == PSD_FP16 ? launch<__half>(a, grid, st) : launch<float>(a, grid, st);
-    if (rc != PSD_OK) return rc;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)((n_rows + kWarps - 1) / kWarps));
-    cfg.blockDim = dim3(kThreads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const cudaError_t err = cudaLaunchKernelEx(&cfg, logits_merge_kernel, (const Part*)a.part, n_rows, a.n_chunks * a.wpr,
-                                               out_token, out_conf, out_lse, status_dev);
-    count_launch();
-    return err == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
+    if (dtype == PSD_BF16) return launch<__nv_bfloat16>(a, grid, n_rows, out_token, out_conf, out_lse, status_dev, st);
+    if (dtype == PSD_FP16) return launch<__half>(a, grid, n_rows, out_token, out_conf, out_lse, status_dev, st);
+    return launch<float>(a, grid, n_rows, out_token, out_conf, out_lse, status_dev, st);
 }
 
 }  // namespace psd
