@@ -17,7 +17,8 @@ namespace {
 
 constexpr int kKeysPerCta = 256;
 constexpr int kQStages = 4;
-constexpr int kWThreads = 320;
+constexpr int kEpilogue = 16;           // warps that sum: two per key tile and quarter, 64 columns of a query tile each
+constexpr int kWThreads = (kEpilogue + 2) * 32;
 constexpr int kMaxSplits = 16;
 
 struct WeightsArgs {
@@ -41,8 +42,9 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     constexpr int TILE = SLABS * kSlabBytes;
     unsigned char* k_tiles = smem;                                   // [2][TILE]
     unsigned char* q_tiles = smem + 2 * TILE;                        // [kQStages][TILE]
-    float* lse_buf = reinterpret_cast<float*>(smem + (2 + kQStages) * TILE);       // [8 warps][2][128]
-    uint64_t* bars = reinterpret_cast<uint64_t*>(lse_buf + 8 * 2 * 128);
+    float* lse_buf = reinterpret_cast<float*>(smem + (2 + kQStages) * TILE);       // [kEpilogue][2][64]
+    float* halves = lse_buf + kEpilogue * 2 * 64;                    // [2][128] sums of the second halves
+    uint64_t* bars = reinterpret_cast<uint64_t*>(halves + 256);
     uint64_t *k_full = bars, *q_full = bars + 1, *q_empty = q_full + kQStages, *s_full = q_empty + kQStages /* [2][2] */,
              *s_empty = s_full + 4, *drain = s_empty + 4;
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
@@ -57,13 +59,13 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     if (threadIdx.x == 0) {
         mbar_init(k_full, 1);
         for (int s = 0; s < kQStages; ++s) { mbar_init(&q_full[s], 1); mbar_init(&q_empty[s], 1); }
-        for (int s = 0; s < 4; ++s) { mbar_init(&s_full[s], 1); mbar_init(&s_empty[s], 4); }
+        for (int s = 0; s < 4; ++s) { mbar_init(&s_full[s], 1); mbar_init(&s_empty[s], 8); }
         mbar_init(drain, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 8 && lane == 0) { tma_prefetch_desc(&map_k); tma_prefetch_desc(&map_q); }
-    if (warp == 9) {
+    if (warp == kEpilogue && lane == 0) { tma_prefetch_desc(&map_k); tma_prefetch_desc(&map_q); }
+    if (warp == kEpilogue + 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -81,7 +83,8 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     const int n_it = q_hi - q_lo;
     const int n_kt = L - key0 > 128 ? 2 : 1;      // key tiles that hold keys
 
-    if (warp == 8) {
+    float total = 0.f;
+    if (warp == kEpilogue) {
         if (n_it > 0) {
             const bool leader = elect_one();
             if (leader) {
@@ -113,7 +116,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 }
             }
         }
-    } else if (warp == 9) {
+    } else if (warp == kEpilogue + 1) {
         if (n_it > 0) {
             const bool leader = elect_one();
             const uint32_t idesc = umma_idesc16(128, a.bf16, false);
@@ -148,66 +151,88 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
             }
         }
     } else {
-        const int t = warp >> 2, quarter = warp & 3;
-        const int key = key0 + t * 128 + quarter * 32 + lane;
-        float* lb = lse_buf + warp * 256;
-        const int RT = a.tq * a.G;                        // rows of a query tile
-        f32x2 sum[2] = {0ull, 0ull};
-        const f32x2 cc = pack2(a.c, a.c);
-        bool ok = true;
-        // -lse * log2 e of this lane's four columns of tile `it`; -inf marks a column that adds nothing
-        auto fetch_lse = [&](int it, float (&v)[4]) {
+        const int t = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;
+        float* lb = lse_buf + warp * 128;
+        float s4[4] = {0.f, 0.f, 0.f, 0.f};
+        // This lane's two columns of every query tile: where their lse is, and which token of the tile they belong to.
+        const float* lp[2];
+        int lt_tok[2];
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int c = lane * 4 + u, tok = (q_lo + it) * a.tq + c / a.G;
-                const float l = c < RT && tok < a.T ? a.lse[((int64_t)b * a.T + tok) * a.Hq + h * a.G + c % a.G] : -INFINITY;
+        for (int u = 0; u < 2; ++u) {
+            const int c = half * 64 + lane * 2 + u;
+            lt_tok[u] = c < a.tq * a.G ? c / a.G : a.T;
+            lp[u] = a.lse + ((int64_t)b * a.T + (int64_t)q_lo * a.tq + c / a.G) * a.Hq + h * a.G + c % a.G;
+        }
+        // -lse * log2 e of the columns of tile `it`; -inf marks a column that adds nothing
+        auto fetch_lse = [&](int it, float (&v)[2]) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const float l = lt_tok[u] + (q_lo + it) * a.tq < a.T ? lp[u][(int64_t)it * a.tq * a.Hq] : -INFINITY;
                 v[u] = l == -INFINITY ? -INFINITY : -l * kLog2e;
             }
         };
-        float nl[4];
-        if (t < n_kt && n_it > 0) fetch_lse(0, nl);
-        for (int it = 0; t < n_kt && it < n_it; ++it) {
-            const int buf = it & 1;
-            float* lt = lb + buf * 128;
-            *reinterpret_cast<float4*>(lt + lane * 4) = make_float4(nl[0], nl[1], nl[2], nl[3]);
-            const bool all = __all_sync(0xffffffffu, nl[0] > -INFINITY && nl[1] > -INFINITY && nl[2] > -INFINITY && nl[3] > -INFINITY);
-            if (it + 1 < n_it) fetch_lse(it + 1, nl);
-            __syncwarp();
-            if (!mbar_wait_warp(&s_full[t * 2 + buf], (it >> 1) & 1, wc)) { ok = false; break; }
-            tc_fence_after();
-            const uint32_t at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((t * 2 + buf) * 128);
-#pragma unroll
-            for (int c = 0; c < 128; c += 32) {
-                uint32_t r[32];
-                tmem_ld32(at + c, r);
-                tmem_wait_ld(r);
-                if (c == 96) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&s_empty[t * 2 + buf]);
-                }
+        // Two chunks of 32 columns per tile: while one is summed the next is on its way from tensor memory, across tiles too,
+        // so that the exponentials never wait for a load.
+        const uint32_t lane_at = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(t * 256 + half * 64);
+        uint32_t r[2][32];
+        auto sum = [&](const uint32_t (&r)[32], const float* lt, bool all) {
+            if (all) {
 #pragma unroll
                 for (int j = 0; j < 32; j += 4) {
-                    const float4 l = *reinterpret_cast<const float4*>(lt + c + j);
-                    float x[4];
-                    unpack2(fma2(pack2(__uint_as_float(r[j]), __uint_as_float(r[j + 1])), cc, pack2(l.x, l.y)), x[0], x[1]);
-                    unpack2(fma2(pack2(__uint_as_float(r[j + 2]), __uint_as_float(r[j + 3])), cc, pack2(l.z, l.w)), x[2], x[3]);
-                    if (!all) {      // absent columns hold whatever the tile held there
-                        x[0] = l.x > -INFINITY || l.x != l.x ? x[0] : -INFINITY;
-                        x[1] = l.y > -INFINITY || l.y != l.y ? x[1] : -INFINITY;
-                        x[2] = l.z > -INFINITY || l.z != l.z ? x[2] : -INFINITY;
-                        x[3] = l.w > -INFINITY || l.w != l.w ? x[3] : -INFINITY;
-                    }
-                    sum[0] = add2(sum[0], pack2(ex2(x[0]), ex2(x[1])));
-                    sum[1] = add2(sum[1], pack2(ex2(x[2]), ex2(x[3])));
+                    const float4 l = *reinterpret_cast<const float4*>(lt + j);
+                    const uint32_t* x = r + j;
+                    s4[0] += ex2(fmaf(__uint_as_float(x[0]), a.c, l.x));
+                    s4[1] += ex2(fmaf(__uint_as_float(x[1]), a.c, l.y));
+                    s4[2] += ex2(fmaf(__uint_as_float(x[2]), a.c, l.z));
+                    s4[3] += ex2(fmaf(__uint_as_float(x[3]), a.c, l.w));
+                }
+            } else {
+                // some columns are absent (what the tile holds there is not used)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) {
+                    const float l = lt[j];
+                    if (l != -INFINITY) s4[0] += ex2(fmaf(__uint_as_float(r[j]), a.c, l));
                 }
             }
+        };
+        float nl[2];
+        bool ok = t < n_kt && n_it > 0;
+        if (ok) {
+            fetch_lse(0, nl);
+            ok = mbar_wait_warp(&s_full[t * 2], 0, wc);
+            tc_fence_after();
+            if (ok) tmem_ld32(lane_at, r[0]);
         }
-        if (ok && key < a.P) {
-            float s0, s1, s2, s3;
-            unpack2(sum[0], s0, s1);
-            unpack2(sum[1], s2, s3);
-            const float total = (s0 + s1) + (s2 + s3);
+        for (int it = 0; ok && it < n_it; ++it) {
+            const int buf = it & 1;
+            float* lt = lb + buf * 64;
+            *reinterpret_cast<float2*>(lt + lane * 2) = make_float2(nl[0], nl[1]);
+            const bool all = __all_sync(0xffffffffu, nl[0] > -INFINITY && nl[1] > -INFINITY);
+            if (it + 1 < n_it) fetch_lse(it + 1, nl);
+            __syncwarp();
+            tmem_wait_ld(r[0]);
+            tmem_ld32(lane_at + buf * 128 + 32, r[1]);
+            sum(r[0], lt, all);
+            tmem_wait_ld(r[1]);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&s_empty[t * 2 + buf]);
+            if (it + 1 < n_it) {
+                ok = mbar_wait_warp(&s_full[t * 2 + (buf ^ 1)], ((it + 1) >> 1) & 1, wc);
+                tc_fence_after();
+                if (ok) tmem_ld32(lane_at + (buf ^ 1) * 128, r[0]);
+            }
+            sum(r[1], lt + 32, all);
+        }
+        total = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+        if (half) halves[t * 128 + quarter * 32 + lane] = total;
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp < kEpilogue && !((warp >> 2) & 1) && !*abort_flag) {
+        const int row = (warp >> 3) * 128 + (warp & 3) * 32 + lane, key = key0 + row;
+        total += halves[row];
+        if (key < a.P) {
             const int64_t o = (int64_t)bh * a.P + key;
             if (a.splits > 1)
                 a.part[(int64_t)split * (gridDim.x / a.key_ctas / a.splits) * a.P + o] = total;
@@ -215,10 +240,8 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                 a.acc_out[o] = key < L ? (a.acc_in ? a.beta * a.acc_in[o] : 0.f) + total : 0.f;
         }
     }
-    tc_fence_before();
-    __syncthreads();
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if (warp == 9) {
+    if (warp == kEpilogue + 1) {
         __syncwarp();
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
@@ -256,7 +279,7 @@ WeightsPlan plan_weights(int B, int D, int M, int Hq, int Hkv, int P) {
 
 template <int SLABS>
 int launch_w(const CUtensorMap& mk, const CUtensorMap& mq, const WeightsArgs& a, int64_t grid, cudaStream_t st) {
-    constexpr int smem = (2 + kQStages) * SLABS * kSlabBytes + 8 * 2 * 128 * 4 + 1024 + 256;
+    constexpr int smem = (2 + kQStages) * SLABS * kSlabBytes + kEpilogue * 2 * 64 * 4 + 1024 + 1024 + 256;
     static_assert(smem <= 227 * 1024, "shared memory of the weights kernel");
     static std::atomic<unsigned long long> set{0};
     if (!ensure_dynamic_smem(weights_tc_kernel<SLABS>, smem, set)) return PSD_ERR_CUDA;
