@@ -81,6 +81,15 @@ __device__ __forceinline__ void umma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, ui
                  ::"r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
+// The same with the rows of tensor memory whose bit is set in off[] left as they are.
+__device__ __forceinline__ void umma_f16_ts_rows(uint32_t tmem_d, uint32_t tmem_a, uint64_t desc_b, uint32_t idesc, const uint32_t (&off)[4],
+                                                 uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %8, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%4, %5, %6, %7}, p;\n\t}"
+                 ::"r"(tmem_d), "r"(tmem_a), "l"(desc_b), "r"(idesc), "r"(off[0]), "r"(off[1]), "r"(off[2]), "r"(off[3]), "r"(accumulate)
+                 : "memory");
+}
+
 // 32 lanes x 32 columns without the wait: the caller waits (tmem_wait_ld) before it uses the values.
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
     asm volatile(

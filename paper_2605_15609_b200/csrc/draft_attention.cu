@@ -370,7 +370,8 @@ int launch_dh(OwnArgs& p, cudaStream_t st) {
 
 size_t draft_attention_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
     if (P == 0) return 256;
-    const PrefixPlan p = plan_prefix(B, D, M, Hq, Hkv, Dh, P);
+    const PrefixPlan p = plan_prefix(B, D, M, Hq, Hkv, Dh, P, S);
+    if (p.fused) return 256;
     return ((size_t)B * D * M * Hq * p.splits * (p.dhp + 1) * 4 + 255) / 256 * 256;
 }
 
@@ -379,11 +380,13 @@ int launch_draft_attention(const void* q, const void* k_prefix, const void* v_pr
                            void* out, float* lse, void* workspace, int32_t* status_dev, cudaStream_t st) {
     OwnArgs p = {q, k_prefix, v_prefix, k_own, v_own, prefix_len, own_len, out, lse, a, 0, 1, nullptr, nullptr, 0, 0};
     if (a.P > 0) {
-        const PrefixPlan plan = plan_prefix(a.B, a.D, a.M, a.Hq, a.Hkv, a.Dh, a.P);
+        const PrefixPlan plan = plan_prefix(a.B, a.D, a.M, a.Hq, a.Hkv, a.Dh, a.P, a.S);
         p.rows = (int64_t)a.B * a.D * a.M * a.Hq;
         float* po = reinterpret_cast<float*>(workspace);
         float* pl = po + p.rows * plan.splits * plan.dhp;
-        if (const int e = launch_prefix_attention(q, k_prefix, v_prefix, prefix_len, a, plan, po, pl, status_dev, st)) return e;
+        const int e = launch_prefix_attention(q, k_prefix, v_prefix, prefix_len, k_own, v_own, own_len, a, plan, po, pl, out, lse,
+                                              status_dev, st);
+        if (e != PSD_OK || plan.fused) return e;
         p.po = po;
         p.pl = pl;
         p.splits = plan.splits;

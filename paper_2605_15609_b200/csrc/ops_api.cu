@@ -35,7 +35,7 @@ int check_attention(const psd_attention_t& a, bool with_out) {
     if (with_out) {
         if (a.causal != 0 && a.causal != 1) return PSD_ERR_SHAPE;
         if (a.out_token <= 0 || a.out_head <= 0 || !strides_ok(a.vp) || !strides_ok(a.ko) || !strides_ok(a.vo) ||
-            !strides_small(a.vp))
+            !strides_small(a.vp) || !strides_small(a.ko) || !strides_small(a.vo))
             return PSD_ERR_SHAPE;
         if (a.out_token % 8 || a.out_head % 8 || !strides_aligned(a.vp) || !strides_aligned(a.ko) || !strides_aligned(a.vo))
             return PSD_ERR_ALIGN;

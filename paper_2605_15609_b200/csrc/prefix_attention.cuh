@@ -5,6 +5,7 @@
 namespace psd {
 
 constexpr int kMaxPrefixSplits = 64;   // two per lane of the warp that joins a row
+constexpr int kMaxOwnTiles = 16;       // tiles of own keys that a query tile may have in the fused form
 
 struct PrefixPlan {
     int tq;        // tokens per query tile (tq * Hq/Hkv <= 128 rows)
@@ -12,12 +13,15 @@ struct PrefixPlan {
     int units;     // CTAs along the query tiles
     int splits;    // partial results per row
     int dhp;       // floats per partial output row: 64 or 128
+    bool fused;    // the kernel takes the own keys too and writes final outputs (splits == 1)
 };
-PrefixPlan plan_prefix(int B, int D, int M, int Hq, int Hkv, int Dh, int P);
+PrefixPlan plan_prefix(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S);
 
-// Partial results of every row over its sequence's prefix: po [splits][rows][dhp] normalised outputs (not written where
-// the split holds no key), pl [splits][rows] base-2 log-sum-exps (-inf there); row = token * Hq + head.
-int launch_prefix_attention(const void* q, const void* k, const void* v, const int32_t* prefix_len, const psd_attention_t& a,
-                            const PrefixPlan& p, float* po, float* pl, int32_t* status_dev, cudaStream_t st);
+// plan.fused: final outputs into out and lse (NULL: not wanted).  Otherwise partial results of every row over its sequence's
+// prefix: po [splits][rows][dhp] normalised outputs (not written where the split holds no key), pl [splits][rows] base-2
+// log-sum-exps (-inf there); row = token * Hq + head.
+int launch_prefix_attention(const void* q, const void* k, const void* v, const int32_t* prefix_len, const void* k_own, const void* v_own,
+                            const int32_t* own_len, const psd_attention_t& a, const PrefixPlan& p, float* po, float* pl, void* out,
+                            float* lse, int32_t* status_dev, cudaStream_t st);
 
 }  // namespace psd

@@ -117,6 +117,35 @@ def test_attention(shape, dtype):
         _check_attention(out, lse, *c, Dh ** -0.5, causal, dtype)
 
 
+# several query tiles over an unsplit prefix: the own keys are further tiles of the same kernel, up to five drafts per tile
+ATT_FUSED = [(2, 6, 32, 2, 2, 64, 100, 32), (3, 6, 32, 3, 1, 128, 255, 32), (4, 5, 33, 2, 2, 72, 140, 150), (3, 3, 150, 4, 2, 128, 1, 150),
+             (4, 9, 31, 7, 1, 96, 200, 40)]
+
+
+@pytest.mark.parametrize("shape", ATT_FUSED)
+@pytest.mark.parametrize("layout", ["dense", "padded"])
+def test_attention_own_keys_after_an_unsplit_prefix(shape, layout):
+    for causal in (False, True):
+        for dtype in ("bf16", "fp16"):
+            c = _attention_case(*shape, dtype, seed=sum(shape) + causal, layout=layout)
+            out, lse = _run_attention(*c, 0.3, causal)
+            _check_attention(out, lse, *c, 0.3, causal, dtype)
+
+
+def test_attention_own_scores_far_from_the_prefix():
+    """Rows whose first keys are their own, far below or above anything another draft of the same tile has; no prefix for
+    one sequence, a long way up from the prefix for another."""
+    q, kp, vp, ko, vo, plen, olen = _attention_case(3, 6, 32, 2, 2, 64, 100, 32, "bf16", 29, full=True)
+    q[:, :, :, 0], ko[..., 0] = 8.0, 0.0
+    for n in range(18):
+        ko[n, :, :, 0] = (-120.0, 60.0, 0.0, -30.0, 90.0, -200.0)[n % 6]
+    plen = [0, 100, 37]
+    c = (q, kp, vp, ko, vo, plen, olen)
+    for causal in (False, True):
+        out, lse = _run_attention(*c, 1.0, causal)
+        _check_attention(out, lse, *c, 1.0, causal, "bf16")
+
+
 @pytest.mark.parametrize("layout", ["heads_first", "padded"])
 @pytest.mark.parametrize("shape", [ATT[2], ATT[5], ATT[7], ATT[12]])
 def test_attention_strides(shape, layout):
@@ -147,7 +176,7 @@ def test_attention_lengths_are_clamped_and_default_to_the_capacity():
     assert bool((z[0] == 0).all()) and bool((z[1] == -float("inf")).all())
 
 
-@pytest.mark.parametrize("shape", [ATT[4], ATT[5], ATT[14]])
+@pytest.mark.parametrize("shape", [ATT[4], ATT[5], ATT[14], ATT_FUSED[0], ATT_FUSED[1], ATT_FUSED[4]])
 def test_a_draft_never_sees_another_drafts_keys(shape):
     """NaN and infinities in one draft's own keys and values change no other draft's outputs, bit for bit."""
     q, kp, vp, ko, vo, plen, olen = _attention_case(*shape, "bf16", 11, full=True)
