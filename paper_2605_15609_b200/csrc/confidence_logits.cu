@@ -9,7 +9,9 @@
 // its own: open = allowed, inside the vocabulary and not special; the special tokens are then edited 32 at a time, with
 // separately rounded operations.  The loop that streams the logits knows nothing but the bits, whatever the edits are (a
 // table in shared memory turns the bits of a 16-byte vector into the mask of its words), and does not load a group of
-// vectors of which no column is open.  What bounds it is the instructions per column (about 8) next to the bytes.
+// vectors of which no column is open.  What bounds it is the instructions per column (about 9, two of them at an eighth and a
+// half of the issue rate) and how many warps hide each other's loads: four CTAs per SM of 64 registers a thread beat three of
+// 80 (8192 x 126464 bf16: 592 against 667 us), and chunks of 4096 columns beat 2048 (the set-up per CTA) and 8192.
 //
 // Sums are kept relative to 2^r, r = the rounded product m * log2 e, so that a term is one FMA and one exponential,
 // 2^(x log2 e - r), and the rounding of r is the same in every term, the maximum's own included: it cancels in
@@ -28,10 +30,8 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxChunk = 16384;      // tokens per CTA: 64 KB of counts
 constexpr int kMinWarpCols = 256;     // columns a warp takes at least (sets the number of records per row)
 constexpr int kRowsPerCta = 64;
-#ifndef PSD_BASE
-#define PSD_BASE 8192
-#endif
-constexpr int kBaseCols = PSD_BASE;
+constexpr int kBaseCols = 4096;       // columns of a row that a warp takes at most
+constexpr int kCtas = 4;              // resident CTAs per SM that registers and shared memory are kept to
 constexpr int kGuard = 36;            // closed words behind a warp's open bits: a group of 1024 columns may reach past them
 constexpr float kHuge = 1e37f;
 
@@ -55,37 +55,41 @@ template <typename T> struct Vec;
 template <> struct Vec<__nv_bfloat16> {
     static constexpr int E = 8;
     static constexpr uint32_t NEG = 0xff80ff80u;           // two times -inf
-    static __device__ __forceinline__ void unpack(const uint4& r, float* x) {
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
-    }
     static __device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+    // two columns, and the larger of two words' columns (exact: a maximum needs no wider type)
+    static __device__ __forceinline__ f32x2 pair(const uint32_t* w, int i) { return pack2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u)); }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        uint32_t d;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+        return d;
+    }
+    static __device__ __forceinline__ float top(uint32_t w) { return fmaxf(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 };
 template <> struct Vec<__half> {
     static constexpr int E = 8;
     static constexpr uint32_t NEG = 0xfc00fc00u;
-    static __device__ __forceinline__ void unpack(const uint4& r, float* x) {
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
-            x[2 * i] = f.x;
-            x[2 * i + 1] = f.y;
-        }
-    }
     static __device__ __forceinline__ float one(const __half* p) { return __half2float(*p); }
+    static __device__ __forceinline__ f32x2 pair(const uint32_t* w, int i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[i]));
+        return pack2(f.x, f.y);
+    }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        uint32_t d;
+        asm("max.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+        return d;
+    }
+    static __device__ __forceinline__ float top(uint32_t w) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+        return fmaxf(f.x, f.y);
+    }
 };
 template <> struct Vec<float> {
     static constexpr int E = 4;
     static constexpr uint32_t NEG = 0xff800000u;
-    static __device__ __forceinline__ void unpack(const uint4& r, float* x) {
-        x[0] = __uint_as_float(r.x); x[1] = __uint_as_float(r.y); x[2] = __uint_as_float(r.z); x[3] = __uint_as_float(r.w);
-    }
     static __device__ __forceinline__ float one(const float* p) { return *p; }
+    static __device__ __forceinline__ f32x2 pair(const uint32_t* w, int i) { return pack2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1])); }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }
+    static __device__ __forceinline__ float top(uint32_t w) { return __uint_as_float(w); }
 };
 
 // Term of x in a sum with maximum m >= x.
@@ -101,7 +105,7 @@ __device__ __forceinline__ float rescaled(float s, float m, float M) {
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 3) logits_kernel(const LogitsArgs a) {
+__global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(const LogitsArgs a) {
     constexpr int E = Vec<T>::E;               // columns of a 16-byte vector
     constexpr int STEP = 32 * E;               // columns of a warp per vector and lane
     constexpr int U = 32 / E;                  // vectors of a group: 32 columns per lane, 1024 per warp
@@ -163,7 +167,7 @@ __global__ void __launch_bounds__(kThreads, 3) logits_kernel(const LogitsArgs a)
         }
         __syncthreads();
     }
-#pragma unroll 4
+#pragma unroll 16
     for (int w = warp; w < words; w += kWarps) {
         const int i = w * 32 + lane;
         const bool sp = i < vw && ((counts && cnt[i] > 0) || (bias && bias[i] != 0.f));
@@ -276,35 +280,43 @@ __global__ void __launch_bounds__(kThreads, 3) logits_kernel(const LogitsArgs a)
                     }
                 }
             }
-            float x[32];
+            uint32_t w[4 * U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const uint4 k = table[bits >> (u * E) & (TABLE - 1)];
                 constexpr uint32_t N = Vec<T>::NEG;
-                Vec<T>::unpack(make_uint4((raw[u].x & k.x) | (N & ~k.x), (raw[u].y & k.y) | (N & ~k.y),
-                                          (raw[u].z & k.z) | (N & ~k.z), (raw[u].w & k.w) | (N & ~k.w)), x + u * E);
+                w[4 * u] = (raw[u].x & k.x) | (N & ~k.x);
+                w[4 * u + 1] = (raw[u].y & k.y) | (N & ~k.y);
+                w[4 * u + 2] = (raw[u].z & k.z) | (N & ~k.z);
+                w[4 * u + 3] = (raw[u].w & k.w) | (N & ~k.w);
             }
-            float q[4];
+            uint32_t q[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = max3(x[i], x[i + 4], x[i + 8]);
+            for (int i = 0; i < 4; ++i) {
+                q[i] = w[i];
 #pragma unroll
-            for (int i = 12; i < 28; i += 8)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) q[k] = max3(q[k], x[i + k], x[i + 4 + k]);
-            const float gm = fmaxf(max3(q[0], x[28], x[29]), max3(max3(q[1], x[30], x[31]), q[2], q[3]));
-            const float mn = fmaxf(m, gm);
-            s = rescaled(s, m, mn);
-            if (gm > m) { best = g; best_bits = bits; }
-            m = mn;
+                for (int k = 4; k < 4 * U; k += 4) q[i] = Vec<T>::larger(q[i], w[i + k]);
+            }
+            const float gm = Vec<T>::top(Vec<T>::larger(Vec<T>::larger(q[0], q[1]), Vec<T>::larger(q[2], q[3])));
+            if (gm > m) {
+                s = rescaled(s, m, gm);
+                best = g;
+                best_bits = bits;
+                m = gm;
+            }
             f32x2 acc[2] = {0ull, 0ull};
-            if (fabsf(mn) <= kHuge || mn == -INFINITY) {
-                const float r = mn == -INFINITY ? 0.f : __fmul_rn(mn, kLog2e);
+            if (fabsf(m) <= kHuge || m == -INFINITY) {
+                const float r = m == -INFINITY ? 0.f : __fmul_rn(m, kLog2e);
                 const f32x2 l2 = pack2(kLog2e, kLog2e), nr = pack2(-r, -r);
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[i & 1] = add2(acc[i & 1], ex2_pair(fma2(pack2(x[2 * i], x[2 * i + 1]), l2, nr)));
+                for (int i = 0; i < U * E / 2; ++i) acc[i & 1] = add2(acc[i & 1], ex2_pair(fma2(Vec<T>::pair(w, i), l2, nr)));
             } else {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) acc[0] = add2(acc[0], pack2(ex2((x[i] - mn) * kLog2e), 0.f));
+                for (int i = 0; i < U * E / 2; ++i) {
+                    float x, y;
+                    unpack2(Vec<T>::pair(w, i), x, y);
+                    acc[0] = add2(acc[0], pack2(ex2((x - m) * kLog2e), ex2((y - m) * kLog2e)));
+                }
             }
             float a0, a1;
             unpack2(add2(acc[0], acc[1]), a0, a1);

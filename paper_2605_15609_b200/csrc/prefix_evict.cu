@@ -1,9 +1,9 @@
 // Eviction from the prefix's cache by accumulated attention weight.
 //
 // Kernel 1, one CTA per (sequence, key head): finds the n-th largest score among the positions that are not kept
-// anyway by a radix select over order-preserving 32-bit keys (11, 11 and 10 bits; histograms in shared memory), then
-// walks the positions in order and writes those above the threshold key, and the first of those equal to it.  The scores
-// of up to kCached positions stay in shared memory after the first read.
+// anyway by a radix select over order-preserving 32-bit keys (11, 11 and 10 bits; four copies of the histogram in shared
+// memory, since scores of one magnitude fall into few bins), then every warp walks a run of positions, counts what it keeps,
+// and, after one scan over the warps, writes it in order.  The keys of up to kCached positions stay in shared memory.
 // Kernel 2 copies the kept rows: 16 bytes per thread, consecutive threads along a row; this is the part that is bound
 // by memory (two rows read and two written per kept position).
 #include "ops_internal.cuh"
@@ -14,7 +14,8 @@ namespace {
 
 constexpr int kSelThreads = 1024;
 constexpr int kBins = 2048;
-constexpr int kCached = 48 * 1024;   // keys held in shared memory (192 KB)
+constexpr int kCopies = 4;
+constexpr int kCached = 40 * 1024;   // keys held in shared memory (160 KB)
 
 // Larger key = higher score; NaN is the lowest, -0 equals +0.
 __device__ __forceinline__ uint32_t score_key(float x) {
@@ -34,11 +35,12 @@ struct SelectArgs {
 
 __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectArgs a) {
     extern __shared__ uint32_t keys[];             // [cached]
-    __shared__ uint32_t hist[kBins];
-    __shared__ uint32_t warp_sum[32];
+    __shared__ uint32_t hist[kCopies][kBins];
+    __shared__ uint32_t warp_sum[32], warp_eq[32];
     __shared__ uint32_t s_digit, s_left;
     const int bh = blockIdx.x, b = bh / a.Hkv, h = bh % a.Hkv;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    for (int i = tid; i < kCopies * kBins; i += kSelThreads) (&hist[0][0])[i] = 0;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int L = a.prefix_len ? min(max(a.prefix_len[b], 0), a.P) : a.P;
     const float* sc = a.scores + (int64_t)bh * a.P;
@@ -52,104 +54,111 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
     }
     // positions [lo, hi) compete for n_free places; the others are kept
     const int lo = min(a.n_sink, L), hi = max(lo, L - a.n_recent);
-    uint32_t threshold = 0, n_equal = 0;            // keep keys > threshold, and the first n_equal equal to it
-    if (L > a.keep) {
-        const bool cached = L <= a.cached;
+    const bool all = L <= a.keep;
+    const bool cached = !all && L <= a.cached;
+    auto key_at = [&](int i) { return cached ? keys[i] : score_key(sc[i]); };
+    uint32_t threshold = 0xffffffffu, n_equal = 0;  // keep keys > threshold, and the first n_equal equal to it
+    __syncthreads();
+    if (!all) {
         uint32_t left = (uint32_t)(a.keep - lo - (L - hi));      // n_free < hi - lo here
         uint32_t prefix = 0, mask = 0;
-        if (left > 0) {
 #pragma unroll 1
-            for (int pass = 0; pass < 3; ++pass) {
-                const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-                const uint32_t digits = pass == 2 ? 1023u : 2047u;
-                for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
-                __syncthreads();
-                for (int i = lo + tid; i < hi; i += kSelThreads) {
-                    uint32_t k;
-                    if (pass == 0 || !cached) {
-                        k = score_key(sc[i]);
+        for (int pass = 0; pass < 3 && left > 0; ++pass) {
+            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+            const uint32_t digits = pass == 2 ? 1023u : 2047u;
+            uint32_t* mine = hist[lane & (kCopies - 1)];
+            if (pass == 0) {
+                // the scores once, eight loads in flight per thread
+#pragma unroll 1
+                for (int i0 = tid; i0 < L; i0 += 8 * kSelThreads) {
+                    float x[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) x[u] = i0 + u * kSelThreads < L ? sc[i0 + u * kSelThreads] : 0.f;
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const int i = i0 + u * kSelThreads;
+                        if (i >= L) break;
+                        const uint32_t k = score_key(x[u]);
                         if (cached) keys[i] = k;
-                    } else {
-                        k = keys[i];
+                        if (i >= lo && i < hi) atomicAdd(&mine[k >> 21], 1u);
                     }
-                    if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & digits], 1u);
                 }
-                __syncthreads();
-                // suffix sums: thread t owns bins 2t, 2t + 1, counted from the top
-                const int b1 = kBins - 1 - 2 * tid, b0 = b1 - 1;
-                const uint32_t c1 = hist[b1], c0 = hist[b0];
-                uint32_t run = c0 + c1;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const uint32_t y = __shfl_up_sync(0xffffffffu, run, o);
-                    if (lane >= o) run += y;
+            } else {
+                for (int i = lo + tid; i < hi; i += kSelThreads) {
+                    const uint32_t k = key_at(i);
+                    if ((k & mask) == prefix) atomicAdd(&mine[(k >> shift) & digits], 1u);
                 }
-                if (lane == 31) warp_sum[warp] = run;
-                __syncthreads();
-                if (warp == 0) {
-                    uint32_t w = warp_sum[lane];
-#pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) {
-                        const uint32_t y = __shfl_up_sync(0xffffffffu, w, o);
-                        if (lane >= o) w += y;
-                    }
-                    warp_sum[lane] = w;
-                }
-                __syncthreads();
-                const uint32_t above = run - c0 - c1 + (warp ? warp_sum[warp - 1] : 0u);   // keys in higher bins
-                if (above < left && above + c1 >= left) { s_digit = b1; s_left = left - above; }
-                else if (above + c1 < left && above + c1 + c0 >= left) { s_digit = b0; s_left = left - above - c1; }
-                __syncthreads();
-                prefix |= s_digit << shift;
-                mask |= digits << shift;
-                left = s_left;
-                __syncthreads();
             }
-            threshold = prefix;
-            n_equal = left;
-        } else {
-            threshold = 0xffffffffu;                 // no score is above this
-        }
-    }
-    // ordered write: per tile of 1024 positions, counts of kept and of equal keys before each thread
-    uint32_t base_above = 0, base_eq = 0;
-    const bool all = L <= a.keep;
-    for (int t0 = 0; t0 < L; t0 += kSelThreads) {
-        const int i = t0 + tid;
-        float x = 0.f;
-        bool above = false, eq = false;
-        if (i < L) {
-            x = sc[i];
-            const uint32_t k = score_key(x);
-            const bool middle = i >= lo && i < hi;
-            above = all || !middle || k > threshold;
-            eq = !above && k == threshold && n_equal > 0;
-        }
-        const uint32_t ba = __ballot_sync(0xffffffffu, above), be = __ballot_sync(0xffffffffu, eq);
-        if (lane == 0) warp_sum[warp] = __popc(ba) | (__popc(be) << 16);
-        __syncthreads();
-        if (warp == 0) {
-            uint32_t w = warp_sum[lane];
+            __syncthreads();
+            // suffix sums: thread t owns bins 2t, 2t + 1, counted from the top (and clears them for the next pass)
+            const int b1 = kBins - 1 - 2 * tid, b0 = b1 - 1;
+            uint32_t c1 = 0, c0 = 0;
+#pragma unroll
+            for (int q = 0; q < kCopies; ++q) {
+                c1 += hist[q][b1];
+                c0 += hist[q][b0];
+                hist[q][b1] = hist[q][b0] = 0;
+            }
+            uint32_t run = c0 + c1;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t y = __shfl_up_sync(0xffffffffu, w, o);
-                if (lane >= o) w += y;
+                const uint32_t y = __shfl_up_sync(0xffffffffu, run, o);
+                if (lane >= o) run += y;
             }
-            warp_sum[lane] = w;
+            if (lane == 31) warp_sum[warp] = run;
+            __syncthreads();
+            uint32_t before = lane < warp ? warp_sum[lane] : 0u;
+            before = __reduce_add_sync(0xffffffffu, before);
+            const uint32_t above = run - c0 - c1 + before;       // keys in higher bins
+            if (above < left && above + c1 >= left) { s_digit = b1; s_left = left - above; }
+            else if (above + c1 < left && above + c1 + c0 >= left) { s_digit = b0; s_left = left - above - c1; }
+            __syncthreads();
+            prefix |= s_digit << shift;
+            mask |= digits << shift;
+            left = s_left;
         }
-        __syncthreads();
-        const uint32_t before = warp ? warp_sum[warp - 1] : 0u, total = warp_sum[31];
-        const uint32_t lt = (1u << lane) - 1u;
-        const uint32_t n_above = base_above + (before & 0xffffu) + __popc(ba & lt);
-        const uint32_t eq_before = base_eq + (before >> 16) + __popc(be & lt);
+        if (left > 0) {
+            threshold = prefix;
+            n_equal = left;
+        }
+    }
+    // ordered write: a warp takes a run of positions, in steps of 32; first counts, then places
+    const int per = (L + 32 * 32 - 1) / (32 * 32) * 32, i0 = warp * per, i1 = min(L, i0 + per);
+    auto flags = [&](int i, bool& above, bool& eq) {
+        above = eq = false;
+        if (i < i1) {
+            const bool forced = all || i < lo || i >= hi;
+            const uint32_t k = forced ? 0u : key_at(i);
+            above = forced || k > threshold;
+            eq = !above && k == threshold && n_equal > 0;
+        }
+    };
+    uint32_t n_above = 0, n_eq = 0;
+#pragma unroll 4
+    for (int i = i0; i < i1; i += 32) {
+        bool above, eq;
+        flags(i + lane, above, eq);
+        n_above += __popc(__ballot_sync(0xffffffffu, above));
+        n_eq += __popc(__ballot_sync(0xffffffffu, eq));
+    }
+    if (lane == 0) { warp_sum[warp] = n_above; warp_eq[warp] = n_eq; }
+    __syncthreads();
+    uint32_t base_above = __reduce_add_sync(0xffffffffu, lane < warp ? warp_sum[lane] : 0u);
+    uint32_t base_eq = __reduce_add_sync(0xffffffffu, lane < warp ? warp_eq[lane] : 0u);
+    const uint32_t lt = (1u << lane) - 1u;
+#pragma unroll 4
+    for (int i = i0; i < i1; i += 32) {
+        bool above, eq;
+        flags(i + lane, above, eq);
+        const uint32_t ba = __ballot_sync(0xffffffffu, above), be = __ballot_sync(0xffffffffu, eq);
+        const uint32_t eq_before = base_eq + __popc(be & lt);
         if (above || (eq && eq_before < n_equal)) {
-            const uint32_t at = n_above + min(eq_before, n_equal);
-            index[at] = i;
-            if (so) so[at] = x;
+            const uint32_t at = base_above + __popc(ba & lt) + min(eq_before, n_equal);
+            index[at] = i + lane;
+            if (so) so[at] = sc[i + lane];
         }
-        base_above += total & 0xffffu;
-        base_eq += total >> 16;
-        __syncthreads();
+        base_above += __popc(ba);
+        base_eq += __popc(be);
     }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
