@@ -15,6 +15,7 @@ namespace {
 constexpr int kSelThreads = 1024;
 constexpr int kBins = 2048;
 constexpr int kCopies = 4;
+constexpr int kPad = 8;              // words between copies beyond the bins: equal bins of different copies are in different banks
 constexpr int kCached = 40 * 1024;   // keys held in shared memory (160 KB)
 
 // Larger key = higher score; NaN is the lowest, -0 equals +0.
@@ -27,20 +28,22 @@ __device__ __forceinline__ uint32_t score_key(float x) {
 struct SelectArgs {
     const float* scores;
     const int32_t* prefix_len;
-    int P, Hkv, keep, n_sink, n_recent, cached;
+    int P, Hkv, keep, n_sink, n_recent;
     int32_t* index;
     float* scores_out;
     int32_t* len_out;
 };
 
+// CACHED: the keys stay in shared memory after the first pass (P <= kCached); otherwise every pass makes them again.
+template <bool CACHED>
 __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectArgs a) {
-    extern __shared__ uint32_t keys[];             // [cached]
-    __shared__ uint32_t hist[kCopies][kBins];
+    extern __shared__ uint32_t keys[];             // [P] if CACHED
+    __shared__ uint32_t hist[kCopies][kBins + kPad];
     __shared__ uint32_t warp_sum[32], warp_eq[32];
     __shared__ uint32_t s_digit, s_left;
     const int bh = blockIdx.x, b = bh / a.Hkv, h = bh % a.Hkv;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    for (int i = tid; i < kCopies * kBins; i += kSelThreads) (&hist[0][0])[i] = 0;
+    for (int i = tid; i < kCopies * (kBins + kPad); i += kSelThreads) (&hist[0][0])[i] = 0;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int L = a.prefix_len ? min(max(a.prefix_len[b], 0), a.P) : a.P;
     const float* sc = a.scores + (int64_t)bh * a.P;
@@ -52,18 +55,25 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
         index[i] = -1;
         if (so) so[i] = 0.f;
     }
-    // positions [lo, hi) compete for n_free places; the others are kept
+    if (L <= a.keep) {
+        for (int i = tid; i < L; i += kSelThreads) {
+            index[i] = i;
+            if (so) so[i] = sc[i];
+        }
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+        return;
+    }
+    // positions [lo, hi) compete for n_free places; the others are kept: their keys are the largest there is (no score's)
     const int lo = min(a.n_sink, L), hi = max(lo, L - a.n_recent);
-    const bool all = L <= a.keep;
-    const bool cached = !all && L <= a.cached;
-    auto key_at = [&](int i) { return cached ? keys[i] : score_key(sc[i]); };
-    uint32_t threshold = 0xffffffffu, n_equal = 0;  // keep keys > threshold, and the first n_equal equal to it
+    auto make_key = [&](int i, float x) { return (unsigned)(i - lo) < (unsigned)(hi - lo) ? score_key(x) : 0xffffffffu; };
+    auto key_at = [&](int i) { return CACHED ? keys[i] : make_key(i, sc[i]); };
+    uint32_t threshold = 0xfffffffeu, n_equal = 0;  // keep keys > threshold, and the first n_equal equal to it
     __syncthreads();
-    if (!all) {
+    {
         uint32_t left = (uint32_t)(a.keep - lo - (L - hi));      // n_free < hi - lo here
         uint32_t prefix = 0, mask = 0;
 #pragma unroll 1
-        for (int pass = 0; pass < 3 && left > 0; ++pass) {
+        for (int pass = 0; pass < 3; ++pass) {
             const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
             const uint32_t digits = pass == 2 ? 1023u : 2047u;
             uint32_t* mine = hist[lane & (kCopies - 1)];
@@ -78,18 +88,20 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
                     for (int u = 0; u < 8; ++u) {
                         const int i = i0 + u * kSelThreads;
                         if (i >= L) break;
-                        const uint32_t k = score_key(x[u]);
-                        if (cached) keys[i] = k;
-                        if (i >= lo && i < hi) atomicAdd(&mine[k >> 21], 1u);
+                        const uint32_t k = make_key(i, x[u]);
+                        if (CACHED) keys[i] = k;
+                        if (k != 0xffffffffu) atomicAdd(&mine[k >> 21], 1u);
                     }
                 }
             } else {
-                for (int i = lo + tid; i < hi; i += kSelThreads) {
+#pragma unroll 4
+                for (int i = tid; i < L; i += kSelThreads) {
                     const uint32_t k = key_at(i);
-                    if ((k & mask) == prefix) atomicAdd(&mine[(k >> shift) & digits], 1u);
+                    if ((k & mask) == prefix && k != 0xffffffffu) atomicAdd(&mine[(k >> shift) & digits], 1u);
                 }
             }
             __syncthreads();
+            if (left == 0) break;                                // every place is taken (the keys have been made)
             // suffix sums: thread t owns bins 2t, 2t + 1, counted from the top (and clears them for the next pass)
             const int b1 = kBins - 1 - 2 * tid, b0 = b1 - 1;
             uint32_t c1 = 0, c0 = 0;
@@ -124,22 +136,12 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
     }
     // ordered write: a warp takes a run of positions, in steps of 32; first counts, then places
     const int per = (L + 32 * 32 - 1) / (32 * 32) * 32, i0 = warp * per, i1 = min(L, i0 + per);
-    auto flags = [&](int i, bool& above, bool& eq) {
-        above = eq = false;
-        if (i < i1) {
-            const bool forced = all || i < lo || i >= hi;
-            const uint32_t k = forced ? 0u : key_at(i);
-            above = forced || k > threshold;
-            eq = !above && k == threshold && n_equal > 0;
-        }
-    };
     uint32_t n_above = 0, n_eq = 0;
 #pragma unroll 4
     for (int i = i0; i < i1; i += 32) {
-        bool above, eq;
-        flags(i + lane, above, eq);
-        n_above += __popc(__ballot_sync(0xffffffffu, above));
-        n_eq += __popc(__ballot_sync(0xffffffffu, eq));
+        const uint32_t k = i + lane < i1 ? key_at(i + lane) : 0u;
+        n_above += __popc(__ballot_sync(0xffffffffu, k > threshold));
+        n_eq += __popc(__ballot_sync(0xffffffffu, k == threshold && i + lane < i1));
     }
     if (lane == 0) { warp_sum[warp] = n_above; warp_eq[warp] = n_eq; }
     __syncthreads();
@@ -148,8 +150,8 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
     const uint32_t lt = (1u << lane) - 1u;
 #pragma unroll 4
     for (int i = i0; i < i1; i += 32) {
-        bool above, eq;
-        flags(i + lane, above, eq);
+        const uint32_t k = i + lane < i1 ? key_at(i + lane) : 0u;
+        const bool above = k > threshold, eq = k == threshold && i + lane < i1;
         const uint32_t ba = __ballot_sync(0xffffffffu, above), be = __ballot_sync(0xffffffffu, eq);
         const uint32_t eq_before = base_eq + __popc(be & lt);
         if (above || (eq && eq_before < n_equal)) {
@@ -212,22 +214,21 @@ psd_kv_strides_t pieces_of(const psd_kv_strides_t& s) { return {s.outer / 8, s.t
 int launch_prefix_evict(const float* scores, const void* k, const void* v, const int32_t* prefix_len,
                         const psd_evict_t& e, void* k_out, void* v_out, int32_t* index, float* scores_out,
                         int32_t* len_out, cudaStream_t st) {
-    SelectArgs s = {scores, prefix_len, e.P, e.Hkv, e.keep, e.n_sink, e.n_recent, e.P < kCached ? e.P : kCached,
-                    index, scores_out, len_out};
-    if (e.P > kCached) s.cached = 0;       // too long to hold: every pass reads the scores again (from L2)
+    SelectArgs s = {scores, prefix_len, e.P, e.Hkv, e.keep, e.n_sink, e.n_recent, index, scores_out, len_out};
+    const bool cached = e.P <= kCached;
     static std::atomic<unsigned long long> smem_set{0};
-    if (!ensure_dynamic_smem(evict_select_kernel, kCached * 4, smem_set)) return PSD_ERR_CUDA;
+    if (!ensure_dynamic_smem(evict_select_kernel<true>, kCached * 4, smem_set)) return PSD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(e.B * e.Hkv);
     cfg.blockDim = dim3(kSelThreads);
-    cfg.dynamicSmemBytes = (size_t)s.cached * 4;
+    cfg.dynamicSmemBytes = cached ? (size_t)e.P * 4 : 0;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    cudaError_t err = cudaLaunchKernelEx(&cfg, evict_select_kernel, s);
+    cudaError_t err = cached ? cudaLaunchKernelEx(&cfg, evict_select_kernel<true>, s) : cudaLaunchKernelEx(&cfg, evict_select_kernel<false>, s);
     count_launch();
     if (err != cudaSuccess) return PSD_ERR_CUDA;
     GatherArgs g = {};
