@@ -355,21 +355,40 @@ int launch_rows(OwnArgs& p, cudaStream_t st) {
     count_launch();
     return e == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
 }
-// Rows per CTA: 64 where that still gives every SM two CTAs, fewer otherwise (then four warps share the keys and the join of
-// a row block).
+// Rows per CTA, in blocks of 16: 64 where that still gives every SM two CTAs, fewer otherwise (then four warps share the keys
+// and the join of a row block).
+int row_blocks_per_cta(int64_t nodes_heads, int rows) {
+    const int64_t want = 2 * sm_count();
+    if (rows > 32 && nodes_heads * ((rows + 63) / 64) >= want) return 4;
+    if (rows > 16 && nodes_heads * ((rows + 31) / 32) >= want) return 2;
+    return 1;
+}
+
+// Whether this kernel walks the prefix too, in one launch: it reads the prefix once per draft instead of once per sequence, but
+// saves a launch and the join.  It does while a wave of its CTAs (three per SM) has few tiles of 64 keys to walk: measured, one
+// launch against two, 4 drafts of 32 tokens: 4 heads of 64, prefix 257: 7 against 15 us, 1024: 13 against 16, 2048: 22 against
+// 16; 32 heads of 128 over 8 key heads, prefix 257: 13 against 16 us, 512: 17 against 20, 1024: 27 against 22.
+bool one_launch(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
+    const int rows = M * (Hq / Hkv);
+    const int64_t nh = (int64_t)B * D * Hkv;
+    const int r = 16 * row_blocks_per_cta(nh, rows);
+    const int64_t ctas = nh * ((rows + r - 1) / r), waves = (ctas + 3 * sm_count() - 1) / (3 * sm_count());
+    return waves * ((P + kKeys - 1) / kKeys) <= (Dh <= 64 ? 16 : 8);
+}
+
 template <typename T, int DHP>
 int launch_dh(OwnArgs& p, cudaStream_t st) {
-    const int rows = p.a.M * (p.a.Hq / p.a.Hkv);
-    const int64_t nh = (int64_t)p.a.B * p.a.D * p.a.Hkv, want = 2 * sm_count();
-    if (rows > 32 && nh * ((rows + 63) / 64) >= want) return launch_rows<T, DHP, 4>(p, st);
-    if (rows > 16 && nh * ((rows + 31) / 32) >= want) return launch_rows<T, DHP, 2>(p, st);
-    return launch_rows<T, DHP, 1>(p, st);
+    switch (row_blocks_per_cta((int64_t)p.a.B * p.a.D * p.a.Hkv, p.a.M * (p.a.Hq / p.a.Hkv))) {
+        case 4: return launch_rows<T, DHP, 4>(p, st);
+        case 2: return launch_rows<T, DHP, 2>(p, st);
+        default: return launch_rows<T, DHP, 1>(p, st);
+    }
 }
 
 }  // namespace
 
 size_t draft_attention_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
-    if (P == 0) return 256;
+    if (one_launch(B, D, M, Hq, Hkv, Dh, P)) return 256;
     const PrefixPlan p = plan_prefix(B, D, M, Hq, Hkv, Dh, P, S);
     if (p.fused) return 256;
     return ((size_t)B * D * M * Hq * p.splits * (p.dhp + 1) * 4 + 255) / 256 * 256;
@@ -379,7 +398,7 @@ int launch_draft_attention(const void* q, const void* k_prefix, const void* v_pr
                            const void* k_own, const void* v_own, const int32_t* own_len, const psd_attention_t& a,
                            void* out, float* lse, void* workspace, int32_t* status_dev, cudaStream_t st) {
     OwnArgs p = {q, k_prefix, v_prefix, k_own, v_own, prefix_len, own_len, out, lse, a, 0, 1, nullptr, nullptr, 0, 0};
-    if (a.P > 0) {
+    if (!one_launch(a.B, a.D, a.M, a.Hq, a.Hkv, a.Dh, a.P)) {
         const PrefixPlan plan = plan_prefix(a.B, a.D, a.M, a.Hq, a.Hkv, a.Dh, a.P, a.S);
         p.rows = (int64_t)a.B * a.D * a.M * a.Hq;
         float* po = reinterpret_cast<float*>(workspace);

@@ -122,6 +122,60 @@ ATT_FUSED = [(2, 6, 32, 2, 2, 64, 100, 32), (3, 6, 32, 3, 1, 128, 255, 32), (4, 
              (4, 9, 31, 7, 1, 96, 200, 40)]
 
 
+# prefixes long enough for the tensor-core kernel: split along the keys, one and several query tiles
+ATT_LONG = [(1, 1, 1, 2, 1, 64, 2100, 3), (2, 3, 1, 8, 2, 128, 1153, 70), (1, 4, 32, 4, 4, 64, 3001, 32), (3, 2, 5, 6, 2, 128, 1279, 5),
+            (2, 2, 40, 14, 2, 80, 1400, 40), (1, 8, 3, 128, 1, 96, 900, 3), (1, 2, 150, 3, 3, 128, 1025, 150)]
+# the same with enough sequences and heads that nothing is split
+ATT_UNSPLIT = [(5, 6, 32, 16, 16, 64, 1200, 32), (4, 5, 33, 20, 20, 72, 700, 150), (10, 3, 20, 56, 8, 128, 650, 20)]
+
+
+@pytest.mark.parametrize("shape", ATT_LONG)
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("layout", ["dense", "heads_first"])
+def test_attention_long_prefix(shape, dtype, layout):
+    for causal in (False, True):
+        c = _attention_case(*shape, dtype, seed=sum(shape) + causal, layout=layout)
+        out, lse = _run_attention(*c, shape[5] ** -0.5, causal)
+        _check_attention(out, lse, *c, shape[5] ** -0.5, causal, dtype)
+
+
+@pytest.mark.parametrize("shape", ATT_UNSPLIT)
+@pytest.mark.parametrize("causal", [False, True])
+def test_attention_unsplit_prefix(shape, causal):
+    dtype = "fp16" if causal else "bf16"
+    c = _attention_case(*shape, dtype, seed=sum(shape), layout="padded" if causal else "dense")
+    out, lse = _run_attention(*c, shape[5] ** -0.5, causal)
+    _check_attention(out, lse, *c, shape[5] ** -0.5, causal, dtype)
+
+
+def test_attention_unsplit_isolation_and_far_scores():
+    """Five drafts to a query tile: NaN in one draft's keys reaches no other draft; scores of one draft far above or below
+    another's of the same tile, with and without a prefix."""
+    q, kp, vp, ko, vo, plen, olen = _attention_case(5, 6, 32, 16, 16, 64, 1200, 32, "bf16", 31, full=True)
+    q[..., 0], ko[..., 0] = 8.0, 0.0
+    for n in range(30):
+        ko[n, :, :, 0] = (-120.0, 60.0, 0.0, -30.0, 90.0, -200.0)[n % 6]
+    plen = [0, 1200, 37, 1, 640]
+    a = _run_attention(q, kp, vp, ko, vo, plen, olen, 1.0, False)
+    _check_attention(*a, q, kp, vp, ko, vo, plen, olen, 1.0, False, "bf16")
+    for bad in (1, 2, 27):
+        ko2, vo2 = ko.clone(), vo.clone()
+        ko2[bad], vo2[bad] = float("nan"), float("inf")
+        b = _run_attention(q, kp, vp, ko2, vo2, plen, olen, 1.0, False)
+        others = [n for n in range(30) if n != bad]
+        assert torch.equal(a[0][others], b[0][others]) and torch.equal(a[1][others], b[1][others])
+        assert bool(torch.isnan(b[0][bad]).all())
+
+
+def test_attention_long_prefix_extreme_scores():
+    """Raises of the running maximum by far more than its threshold, in both directions, in several tiles."""
+    c = list(_attention_case(1, 2, 64, 4, 2, 128, 2500, 64, "bf16", 37, full=True))
+    for at, f in ((5, 20.0), (500, -60.0), (1300, 60.0), (2499, 90.0)):
+        c[1][0, at] *= f
+    out, lse = _run_attention(*c, 0.5, False)
+    _check_attention(out, lse, *c, 0.5, False, "bf16")
+
+
 @pytest.mark.parametrize("shape", ATT_FUSED)
 @pytest.mark.parametrize("layout", ["dense", "padded"])
 def test_attention_own_keys_after_an_unsplit_prefix(shape, layout):
