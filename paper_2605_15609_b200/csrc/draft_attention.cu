@@ -64,7 +64,7 @@ struct OwnArgs {
     float* lse;
     psd_attention_t a;
     int row_blocks;      // CTAs per (node, key head)
-    int stages;          // 1: no more than one tile of keys, 2
+    int stages;          // tiles of keys in shared memory: 2 (the next one is loaded ahead) or 1
     // partial results over the prefix (prefix_attention.cu), or NULL: this kernel walks the prefix's keys itself
     const float *po, *pl;
     int splits;          // <= kMaxPrefixSplits
@@ -159,7 +159,7 @@ __device__ __forceinline__ void join_rows(const OwnArgs& p, const float* so, con
 }
 
 template <typename T, int DHP, int WM>
-__global__ void __launch_bounds__(kThreads) draft_attention_kernel(const OwnArgs p) {
+__global__ void __launch_bounds__(kThreads, WM == 1 ? 4 : 3) draft_attention_kernel(const OwnArgs p) {
     constexpr int WK = 4 / WM, KPW = kKeys / WK;      // warps per row block, keys per warp and tile
     constexpr int LD = DHP + 8;                        // padded row of a tile (bank-conflict-free ldmatrix)
     constexpr int NQ = DHP / 16, NO = DHP / 8, NS = KPW / 8;
@@ -228,16 +228,18 @@ __global__ void __launch_bounds__(kThreads) draft_attention_kernel(const OwnArgs
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    if (tiles_n > 0) fetch(0, 0);
+    const bool ahead = p.stages == 2;
+    if (ahead && tiles_n > 0) fetch(0, 0);
     for (int t = 0; t < tiles_n; ++t) {
-        if (t + 1 < tiles_n) {
+        if (!ahead) fetch(t, 0);
+        if (ahead && t + 1 < tiles_n) {
             fetch(t + 1, (t + 1) & 1);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
         } else {
             asm volatile("cp.async.wait_group 0;" ::: "memory");
         }
         __syncthreads();
-        const T* kt = tiles + (t & 1) * 2 * kKeys * LD + wk * KPW * LD;
+        const T* kt = tiles + (ahead ? t & 1 : 0) * 2 * kKeys * LD + wk * KPW * LD;
         const T* vt = kt + kKeys * LD;
         float s[NS][4];
 #pragma unroll
@@ -336,7 +338,8 @@ int launch_rows(OwnArgs& p, cudaStream_t st) {
     const int64_t grid = (int64_t)a.B * a.D * a.Hkv * p.row_blocks;
     if (grid > INT32_MAX) return PSD_ERR_SHAPE;
     const int64_t tiles = (int64_t)(p.po ? 0 : (a.P + kKeys - 1) / kKeys) + (a.S + kKeys - 1) / kKeys;
-    p.stages = tiles > 1 ? 2 : 1;
+    // one stage where more CTAs than fit with two want to be resident: the others' arithmetic then hides a CTA's loads
+    p.stages = tiles > 1 && grid <= 3 * sm_count() ? 2 : 1;
     constexpr int tile_bytes = 2 * kKeys * (DHP + 8) * 2, join_bytes = (4 * 16 * (DHP + 8) + 4 * 16 * 2) * 4;
     const int smem = p.stages * tile_bytes > join_bytes ? p.stages * tile_bytes : join_bytes;
     static std::atomic<unsigned long long> set{0};
