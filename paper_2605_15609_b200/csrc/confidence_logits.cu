@@ -1,8 +1,8 @@
 // Token, confidence and log-sum-exp of rows of logits under penalties, biases and grammar masks.
 //
 // One pass over the logits (the only large operand): a CTA takes a few rows that share one text (a draft) and one
-// bias row, and a chunk of the vocabulary; a warp walks a row's columns with a running maximum m and sum s per lane, 32
-// columns at a time, and writes one (max, sum, where) record per row and chunk; a second kernel merges them.
+// bias row, and a chunk of the vocabulary; a warp walks a row's columns with a running maximum m and sum s per lane, four
+// 16-byte vectors at a time, and writes one (max, sum, where) record per row and chunk; a second kernel merges them.
 //
 // The edits touch few tokens.  The CTA counts the text's tokens of its chunk in shared memory once for all its rows and
 // lists every token that has a count or a bias ("special"), in order.  Per row, a warp puts down one bit per column of
@@ -11,7 +11,7 @@
 // table in shared memory turns the bits of a 16-byte vector into the mask of its words), and does not load a group of
 // vectors of which no column is open.  What bounds it is the instructions per column (about 9, two of them at an eighth and a
 // half of the issue rate) and how many warps hide each other's loads: four CTAs per SM of 64 registers a thread beat three of
-// 80 (8192 x 126464 bf16: 592 against 667 us), and chunks of 4096 columns beat 2048 (the set-up per CTA) and 8192.
+// 80 (8192 x 126464 bf16, before the prefetch: 592 against 667 us), and chunks of 4096 columns beat 2048 (the set-up per CTA) and 8192.
 //
 // Sums are kept relative to 2^r, r = the rounded product m * log2 e, so that a term is one FMA and one exponential,
 // 2^(x log2 e - r), and the rounding of r is the same in every term, the maximum's own included: it cancels in
@@ -33,10 +33,11 @@ constexpr int kRowsPerCta = 64;
 constexpr int kBaseCols = 4096;       // columns of a row that a warp takes at most
 constexpr int kCtas = 4;              // resident CTAs per SM that registers and shared memory are kept to
 constexpr int kGuard = 36;            // closed words behind a warp's open bits: a group of 1024 columns may reach past them
+constexpr int U = 4;                  // vectors of a group and lane
 constexpr float kHuge = 1e37f;
 
 // A warp's record of its columns of a row.  bits == 0: `at` is the column itself (INT32_MAX: none).  Otherwise the maximum is
-// in the group of 32 columns (one lane's vectors) that starts at column `at`, and those with a bit are open.
+// in the group of columns (one lane's four vectors) that starts at column `at`, and those with a bit are open.
 struct Part { float m, s; int32_t at; uint32_t bits; };
 
 struct LogitsArgs {
@@ -108,7 +109,7 @@ template <typename T>
 __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(const LogitsArgs a) {
     constexpr int E = Vec<T>::E;               // columns of a 16-byte vector
     constexpr int STEP = 32 * E;               // columns of a warp per vector and lane
-    constexpr int U = 32 / E;                  // vectors of a group: 32 columns per lane, 1024 per warp
+    constexpr int GC = U * STEP, GW = GC / 32; // columns of a group (1024, or 512 of 4 bytes), and their words of open bits
     constexpr int TABLE = 1 << E;
     extern __shared__ __align__(16) int32_t sh[];
     uint4* table = reinterpret_cast<uint4*>(sh);                    // [TABLE] masks of a vector's words
@@ -144,6 +145,18 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(const LogitsArg
     for (int i = lane; i < kGuard + 1; i += 32) open[i ? cols / 32 + i - 1 : -1] = 0u;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (a.merge_early) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    // A row's chunk starts on its way into L2 while the row before is worked on (whole 16-byte granules; 590 against 564 us with
+    // it.  The first row's as well, under the set-up: 553, but 128 rows of 4 bytes, one per warp, then lose 2 of 27 us).
+    const int c0 = (warp % a.wpr) * cols;
+    const int len = max(0, min(cols, vw - c0));            // columns of this warp that exist
+    auto row_at = [&](int rr) { return reinterpret_cast<const T*>(a.logits) + (row0 + rr) * a.stride + v0 + c0; };   // column 0
+    auto prefetch = [&](int rr) {
+        if (lane == 0 && rr < n_rows && len > 0) {
+            const T* lg = row_at(rr);
+            const int back = (int)((reinterpret_cast<uintptr_t>(lg) & 15) / sizeof(T)), bytes = ((len + back) * (int)sizeof(T) + 15) / 16 * 16;
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(lg - back), "r"(bytes) : "memory");
+        }
+    };
     if (counts) {
         for (int i = threadIdx.x; i < a.chunk; i += kThreads) cnt[i] = 0;
         __syncthreads();
@@ -200,13 +213,12 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(const LogitsArg
     }
     __syncthreads();
 
-    const int c0 = (warp % a.wpr) * cols;
-    const int len = max(0, min(cols, vw - c0));            // columns of this warp that exist
     const int n_split = a.n_chunks * a.wpr;
     const int sp0 = first[c0 / 32], sp1 = first[(c0 + cols) / 32];
     for (int rr = warp / a.wpr; rr < n_rows; rr += kWarps / a.wpr) {
         const int64_t row = row0 + rr;
-        const T* lg = reinterpret_cast<const T*>(a.logits) + row * a.stride + v0 + c0;    // this warp's column 0
+        const T* lg = row_at(rr);
+        prefetch(rr + kWarps / a.wpr);
         // Vectors are aligned in memory: with rows that are not, the first one starts `back` columns ahead of column 0.
         const int back = (int)((reinterpret_cast<uintptr_t>(lg) & 15) / sizeof(T));
         const uint32_t* allow = a.e.allow ? a.e.allow + (row / a.rows_per_allow) * (int64_t)a.words + (v0 + c0) / 32 : nullptr;
@@ -250,25 +262,25 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(const LogitsArg
         float m = -INFINITY, s = 0.f;
         int best = -1;
         uint32_t best_bits = 0u;
-        const int groups = len > 0 ? (len + back + 1023) / 1024 : 0;
+        const int groups = len > 0 ? (len + back + GC - 1) / GC : 0;
 #pragma unroll 1
         for (int g = 0; g < groups; ++g) {
             uint32_t bits = 0u;                            // of this lane's 32 columns
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const uint32_t* w = my_open + g * 32 + u * (STEP / 32);
+                const uint32_t* w = my_open + g * GW + u * (STEP / 32);
                 const uint32_t b = back ? __funnelshift_r(w[0], w[1], shift) : w[0] >> shift;
                 bits |= (b & (TABLE - 1)) << (u * E);
             }
             if (!__any_sync(0xffffffffu, bits)) continue;
             uint4 raw[U];
-            if (g * 1024 - back >= lo && (g + 1) * 1024 - back <= hi) {
+            if (g * GC - back >= lo && (g + 1) * GC - back <= hi) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) raw[u] = __ldcs(reinterpret_cast<const uint4*>(my + g * 1024 + u * STEP));
+                for (int u = 0; u < U; ++u) raw[u] = __ldcs(reinterpret_cast<const uint4*>(my + g * GC + u * STEP));
             } else {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const int i = g * 1024 + u * STEP + lane * E - back;
+                    const int i = g * GC + u * STEP + lane * E - back;
                     raw[u] = make_uint4(0, 0, 0, 0);
                     if (i >= lo && i + E <= hi) {
                         raw[u] = __ldcs(reinterpret_cast<const uint4*>(lg + i));
@@ -334,13 +346,13 @@ __global__ void __launch_bounds__(kThreads, kCtas) logits_kernel(const LogitsArg
         if (__popc(in_group) == 1 && in_special == 0u) {
             // one lane's group holds it: the merge looks the column up if this record wins
             const int l = __ffs(in_group) - 1;
-            p.at = v0 + c0 + __shfl_sync(0xffffffffu, best, l) * 1024 + l * E - back;
+            p.at = v0 + c0 + __shfl_sync(0xffffffffu, best, l) * GC + l * E - back;
             p.bits = __shfl_sync(0xffffffffu, best_bits, l);
         } else if (in_group | in_special) {
             int at = sm == top ? sa : INT32_MAX;
             if (m == top && best >= 0) {
-                for (int k = 0; k < 32; ++k) {             // a group's columns ascend with k
-                    const int i = best * 1024 + (k / E) * STEP + lane * E + k % E - back;
+                for (int k = 0; k < U * E; ++k) {          // a group's columns ascend with k
+                    const int i = best * GC + (k / E) * STEP + lane * E + k % E - back;
                     if (best_bits >> k & 1u && Vec<T>::one(lg + i) == top) { at = min(at, i); break; }
                 }
             }
@@ -405,13 +417,18 @@ __global__ void __launch_bounds__(kThreads) logits_merge_kernel(const Part* __re
     }
 }
 
-// Columns per CTA and warps per row.  A warp should have a few thousand columns (the count of the text and the final
-// reduction of a row are paid per CTA and per warp), and the grid at least two CTAs per SM.
-void choose_chunk(int64_t units, int rows, int V, int& chunk, int& wpr) {
+// Rows and columns per CTA, warps per row.  A warp should have a row of kBaseCols columns or several, since the set-up of the
+// special tokens is paid per CTA and the reduction per row and chunk; a small batch is spread over the SMs first by rows (128
+// x 126465 fp32, 496 CTAs either way: 8 rows x 4096 columns 27 us, 32 rows x 1024 columns 34 us), then by columns.
+void choose_shape(int64_t units, int unit_rows, int V, int& rows, int& chunk, int& wpr) {
+    const int64_t want = 3 * (int64_t)sm_count();
+    rows = unit_rows < kRowsPerCta ? unit_rows : kRowsPerCta;
+    const int64_t chunks = (V + kBaseCols - 1) / kBaseCols;
+    while (rows > kWarps && units * ((unit_rows + rows - 1) / rows) * chunks < want) rows = (rows + 1) / 2;
     wpr = rows >= 8 ? 1 : rows >= 4 ? 2 : rows >= 2 ? 4 : 8;
     chunk = kBaseCols * wpr < kMaxChunk ? kBaseCols * wpr : kMaxChunk;
-    const int64_t want = 2 * (int64_t)sm_count();
-    while (chunk / wpr > kMinWarpCols && units * ((V + chunk - 1) / chunk) < want) chunk /= 2;
+    units *= (unit_rows + rows - 1) / rows;
+    while (chunk / wpr > kMinWarpCols && units * ((V + chunk - 1) / chunk) < 2 * (int64_t)sm_count()) chunk /= 2;
 }
 
 int shared_bytes(int chunk, int wpr, int E) {
@@ -468,11 +485,9 @@ int launch_confidence_logits(const void* logits, int dtype, int64_t row_stride, 
     a.rows_per_allow = (int)(n_rows / (e.allow ? e.allow_rows : 1));
     a.words = (V + 31) / 32;
     a.unit_rows = e.bias ? gcd_int(M, a.rows_per_bias) : M;
-    a.slices = (a.unit_rows + kRowsPerCta - 1) / kRowsPerCta;
-    a.rows_per_cta = (a.unit_rows + a.slices - 1) / a.slices;
+    choose_shape(n_rows / a.unit_rows, a.unit_rows, V, a.rows_per_cta, a.chunk, a.wpr);
     a.slices = (a.unit_rows + a.rows_per_cta - 1) / a.rows_per_cta;
     const int64_t units = n_rows / a.unit_rows * a.slices;
-    choose_chunk(units, a.rows_per_cta, V, a.chunk, a.wpr);
     a.n_chunks = (V + a.chunk - 1) / a.chunk;
     a.part = reinterpret_cast<Part*>(workspace);
     const int64_t grid = units * a.n_chunks;
