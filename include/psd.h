@@ -534,7 +534,8 @@ size_t psd_attention_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t Hq
  * weights are rounded to the inputs' type before they multiply V, out is rounded once at the end.
  *   prefix_len [B] int32, device, or NULL for P everywhere;  own_len [B*D] int32, device, or NULL for S;
  *   values outside [0, P] ([0, S]) are clamped.  What lies past a length is never used, whatever it holds, and
- *   a draft's outputs never depend on another draft's keys.  P = 0 (S = 0): the pointers may be NULL.
+ *   a draft's outputs never depend on another draft's keys (with `causal`, values of own keys that a row of the
+ *   same draft does not see must be finite: they are multiplied by 0).  P = 0 (S = 0): the pointers may be NULL.
  *   q, k_*, v_*, out 16-byte aligned, their strides multiples of 8 elements (PSD_ERR_ALIGN otherwise)
  *   lse [B*D*M, Hq] fp32 or NULL;  workspace 256-byte aligned, >= psd_attention_workspace_bytes
  *   status_dev NULL, or the status word (PSD_ERR_TIMEOUT: outputs invalid)
