@@ -9,8 +9,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kTileRows128 = 128;                  // rows of an operand tile
-constexpr int kSlabBytes = kTileRows128 * 128;     // 128 rows x 64 elements of 2 bytes: one swizzled slab
+constexpr int kSlabBytes = 128 * 128;     // 128 rows x 64 elements of 2 bytes: one swizzled slab
 constexpr int kSlabElems = 64;
 
 // ---- TMA ----------------------------------------------------------------------------------------
@@ -167,60 +166,32 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-    f32x2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
 
-// ---- 2^x on the FMA pipes ---------------------------------------------------------------------------
-// ex2 runs at 16 results per clock and SM, an eighth of the fp32 rate, and the kernels here need one per score; part of
-// the scores go through a polynomial instead.  x = n + f with n the nearest integer (rounded by adding 1.5 * 2^23, whose
-// low bits then hold n; 127 more makes them the exponent field of 2^n), f in [-1/2, 1/2], 2^f by a polynomial whose
-// coefficients minimise the largest relative error on that interval (degree 4: 2.6e-6, degree 5: 7.5e-8, then fp32
-// rounding).  x is clamped to [-126, 127.5]; NaN stays NaN.  Degree 4 is for weights that are rounded to 16 bits next.
-template <int DEG, bool CLAMP_HIGH>
-__device__ __forceinline__ f32x2 ex2_poly(f32x2 x) {
-    float a, b;
-    unpack2(x, a, b);
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(-126.0f));
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(b) : "f"(-126.0f));
-    if (CLAMP_HIGH) {
-        asm("min.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(127.5f));
-        asm("min.NaN.f32 %0, %0, %1;" : "+f"(b) : "f"(127.5f));
-    }
-    x = pack2(a, b);
-    const f32x2 magic = pack2(12583039.0f, 12583039.0f), neg = pack2(-12583039.0f, -12583039.0f), minus = pack2(-1.f, -1.f);
-    const f32x2 t = add2(x, magic);
-    const f32x2 f = fma2(add2(t, neg), minus, x);
-    auto c = [](float v) { return pack2(v, v); };
-    f32x2 p;
-    if (DEG == 4) {
-        p = fma2(c(0.009570102207362652f), f, c(0.05591785907745361f));
-        p = fma2(p, f, c(0.240247443318367f));
-        p = fma2(p, f, c(0.6931217908859253f));
-        p = fma2(p, f, c(0.9999992847442627f));
-    } else {
-        p = fma2(c(0.0013276472454890609f), f, c(0.009675540961325169f));
-        p = fma2(p, f, c(0.05550713092088699f));
-        p = fma2(p, f, c(0.24022120237350464f));
-        p = fma2(p, f, c(0.6931469440460205f));
-        p = fma2(p, f, c(1.0000001192092896f));
-    }
-    float ta, tb;
-    unpack2(t, ta, tb);
-    return mul2(p, pack2(__uint_as_float(__float_as_uint(ta) << 23), __uint_as_float(__float_as_uint(tb) << 23)));
-}
+// (2^x stays with ex2: a polynomial on the fp32 pipes takes 10 cycles of a scheduler per 32 results, ex2 takes 8.)
 __device__ __forceinline__ f32x2 ex2_pair(f32x2 x) {
     float a, b;
     unpack2(x, a, b);
     return pack2(ex2(a), ex2(b));
+}
+
+// ---- host: register shares --------------------------------------------------------------------------------
+// A kernel whose warps trade registers (setmaxnreg) waits forever if its shares add up to more than it was launched with:
+// the launch is refused unless the compiler gave it at least `need` registers a thread.
+template <typename Kernel>
+bool launched_with(Kernel kernel, int need, std::atomic<int>& seen) {
+    int n = seen.load(std::memory_order_relaxed);
+    if (n == 0) {
+        cudaFuncAttributes f;
+        if (cudaFuncGetAttributes(&f, kernel) != cudaSuccess) return false;
+        n = f.numRegs;
+        seen.store(n, std::memory_order_relaxed);
+    }
+    return n >= need;
 }
 
 // ---- host: tensor maps --------------------------------------------------------------------------------

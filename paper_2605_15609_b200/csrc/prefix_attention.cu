@@ -5,7 +5,8 @@
 // in tensor memory (4 x 128 columns: all of it).  With two or more tiles the streams take two query tiles over the same
 // keys, so every K and V tile in shared memory serves 256 rows; with one tile they take the two halves of the CTA's
 // keys.  One warp loads K and V tiles by TMA into a ring, one issues the products, and four warps per stream do the
-// softmax: a thread owns a row (TMEM lane), so maxima and sums need no other thread.  While one stream's softmax runs, the tensor cores work on the other stream:
+// softmax: a thread owns a row (TMEM lane), so maxima and sums need no other thread.  While one stream's softmax runs, the
+// tensor cores work on the other stream:
 //   .. PV0(j) S0(j+1) | PV1(j) S1(j+1) | PV0(j+1) ..      (S0(j+1) overwrites the scores whose weights PV0(j) just read)
 // The weights P overwrite the scores in tensor memory as packed 16-bit pairs and are the A operand of PV, which starts on
 // the first half of the weights while the others are computed.
@@ -18,6 +19,10 @@
 // one draft at a time: its products leave the rows of other drafts as they are (a mask of tensor-memory rows), so what one
 // draft's keys and values hold cannot reach another, and the CTA writes final outputs.  Otherwise partial results go to
 // draft_attention_kernel, which takes the own keys and joins.
+//
+// Bound, for Dh = 128, by products and exponentials alike (2048 cycles each per 256 rows x 128 keys); measured 3500 cycles, the
+// chain scores -> softmax -> weights -> product of a stream: 16 sequences x 8 key heads x 2048 rows over up to 8192 keys (668
+// GFLOP) in 601 us, 1.1 PFLOP/s, where the board's power limit already holds the clock at 1840-1900 MHz.
 //
 // Keys past the prefix's end are masked in the scores, and their V rows are zeroed in shared memory before the product,
 // since 0 * NaN would spoil a row.
@@ -56,6 +61,7 @@ struct PrefixArgs {
     int64_t out_token, out_head;
     float c;                   // scale * log2 e
     long long wait_limit;
+    int stall_test;            // PSD_TUNE_SELFTEST_STALL
 };
 
 __device__ __forceinline__ uint32_t pack16(float lo, float hi, bool bf16) {
@@ -76,8 +82,9 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
     unsigned char* ring = smem + 2 * TILE;                           // [NS][TILE]
     uint64_t* bars = reinterpret_cast<uint64_t*>(ring + NS * TILE);
     uint64_t *q_full = bars, *full = bars + 1, *empty = full + NS, *s_full = empty + NS /* [2] */, *p_half = s_full + 2, *p_ready = p_half + 2,
-             *o_done = p_ready + 2 /* [2] */, *drain = o_done + 2;
-    uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
+             *o_done = p_ready + 2 /* [2] */, *drain = o_done + 2,
+             *never = drain + 1 /* nothing arrives on it: self-test of the give-up path */;
+    uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(never + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
     volatile int* sequence = abort_flag + 1;
     int* n_own = const_cast<int*>(abort_flag) + 2;                  // [2] own tiles of the streams
@@ -99,6 +106,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         for (int s = 0; s < NS; ++s) { mbar_init(&full[s], 1); mbar_init(&empty[s], 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(&s_full[s], 1); mbar_init(&p_half[s], 4); mbar_init(&p_ready[s], 4); mbar_init(&o_done[s], 1); }
         mbar_init(drain, 1);
+        mbar_init(never, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -199,6 +207,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                     }
                 }
                 ++item;
+                if (a.stall_test && item == 1 && !mbar_wait_warp(never, 0, wc)) ok = false;
             }
             if (!ok) {
                 // giving up: no copy may be in flight when the CTA exits
@@ -485,6 +494,8 @@ int launch_p(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv
     static_assert(smem <= 227 * 1024, "shared memory of the prefix kernel");
     static std::atomic<unsigned long long> set{0};
     if (!ensure_dynamic_smem(prefix_attention_kernel<SLABS, BF16>, smem, set)) return PSD_ERR_CUDA;
+    static std::atomic<int> regs{0};      // 8 warps of 208 and 4 of 80 registers a thread
+    if (!launched_with(prefix_attention_kernel<SLABS, BF16>, (256 * 208 + 128 * 80 + kPThreads - 1) / kPThreads, regs)) return PSD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(kPThreads);
@@ -566,6 +577,7 @@ int launch_prefix_attention(const void* q, const void* k, const void* v, const i
     x.out_token = a.out_token; x.out_head = a.out_head;
     x.c = a.scale * kLog2e;
     x.wait_limit = wait_limit_cycles();
+    x.stall_test = selftest_stall();
     if (p.dhp == 64) return bf16 ? launch_p<1, true>(mq, mk, mv, mko, mvo, x, grid, st) : launch_p<1, false>(mq, mk, mv, mko, mvo, x, grid, st);
     return bf16 ? launch_p<2, true>(mq, mk, mv, mko, mvo, x, grid, st) : launch_p<2, false>(mq, mk, mv, mko, mvo, x, grid, st);
 }

@@ -12,7 +12,8 @@
 // (deep sweep: one CTA per unit 534 us, equal shares of all units 582 us, of the units with keys 448 us).
 //
 // Warps 0-15 sum: eight per key tile, two per quarter, each with 64 columns of every query tile; warp 16 loads, warp 17
-// issues the products.  Accumulators are double-buffered per key tile (4 x 128 TMEM columns).  One exponential per score is
+// issues the products.  Accumulators are double-buffered per key tile (4 x 128
+// TMEM columns).  One exponential per score is
 // what bounds the kernel: 16 per clock and SM, 8 cycles of a scheduler per 32 scores.  (A polynomial in place of part of them
 // was measured slower at every share: packed fp32 runs at half the rate of single, so the polynomial costs 10 cycles.)
 #include "attn_tc.cuh"
@@ -39,6 +40,7 @@ struct WeightsArgs {
     float c, beta;
     int bf16;
     long long wait_limit;
+    int stall_test;                 // PSD_TUNE_SELFTEST_STALL
 };
 
 template <int SLABS>
@@ -54,8 +56,8 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
     uint64_t* bars = reinterpret_cast<uint64_t*>(halves + 256);
     uint64_t *k_full = bars, *k_empty = k_full + 1, *q_full = k_empty + 1, *q_empty = q_full + kQStages,
              *s_full = q_empty + kQStages /* [2][2] */, *s_empty = s_full + 4, *x_full = s_empty + 4 /* [8] */, *x_empty = x_full + 8 /* [8] */,
-             *drain = x_empty + 8;
-    uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(drain + 1);
+             *drain = x_empty + 8, *never = drain + 1 /* nothing arrives on it: self-test of the give-up path */;
+    uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(never + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
     int* ends = const_cast<int*>(abort_flag) + 1;                    // [kMaxSeqs] key units of the sequences up to and with b
 
@@ -67,6 +69,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
         for (int s = 0; s < 4; ++s) { mbar_init(&s_full[s], 1); mbar_init(&s_empty[s], 8); }
         for (int s = 0; s < 8; ++s) { mbar_init(&x_full[s], 1); mbar_init(&x_empty[s], 1); }
         mbar_init(drain, 1);
+        mbar_init(never, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -174,6 +177,7 @@ weights_tc_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_consta
                     for (int c = 0; c < SLABS; ++c)
                         tma_load_3d(q_tiles + s * TILE + c * kSlabBytes, &map_q, &q_full[s], c * kSlabElems, x.h * a.G, x.b * a.T + (x.q_lo + it) * a.tq);
                 }
+                if (a.stall_test && qi == 0 && !mbar_wait_warp(never, 0, wc)) { ok = false; ++qi; break; }
             }
         }
         if (!ok) {
@@ -397,6 +401,8 @@ int launch_w(const CUtensorMap& mk, const CUtensorMap& mq, const WeightsArgs& a,
     static_assert(smem <= 227 * 1024, "shared memory of the weights kernel");
     static std::atomic<unsigned long long> set{0};
     if (!ensure_dynamic_smem(weights_tc_kernel<SLABS>, smem, set)) return PSD_ERR_CUDA;
+    static std::atomic<int> regs{0};      // 16 warps of 104 and 4 of 64 registers a thread
+    if (!launched_with(weights_tc_kernel<SLABS>, (kEpilogue * 32 * 104 + 128 * 64) / kWThreads, regs)) return PSD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     const int sms = sm_count();
     cfg.gridDim = dim3(a.units < sms ? a.units : sms);
@@ -440,7 +446,7 @@ int launch_prefix_weights(const void* q, const void* k_prefix, const int32_t* pr
         return PSD_ERR_CUDA;
     WeightsArgs w = {prefix_len, lse, acc_in, acc_out, reinterpret_cast<float*>(workspace), status_dev, a.D * a.M, a.Hq / a.Hkv, a.Hq,
                      a.Hkv, a.Dh, a.P, p.tq, p.n_qt, p.key_ctas, p.splits, a.B * a.Hkv, (int)units, a.kp.outer ? 1 : 0, a.kp.head ? 1 : 0,
-                     a.scale * kLog2e, beta, a.dtype == PSD_BF16 ? 1 : 0, wait_limit_cycles()};
+                     a.scale * kLog2e, beta, a.dtype == PSD_BF16 ? 1 : 0, wait_limit_cycles(), selftest_stall()};
     return a.Dh <= 64 ? launch_w<1>(mk, mq, w, st) : launch_w<2>(mk, mq, w, st);
 }
 

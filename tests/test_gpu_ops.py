@@ -541,3 +541,31 @@ def test_logits_feed_the_policy():
     psd.psd_select_unmask(c, t, tokens, mask, psd.policy(tau=0.9, k_min=1), sel, n_sel, pos)
     assert sel[0].tolist() == [1, 1, 0, 1, 1, 1, 1, 1] and mask[0, 2].item() == 1
     assert tokens[0].tolist() == [V if i == 2 else i * 7 for i in range(M)]
+
+
+# ---- waits that run out -------------------------------------------------------------------------------------------------------
+
+def test_waits_that_run_out_are_reported_and_the_next_call_is_fine():
+    """With PSD_TUNE_SELFTEST_STALL the loader of every CTA waits, after its first tile, on a barrier that nothing arrives on: the
+    wait runs out (400 000 cycles here), the kernels report PSD_ERR_TIMEOUT, let their own copies and products finish and return;
+    with the knobs back the next call is right."""
+    c = _attention_case(1, 2, 64, 8, 2, 128, 2500, 64, "bf16", 41, full=True)
+    q, kp, vp, ko, vo, plen, olen = c
+    N, M, Hq, Dh = q.shape
+    out, lse = torch.empty_like(q), torch.zeros(N, M, Hq, device="cuda")
+    ws = torch.zeros(psd.psd_attention_workspace_bytes(1, 2, 64, 8, 2, 128, 2500, 64), dtype=torch.uint8, device="cuda")
+    acc = torch.zeros(1, 2, 2500, device="cuda")
+    ws2 = torch.zeros(psd.psd_weights_workspace_bytes(1, 2, 64, 8, 2, 128, 2500), dtype=torch.uint8, device="cuda")
+    s1, s2 = _i32([0]), _i32([0])
+    assert psd.psd_set_tuning(psd.PSD_TUNE_WAIT_LIMIT, 400) == 0 and psd.psd_set_tuning(psd.PSD_TUNE_SELFTEST_STALL, 1) == 0
+    try:
+        psd.psd_draft_attention(q, kp, vp, out, lse, ko, vo, workspace=ws, status=s1)
+        torch.cuda.synchronize()
+        psd.psd_prefix_weights(q, kp, lse, acc, workspace=ws2, status=s2)
+        torch.cuda.synchronize()
+    finally:
+        psd.psd_set_tuning(psd.PSD_TUNE_SELFTEST_STALL, 0)
+        psd.psd_set_tuning(psd.PSD_TUNE_WAIT_LIMIT, 4_000_000)
+    assert int(s1.item()) == int(s2.item()) == psd.PSD_ERR_TIMEOUT
+    out, lse = _run_attention(*c, Dh ** -0.5, False)
+    _check_attention(out, lse, *c, Dh ** -0.5, False, "bf16")
