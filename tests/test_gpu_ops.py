@@ -343,6 +343,9 @@ def test_weights_of_an_attention_pass_sum_to_its_rows():
 EVICT = [  # B, Hkv, Dh, P, keep, sink, recent
     (1, 1, 8, 1, 1, 0, 0), (1, 2, 64, 50, 50, 1, 1), (1, 2, 64, 50, 80, 1, 1), (2, 3, 128, 1000, 250, 4, 32), (3, 2, 96, 1025, 1, 0, 0),
     (3, 4, 80, 3000, 1000, 0, 1000), (2, 1, 64, 5000, 700, 700, 0), (1, 2, 128, 2048, 2047, 3, 5), (1, 1, 64, 60000, 5000, 4, 100),
+    # several CTAs per head, some with nothing to do; keys that stay in shared memory and (the last) that do not
+    (3, 2, 64, 9001, 3000, 4, 64), (5, 3, 8, 16385, 1, 0, 0), (4, 8, 64, 20000, 19990, 100, 9000), (3, 16, 16, 33000, 2500, 30, 40),
+    (1, 2, 8, 300000, 9000, 4, 100),
 ]
 
 
