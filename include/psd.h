@@ -563,8 +563,8 @@ int psd_prefix_weights(const void* q, const void* k_prefix, const int32_t* prefi
 /* Shapes of psd_prefix_evict. */
 typedef struct psd_evict_t {
     int32_t B, Hkv, Dh;       /* as above                                                                    */
-    int32_t P;                /* capacity of the cache, >= 1                                                 */
-    int32_t keep;             /* keys to keep per sequence and key head, >= 1                                 */
+    int32_t P;                /* capacity of the cache, 1 .. 2^30                                             */
+    int32_t keep;             /* keys to keep per sequence and key head, 1 .. 2^30                             */
     int32_t n_sink, n_recent; /* always keep the first n_sink and the last n_recent; both >= 0, sum <= keep   */
     int32_t dtype;            /* PSD_BF16 or PSD_FP16 */
     psd_kv_strides_t k, v;    /* [B, P, Hkv, Dh] */
@@ -591,7 +591,7 @@ typedef struct psd_logits_edit_t {
     const int32_t* draft_mask;   /* [B*D, M] their own draft (both or neither)                                    */
     const float* bias;           /* [bias_rows, V] fp32                                                           */
     const uint32_t* allow;       /* [allow_rows, ceil(V/32)]: bit v%32 of word v/32 set = token v may be chosen     */
-    int32_t history_cap;         /* >= 0 */
+    int32_t history_cap;         /* 0 .. 2^30 */
     int32_t bias_rows;           /* divides B*D*M: row r uses bias row r / (B*D*M / bias_rows)                      */
     int32_t allow_rows;          /* likewise                                                                       */
     float repetition;            /* > 0, finite; 1 = none */
@@ -611,7 +611,8 @@ size_t psd_logits_workspace_bytes(int32_t n_rows, int32_t V);
  * out_token, out_conf, out_lse are those of psd_confidence over x.  A row in which no token is left (or all that are left
  * have x = -inf) gives token -1, confidence 0 and lse -inf; it is not counted as non-finite, and its token must not be
  * committed.  A NaN or +inf among the tokens left gives confidence NaN and is counted in status_dev.
- *   logits [B*D*M, V] bf16, fp16 or fp32 (dtype), rows row_stride >= V elements apart, aligned to their element
+ *   logits [B*D*M, V] bf16, fp16 or fp32 (dtype), rows row_stride >= V elements apart, aligned to their element;
+ *     B*D*M and V at most 2^30
  *   edit: HOST pointer, NULL = no edits;  workspace >= psd_logits_workspace_bytes(B*D*M, V), 256-byte aligned
  */
 int psd_confidence_logits(const void* logits, int32_t dtype, int64_t row_stride, int32_t B, int32_t D, int32_t M, int32_t V,

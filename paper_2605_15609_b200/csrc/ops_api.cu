@@ -10,6 +10,9 @@ inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_
 bool heads_ok(int32_t Hq, int32_t Hkv, int32_t Dh) {
     return Hq >= 1 && Hkv >= 1 && Hq % Hkv == 0 && Hq / Hkv <= 128 && Dh >= 8 && Dh <= 128 && Dh % 8 == 0;
 }
+// Lengths that kernels walk in steps of thousands with 32-bit positions: a step past the end must not overflow.
+constexpr int32_t kMostSteps = 1 << 30;
+
 // Rows (tokens times heads) and head-blocks of the grids are indexed with 32 bits; everything that is
 // multiplied by a stride is computed in 64.
 bool attention_sizes_ok(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P, int32_t S) {
@@ -95,7 +98,7 @@ int psd_prefix_weights(const void* q, const void* k_prefix, const int32_t* prefi
 int psd_prefix_evict(const float* scores, const void* k, const void* v, const int32_t* prefix_len, const psd_evict_t* e,
                      void* k_out, void* v_out, int32_t* index, float* scores_out, int32_t* len_out, void* cuda_stream) {
     if (!scores || !k || !v || !e || !k_out || !v_out || !index) return PSD_ERR_NULL;
-    if (e->B < 1 || !heads_ok(e->Hkv, e->Hkv, e->Dh) || e->P < 1 || e->P > INT32_MAX - 1024 || e->keep < 1 ||
+    if (e->B < 1 || !heads_ok(e->Hkv, e->Hkv, e->Dh) || e->P < 1 || e->P > kMostSteps || e->keep < 1 || e->keep > kMostSteps ||
         e->n_sink < 0 || e->n_recent < 0 || (int64_t)e->n_sink + e->n_recent > e->keep ||
         (int64_t)e->B * e->Hkv > INT32_MAX / 2)
         return PSD_ERR_SHAPE;
@@ -114,7 +117,7 @@ int psd_prefix_evict(const float* scores, const void* k, const void* v, const in
 }
 
 size_t psd_logits_workspace_bytes(int32_t n_rows, int32_t V) {
-    if (n_rows < 1 || V < 1 || V >= 2147483647 - 256) return 0;
+    if (n_rows < 1 || V < 1 || n_rows > kMostSteps || V > kMostSteps) return 0;
     return confidence_logits_workspace(n_rows, V);
 }
 
@@ -122,8 +125,8 @@ int psd_confidence_logits(const void* logits, int32_t dtype, int64_t row_stride,
                           const psd_logits_edit_t* edit, int32_t* out_token, float* out_conf, float* out_lse,
                           void* workspace, size_t workspace_bytes, int32_t* status_dev, void* cuda_stream) {
     if (!logits || !out_token || !out_conf || !workspace) return PSD_ERR_NULL;
-    if (B < 1 || D < 1 || M < 1 || V < 1 || V >= 2147483647 - 256 || row_stride < V) return PSD_ERR_SHAPE;
-    if ((int64_t)B * D > INT32_MAX || (int64_t)B * D * M > INT32_MAX) return PSD_ERR_SHAPE;
+    if (B < 1 || D < 1 || M < 1 || V < 1 || V > kMostSteps || row_stride < V) return PSD_ERR_SHAPE;
+    if ((int64_t)B * D > kMostSteps || (int64_t)B * D * M > kMostSteps) return PSD_ERR_SHAPE;
     const int64_t n_rows = (int64_t)B * D * M;
     if (dtype != PSD_BF16 && dtype != PSD_FP16 && dtype != PSD_FP32) return PSD_ERR_UNSUPPORTED;
     psd_logits_edit_t e = {};
@@ -134,7 +137,7 @@ int psd_confidence_logits(const void* logits, int32_t dtype, int64_t row_stride,
         if (e.reserved != 0) return PSD_ERR_UNSUPPORTED;
         if (!(e.repetition > 0.f) || !std::isfinite(e.repetition) || !std::isfinite(e.presence) || !std::isfinite(e.frequency))
             return PSD_ERR_SHAPE;
-        if (e.history_cap < 0 || (e.bias && (e.bias_rows < 1 || n_rows % e.bias_rows)) ||
+        if (e.history_cap < 0 || e.history_cap > kMostSteps || (e.bias && (e.bias_rows < 1 || n_rows % e.bias_rows)) ||
             (e.allow && (e.allow_rows < 1 || n_rows % e.allow_rows)))
             return PSD_ERR_SHAPE;
         if ((e.draft_tokens == nullptr) != (e.draft_mask == nullptr) || (e.history_cap > 0 && !e.history && e.history_len))

@@ -5,7 +5,7 @@
 // shared memory, since scores of one magnitude fall into few bins; the CTAs add up one another's counts over distributed
 // shared memory and so all take the same digit), then every warp walks a run of positions, counts what it keeps, and, after
 // one scan over the warps and CTAs, writes it in order.  The keys of up to kCached positions per CTA stay in shared memory.
-// 64 heads of up to 32768 positions: 27 us with one CTA per head, 22 with two, 28 with four (two to an SM); each
+// 64 heads of up to 32768 positions: 27 us with one CTA per head, 21 with two, 28 with four (two to an SM); each
 // cluster barrier costs about 0.7 us.
 // Kernel 2 copies the kept rows: 16 bytes per thread, consecutive threads along a row; this is the part that is bound
 // by memory (two rows read and two written per kept position): 64 heads, 8192 of up to 32768 keys of 128 x 2 bytes, 537 MB, in 89
@@ -56,7 +56,7 @@ struct SelectArgs {
     const float* scores;
     const int32_t* prefix_len;
     int P, Hkv, keep, n_sink, n_recent;
-    int n_cta;                    // CTAs of a head: one cluster
+    int log_cta, own;             // a cluster of 1 << log_cta CTAs per head, `own` positions for each
     int32_t* index;
     float* scores_out;
     int32_t* len_out;
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
     __shared__ __align__(8) uint32_t cta_sum[2];                // this CTA's keys above and equal to the threshold
     __shared__ uint32_t warp_sum[32], warp_eq[32];
     __shared__ uint32_t s_digit, s_left;
-    const int n_cta = a.n_cta, rank = blockIdx.x % n_cta, bh = blockIdx.x / n_cta, b = bh / a.Hkv, h = bh % a.Hkv;
+    const int n_cta = 1 << a.log_cta, rank = blockIdx.x & (n_cta - 1), bh = blockIdx.x >> a.log_cta, b = bh / a.Hkv, h = bh % a.Hkv;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     for (int i = tid; i < kCopies * (kBins + kPad); i += kSelThreads) (&hist[0][0])[i] = 0;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(kSelThreads) evict_select_kernel(const SelectA
         return;
     }
     // this CTA's positions [c0, c1); the whole cluster takes the same decisions, so it meets at every barrier
-    const int own = (a.P + n_cta * 32 - 1) / (n_cta * 32) * 32, c0 = min(L, rank * own), c1 = min(L, c0 + own);
+    const int c0 = min(L, rank * a.own), c1 = min(L, c0 + a.own);
     uint32_t* keys = dynamic + (n_cta > 1 ? 2 * kBins : 0);
     // positions [lo, hi) compete for n_free places; the others are kept: their keys are the largest there is (no score's)
     const int lo = min(a.n_sink, L), hi = max(lo, L - a.n_recent);
@@ -279,10 +279,10 @@ int launch_prefix_evict(const float* scores, const void* k, const void* v, const
                         int32_t* len_out, cudaStream_t st) {
     // CTAs per head: as many as keep a wave of them on the SMs and 4096 positions to each (below that a barrier costs more than
     // the positions)
-    int n_cta = 1;
-    while (n_cta < kMaxCluster && (int64_t)e.B * e.Hkv * n_cta * 2 <= sm_count() && e.P / (n_cta * 2) >= 4096) n_cta *= 2;
-    SelectArgs s = {scores, prefix_len, e.P, e.Hkv, e.keep, e.n_sink, e.n_recent, n_cta, index, scores_out, len_out};
-    const int own = (e.P + n_cta * 32 - 1) / (n_cta * 32) * 32;
+    int log_cta = 0;
+    while ((2 << log_cta) <= kMaxCluster && ((int64_t)e.B * e.Hkv * 2 << log_cta) <= sm_count() && e.P >> (log_cta + 1) >= 4096) ++log_cta;
+    const int n_cta = 1 << log_cta, own = (int)(((int64_t)e.P + n_cta * 32 - 1) / (n_cta * 32) * 32);
+    SelectArgs s = {scores, prefix_len, e.P, e.Hkv, e.keep, e.n_sink, e.n_recent, log_cta, own, index, scores_out, len_out};
     const bool cached = own <= kCached;
     const int counts = n_cta > 1 ? 2 * kBins * 4 : 0;
     static std::atomic<unsigned long long> smem_set{0}, smem_set_far{0};

@@ -125,6 +125,22 @@ def test_logits_refusals():
     assert call(n=16) == psd.PSD_ERR_WORKSPACE
 
 
+def test_lengths_whose_last_step_would_overflow_are_refused():
+    """Kernels walk these lengths in steps of thousands with 32-bit positions."""
+    far = (1 << 30) + 1
+    st = psd.PsdKvStrides(12800, 128, 64)
+    for kw in (dict(P=far), dict(keep=far)):
+        f = dict(B=1, Hkv=2, Dh=64, P=100, keep=10, n_sink=2, n_recent=3, dtype=psd.PSD_BF16)
+        f.update(kw)
+        e = psd.PsdEvict(**f, k=st, v=st, k_out=st, v_out=st)
+        assert L.psd_prefix_evict(FAKE, FAKE, FAKE, None, ctypes.byref(e), FAKE, FAKE, FAKE, None, None, None) == psd.PSD_ERR_SHAPE, kw
+    for B, M, V, cap in ((1, 1, far, 0), (1, far, 8, 0), (far, 1, 8, 0), (1, 1, 8, far)):
+        e = psd.PsdLogitsEdit(history=FAKE, history_cap=cap, bias_rows=1, allow_rows=1, repetition=1.0)
+        assert L.psd_confidence_logits(FAKE, psd.PSD_BF16, V, B, 1, M, V, ctypes.byref(e), FAKE, FAKE, None, FAKE, 1 << 50, None,
+                                       None) == psd.PSD_ERR_SHAPE
+    assert psd.psd_logits_workspace_bytes(far, 8) == psd.psd_logits_workspace_bytes(8, far) == 0
+
+
 def test_struct_layouts():
     assert ctypes.sizeof(psd.PsdKvStrides) == 24 and ctypes.sizeof(psd.PsdAttention) == 48 + 32 + 96
     assert ctypes.sizeof(psd.PsdEvict) == 32 + 96 and ctypes.sizeof(psd.PsdLogitsEdit) == 48 + 28 + 4
