@@ -185,9 +185,13 @@ int psd_merge_partials(const float* max, const float* sumexp, const int32_t* arg
  * (Sec. 3.2 Stage 1; App. B.2 for the threshold rule.)
  *
  * conf, tok are [B, n_nodes, M]; block b reads the rows of node node[b] (node 0 when node is
- * NULL).  Over the masked slots of block b, ranked by (confidence descending, slot ascending; NaN
- * last):  n_thr = #{c_i > tau},  n = min(#masked, k_max or inf, max(n_thr, k_min)),  T = the first
+ * NULL).  A prediction tok < 0 is no token (psd_confidence_logits gives -1 where nothing may be chosen):
+ * here and in the calls below its slot is not counted, committed or speculated, and agrees with nothing.
+ * Over the other masked slots of block b, the candidates, ranked by (confidence descending, slot ascending;
+ * NaN last):  n_thr = #{c_i > tau},  n = min(#candidates, k_max or inf, max(n_thr, k_min)),  T = the first
  * n.  Then tokens[b,i] = tok[i] and mask[b,i] = 0 for i in T; every other slot is left untouched.
+ * n_sel[b] = 0 with slots still masked means that none of them has a token: the block is at a dead end, and
+ * the same state will give the same answer again, so a loop has to change what is allowed there or stop.
  *
  *   tokens, mask [B, M] int32, in/out
  *   sel      [B, M] int32 out: 1 where i in T, else 0
@@ -205,7 +209,7 @@ int psd_select_unmask(const float* conf, const int32_t* tok, const int32_t* node
  *
  * conf, tok [B, n_nodes, M] are the cached predictions the step started from (node selection as in
  * psd_select_unmask); tokens, mask [B, M] are the state AFTER psd_select_unmask.  With m masked
- * slots left, sigma orders them by (cached confidence descending, slot ascending; NaN last);
+ * slots left that have a token (tok >= 0), sigma orders them by (cached confidence descending, slot ascending; NaN last);
  * node d fills S_d = {sigma_1 .. sigma_{n_d}}, n_d = min(m, d * s), s = stride or k_min:
  *   draft_tokens[b,d,i] = tok[i] if i in S_d else tokens[b,i];   draft_mask[b,d,i] = mask[b,i] and i not in S_d.
  * Node 0 is the root (S_0 empty).  A block with m = 0 yields D copies of its state and n_fill = 0.
@@ -228,7 +232,8 @@ int psd_build_drafts(const float* conf, const int32_t* tok, const int32_t* node,
  * node d >= 1 is accepted iff node d-1 is and every slot i = sigma_j, n_{d-1} < j <= n_d, passes
  * A_pi against node d-1's predictions (p.accept_mode).  k* is the accepted node that fills the
  * most slots, lowest index among equals.  Then tokens, mask <- draft k*, and every slot still
- * masked in draft k* whose confV[b,k*,i] > tau is committed to tokV[b,k*,i] as well.
+ * masked in draft k* whose confV[b,k*,i] > tau is committed to tokV[b,k*,i] as well (tokens below 0 agree
+ * with nothing and are not committed).
  *
  *   tokens, mask     [B, M] int32 out (fully written)
  *   k_star           [B] int32 out
@@ -609,8 +614,8 @@ size_t psd_logits_workspace_bytes(int32_t n_rows, int32_t V);
  *   c > 0:  x = l > 0 ? l / repetition : l * repetition;  x = x - (frequency * c + presence);   else x = l
  *   x = x + bias;   tokens whose allow bit is 0 drop out, whatever their logit holds.
  * out_token, out_conf, out_lse are those of psd_confidence over x.  A row in which no token is left (or all that are left
- * have x = -inf) gives token -1, confidence 0 and lse -inf; it is not counted as non-finite, and its token must not be
- * committed.  A NaN or +inf among the tokens left gives confidence NaN and is counted in status_dev.
+ * have x = -inf) gives token -1, confidence 0 and lse -inf; it is not counted as non-finite, and psd_select_unmask,
+ * psd_build_drafts and psd_verify_accept take its slot for one without a token: it stays masked.  A NaN or +inf among the tokens left gives confidence NaN and is counted in status_dev.
  *   logits [B*D*M, V] bf16, fp16 or fp32 (dtype), rows row_stride >= V elements apart, aligned to their element;
  *     B*D*M and V at most 2^30
  *   edit: HOST pointer, NULL = no edits;  workspace >= psd_logits_workspace_bytes(B*D*M, V), 256-byte aligned

@@ -176,9 +176,10 @@ def policy_count(conf_row, slots, p: Policy) -> int:
     return min(n, len(slots))
 
 
-def policy_set(conf_row, mask_row, p: Policy):
-    """T = pi(x, c): the policy_count highest-confidence masked slots, in rank order."""
-    slots = [i for i in range(len(mask_row)) if mask_row[i] != 0]
+def policy_set(conf_row, mask_row, p: Policy, tok_row):
+    """T = pi(x, c): the policy_count highest-confidence masked slots, in rank order.  A prediction below 0
+    is no token (nothing may be chosen there): its slot is no candidate."""
+    slots = [i for i in range(len(mask_row)) if mask_row[i] != 0 and tok_row[i] >= 0]
     order = sorted(slots, key=lambda i: _rank_key(conf_row, i))
     return order[:policy_count(conf_row, slots, p)]
 
@@ -200,7 +201,7 @@ def select_unmask(conf, tok, tokens, mask, p: Policy):
     n_sel = np.zeros(B, dtype=np.int32)
     sel_pos = np.full((B, M), -1, dtype=np.int32)
     for b in range(B):
-        T = policy_set(conf[b], mask[b], p)
+        T = policy_set(conf[b], mask[b], p, tok[b])
         n_sel[b] = len(T)
         for r, i in enumerate(T):
             sel[b, i] = 1
@@ -214,7 +215,7 @@ def build_drafts(conf, tok, tokens, mask, p: Policy):
     """Stage 2 (Sec. 3.2; Algorithm 1 "Stage 2"; Eq. (2)) for a chain of D nodes.
 
     conf, tok: the cached step-t predictions [B, M]; tokens, mask: the state after Stage 1.
-    sigma = still-masked slots by descending step-t confidence; node d fills
+    sigma = still-masked slots that have a token (tok >= 0) by descending step-t confidence; node d fills
     S_d = {sigma_1 .. sigma_{n_d}}, n_d = min(m, d*stride); draft d is Eq. (2).
     Returns sigma[B, M] (-1 padded), n_fill[B, D], draft_tokens[B, D, M], draft_mask[B, D, M].
     """
@@ -230,7 +231,7 @@ def build_drafts(conf, tok, tokens, mask, p: Policy):
     draft_tokens = np.empty((B, D, M), dtype=np.int32)
     draft_mask = np.empty((B, D, M), dtype=np.int32)
     for b in range(B):
-        residual = [i for i in range(M) if mask[b, i] != 0]
+        residual = [i for i in range(M) if mask[b, i] != 0 and tok[b, i] >= 0]
         order = sorted(residual, key=lambda i: _rank_key(conf[b], i))
         m = len(order)
         sigma[b, :m] = order
@@ -275,14 +276,14 @@ def verify_accept(tokV, confV, sigma, n_fill, draft_tokens, draft_mask, p: Polic
             pol = None
             for j in range(int(n_fill[b, parent]), int(n_fill[b, d])):
                 i = int(sigma[b, j])
-                agree = int(tokV[b, parent, i]) == int(draft_tokens[b, d, i])
+                agree = int(tokV[b, parent, i]) == int(draft_tokens[b, d, i]) >= 0
                 if p.accept_mode == ACCEPT_AGREE_AND_CONF:
                     good = agree and float(confV[b, parent, i]) > p.tau
                 elif p.accept_mode == ACCEPT_AGREE_ONLY:
                     good = agree
                 else:
                     if pol is None:
-                        pol = set(policy_set(confV[b, parent], draft_mask[b, parent], p))
+                        pol = set(policy_set(confV[b, parent], draft_mask[b, parent], p, tokV[b, parent]))
                     good = agree and i in pol
                 ok = ok and good
             accepted[b, d] = 1 if ok else 0
@@ -296,7 +297,7 @@ def verify_accept(tokV, confV, sigma, n_fill, draft_tokens, draft_mask, p: Polic
         mask[b] = draft_mask[b, best]
         extra = 0
         for i in range(M):
-            if mask[b, i] != 0 and float(confV[b, best, i]) > p.tau:
+            if mask[b, i] != 0 and float(confV[b, best, i]) > p.tau and tokV[b, best, i] >= 0:
                 tokens[b, i] = tokV[b, best, i]
                 mask[b, i] = 0
                 extra += 1
@@ -419,7 +420,7 @@ def build_drafts_dag(conf, tok, tokens, mask, p: Policy, node_ranks):
     draft_tokens = np.empty((B, K, M), dtype=np.int32)
     draft_mask = np.empty((B, K, M), dtype=np.int32)
     for b in range(B):
-        residual = [i for i in range(M) if mask[b, i] != 0]
+        residual = [i for i in range(M) if mask[b, i] != 0 and tok[b, i] >= 0]
         order = sorted(residual, key=lambda i: _rank_key(conf[b], i))
         m = len(order)
         sigma[b, :m] = order
@@ -473,14 +474,14 @@ def verify_accept_dag(tokV, confV, sigma, draft_tokens, draft_mask, p: Policy, n
                     continue
                 ok = True
                 for i in S[k] - S[q]:
-                    agree = int(tokV[b, q, i]) == int(draft_tokens[b, k, i])
+                    agree = int(tokV[b, q, i]) == int(draft_tokens[b, k, i]) >= 0
                     if p.accept_mode == ACCEPT_AGREE_AND_CONF:
                         good = agree and float(confV[b, q, i]) > p.tau
                     elif p.accept_mode == ACCEPT_AGREE_ONLY:
                         good = agree
                     else:
                         if q not in pol:
-                            pol[q] = set(policy_set(confV[b, q], draft_mask[b, q], p))
+                            pol[q] = set(policy_set(confV[b, q], draft_mask[b, q], p, tokV[b, q]))
                         good = agree and i in pol[q]
                     ok = ok and good
                 if ok:
@@ -496,7 +497,7 @@ def verify_accept_dag(tokV, confV, sigma, draft_tokens, draft_mask, p: Policy, n
         mask[b] = draft_mask[b, best]
         extra = 0
         for i in range(M):
-            if mask[b, i] != 0 and float(confV[b, best, i]) > p.tau:
+            if mask[b, i] != 0 and float(confV[b, best, i]) > p.tau and tokV[b, best, i] >= 0:
                 tokens[b, i] = tokV[b, best, i]
                 mask[b, i] = 0
                 extra += 1

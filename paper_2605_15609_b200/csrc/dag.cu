@@ -38,7 +38,9 @@ __global__ void build_dag_kernel(const float* __restrict__ conf, const int32_t* 
     const size_t src = ((size_t)b * n_nodes_in + nd) * M;
     const size_t st = (size_t)b * M;
     const float c = in ? conf[src + i] : 0.f;
-    const int mk = in ? (mask[st + i] != 0) : 0;
+    const int32_t pred = in ? tok[src + i] : -1;
+    const int masked = in ? (mask[st + i] != 0) : 0;
+    const int mk = masked && pred >= 0;          // slots that can be speculated (a prediction below 0 is no token)
     s_conf[i] = c;
     s_flag[i] = mk;
     const int m = __syncthreads_count(mk);
@@ -50,14 +52,13 @@ __global__ void build_dag_kernel(const float* __restrict__ conf, const int32_t* 
     if (mk) sigma[st + rank] = i;
     const uint64_t valid = valid_ranks(m);
     const int32_t cur = in ? tokens[st + i] : 0;
-    const int32_t pred = mk ? tok[src + i] : 0;
     for (int k = 0; k < K; ++k) {
         if (i == 0) n_fill[(size_t)b * K + k] = __popcll(g.ranks[k] & valid);
         if (in) {
             const bool fill = mk && rank < 64 && ((g.ranks[k] >> rank) & 1ull);      // i in S_k
             const size_t o = ((size_t)b * K + k) * M + i;
             draft_tokens[o] = fill ? pred : cur;       // Eq. (2)
-            draft_mask[o] = (mk && !fill) ? 1 : 0;
+            draft_mask[o] = (masked && !fill) ? 1 : 0;
         }
     }
 }
@@ -82,7 +83,7 @@ __global__ void accept_dag_kernel(const int32_t* __restrict__ tokV, const float*
     __syncthreads();
     if (have) atomicAdd(&s_m, have);
     __syncthreads();
-    const int m_res = s_m;                       // residual masked slots = valid ranks
+    const int m_res = s_m;                       // slots in sigma = valid ranks
     const int n_ranks = min(m_res, 64);
 
     // pass[p] bit j: slot sigma_j passes A_pi against node p's predictions
@@ -93,7 +94,8 @@ __global__ void accept_dag_kernel(const int32_t* __restrict__ tokV, const float*
         if (holder >= 0) {
             const int i = sigma[st + j];
             const size_t po = blk + (size_t)q * M;
-            const bool agree = tokV[po + i] == draft_tokens[blk + (size_t)holder * M + i];
+            const int32_t x = draft_tokens[blk + (size_t)holder * M + i];
+            const bool agree = x >= 0 && tokV[po + i] == x;
             if (p.accept_mode == PSD_ACCEPT_AGREE_ONLY) {
                 ok = agree;
             } else if (p.accept_mode == PSD_ACCEPT_AGREE_AND_CONF) {
@@ -101,10 +103,10 @@ __global__ void accept_dag_kernel(const int32_t* __restrict__ tokV, const float*
             } else {
                 // the policy on node q's draft: is slot i among the positions it would commit?
                 const float ci = confV[po + i];
-                const bool mi = draft_mask[po + i] != 0;
+                const bool mi = draft_mask[po + i] != 0;      // (agree: it has a token)
                 int n_masked = 0, n_thr = 0, rk = 0;
                 for (int t = 0; t < M; ++t) {
-                    const bool mt = draft_mask[po + t] != 0;
+                    const bool mt = draft_mask[po + t] != 0 && tokV[po + t] >= 0;
                     const float ct = confV[po + t];
                     n_masked += mt;
                     n_thr += mt && ct > p.tau;
@@ -156,7 +158,7 @@ __global__ void accept_dag_kernel(const int32_t* __restrict__ tokV, const float*
         const size_t o = blk + (size_t)best * M + i;
         int32_t t = draft_tokens[o];
         int mk = draft_mask[o] != 0;
-        if (mk && confV[o] > p.tau) { t = tokV[o]; mk = 0; ++extra; }
+        if (mk && confV[o] > p.tau && tokV[o] >= 0) { t = tokV[o]; mk = 0; ++extra; }
         tokens[st + i] = t;
         mask[st + i] = mk;
     }

@@ -7,6 +7,8 @@
 // Each stage is a __device__ body that works for any block size >= M (and >= D for acceptance).
 // The bodies take plain (not __restrict__) pointers: in the fused kernel a later stage reads what an
 // earlier stage of the same launch wrote, so no load may go through the read-only data path.
+// A prediction below 0 is no token (psd_confidence_logits gives -1 where nothing may be chosen): no stage counts, commits,
+// speculates or agrees with it.
 // The stand-alone kernels wrap one body each, and step_tail_kernel runs the split-V merge and the
 // three bodies back to back for one sequence block, so that a whole step is two launches.
 #include "combine.cuh"
@@ -31,7 +33,8 @@ __device__ __forceinline__ void select_body(float* s_conf, int* s_flag,
     const size_t src = ((size_t)b * n_nodes + node_of(node, b, n_nodes)) * M;
     const size_t st = (size_t)b * M;
     const float c = in ? conf[src + i] : 0.f;
-    const int mk = in ? (mask[st + i] != 0) : 0;
+    const int32_t pred = in ? tok[src + i] : -1;
+    const int mk = in ? (mask[st + i] != 0 && pred >= 0) : 0;      // candidates: masked, and there is a token to commit
     s_conf[i] = c;
     s_flag[i] = mk;
     const int n_masked = __syncthreads_count(mk);
@@ -45,7 +48,7 @@ __device__ __forceinline__ void select_body(float* s_conf, int* s_flag,
     }
     if (chosen) {
         sel_pos[st + rank] = i;
-        tokens[st + i] = tok[src + i];   // Eq. (1)
+        tokens[st + i] = pred;   // Eq. (1)
         mask[st + i] = 0;
     }
     if (i == 0) n_sel[b] = n;
@@ -63,7 +66,9 @@ __device__ __forceinline__ void build_body(float* s_conf, int* s_flag,
     const size_t src = ((size_t)b * n_nodes + node_of(node, b, n_nodes)) * M;
     const size_t st = (size_t)b * M;
     const float c = in ? conf[src + i] : 0.f;
-    const int mk = in ? (mask[st + i] != 0) : 0;
+    const int32_t pred = in ? tok[src + i] : -1;
+    const int masked = in ? (mask[st + i] != 0) : 0;
+    const int mk = masked && pred >= 0;                // slots that can be speculated
     s_conf[i] = c;
     s_flag[i] = mk;
     const int m = __syncthreads_count(mk);
@@ -72,7 +77,6 @@ __device__ __forceinline__ void build_body(float* s_conf, int* s_flag,
     if (mk) sigma[st + rank] = i;
     const long long s = p.stride > 0 ? p.stride : p.k_min;
     const int32_t cur = in ? tokens[st + i] : 0;
-    const int32_t pred = mk ? tok[src + i] : 0;
     for (int d = 0; d < D; ++d) {
         const int n_d = (int)min((long long)m, (long long)d * s);
         if (i == 0) n_fill[(size_t)b * D + d] = n_d;
@@ -80,7 +84,7 @@ __device__ __forceinline__ void build_body(float* s_conf, int* s_flag,
             const bool fill = mk && rank < n_d;       // i in S_d
             const size_t o = ((size_t)b * D + d) * M + i;
             draft_tokens[o] = fill ? pred : cur;      // Eq. (2)
-            draft_mask[o] = (mk && !fill) ? 1 : 0;
+            draft_mask[o] = (masked && !fill) ? 1 : 0;
         }
     }
 }
@@ -117,7 +121,10 @@ __device__ __forceinline__ void accept_body(float* s_conf, int* s_flag, int* s_r
         for (int d = D - 1; d >= 1; --d)
             if (s_nfill[d] > r) dd = d;
     bool agree = false;
-    if (dd < D) agree = tokV[blk + (size_t)(dd - 1) * M + i] == draft_tokens[blk + (size_t)dd * M + i];
+    if (dd < D) {
+        const int32_t x = draft_tokens[blk + (size_t)dd * M + i];
+        agree = x >= 0 && tokV[blk + (size_t)(dd - 1) * M + i] == x;
+    }
 
     int first_fail = D;
     if (p.accept_mode != PSD_ACCEPT_AGREE_AND_POLICY) {
@@ -133,7 +140,7 @@ __device__ __forceinline__ void accept_body(float* s_conf, int* s_flag, int* s_r
         for (int d = 1; d < D; ++d) {
             const size_t par = blk + (size_t)(d - 1) * M;
             const float c = in ? confV[par + i] : 0.f;
-            const int mk = in ? (draft_mask[par + i] != 0) : 0;
+            const int mk = in ? (draft_mask[par + i] != 0 && tokV[par + i] >= 0) : 0;
             __syncthreads();
             s_conf[i] = c;
             s_flag[i] = mk;
@@ -161,7 +168,8 @@ __device__ __forceinline__ void accept_body(float* s_conf, int* s_flag, int* s_r
         const size_t o = blk + (size_t)best * M + i;
         t = draft_tokens[o];
         mk = draft_mask[o] != 0;
-        extra = mk && confV[o] > p.tau;     // the verifier's own predictions on node k* that pass the threshold
+        // the verifier's own predictions on node k* that pass the threshold
+        extra = mk && confV[o] > p.tau && tokV[o] >= 0;
         if (extra) { t = tokV[o]; mk = 0; }
         tokens[st + i] = t;
         mask[st + i] = mk;

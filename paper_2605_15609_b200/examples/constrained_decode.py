@@ -80,7 +80,7 @@ def decode(B=4, D=4, blocks=4, budget=96, V=4000, seed=0, allowed=0.5):
     i32 = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")  # noqa: E731
     # a grammar: which tokens may appear at all (one row of bits for every row of logits)
     legal = torch.rand(V, generator=g, device="cuda") < allowed
-    legal[:2] = True
+    legal[:2] = allowed > 0        # (0: a grammar that allows nothing, a dead end)
     bits = torch.zeros((V + 31) // 32 * 32, dtype=torch.int64, device="cuda")
     bits[:V] = legal
     allow = (bits.view(-1, 32) << torch.arange(32, device="cuda")).sum(1).to(torch.int32)[None]
@@ -128,7 +128,10 @@ def decode(B=4, D=4, blocks=4, budget=96, V=4000, seed=0, allowed=0.5):
         tokens, mask = torch.full((B, M), V, dtype=torch.int32, device="cuda"), torch.ones(B, M, dtype=torch.int32, device="cuda")
         while int(mask.sum()):
             tok, conf, _ = forward(tokens, mask, 1)
-            psd.psd_select_unmask(conf, tok, tokens, mask, p, i32(B, M), i32(B), i32(B, M))
+            n_sel = i32(B)
+            psd.psd_select_unmask(conf, tok, tokens, mask, p, i32(B, M), n_sel, i32(B, M))
+            if bool(((n_sel == 0) & (mask.sum(1) > 0)).any()):
+                raise RuntimeError("dead end: the grammar leaves no token for any masked slot of a sequence")
             sigma, n_fill, draft_tokens, draft_mask = i32(B, M), i32(B, D), i32(B, D, M), i32(B, D, M)
             psd.psd_build_drafts(conf, tok, tokens, mask, p, sigma, n_fill, draft_tokens, draft_mask)
             tok, conf, _ = forward(draft_tokens.view(B * D, M), draft_mask.view(B * D, M), D)
