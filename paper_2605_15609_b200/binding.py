@@ -538,9 +538,17 @@ _pack_evict = struct.Struct("=8i12q").pack
 _pack_edit = struct.Struct("=6Q3i3fi4x").pack
 
 
-def _raw_stream(stream):
+def _here(stream, *tensors):
+    """The handle of the stream to launch on.  All tensors (None: not given) have to be on the current CUDA device, since the
+    kernels would follow any other address as well: a list of lengths left on the host would fault the GPU."""
+    dev = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"psd binding: tensors of one call are on one CUDA device, got {tensors[0].device} and {t.device}")
+    if dev < 0 or dev != torch._C._cuda_getDevice():
+        raise ValueError(f"psd binding: tensors have to be on the current CUDA device, got {tensors[0].device}")
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return torch._C._cuda_getCurrentRawStream(dev)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -564,28 +572,34 @@ def _want_n(t, n, dtype, name):
 
 def _space(t):
     """(address, bytes) of a workspace."""
-    return (None, 0) if t is None else (_ptr(t), t.numel() * t.element_size())
+    return (None, 0) if t is None else (_ptr(t), t.nbytes)
 
 
-def _tokens_strides(t, name):
+def _tokens_strides(t, N, M, H, Dh, name):
     """(token, head) strides of [N, M, H, Dh] whose first two dimensions are one run of tokens."""
-    N, M, H, Dh = t.shape
     sn, sm, sh, sd = t.stride()
     if (sd != 1 and Dh > 1) or (N > 1 and M > 1 and sn != M * sm):
         raise ValueError(f"psd binding: {name} needs a dense last dimension and nodes M tokens apart")
     return (sm if M > 1 else sn if N > 1 else H * Dh), (sh if H > 1 else Dh)
 
 
-def _kv_strides(t, name):
+_NO_CACHE = (0, 8, 0, 0, 8, 0)
+
+
+def _kv_strides(strides, no, nt, nh, nd, name):
     """(outer, token, head) strides of a cache; that of a dimension of one is never walked: 0 (shared), or the smallest the
     library takes."""
-    if t is None:
-        return 0, 8, 0
-    no, nt, nh, nd = t.shape
-    so, st, sh, sd = t.stride()
+    so, st, sh, sd = strides
     if sd != 1 and nd > 1:
         raise ValueError(f"psd binding: {name} needs a dense last dimension")
     return so if no > 1 else 0, st if nt > 1 else 8, sh if nh > 1 else 0
+
+
+def _pair_strides(k, v, no, nt, nh, nd, name):
+    """Strides of a cache's keys and of its values (one shape, and mostly one layout)."""
+    of_k, of_v = k.stride(), v.stride()
+    s = _kv_strides(of_k, no, nt, nh, nd, name)
+    return s + s if of_v == of_k else s + _kv_strides(of_v, no, nt, nh, nd, name)
 
 
 def _one_type(dt, *tensors):
@@ -603,28 +617,32 @@ def psd_draft_attention(q, k_prefix, v_prefix, out, lse=None, k_own=None, v_own=
                         scale=None, causal=False, workspace=None, status=None, stream=None):
     """q [B*D, M, Hq, Dh] over the prefix caches [B, P, Hkv, Dh] and each node's own keys [B*D, S, Hkv, Dh] -> out
     (like q) and lse [B*D, M, Hq].  Strided tensors are taken as they are; ``scale`` defaults to 1/sqrt(Dh)."""
-    N, M, Hq, Dh = q.shape
-    B, P, Hkv, dk = k_prefix.shape
+    rows, cache = q.shape, k_prefix.shape
+    N, M, Hq, Dh = rows
+    B, P, Hkv, dk = cache
     if B < 1 or N % B or dk != Dh:
         raise ValueError("psd binding: q [B*D, M, Hq, Dh] and k_prefix [B, P, Hkv, Dh] do not belong together")
-    if v_prefix.shape != k_prefix.shape or out.shape != q.shape or (k_own is None) != (v_own is None):
+    if v_prefix.shape != cache or out.shape != rows or (k_own is None) != (v_own is None):
         raise ValueError("psd binding: keys and values, and out and q, have one shape; k_own and v_own come together")
-    S, ko, vo = 0, None, None
+    S, ko, vo, own = 0, None, None, _NO_CACHE
     if k_own is not None:
-        S = k_own.shape[1]
-        if k_own.shape != (N, S, Hkv, Dh) or v_own.shape != k_own.shape:
+        shape = k_own.shape
+        S = shape[1]
+        if shape != (N, S, Hkv, Dh) or v_own.shape != shape:
             raise ValueError("psd binding: k_own and v_own are [B*D, S, Hkv, Dh]")
+        own = _pair_strides(k_own, v_own, N, S, Hkv, Dh, "k_own, v_own")
         ko, vo = k_own.data_ptr() or None, v_own.data_ptr() or None
     a = _pack_attention(B, N // B, M, Hq, Hkv, Dh, P, S, _one_type(q.dtype, k_prefix, v_prefix, k_own, v_own, out),
-                        1 if causal else 0, Dh ** -0.5 if scale is None else scale, 0, *_tokens_strides(q, "q"),
-                        *_tokens_strides(out, "out"), *_kv_strides(k_prefix, "k_prefix"),
-                        *_kv_strides(v_prefix, "v_prefix"), *_kv_strides(k_own, "k_own"), *_kv_strides(v_own, "v_own"))
+                        1 if causal else 0, Dh ** -0.5 if scale is None else scale, 0,
+                        *_tokens_strides(q, N, M, Hq, Dh, "q"), *_tokens_strides(out, N, M, Hq, Dh, "out"),
+                        *_pair_strides(k_prefix, v_prefix, B, P, Hkv, Dh, "k_prefix, v_prefix"), *own)
+    stream = _here(stream, q, k_prefix, v_prefix, out, lse, k_own, v_own, prefix_len, own_len, workspace, status)
     ws, ws_bytes = _space(workspace)
     _check(LIB.psd_draft_attention(q.data_ptr(), k_prefix.data_ptr() or None, v_prefix.data_ptr() or None,
                                    _want(prefix_len, (B,), _I32, "prefix_len"), ko, vo,
                                    _want(own_len, (N,), _I32, "own_len"), a, out.data_ptr(),
-                                   _want(lse, (N, M, Hq), _F32, "lse"), ws, ws_bytes, _ptr(status),
-                                   _raw_stream(stream)), "psd_draft_attention")
+                                   _want(lse, (N, M, Hq), _F32, "lse"), ws, ws_bytes, _ptr(status), stream),
+           "psd_draft_attention")
 
 
 def psd_weights_workspace_bytes(B, D, M, Hq, Hkv, Dh, P) -> int:
@@ -640,31 +658,35 @@ def psd_prefix_weights(q, k_prefix, lse, acc_out, acc_in=None, beta=1.0, prefix_
     if B < 1 or N % B or dk != Dh:
         raise ValueError("psd binding: q [B*D, M, Hq, Dh] and k_prefix [B, P, Hkv, Dh] do not belong together")
     a = _pack_attention(B, N // B, M, Hq, Hkv, Dh, P, 0, _one_type(q.dtype, k_prefix), 0,
-                        Dh ** -0.5 if scale is None else scale, 0, *_tokens_strides(q, "q"), 0, 0,
-                        *_kv_strides(k_prefix, "k_prefix"), 0, 0, 0, 0, 0, 0, 0, 0, 0)
+                        Dh ** -0.5 if scale is None else scale, 0,
+                        *_tokens_strides(q, N, M, Hq, Dh, "q"), 0, 0,
+                        *_kv_strides(k_prefix.stride(), B, P, Hkv, Dh, "k_prefix"), 0, 0, 0, 0, 0, 0, 0, 0, 0)
     sums = (B, Hkv, P)
+    stream = _here(stream, q, k_prefix, lse, acc_out, acc_in, prefix_len, workspace, status)
     ws, ws_bytes = _space(workspace)
     _check(LIB.psd_prefix_weights(q.data_ptr(), k_prefix.data_ptr() or None, _want(prefix_len, (B,), _I32, "prefix_len"),
                                   _want(lse, (N, M, Hq), _F32, "lse"), a, beta, _want(acc_in, sums, _F32, "acc_in"),
-                                  _want(acc_out, sums, _F32, "acc_out"), ws, ws_bytes, _ptr(status),
-                                  _raw_stream(stream)), "psd_prefix_weights")
+                                  _want(acc_out, sums, _F32, "acc_out"), ws, ws_bytes, _ptr(status), stream),
+           "psd_prefix_weights")
 
 
 def psd_prefix_evict(scores, k, v, k_out, v_out, index, scores_out=None, len_out=None, prefix_len=None, n_sink=0,
                      n_recent=0, stream=None):
     """Keep index.shape[2] keys per sequence and key head of the caches k, v [B, P, Hkv, Dh]: packed into k_out, v_out
     [B, keep, Hkv, Dh], their positions into index [B, Hkv, keep]."""
-    B, P, Hkv, Dh = k.shape
+    cache, kept_rows = k.shape, k_out.shape
+    B, P, Hkv, Dh = cache
     keep = index.shape[-1]
-    if v.shape != k.shape or k_out.shape != (B, keep, Hkv, Dh) or v_out.shape != k_out.shape:
+    if v.shape != cache or kept_rows != (B, keep, Hkv, Dh) or v_out.shape != kept_rows:
         raise ValueError("psd binding: k, v are [B, P, Hkv, Dh], k_out, v_out [B, keep, Hkv, Dh]")
-    e = _pack_evict(B, Hkv, Dh, P, keep, n_sink, n_recent, _one_type(k.dtype, v, k_out, v_out), *_kv_strides(k, "k"),
-                    *_kv_strides(v, "v"), *_kv_strides(k_out, "k_out"), *_kv_strides(v_out, "v_out"))
+    e = _pack_evict(B, Hkv, Dh, P, keep, n_sink, n_recent, _one_type(k.dtype, v, k_out, v_out),
+                    *_pair_strides(k, v, B, P, Hkv, Dh, "k, v"), *_pair_strides(k_out, v_out, B, keep, Hkv, Dh, "k_out, v_out"))
+    stream = _here(stream, k, v, scores, k_out, v_out, index, scores_out, len_out, prefix_len)
     kept = (B, Hkv, keep)
     _check(LIB.psd_prefix_evict(_want(scores, (B, Hkv, P), _F32, "scores"), k.data_ptr(), v.data_ptr(),
                                 _want(prefix_len, (B,), _I32, "prefix_len"), e, k_out.data_ptr(), v_out.data_ptr(),
                                 _want(index, kept, _I32, "index"), _want(scores_out, kept, _F32, "scores_out"),
-                                _want(len_out, (B,), _I32, "len_out"), _raw_stream(stream)), "psd_prefix_evict")
+                                _want(len_out, (B,), _I32, "len_out"), stream), "psd_prefix_evict")
 
 
 def psd_logits_workspace_bytes(n_rows: int, V: int) -> int:
@@ -683,11 +705,16 @@ def psd_confidence_logits(logits, out_token, out_conf, out_lse=None, B=None, D=1
     row, one = logits.stride()
     if B * D * M != R or (one != 1 and V > 1):
         raise ValueError("psd binding: logits [B*D*M, V] needs a dense last dimension")
+    stream = _here(stream, logits, out_token, out_conf, out_lse, history, history_len, draft_tokens, draft_mask, bias, allow,
+                   workspace, status)
     T = bias_rows = allow_rows = 0
     h = hl = dt = dm = bi = al = 0
     if history is not None:
-        T = history.shape[1]
-        h = _want(history, (B, T), _I32, "history")
+        shape = history.shape
+        T = shape[1]
+        if shape[0] != B:
+            raise ValueError(f"psd binding: history must have {B} rows, got {tuple(shape)}")
+        h = _want_n(history, B * T, _I32, "history")
         hl = _want(history_len, (B,), _I32, "history_len") or 0
     if draft_tokens is not None:
         dt = _want_n(draft_tokens, R, _I32, "draft_tokens")
@@ -703,5 +730,5 @@ def psd_confidence_logits(logits, out_token, out_conf, out_lse=None, B=None, D=1
     ws, ws_bytes = _space(workspace)
     _check(LIB.psd_confidence_logits(logits.data_ptr(), _DTYPES.get(logits.dtype, -1), row if R > 1 else V, B, D, M, V, e,
                                      _want_n(out_token, R, _I32, "out_token"), _want_n(out_conf, R, _F32, "out_conf"),
-                                     _want_n(out_lse, R, _F32, "out_lse"), ws, ws_bytes, _ptr(status),
-                                     _raw_stream(stream)), "psd_confidence_logits")
+                                     _want_n(out_lse, R, _F32, "out_lse"), ws, ws_bytes, _ptr(status), stream),
+           "psd_confidence_logits")
