@@ -536,7 +536,8 @@ size_t psd_attention_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t Hq
  * own keys of node (b, d) that `causal` lets it see:
  *   s_j = scale * q[t,h] . K_j,   lse[t,h] = ln sum_j exp(s_j),   out[t,h] = sum_j exp(s_j - lse) V_j.
  * A row without keys gives out = 0 and lse = -inf.  Scores, softmax statistics and sums are fp32, the
- * weights are rounded to the inputs' type before they multiply V, out is rounded once at the end.
+ * weights are rounded to the inputs' type before they multiply V (fp16: kept large enough that none is off by more
+ * than 2^-32 of the row's largest beside its rounding), out is rounded once at the end.
  *   prefix_len [B] int32, device, or NULL for P everywhere;  own_len [B*D] int32, device, or NULL for S;
  *   values outside [0, P] ([0, S]) are clamped.  What lies past a length is never used, whatever it holds, and
  *   a draft's outputs never depend on another draft's keys (with `causal`, values of own keys that a row of the

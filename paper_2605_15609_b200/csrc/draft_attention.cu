@@ -19,8 +19,11 @@ namespace {
 constexpr int kKeys = 64;        // keys per tile
 constexpr int kThreads = 128;
 
+// ROOM: weights are kept 2^ROOM larger than relative to the row's maximum.  fp16 holds nothing below 2^-25, and thousands of keys
+// that far below a maximum count together; with the largest weight at 2^15 nothing above 2^-40 of it is lost.
 template <typename T> struct Mma;
 template <> struct Mma<__nv_bfloat16> {
+    static constexpr float ROOM = 0.f;
     static __device__ __forceinline__ void run(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -33,6 +36,7 @@ template <> struct Mma<__nv_bfloat16> {
     }
 };
 template <> struct Mma<__half> {
+    static constexpr float ROOM = 15.f;
     static __device__ __forceinline__ void run(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -270,8 +274,8 @@ __global__ void __launch_bounds__(kThreads, WM == 1 ? 4 : 3) draft_attention_ker
         for (int u = 0; u < 2; ++u) {
             mx[u] = fmaxf(mx[u], __shfl_xor_sync(0xffffffffu, mx[u], 1));
             mx[u] = fmaxf(mx[u], __shfl_xor_sync(0xffffffffu, mx[u], 2));
-            base[u] = mx[u] == -INFINITY ? 0.f : mx[u];
-            f[u] = m[u] == mx[u] ? 1.f : ex2(m[u] - base[u]);
+            f[u] = m[u] == mx[u] ? 1.f : ex2(m[u] - mx[u]);
+            base[u] = mx[u] == -INFINITY ? 0.f : mx[u] - Mma<T>::ROOM;
             m[u] = mx[u];
             l[u] *= f[u];
         }
@@ -308,7 +312,7 @@ __global__ void __launch_bounds__(kThreads, WM == 1 ? 4 : 3) draft_attention_ker
     // every warp's rows to shared memory (the tiles are no longer needed: the loop ends with a barrier)
     constexpr int OLD = DHP + 8;                             // padded row: the float2 stores of 8 rows hit different banks
     float* so = reinterpret_cast<float*>(smem);              // [4 warps][16][OLD]
-    float* sm = so + 4 * 16 * OLD;                           // [4 warps][16] maxima, then sums
+    float* sm = so + 4 * 16 * OLD;                           // [4 warps][16] references, then sums
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const int r = warp * 16 + (lane >> 2) + 8 * u;
@@ -316,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, WM == 1 ? 4 : 3) draft_attention_ker
         for (int n = 0; n < NO; ++n)
             *reinterpret_cast<float2*>(&so[r * OLD + n * 8 + (lane & 3) * 2]) = make_float2(o[n][2 * u], o[n][2 * u + 1]);
         if ((lane & 3) == 0) {
-            sm[r] = m[u];
+            sm[r] = m[u] - Mma<T>::ROOM;      // what outputs and sums are relative to
             sm[64 + r] = l[u];
         }
     }

@@ -13,7 +13,9 @@
 //
 // The running maximum is only raised, and O rescaled, when a row's maximum grew by more than 2^8: weights may then be as
 // large as 2^8, which costs no accuracy in a floating type, and rescaling O (reading and writing 128 x Dh of tensor
-// memory) becomes rare.
+// memory) becomes rare.  In fp16 weights are kept 2^7 larger still, up to 2^15 of its 2^16: it holds nothing below 2^-25,
+// and thousands of keys that far below a row's maximum count together (4000 keys 2^-26.7 below it were nearly all lost otherwise,
+// 3.7e-5 of the output); a weight is then off by 2^-32 of the maximum at most.
 //
 // Where the prefix is not split (many rows), the drafts' own keys follow it in the same kernel as further tiles of the list,
 // one draft at a time: its products leave the rows of other drafts as they are (a mask of tensor-memory rows), so what one
@@ -34,6 +36,7 @@ namespace {
 
 constexpr int kPThreads = 384;              // warps 0-3, 4-7: softmax of stream 0, 1; 8: TMA; 9: MMA; 10, 11 idle
 constexpr float kRaise = 8.0f;              // growth of a row's maximum (log2) that triggers a rescale
+constexpr float kHalfRoom = 7.0f;           // fp16: how far (log2) the reference is set below the maximum
 
 constexpr int kMaxSorted = 128;             // sequences that are put in order of length
 constexpr int kBarBytes = 1024;             // barriers, flags and the lists of own tiles
@@ -315,7 +318,7 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
         const f32x2 cc = pack2(a.c, a.c);
-        float m = 0.f, l = 0.f;          // reference maximum (scaled by c) and sum relative to it
+        float m = 0.f, l = 0.f;          // reference (scaled by c) and sum relative to it
         bool fresh = true;               // no score seen yet
         bool ok = true;
         const int n = s ? nt1 : nt0, np = s ? np1 : np0, first_tile = s ? t01 : t00;
@@ -361,7 +364,8 @@ prefix_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
                 for (int i = 3; i < 31; i += 2) u[c] = max3(u[c], x(i), x(i + 1));
                 u[c] = fmaxf(u[c], x(31));
             }
-            const float top = fmaxf(max3(u[0], u[1], u[2]), u[3]) * a.c;
+            // the reference that this tile's maximum asks for
+            const float high = fmaxf(max3(u[0], u[1], u[2]), u[3]), top = BF16 ? high * a.c : fmaf(high, a.c, -kHalfRoom);
             const bool raise = top > (fresh ? -INFINITY : m + kRaise);
             if (__any_sync(0xffffffffu, raise)) {
                 // the first scores of a row, or (rare) a much higher maximum: set the reference and rescale what has been summed
