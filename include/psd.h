@@ -525,7 +525,11 @@ typedef struct psd_attention_t {
     psd_kv_strides_t ko, vo;     /* own keys and values [B*D, S, Hkv, Dh]                                     */
 } psd_attention_t;
 
-/* Bytes of scratch psd_draft_attention needs (0 = bad sizes; the smallest value for good ones is 256). */
+/*
+ * Bytes of scratch psd_draft_attention needs (0 = bad sizes; the smallest value for good ones is 256).  With the other
+ * sizes fixed the answer grows with B, D, P and S, and it serves every call with smaller ones: a workspace made for a
+ * service's largest batch, drafts and cache stays large enough when sequences finish.
+ */
 size_t psd_attention_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P,
                                      int32_t S);
 
@@ -551,7 +555,7 @@ int psd_draft_attention(const void* q, const void* k_prefix, const void* v_prefi
                         void* out, float* lse, void* workspace, size_t workspace_bytes, int32_t* status_dev,
                         void* cuda_stream);
 
-/* Bytes of scratch psd_prefix_weights needs (0 = bad sizes). */
+/* Bytes of scratch psd_prefix_weights needs (0 = bad sizes); grows with B, D, M and P and serves calls with smaller ones. */
 size_t psd_weights_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P);
 
 /*
@@ -605,7 +609,7 @@ typedef struct psd_logits_edit_t {
     int32_t reserved;            /* 0 */
 } psd_logits_edit_t;
 
-/* Bytes of scratch psd_confidence_logits needs (0 = bad sizes). */
+/* Bytes of scratch psd_confidence_logits needs (0 = bad sizes); grows with n_rows and V and serves calls with fewer. */
 size_t psd_logits_workspace_bytes(int32_t n_rows, int32_t V);
 
 /*

@@ -375,12 +375,13 @@ int row_blocks_per_cta(int64_t nodes_heads, int rows) {
 // saves a launch and the join.  It does while a wave of its CTAs (three per SM) has few tiles of 64 keys to walk: measured, one
 // launch against two, 4 drafts of 32 tokens: 4 heads of 64, prefix 257: 7 against 15 us, 1024: 13 against 16, 2048: 22 against
 // 16; 32 heads of 128 over 8 key heads, prefix 257: 13 against 16 us, 512: 17 against 20, 1024: 27 against 22.
+int one_launch_tiles(int Dh) { return Dh <= 64 ? 16 : 8; }
 bool one_launch(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
     const int rows = M * (Hq / Hkv);
     const int64_t nh = (int64_t)B * D * Hkv;
     const int r = 16 * row_blocks_per_cta(nh, rows);
     const int64_t ctas = nh * ((rows + r - 1) / r), waves = (ctas + 3 * sm_count() - 1) / (3 * sm_count());
-    return waves * ((P + kKeys - 1) / kKeys) <= (Dh <= 64 ? 16 : 8);
+    return waves * ((P + kKeys - 1) / kKeys) <= one_launch_tiles(Dh);
 }
 
 template <typename T, int DHP>
@@ -394,11 +395,40 @@ int launch_dh(OwnArgs& p, cudaStream_t st) {
 
 }  // namespace
 
-size_t draft_attention_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
+// Bytes of `rows` partial results, rounded up.
+static size_t partial_bytes(int64_t rows, int dhp) { return rows == 0 ? 256 : ((size_t)rows * (dhp + 1) * 4 + 255) / 256 * 256; }
+
+size_t draft_attention_needs(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
     if (one_launch(B, D, M, Hq, Hkv, Dh, P)) return 256;
     const PrefixPlan p = plan_prefix(B, D, M, Hq, Hkv, Dh, P, S);
-    if (p.fused) return 256;
-    return ((size_t)B * D * M * Hq * p.splits * (p.dhp + 1) * 4 + 255) / 256 * 256;
+    return partial_bytes(p.fused ? 0 : (int64_t)B * D * M * Hq * p.splits, p.dhp);
+}
+
+// What these sizes and all with smaller B, D, P and S need at most: a large batch may need nothing where a small one splits its
+// keys, and a caller whose batch shrinks keeps its workspace.  Two bounds on the partial results of a split form: its CTAs fill the
+// SMs once (2 * 128 rows each), and the splits are bounded by the prefix.
+size_t draft_attention_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
+    const int64_t sms = sm_count(), G = Hq / Hkv, tq = 128 / G, T = (int64_t)D * M, tiles = (P + 127) / 128;
+    const int64_t once = 2 * sms * tq * G, rows = (int64_t)B * T * Hq;
+    const int dhp = Dh <= 64 ? 64 : 128;
+    // One launch at every smaller size: smaller batches use smaller blocks of rows, but then at most 4 CTAs per SM, two waves.
+    const int most = M * (int)G > 32 ? 64 : M * (int)G > 16 ? 32 : 16;
+    const int64_t ctas = (int64_t)B * D * Hkv * ((M * G + most - 1) / most), waves = (ctas + 3 * sms - 1) / (3 * sms);
+    if ((waves < 2 ? 2 : waves) * ((P + kKeys - 1) / kKeys) <= one_launch_tiles(Dh)) return 256;
+    auto least = [](int64_t a, int64_t b) { return a < b ? a : b; };
+    auto larger = [](int64_t a, int64_t b) { return a > b ? a : b; };
+    int64_t partial = 0;
+    if (M <= tq) {
+        // one query tile, at least two splits
+        const int64_t r = (int64_t)B * least(T, tq) * Hq;
+        partial = least(r * larger(2, least(tiles / 2, kMaxPrefixSplits)), larger(2 * r, once));
+    }
+    if (T > tq) {
+        if (!fuses_own(M, (int)tq, S)) partial = larger(partial, rows);
+        if (tiles >= 4) partial = larger(partial, least(rows * least(tiles / 2, kMaxPrefixSplits), once));
+    }
+    const size_t all = partial_bytes(partial, dhp), here = draft_attention_needs(B, D, M, Hq, Hkv, Dh, P, S);
+    return all > here ? all : here;
 }
 
 int launch_draft_attention(const void* q, const void* k_prefix, const void* v_prefix, const int32_t* prefix_len,

@@ -70,7 +70,7 @@ int psd_draft_attention(const void* q, const void* k_prefix, const void* v_prefi
         !aligned(out, 16) || !aligned(workspace, 256) || !aligned(prefix_len, 4) || !aligned(own_len, 4) ||
         !aligned(lse, 4) || !aligned(status_dev, 4))
         return PSD_ERR_ALIGN;
-    if (workspace_bytes < draft_attention_workspace(a->B, a->D, a->M, a->Hq, a->Hkv, a->Dh, a->P, a->S))
+    if (workspace_bytes < draft_attention_needs(a->B, a->D, a->M, a->Hq, a->Hkv, a->Dh, a->P, a->S))
         return PSD_ERR_WORKSPACE;
     return launch_draft_attention(q, k_prefix, v_prefix, prefix_len, k_own, v_own, own_len, *a, out, lse, workspace,
                                   status_dev, reinterpret_cast<cudaStream_t>(cuda_stream));
@@ -78,7 +78,7 @@ int psd_draft_attention(const void* q, const void* k_prefix, const void* v_prefi
 
 size_t psd_weights_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P) {
     if (!attention_sizes_ok(B, D, M, Hq, Hkv, Dh, P, 0) || P < 1) return 0;
-    return prefix_weights_workspace(B, D, M, Hq, Hkv, Dh, P);
+    return prefix_weights_workspace(B, D, M, Hq, Hkv, P);
 }
 
 int psd_prefix_weights(const void* q, const void* k_prefix, const int32_t* prefix_len, const float* lse,
@@ -90,7 +90,7 @@ int psd_prefix_weights(const void* q, const void* k_prefix, const int32_t* prefi
     if (!aligned(q, 16) || !aligned(k_prefix, 16) || !aligned(workspace, 256) || !aligned(prefix_len, 4) ||
         !aligned(lse, 4) || !aligned(acc_in, 4) || !aligned(acc_out, 4) || !aligned(status_dev, 4))
         return PSD_ERR_ALIGN;
-    if (workspace_bytes < prefix_weights_workspace(a->B, a->D, a->M, a->Hq, a->Hkv, a->Dh, a->P)) return PSD_ERR_WORKSPACE;
+    if (workspace_bytes < prefix_weights_needs(a->B, a->D, a->M, a->Hq, a->Hkv, a->P)) return PSD_ERR_WORKSPACE;
     return launch_prefix_weights(q, k_prefix, prefix_len, lse, *a, beta, acc_in, acc_out, workspace, status_dev,
                                  reinterpret_cast<cudaStream_t>(cuda_stream));
 }

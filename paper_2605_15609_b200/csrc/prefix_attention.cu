@@ -517,6 +517,13 @@ int launch_p(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv
 
 }  // namespace
 
+// Own keys in the same kernel: when nothing is split (one result per row) and the drafts of a query tile are few.  A draft
+// costs a tile however few keys it has: with a tile of 32 single-token drafts the kernel of their own is the cheaper way.
+bool fuses_own(int M, int tq, int S) {
+    const int drafts = (tq + M - 2) / M + 1;
+    return (int64_t)drafts * ((S + 127) / 128) <= kMaxOwnTiles && drafts <= 5;
+}
+
 // How the prefix's keys are split.  A CTA takes two query tiles (or the only one twice, over two ranges of keys); when
 // (sequence, key head, tile pair) alone leaves SMs idle the keys are split, down to kMinTiles tiles of 128 keys per split.
 PrefixPlan plan_prefix(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
@@ -534,11 +541,7 @@ PrefixPlan plan_prefix(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int 
     if (s < 1) s = 1;
     p.splits = (int)s * per;
     p.dhp = Dh <= 64 ? 64 : 128;
-    // Own keys in the same kernel: when nothing is split (one result per row) and the drafts of a query tile are few.  A draft
-    // costs a tile however few keys it has: with a tile of 32 single-token drafts the kernel of their own is the cheaper way.
-    const int drafts = (p.tq + M - 2) / M + 1;
-    const int64_t own = (int64_t)drafts * ((S + 127) / 128);
-    p.fused = p.n_qt > 1 && p.splits == 1 && own <= kMaxOwnTiles && drafts <= 5;
+    p.fused = p.n_qt > 1 && p.splits == 1 && fuses_own(M, p.tq, S);
     return p;
 }
 

@@ -15,6 +15,7 @@ struct PrefixPlan {
     int dhp;       // floats per partial output row: 64 or 128
     bool fused;    // the kernel takes the own keys too and writes final outputs (splits == 1)
 };
+bool fuses_own(int M, int tq, int S);   // whether a query tile's own keys can follow an unsplit prefix in the same kernel
 PrefixPlan plan_prefix(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S);
 
 // plan.fused: final outputs into out and lse (NULL: not wanted).  Otherwise partial results of every row over its sequence's

@@ -430,9 +430,18 @@ int launch_w(const CUtensorMap& mk, const CUtensorMap& mq, const WeightsArgs& a,
 
 }  // namespace
 
-size_t prefix_weights_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
+size_t prefix_weights_needs(int B, int D, int M, int Hq, int Hkv, int P) {
     const WeightsPlan p = plan_weights(B, D, M, Hq, Hkv, P);
     return p.splits > 1 ? ((size_t)p.splits * B * Hkv * P * 4 + 255) / 256 * 256 : 256;
+}
+
+// What these sizes and all with smaller B, D, M and P need at most: units of 256 keys are split only while the splits of all of them
+// fit the SMs, so a large batch may need nothing where a small one does.
+size_t prefix_weights_workspace(int B, int D, int M, int Hq, int Hkv, int P) {
+    const int n_qt = plan_weights(B, D, M, Hq, Hkv, P).n_qt;
+    if (n_qt == 1) return 256;
+    const int64_t most = (int64_t)B * Hkv * P * (n_qt < kMaxSplits ? n_qt : kMaxSplits), once = (int64_t)sm_count() * kKeysPerCta;
+    return ((size_t)(most < once ? most : once) * 4 + 255) / 256 * 256;
 }
 
 int launch_prefix_weights(const void* q, const void* k_prefix, const int32_t* prefix_len, const float* lse,
