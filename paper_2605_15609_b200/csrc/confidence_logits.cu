@@ -463,10 +463,24 @@ int launch(const LogitsArgs& a, int64_t grid, int64_t n_rows, int32_t* out_token
 
 }  // namespace
 
+// Rows of a unit: of one draft, and of one bias row where there are several.
+static int rows_per_unit(int64_t n_rows, int M, int bias_rows) { return bias_rows > 0 ? gcd_int(M, (int)(n_rows / bias_rows)) : M; }
+
+size_t confidence_logits_needs(int64_t n_rows, int M, int V, int bias_rows) {
+    const int unit_rows = rows_per_unit(n_rows, M, bias_rows);
+    int rows, chunk, wpr;
+    choose_shape(n_rows / unit_rows, unit_rows, V, rows, chunk, wpr);
+    return (size_t)n_rows * ((V + chunk - 1) / chunk * wpr) * sizeof(Part);
+}
+
+// The most records that n_rows rows of V columns or fewer can have, however they are cut into units.  Warps begin with kBaseCols
+// columns, or 2048 where eight share a row, and the last chunk's may have none.  They get fewer, kMinWarpCols at least, only
+// while the CTAs do not fill the SMs twice, so then there are fewer than 4 CTAs per SM, of rows x warps per row <= kRowsPerCta.
 size_t confidence_logits_workspace(int64_t n_rows, int V) {
-    // a chunk holds at least kMinWarpCols columns per warp
-    const int64_t n_split = (V + kMinWarpCols - 1) / kMinWarpCols + kMaxChunk / kMinWarpCols;
-    return ((size_t)n_rows * n_split * sizeof(Part) + 255) / 256 * 256;
+    const int64_t wide = n_rows * (V / (kMaxChunk / kWarps) + 1 + kWarps);
+    const int64_t narrow = n_rows * ((V + kMinWarpCols - 1) / kMinWarpCols + kWarps), few = 4 * (int64_t)sm_count() * kRowsPerCta;
+    const int64_t spread = narrow < few ? narrow : few;
+    return ((size_t)(wide > spread ? wide : spread) * sizeof(Part) + 255) / 256 * 256;
 }
 
 int launch_confidence_logits(const void* logits, int dtype, int64_t row_stride, int B, int D, int M, int V,
@@ -484,7 +498,7 @@ int launch_confidence_logits(const void* logits, int dtype, int64_t row_stride, 
     a.rows_per_bias = (int)(n_rows / (e.bias ? e.bias_rows : 1));
     a.rows_per_allow = (int)(n_rows / (e.allow ? e.allow_rows : 1));
     a.words = (V + 31) / 32;
-    a.unit_rows = e.bias ? gcd_int(M, a.rows_per_bias) : M;
+    a.unit_rows = rows_per_unit(n_rows, M, e.bias ? e.bias_rows : 0);
     choose_shape(n_rows / a.unit_rows, a.unit_rows, V, a.rows_per_cta, a.chunk, a.wpr);
     a.slices = (a.unit_rows + a.rows_per_cta - 1) / a.rows_per_cta;
     const int64_t units = n_rows / a.unit_rows * a.slices;

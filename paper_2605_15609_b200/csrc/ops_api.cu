@@ -150,7 +150,7 @@ int psd_confidence_logits(const void* logits, int32_t dtype, int64_t row_stride,
         !aligned(e.history_len, 4) || !aligned(e.draft_tokens, 4) || !aligned(e.draft_mask, 4) || !aligned(e.bias, 4) ||
         !aligned(e.allow, 4))
         return PSD_ERR_ALIGN;
-    if (workspace_bytes < confidence_logits_workspace(n_rows, V)) return PSD_ERR_WORKSPACE;
+    if (workspace_bytes < confidence_logits_needs(n_rows, M, V, e.bias ? e.bias_rows : 0)) return PSD_ERR_WORKSPACE;
     return launch_confidence_logits(logits, dtype, row_stride, B, D, M, V, e, out_token, out_conf, out_lse, workspace,
                                     status_dev, reinterpret_cast<cudaStream_t>(cuda_stream));
 }

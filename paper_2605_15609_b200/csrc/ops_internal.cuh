@@ -31,6 +31,7 @@ int launch_prefix_evict(const float* scores, const void* k, const void* v, const
 int launch_confidence_logits(const void* logits, int dtype, int64_t row_stride, int B, int D, int M, int V,
                              const psd_logits_edit_t& e, int32_t* out_token, float* out_conf, float* out_lse,
                              void* workspace, int32_t* status_dev, cudaStream_t st);
+size_t confidence_logits_needs(int64_t n_rows, int M, int V, int bias_rows);      // bias_rows 0: no bias
 size_t confidence_logits_workspace(int64_t n_rows, int V);
 
 }  // namespace psd

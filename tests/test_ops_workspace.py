@@ -54,3 +54,9 @@ def test_sizes_stay_near_what_is_used():
     assert psd.psd_attention_workspace_bytes(16, 8, 64, 32, 8, 128, 8192, 64) <= 148 * 256 * 129 * 4 + 256
     assert psd.psd_weights_workspace_bytes(16, 8, 64, 32, 8, 128, 8192) <= 148 * 256 * 4 + 256
     assert psd.psd_attention_workspace_bytes(1, 4, 32, 4, 4, 64, 257, 32) == 256
+
+
+def test_logits_workspace_stays_near_what_is_used():
+    """One record of 16 bytes per row and warp: 31 warps of 4096 columns for a row of 126464 in a large batch (it was 558 records)."""
+    assert psd.psd_logits_workspace_bytes(8192, 126464) <= 8192 * 3 * 31 * 16
+    assert psd.psd_logits_workspace_bytes(1, 126464) <= 558 * 16 + 256
