@@ -534,6 +534,16 @@ size_t psd_attention_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t Hq
                                      int32_t S);
 
 /*
+ * Names of the kernels that psd_draft_attention launches at these sizes (static storage; NULL = bad sizes):
+ * "draft_attention_kernel" (one kernel walks the prefix and the own keys), "prefix_attention_kernel" (the drafts' own
+ * keys follow an unsplit prefix), or "prefix_attention_kernel+draft_attention_kernel" (partial results over the prefix,
+ * then the own keys and the join).  splits, if not NULL, receives the partial results per row (0 in the first form).
+ * For reports: it computes nothing.
+ */
+const char* psd_attention_kernel_names(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P,
+                                       int32_t S, int32_t* splits);
+
+/*
  * psd_draft_attention — attention of all drafts' tokens over the shared prefix, read once for all of a
  * sequence's drafts, and over each draft's own keys.
  * For token t = (b, d, i) and head h, over the keys K_j = prefix keys j < prefix_len[b] of sequence b and

@@ -14,7 +14,7 @@ from .binding import (ACCEPT_AGREE_AND_CONF, ACCEPT_AGREE_AND_POLICY, ACCEPT_AGR
                       table_body_address, table_body_user, psd_table_body, PsdDag, psd_dag_init,
                       psd_build_drafts_dag, psd_verify_accept_dag, psd_step_dag, PsdDecodeStats, PsdTableBody, ORDER_TWO_PASSES,
                       ORDER_ONE_PASS, PSD_BF16, PSD_FP16, PSD_FP32, PsdAttention, PsdEvict, PsdKvStrides, PsdLogitsEdit,
-                      psd_attention_workspace_bytes, psd_draft_attention, psd_weights_workspace_bytes, psd_prefix_weights,
+                      psd_attention_workspace_bytes, psd_attention_kernel_names, psd_draft_attention, psd_weights_workspace_bytes, psd_prefix_weights,
                       psd_prefix_evict, psd_logits_workspace_bytes, psd_confidence_logits)
 
 __all__ = [n for n in dir() if not n.startswith("_")]

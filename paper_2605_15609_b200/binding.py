@@ -152,6 +152,8 @@ def _load() -> ctypes.CDLL:
     lib.psd_table_body.argtypes = [_vp, _vp, _vp, _i32, _i32, _vp, _vp]
     lib.psd_attention_workspace_bytes.restype = _sz
     lib.psd_attention_workspace_bytes.argtypes = [_i32] * 8
+    lib.psd_attention_kernel_names.restype = ctypes.c_char_p
+    lib.psd_attention_kernel_names.argtypes = [_i32] * 8 + [_vp]
     lib.psd_draft_attention.restype = ctypes.c_int
     lib.psd_draft_attention.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp,
                                         _sz, _vp, _vp]
@@ -611,6 +613,13 @@ def _one_type(dt, *tensors):
 
 def psd_attention_workspace_bytes(B, D, M, Hq, Hkv, Dh, P, S) -> int:
     return int(LIB.psd_attention_workspace_bytes(B, D, M, Hq, Hkv, Dh, P, S))
+
+
+def psd_attention_kernel_names(B, D, M, Hq, Hkv, Dh, P, S):
+    """(names of the kernels that psd_draft_attention launches at these sizes, partial results per row), or None."""
+    splits = _i32(0)
+    names = LIB.psd_attention_kernel_names(B, D, M, Hq, Hkv, Dh, P, S, ctypes.byref(splits))
+    return None if names is None else (names.decode(), splits.value)
 
 
 def psd_draft_attention(q, k_prefix, v_prefix, out, lse=None, k_own=None, v_own=None, prefix_len=None, own_len=None,

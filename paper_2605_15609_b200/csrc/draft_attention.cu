@@ -431,6 +431,16 @@ size_t draft_attention_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, i
     return all > here ? all : here;
 }
 
+const char* draft_attention_kernels(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S, int32_t* splits) {
+    if (one_launch(B, D, M, Hq, Hkv, Dh, P)) {
+        if (splits) *splits = 0;
+        return "draft_attention_kernel";
+    }
+    const PrefixPlan p = plan_prefix(B, D, M, Hq, Hkv, Dh, P, S);
+    if (splits) *splits = p.splits;
+    return p.fused ? "prefix_attention_kernel" : "prefix_attention_kernel+draft_attention_kernel";
+}
+
 int launch_draft_attention(const void* q, const void* k_prefix, const void* v_prefix, const int32_t* prefix_len,
                            const void* k_own, const void* v_own, const int32_t* own_len, const psd_attention_t& a,
                            void* out, float* lse, void* workspace, int32_t* status_dev, cudaStream_t st) {

@@ -59,6 +59,12 @@ size_t psd_attention_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t Hq
     return draft_attention_workspace(B, D, M, Hq, Hkv, Dh, P, S);
 }
 
+const char* psd_attention_kernel_names(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P, int32_t S,
+                                       int32_t* splits) {
+    if (!attention_sizes_ok(B, D, M, Hq, Hkv, Dh, P, S)) return nullptr;
+    return draft_attention_kernels(B, D, M, Hq, Hkv, Dh, P, S, splits);
+}
+
 int psd_draft_attention(const void* q, const void* k_prefix, const void* v_prefix, const int32_t* prefix_len,
                         const void* k_own, const void* v_own, const int32_t* own_len, const psd_attention_t* a,
                         void* out, float* lse, void* workspace, size_t workspace_bytes, int32_t* status_dev,

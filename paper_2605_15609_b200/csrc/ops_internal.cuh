@@ -11,6 +11,7 @@ namespace psd {
 int launch_draft_attention(const void* q, const void* k_prefix, const void* v_prefix, const int32_t* prefix_len,
                            const void* k_own, const void* v_own, const int32_t* own_len, const psd_attention_t& a,
                            void* out, float* lse, void* workspace, int32_t* status_dev, cudaStream_t st);
+const char* draft_attention_kernels(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S, int32_t* splits);
 // bytes that a call writes, and what the public size function answers: that of this and of all smaller batches
 size_t draft_attention_needs(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S);
 size_t draft_attention_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S);
