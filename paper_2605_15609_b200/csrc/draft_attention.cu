@@ -373,10 +373,22 @@ int row_blocks_per_cta(int64_t nodes_heads, int rows) {
 
 // Whether this kernel walks the prefix too, in one launch: it reads the prefix once per draft instead of once per sequence, but
 // saves a launch and the join.  It does while a wave of its CTAs (three per SM) has few tiles of 64 keys to walk: measured, one
-// launch against two, 4 drafts of 32 tokens: 4 heads of 64, prefix 257: 7 against 15 us, 1024: 13 against 16, 2048: 22 against
-// 16; 32 heads of 128 over 8 key heads, prefix 257: 13 against 16 us, 512: 17 against 20, 1024: 27 against 22.
+// launch against two, 4 drafts of 32 tokens: 4 heads of 64, prefix 257: 7 against 15 us, 1024: 14 against 17, 1536: 18 against
+// 17, 2048: 23 against 17; 32 heads of 128 over 8 key heads, prefix 257: 14 against 16 us, 512: 18 against 20, 768: 24 against 22;
+// the same heads, drafts of 2 tokens, 257: 11 against 14, 512: 14 against 14, 1024: 24 against 15; 16 sequences of one token, 512:
+// 14 against 17, 1024: 24 against 22.
+// Where the tensor-core kernel can take the own keys as well, it is one launch too and wins with rows for a third of the SMs (a CTA
+// has up to 256; 8 sequences of 8 drafts of 4 tokens, 16 heads of 128 over 2, prefix 257, 16 CTAs: 24 against 14 us): 32 heads of 128 over 8, 4
+// drafts of 32 tokens, prefix 128: 4 sequences 13 against 26 us, 16 sequences 28 against 63, 32 sequences 50 against 109; 8
+// sequences, 32 heads of 64 over 4, prefix 512: 17 against 50.  It then loses only while the prefix is short and its tiles hold
+// several drafts, each a tile of own keys: 5 sequences of 4 drafts of 33 tokens, 16 heads of 64, prefix 64: 17 against 11, 257: 21
+// against 19, 512: 22 against 25, heads of 128, prefix 64: 18 against 17, 128: 18 against 20, 257: 23 against 30.
 int one_launch_tiles(int Dh) { return Dh <= 64 ? 16 : 8; }
-bool one_launch(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
+bool one_launch(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
+    const PrefixPlan plan = plan_prefix(B, D, M, Hq, Hkv, Dh, P, S);
+    if (P > 0 && plan.fused && 3 * (int64_t)B * Hkv * plan.units >= sm_count() &&
+        (P > (Dh <= 64 ? 320 : 128) || drafts_per_tile(M, plan.tq) < 4))
+        return false;
     const int rows = M * (Hq / Hkv);
     const int64_t nh = (int64_t)B * D * Hkv;
     const int r = 16 * row_blocks_per_cta(nh, rows);
@@ -399,7 +411,7 @@ int launch_dh(OwnArgs& p, cudaStream_t st) {
 static size_t partial_bytes(int64_t rows, int dhp) { return rows == 0 ? 256 : ((size_t)rows * (dhp + 1) * 4 + 255) / 256 * 256; }
 
 size_t draft_attention_needs(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
-    if (one_launch(B, D, M, Hq, Hkv, Dh, P)) return 256;
+    if (one_launch(B, D, M, Hq, Hkv, Dh, P, S)) return 256;
     const PrefixPlan p = plan_prefix(B, D, M, Hq, Hkv, Dh, P, S);
     return partial_bytes(p.fused ? 0 : (int64_t)B * D * M * Hq * p.splits, p.dhp);
 }
@@ -411,7 +423,7 @@ size_t draft_attention_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, i
     const int64_t sms = sm_count(), G = Hq / Hkv, tq = 128 / G, T = (int64_t)D * M, tiles = (P + 127) / 128;
     const int64_t once = 2 * sms * tq * G, rows = (int64_t)B * T * Hq;
     const int dhp = Dh <= 64 ? 64 : 128;
-    // One launch at every smaller size: smaller batches use smaller blocks of rows, but then at most 4 CTAs per SM, two waves.
+    // One launch (or no partial results) at every smaller size: smaller batches use smaller blocks of rows, but then at most 4 CTAs per SM, two waves.
     const int most = M * (int)G > 32 ? 64 : M * (int)G > 16 ? 32 : 16;
     const int64_t ctas = (int64_t)B * D * Hkv * ((M * G + most - 1) / most), waves = (ctas + 3 * sms - 1) / (3 * sms);
     if ((waves < 2 ? 2 : waves) * ((P + kKeys - 1) / kKeys) <= one_launch_tiles(Dh)) return 256;
@@ -432,7 +444,7 @@ size_t draft_attention_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, i
 }
 
 const char* draft_attention_kernels(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S, int32_t* splits) {
-    if (one_launch(B, D, M, Hq, Hkv, Dh, P)) {
+    if (one_launch(B, D, M, Hq, Hkv, Dh, P, S)) {
         if (splits) *splits = 0;
         return "draft_attention_kernel";
     }
@@ -445,7 +457,7 @@ int launch_draft_attention(const void* q, const void* k_prefix, const void* v_pr
                            const void* k_own, const void* v_own, const int32_t* own_len, const psd_attention_t& a,
                            void* out, float* lse, void* workspace, int32_t* status_dev, cudaStream_t st) {
     OwnArgs p = {q, k_prefix, v_prefix, k_own, v_own, prefix_len, own_len, out, lse, a, 0, 1, nullptr, nullptr, 0, 0};
-    if (!one_launch(a.B, a.D, a.M, a.Hq, a.Hkv, a.Dh, a.P)) {
+    if (!one_launch(a.B, a.D, a.M, a.Hq, a.Hkv, a.Dh, a.P, a.S)) {
         const PrefixPlan plan = plan_prefix(a.B, a.D, a.M, a.Hq, a.Hkv, a.Dh, a.P, a.S);
         p.rows = (int64_t)a.B * a.D * a.M * a.Hq;
         float* po = reinterpret_cast<float*>(workspace);

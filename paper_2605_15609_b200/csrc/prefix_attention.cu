@@ -517,11 +517,16 @@ int launch_p(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv
 
 }  // namespace
 
+int drafts_per_tile(int M, int tq) { return (tq + M - 2) / M + 1; }
+
 // Own keys in the same kernel: when nothing is split (one result per row) and the drafts of a query tile are few.  A draft
-// costs a tile however few keys it has: with a tile of 32 single-token drafts the kernel of their own is the cheaper way.
+// costs a tile however few keys it has, which a kernel of their own does not.  Measured, 32 own keys, in this kernel against two: 16
+// sequences of 16 drafts, 32 heads of 128 over 8, prefix 1024, 3 drafts to a tile 116 against 198 us, 5: 71 against 111, 9: 47
+// against 61, 12: 50 against 56; 32 drafts, 16 heads of 64, prefix 2048, 5: 304 against 423, 9: 209 against 229, prefix 1024, 10: 170
+// against 170, 12: 177 against 158.
 bool fuses_own(int M, int tq, int S) {
-    const int drafts = (tq + M - 2) / M + 1;
-    return (int64_t)drafts * ((S + 127) / 128) <= kMaxOwnTiles && drafts <= 5;
+    const int drafts = drafts_per_tile(M, tq);
+    return (int64_t)drafts * ((S + 127) / 128) <= kMaxOwnTiles && drafts <= 9;
 }
 
 // How the prefix's keys are split.  A CTA takes two query tiles (or the only one twice, over two ranges of keys); when

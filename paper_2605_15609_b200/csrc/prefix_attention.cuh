@@ -15,6 +15,7 @@ struct PrefixPlan {
     int dhp;       // floats per partial output row: 64 or 128
     bool fused;    // the kernel takes the own keys too and writes final outputs (splits == 1)
 };
+int drafts_per_tile(int M, int tq);     // drafts of M tokens that a query tile of tq tokens meets at most
 bool fuses_own(int M, int tq, int S);   // whether a query tile's own keys can follow an unsplit prefix in the same kernel
 PrefixPlan plan_prefix(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S);
 

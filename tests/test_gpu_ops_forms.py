@@ -259,3 +259,28 @@ def test_offsets_past_32_bits_under_a_tensor_map(far):
 def test_kernel_names():
     assert psd.psd_attention_kernel_names(0, 1, 1, 1, 1, 8, 1, 1) is None
     assert psd.psd_attention_kernel_names(1, 1, 1, 1, 1, 8, 0, 1) == (ONE, 0)
+
+
+@pytest.mark.parametrize("P", [1, 30, 100, 128, 130])
+@pytest.mark.parametrize("shape", [(16, 4, 32, 32, 8, 128, 32), (8, 4, 32, 32, 4, 64, 20), (16, 16, 4, 32, 8, 128, 4), (12, 9, 16, 8, 8, 64, 3)])
+def test_own_keys_behind_a_short_unsplit_prefix(shape, P):
+    """Prefixes shorter than a tile of keys, up to nine drafts to a tile."""
+    drafts = (128 // (shape[3] // shape[4]) + shape[2] - 2) // shape[2] + 1
+    shape = (*shape[:6], P + 321 if drafts > 3 else P, shape[6])           # (several drafts to a tile: from longer prefixes on)
+    assert _form(shape) == (FUSED, 1)
+    for causal in (False, True):
+        c = _attention_case(*shape, "bf16", seed=P + causal)
+        _check(_run_attention(*c, 0.2, causal), c, 0.2, causal, "bf16")
+
+
+@pytest.mark.parametrize("shape", [(16, 16, 4, 32, 8, 128, 1024, 32), (8, 64, 2, 64, 8, 128, 1024, 2), (16, 32, 16, 16, 16, 64, 700, 16)])
+def test_nine_drafts_to_a_tile(shape):
+    assert _form(shape) == (FUSED, 1)
+    q, kp, vp, ko, vo, plen, olen = c = _attention_case(*shape, "fp16", seed=5)
+    a = _run_attention(*c, 0.2, True)
+    _check(a, c, 0.2, True, "fp16")
+    ko2, vo2 = ko.clone(), vo.clone()
+    ko2[9], vo2[9] = float("nan"), float("nan")
+    b = _run_attention(q, kp, vp, ko2, vo2, plen, olen, 0.2, True)
+    others = [n for n in range(q.shape[0]) if n != 9]
+    assert torch.equal(a[0][others], b[0][others]) and torch.equal(a[1][others], b[1][others])
