@@ -630,7 +630,8 @@ size_t psd_logits_workspace_bytes(int32_t n_rows, int32_t V);
  *   x = x + bias;   tokens whose allow bit is 0 drop out, whatever their logit holds.
  * out_token, out_conf, out_lse are those of psd_confidence over x.  A row in which no token is left (or all that are left
  * have x = -inf) gives token -1, confidence 0 and lse -inf; it is not counted as non-finite, and psd_select_unmask,
- * psd_build_drafts and psd_verify_accept take its slot for one without a token: it stays masked.  A NaN or +inf among the tokens left gives confidence NaN and is counted in status_dev.
+ * psd_build_drafts and psd_verify_accept take its slot for one without a token: it stays masked.  A NaN or +inf among the tokens left gives confidence NaN and is counted in status_dev (the token is then
+ * that of the largest value that is no NaN, -1 if there is none above -inf).
  *   logits [B*D*M, V] bf16, fp16 or fp32 (dtype), rows row_stride >= V elements apart, aligned to their element;
  *     B*D*M and V at most 2^30
  *   edit: HOST pointer, NULL = no edits;  workspace >= psd_logits_workspace_bytes(B*D*M, V), 256-byte aligned

@@ -25,8 +25,7 @@ __device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, u
 }
 
 // A bounded wait of a whole warp: every lane gets the same answer, so that warp-wide instructions may follow.  The loop must
-// not be unrolled: 256 tries in a row at every wait made 137 KB of code out of the prefix attention's kernel, more than the
-// instruction caches hold, and the code between two waits was then fetched from L2 every time.
+// not be unrolled: hundreds of tries in a row at every wait would make most of a kernel's code out of waits.
 __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, const WaitCtx& w) {
     bool r = mbar_try_wait(bar, parity);
     if (!r) {

@@ -23,8 +23,9 @@
 // draft_attention_kernel, which takes the own keys and joins.
 //
 // Bound, for Dh = 128, by products and exponentials alike (2048 cycles each per 256 rows x 128 keys); measured 3500 cycles, the
-// chain scores -> softmax -> weights -> product of a stream: 16 sequences x 8 key heads x 2048 rows over up to 8192 keys (668
-// GFLOP) in 601 us, 1.1 PFLOP/s, where the board's power limit already holds the clock at 1840-1900 MHz.
+// chain scores -> softmax -> weights -> product of a stream: 16 sequences x 8 key heads x 2048 rows over up to 8192 keys (mean 0.63
+// of that, 705 GFLOP) in 705 us, 1.0 PFLOP/s (0.96-1.0 over seeds of mean 0.56-0.66, 635-760 us), where the board's power limit
+// already holds the clock at 1840-1900 MHz.
 //
 // Keys past the prefix's end are masked in the scores, and their V rows are zeroed in shared memory before the product,
 // since 0 * NaN would spoil a row.
