@@ -641,6 +641,125 @@ int psd_confidence_logits(const void* logits, int32_t dtype, int64_t row_stride,
                           void* workspace, size_t workspace_bytes, int32_t* status_dev, void* cuda_stream);
 
 /*
+ * ---- A step in 8 bits: rotation, the prefix's cache and the LM head in codes -----------------------------
+ *
+ * CODES are int8 numbers from -127 to 127 that stand for code * scale.  One scale serves a row of a matrix, or the
+ * tokens of a block of one key head in a cache.  Over a unit x of numbers, in fp32, each operation rounded on its own:
+ *   scale = max(max |x| * fp32(1/127), 2^-126),   r = 1 / scale,   code = rint(x * r)      (ties to even).
+ * A unit that holds a NaN or an infinity gets the scale NaN and codes 0.  Scales made elsewhere are >= 0 (or NaN).
+ */
+
+/* How psd_rope_frequencies scales a context of `original` tokens by `factor`. */
+#define PSD_ROPE_PLAIN 0     /* f[j] = base^(-2j/rotary)                                                              */
+#define PSD_ROPE_LINEAR 1    /* f[j] / factor                                                                         */
+#define PSD_ROPE_STRETCHED 2 /* base * factor^(rotary / (rotary - 2)) in place of base (rotary > 2)                   */
+#define PSD_ROPE_BY_PARTS 3  /* with n = original * f[j] / 2 pi turns over the original context and
+                                w = clamp((n - low) / (high - low), 0, 1):  w * f[j] + (1 - w) * f[j] / factor        */
+
+/*
+ * psd_rope_frequencies — the table that psd_rotate_qk reads, computed on the host in 64 bits.
+ *   rotary even, 2 .. 128;  base > 1;  factor >= 1;  BY_PARTS: original >= 1, 0 <= low < high (others do not read them)
+ *   frequency [rotary/2] HOST out, radians per position;  gain HOST out or NULL: 1, BY_PARTS 0.1 ln(factor) + 1
+ */
+int psd_rope_frequencies(int32_t rotary, double base, int32_t kind, double factor, double original, double low, double high,
+                         double* frequency, float* gain);
+
+/* Shapes of psd_rotate_qk. */
+typedef struct psd_rotate_t {
+    int32_t n_tokens;     /* T >= 1                                                                          */
+    int32_t Hq, Hkv, Dh;  /* heads, >= 0, not both 0 (0: q, or k and v, are not read); 8 <= Dh <= 128, Dh % 8 == 0 */
+    int32_t dtype;        /* PSD_BF16 or PSD_FP16: q, k, v, weights and outputs                               */
+    int32_t rotary;       /* the first `rotary` numbers of a head are rotated: even, 0 .. Dh                  */
+    int32_t interleaved;  /* pairs: 0 (j, j + rotary/2), 1 (2j, 2j + 1)                                       */
+    int32_t n_slots;      /* with slots: rows of k_out and v_out                                              */
+    float eps;            /* > 0, finite */
+    float gain;           /* > 0, finite: factor of sines and cosines */
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head;                         /* element strides, > 0 */
+    int64_t q_out_token, q_out_head, k_out_token, k_out_head, v_out_token, v_out_head;
+} psd_rotate_t;
+
+/*
+ * psd_rotate_qk — norms of queries and keys for each head, their position rotation, and the filing of keys and values in a
+ * cache, in one pass.  For token t and a head x of q (of k):
+ *   y = x * w / sqrt(mean(x^2) + eps) with w = q_norm (k_norm), or y = x where that is NULL;
+ *   (z_a, z_b) = gain * (y_a cos u - y_b sin u, y_b cos u + y_a sin u),  u = position[t] * frequency[j],
+ * for the pairs (a, b) of the first `rotary` numbers; the others are y.  fp32 (the angles 64 bits), rounded once.
+ *   q [T, Hq, Dh] -> q_out;  k [T, Hkv, Dh] -> k_out[at];  v [T, Hkv, Dh] (NULL: none) -> v_out[at] unchanged
+ *   at = t, or slot[t] ([T] int32, device): tokens whose slot lies outside [0, n_slots) are not filed.  No slot is named
+ *   twice in a call.  Rows of k_out and v_out that no token names are left as they are.
+ *   position [T] int32 (any value), frequency [rotary/2] fp64, device; rotary = 0: both may be NULL
+ *   q_norm, k_norm [Dh] or NULL.  Outputs are the inputs themselves (same strides, no slots) or do not overlap them.
+ *   pointers 16-byte aligned (position, slot 4, frequency 8), strides multiples of 8 elements (PSD_ERR_ALIGN)
+ */
+int psd_rotate_qk(const void* q, const void* k, const void* v, const int32_t* position, const double* frequency,
+                  const void* q_norm, const void* k_norm, const int32_t* slot, const psd_rotate_t* r, void* q_out, void* k_out,
+                  void* v_out, void* cuda_stream);
+
+/*
+ * psd_quantize_rows — codes [n_rows, H] and scale [n_rows] of the rows of x [n_rows, H] (bf16 or fp16), one scale a row:
+ * an LM head for psd_confidence_q8, for instance.
+ *   H >= 8, H % 8 == 0;  row_stride >= H elements, code_stride >= H, both multiples of 8;  x 16-byte, codes 8-byte aligned
+ */
+int psd_quantize_rows(const void* x, int32_t dtype, int64_t row_stride, int64_t n_rows, int32_t H, int8_t* codes,
+                      int64_t code_stride, float* scale, void* cuda_stream);
+
+/* Shapes of psd_prefix_quantize. */
+typedef struct psd_quantize_t {
+    int32_t B, Hkv, Dh;               /* 8 <= Dh <= 128, Dh % 8 == 0                                              */
+    int32_t P;                        /* capacity of the caches, 1 .. 2^30                                        */
+    int32_t block;                    /* tokens per scale: 16, 32, 64 or 128                                      */
+    int32_t dtype;                    /* PSD_BF16 or PSD_FP16: k, v                                               */
+    int32_t span;                     /* end - begin at most (the host's bound, for the launch); 0 = P             */
+    int32_t reserved;                 /* 0 */
+    psd_kv_strides_t k, v;            /* [B, P, Hkv, Dh], elements                                                */
+    psd_kv_strides_t k_codes, v_codes; /* [B, P, Hkv, Dh], bytes; no stride 0 where the dimension is more than one */
+} psd_quantize_t;
+
+/*
+ * psd_prefix_quantize — tokens begin[b] .. end[b] - 1 of a prefix's keys and values enter its 8-bit cache.
+ * One scale serves block j (tokens j * block .. (j + 1) * block - 1) of a key head, over the tokens of the block below
+ * end[b]; a range that begins inside a block codes that block again from its first token, which k and v must still hold.
+ *   begin, end [B] int32, device, clamped to [0, P]; NULL: 0, P.  end is cut to begin + span.  begin >= end: nothing.
+ *   k_scale, v_scale [B, Hkv, ceil(P / block)] fp32.  Blocks without tokens of the range, and codes from end[b] on,
+ *   are left as they are; what k and v hold there is not read.
+ *   k, v 16-byte aligned, strides multiples of 8; codes 8-byte aligned, strides multiples of 8
+ */
+int psd_prefix_quantize(const void* k, const void* v, const int32_t* begin, const int32_t* end, const psd_quantize_t* q,
+                        int8_t* k_codes, int8_t* v_codes, float* k_scale, float* v_scale, void* cuda_stream);
+
+/* Bytes of scratch psd_draft_attention_q8 needs (0 = bad sizes); grows with B, D, P and S and serves calls with smaller ones. */
+size_t psd_attention_q8_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P, int32_t S);
+
+/*
+ * psd_draft_attention_q8 — psd_draft_attention with a prefix in codes: key j of the prefix is k_codes[b, j, h] *
+ * k_scale[b, h, j / block], and so are the values; the drafts' own keys and values are 16-bit as there.
+ *   block 16, 32, 64 or 128;  Dh % 16 == 0;  a->kp, a->vp are in bytes, multiples of 16;  codes 16-byte aligned
+ *   k_scale, v_scale [B, Hkv, ceil(P / block)] fp32; neither codes nor scales past a length are used.  A scale NaN makes
+ *   the outputs that draw on its block NaN.  Scores, statistics and sums are fp32, weights over the prefix are rounded to
+ *   fp16 (none is off by more than 2^-30 of the row's largest beside that), the codes enter exactly.
+ *   Other arguments as for psd_draft_attention.
+ */
+int psd_draft_attention_q8(const void* q, const int8_t* k_codes, const int8_t* v_codes, const float* k_scale,
+                           const float* v_scale, int32_t block, const int32_t* prefix_len, const void* k_own,
+                           const void* v_own, const int32_t* own_len, const psd_attention_t* a, void* out, float* lse,
+                           void* workspace, size_t workspace_bytes, int32_t* status_dev, void* cuda_stream);
+
+/* Bytes of scratch psd_confidence_q8 needs (0 = bad sizes); grows with n_rows, H and V. */
+size_t psd_confidence_q8_workspace_bytes(int32_t n_rows, int32_t H, int32_t V);
+
+/*
+ * psd_confidence_q8 — psd_confidence over an LM head in codes.  The hidden rows [n_rows, H] (bf16 or fp16) are coded as
+ * psd_quantize_rows does; with n = sum_j x_code[r,j] * w_code[v,j] (exact),
+ *   l[r,v] = fp32(fp32(fp32(n) * w_scale[v]) * x_scale[r]),
+ * and token, confidence and lse are those of psd_confidence over l (the lowest v among equal l).
+ *   H % 64 == 0, H <= 131072;  hidden, w_codes [V, H] 16-byte aligned;  w_scale [V] fp32
+ *   workspace 256-byte aligned;  status_dev as for psd_confidence: counts the rows without a finite confidence
+ */
+int psd_confidence_q8(const void* hidden, int32_t dtype, const int8_t* w_codes, const float* w_scale, int32_t n_rows, int32_t H,
+                      int32_t V, int32_t* out_token, float* out_conf, float* out_lse, void* workspace, size_t workspace_bytes,
+                      int32_t* status_dev, void* cuda_stream);
+
+/*
  * Which kernel psd_confidence uses.  Process-wide; returns the previous value, or PSD_ERR_SHAPE for
  * an unknown value.
  *   0  (default) the tcgen05/TMA kernels, chosen by size: pairs of CTAs on one tile of 256 rows

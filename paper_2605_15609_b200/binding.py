@@ -16,7 +16,7 @@ import torch
 
 from . import build as _build
 
-_i32, _i64, _f32, _vp, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t
+_i32, _i64, _f32, _f64, _vp, _sz = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_double, ctypes.c_void_p, ctypes.c_size_t
 
 PSD_OK = 0
 PSD_ERR_NULL, PSD_ERR_SHAPE, PSD_ERR_ALIGN, PSD_ERR_WORKSPACE = -1, -2, -3, -4
@@ -78,6 +78,19 @@ class PsdLogitsEdit(ctypes.Structure):
     _fields_ = [*[(n, _vp) for n in ("history", "history_len", "draft_tokens", "draft_mask", "bias", "allow")],
                 *[(n, _i32) for n in ("history_cap", "bias_rows", "allow_rows")],
                 *[(n, _f32) for n in ("repetition", "presence", "frequency")], ("reserved", _i32)]
+
+
+class PsdRotate(ctypes.Structure):
+    """psd_rotate_t"""
+    _fields_ = [*[(n, _i32) for n in ("n_tokens", "Hq", "Hkv", "Dh", "dtype", "rotary", "interleaved", "n_slots")],
+                ("eps", _f32), ("gain", _f32),
+                *[(f"{n}_{d}", _i64) for n in ("q", "k", "v", "q_out", "k_out", "v_out") for d in ("token", "head")]]
+
+
+class PsdQuantize(ctypes.Structure):
+    """psd_quantize_t"""
+    _fields_ = [*[(n, _i32) for n in ("B", "Hkv", "Dh", "P", "block", "dtype", "span", "reserved")],
+                *[(n, PsdKvStrides) for n in ("k", "v", "k_codes", "v_codes")]]
 
 
 # psd_body_fn
@@ -169,6 +182,22 @@ def _load() -> ctypes.CDLL:
     lib.psd_confidence_logits.restype = ctypes.c_int
     lib.psd_confidence_logits.argtypes = [_vp, _i32, _i64, _i32, _i32, _i32, _i32, _vp, _vp,
                                           _vp, _vp, _vp, _sz, _vp, _vp]
+    lib.psd_rope_frequencies.restype = ctypes.c_int
+    lib.psd_rope_frequencies.argtypes = [_i32, _f64, _i32, _f64, _f64, _f64, _f64, _vp, _vp]
+    lib.psd_rotate_qk.restype = ctypes.c_int
+    lib.psd_rotate_qk.argtypes = [_vp] * 13
+    lib.psd_quantize_rows.restype = ctypes.c_int
+    lib.psd_quantize_rows.argtypes = [_vp, _i32, _i64, _i64, _i32, _vp, _i64, _vp, _vp]
+    lib.psd_prefix_quantize.restype = ctypes.c_int
+    lib.psd_prefix_quantize.argtypes = [_vp] * 10
+    lib.psd_attention_q8_workspace_bytes.restype = _sz
+    lib.psd_attention_q8_workspace_bytes.argtypes = [_i32] * 8
+    lib.psd_draft_attention_q8.restype = ctypes.c_int
+    lib.psd_draft_attention_q8.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
+    lib.psd_confidence_q8_workspace_bytes.restype = _sz
+    lib.psd_confidence_q8_workspace_bytes.argtypes = [_i32] * 3
+    lib.psd_confidence_q8.restype = ctypes.c_int
+    lib.psd_confidence_q8.argtypes = [_vp, _i32, _vp, _vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
     lib.psd_set_confidence_impl.restype = ctypes.c_int
     lib.psd_set_confidence_impl.argtypes = [ctypes.c_int]
     lib.psd_set_tuning.restype = ctypes.c_int
@@ -741,3 +770,171 @@ def psd_confidence_logits(logits, out_token, out_conf, out_lse=None, B=None, D=1
                                      _want_n(out_token, R, _I32, "out_token"), _want_n(out_conf, R, _F32, "out_conf"),
                                      _want_n(out_lse, R, _F32, "out_lse"), ws, ws_bytes, _ptr(status), stream),
            "psd_confidence_logits")
+
+
+# ---- a step in 8 bits: rotation, the prefix's cache and the LM head in codes -----------------------------------------------
+
+PSD_ROPE_PLAIN, PSD_ROPE_LINEAR, PSD_ROPE_STRETCHED, PSD_ROPE_BY_PARTS = 0, 1, 2, 3
+_F64, _I8 = torch.float64, torch.int8
+_pack_rotate = struct.Struct("=8i2f12q").pack
+_pack_quantize = struct.Struct("=8i12q").pack
+
+
+def psd_rope_frequencies(rotary, base=10000.0, kind=PSD_ROPE_PLAIN, factor=1.0, original=0.0, low=1.0, high=32.0):
+    """(frequencies [rotary/2] float64 on the CPU, the gain that goes with them) for psd_rotate_qk."""
+    table, gain = torch.empty(max(int(rotary) // 2, 1), dtype=_F64), _f32(1.0)
+    _check(LIB.psd_rope_frequencies(int(rotary), float(base), int(kind), float(factor), float(original), float(low), float(high),
+                                    table.data_ptr(), ctypes.byref(gain)), "psd_rope_frequencies")
+    return table, gain.value
+
+
+def _heads_strides(t, name):
+    """(tokens, heads, token stride, head stride) of [T, H, Dh], or of [N, M, H, Dh] whose first two dimensions are one run."""
+    if t.dim() == 4:
+        N, M, H, Dh = t.shape
+        token, head = _tokens_strides(t, N, M, H, Dh, name)
+        return N * M, H, Dh, token, head
+    T, H, Dh = t.shape
+    st, sh, sd = t.stride()
+    if sd != 1 and Dh > 1:
+        raise ValueError(f"psd binding: {name} needs a dense last dimension")
+    return T, H, Dh, st if T > 1 else H * Dh, sh if H > 1 else Dh
+
+
+def psd_rotate_qk(q, k, q_out, k_out, position, frequency, v=None, v_out=None, slot=None, q_norm=None, k_norm=None, eps=1e-6,
+                  interleaved=False, gain=1.0, stream=None):
+    """Norms and position rotation of q [T, Hq, Dh] and k [T, Hkv, Dh] (or [N, M, H, Dh]; either may be None with its output)
+    into q_out and k_out, v into v_out; with ``slot`` [T] int32, token t of k and v goes to row slot[t].  ``frequency``
+    [rotary/2] float64 says how much of a head is rotated (None: nothing)."""
+    some = q if q is not None else k
+    T, Hq, Hkv, Dh, qs, ks, vs = 0, 0, 0, some.shape[-1], (8, 8, 8, 8), (8, 8, 8, 8), (8, 8, 8, 8)
+    n_slots = 0
+    if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (v is None) != (v_out is None):
+        raise ValueError("psd binding: q, k and v come with their outputs")
+    if q is not None:
+        T, Hq, _, a, b = _heads_strides(q, "q")
+        To, Ho, Do, c, d = _heads_strides(q_out, "q_out")
+        if (To, Ho, Do) != (T, Hq, Dh):
+            raise ValueError("psd binding: q_out has q's tokens and heads")
+        qs = (a, b, c, d)
+    for name, x, y in (("k", k, k_out), ("v", v, v_out)):
+        if x is None:
+            continue
+        Tx, H, Dx, a, b = _heads_strides(x, name)
+        To, Ho, Do, c, d = _heads_strides(y, name + "_out")
+        if name == "v" and (k is None or H != Hkv) or Dx != Dh or (q is not None or name == "v") and Tx != T or (Ho, Do) != (H, Dh):
+            raise ValueError("psd binding: q, k, v are [T, heads, Dh] of the same tokens; k and v, and their outputs, have the same heads")
+        T, Hkv = Tx, H
+        if slot is None and To != T:
+            raise ValueError(f"psd binding: {name}_out has {name}'s tokens where there are no slots")
+        if slot is not None:
+            if name == "v" and To != n_slots:
+                raise ValueError("psd binding: k_out and v_out have one number of slots")
+            n_slots = To
+        if name == "k":
+            ks = (a, b, c, d)
+        else:
+            vs = (a, b, c, d)
+    rotary = 0 if frequency is None else 2 * frequency.numel()
+    r = _pack_rotate(T, Hq, Hkv, Dh, _one_type(some.dtype, q, k, v, q_out, k_out, v_out, q_norm, k_norm), rotary,
+                     1 if interleaved else 0, n_slots, eps, gain, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], qs[2], qs[3], ks[2], ks[3],
+                     vs[2], vs[3])
+    stream = _here(stream, some, q, k, v, q_out, k_out, v_out, position, frequency, slot, q_norm, k_norm)
+    _check(LIB.psd_rotate_qk(None if q is None else q.data_ptr(), None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
+                             _want_n(position, T, _I32, "position"), _want_n(frequency, rotary // 2, _F64, "frequency"),
+                             _want(q_norm, (Dh,), some.dtype, "q_norm"), _want(k_norm, (Dh,), some.dtype, "k_norm"),
+                             _want_n(slot, T, _I32, "slot"), r, None if q is None else q_out.data_ptr(),
+                             None if k is None else k_out.data_ptr(), None if v is None else v_out.data_ptr(), stream), "psd_rotate_qk")
+
+
+def psd_quantize_rows(x, codes, scale, stream=None):
+    """Codes [R, H] int8 and scale [R] of the rows of x [R, H] (bf16 or fp16); rows may be strided."""
+    R, H = x.shape
+    if codes.shape != x.shape or codes.dtype is not _I8 or (x.stride(1) != 1 or codes.stride(1) != 1) and H > 1:
+        raise ValueError("psd binding: x [R, H] and codes [R, H] int8 need a dense last dimension")
+    stream = _here(stream, x, codes, scale)
+    _check(LIB.psd_quantize_rows(x.data_ptr(), _DTYPES.get(x.dtype, -1), x.stride(0) if R > 1 else H, R, H, codes.data_ptr(),
+                                 codes.stride(0) if R > 1 else H, _want(scale, (R,), _F32, "scale"), stream), "psd_quantize_rows")
+
+
+def psd_prefix_quantize(k, v, k_codes, v_codes, k_scale, v_scale, block=32, begin=None, end=None, span=0, stream=None):
+    """Tokens [begin[b], end[b]) of the caches k, v [B, P, Hkv, Dh] into codes [B, P, Hkv, Dh] int8 with scales
+    [B, Hkv, ceil(P / block)].  ``span``: the most tokens of any range, where the host knows (0: P)."""
+    cache = k.shape
+    B, P, Hkv, Dh = cache
+    if v.shape != cache or k_codes.shape != cache or v_codes.shape != cache or k_codes.dtype is not _I8 or v_codes.dtype is not _I8:
+        raise ValueError("psd binding: k, v and their codes (int8) are [B, P, Hkv, Dh]")
+    if block < 1:
+        raise ValueError("psd binding: block must be positive")
+    q = _pack_quantize(B, Hkv, Dh, P, block, _one_type(k.dtype, v), span, 0, *_pair_strides(k, v, B, P, Hkv, Dh, "k, v"),
+                       *_pair_strides(k_codes, v_codes, B, P, Hkv, Dh, "k_codes, v_codes"))
+    stream = _here(stream, k, v, k_codes, v_codes, k_scale, v_scale, begin, end)
+    sc = (B, Hkv, -(-P // block))
+    _check(LIB.psd_prefix_quantize(k.data_ptr(), v.data_ptr(), _want(begin, (B,), _I32, "begin"), _want(end, (B,), _I32, "end"), q,
+                                   k_codes.data_ptr(), v_codes.data_ptr(), _want(k_scale, sc, _F32, "k_scale"),
+                                   _want(v_scale, sc, _F32, "v_scale"), stream), "psd_prefix_quantize")
+
+
+def psd_attention_q8_workspace_bytes(B, D, M, Hq, Hkv, Dh, P, S) -> int:
+    return int(LIB.psd_attention_q8_workspace_bytes(B, D, M, Hq, Hkv, Dh, P, S))
+
+
+def _codes_strides(strides, no, nt, nh, nd, name):
+    """As _kv_strides, for codes: the smallest stride the library takes is 16."""
+    so, st, sh, sd = strides
+    if sd != 1 and nd > 1:
+        raise ValueError(f"psd binding: {name} needs a dense last dimension")
+    return so if no > 1 else 0, st if nt > 1 else 16, sh if nh > 1 else 0
+
+
+def psd_draft_attention_q8(q, k_codes, v_codes, k_scale, v_scale, out, lse=None, k_own=None, v_own=None, block=32, prefix_len=None,
+                           own_len=None, scale=None, causal=False, workspace=None, status=None, stream=None):
+    """psd_draft_attention over prefix caches in codes [B, P, Hkv, Dh] int8 with scales [B, Hkv, ceil(P / block)]."""
+    rows, cache = q.shape, k_codes.shape
+    N, M, Hq, Dh = rows
+    B, P, Hkv, dk = cache
+    if B < 1 or N % B or dk != Dh:
+        raise ValueError("psd binding: q [B*D, M, Hq, Dh] and k_codes [B, P, Hkv, Dh] do not belong together")
+    if v_codes.shape != cache or k_codes.dtype is not _I8 or v_codes.dtype is not _I8:
+        raise ValueError("psd binding: k_codes and v_codes are int8 of one shape")
+    if out.shape != rows or (k_own is None) != (v_own is None) or block < 1:
+        raise ValueError("psd binding: out and q have one shape, k_own and v_own come together, block is positive")
+    S, ko, vo, own = 0, None, None, _NO_CACHE
+    if k_own is not None:
+        shape = k_own.shape
+        S = shape[1]
+        if shape != (N, S, Hkv, Dh) or v_own.shape != shape:
+            raise ValueError("psd binding: k_own and v_own are [B*D, S, Hkv, Dh]")
+        own = _pair_strides(k_own, v_own, N, S, Hkv, Dh, "k_own, v_own")
+        ko, vo = k_own.data_ptr() or None, v_own.data_ptr() or None
+    a = _pack_attention(B, N // B, M, Hq, Hkv, Dh, P, S, _one_type(q.dtype, k_own, v_own, out), 1 if causal else 0,
+                        Dh ** -0.5 if scale is None else scale, 0, *_tokens_strides(q, N, M, Hq, Dh, "q"),
+                        *_tokens_strides(out, N, M, Hq, Dh, "out"), *_codes_strides(k_codes.stride(), B, P, Hkv, Dh, "k_codes"),
+                        *_codes_strides(v_codes.stride(), B, P, Hkv, Dh, "v_codes"), *own)
+    stream = _here(stream, q, k_codes, v_codes, k_scale, v_scale, out, lse, k_own, v_own, prefix_len, own_len, workspace, status)
+    sc = (B, Hkv, -(-P // block))
+    ws, ws_bytes = _space(workspace)
+    _check(LIB.psd_draft_attention_q8(q.data_ptr(), k_codes.data_ptr() or None, v_codes.data_ptr() or None,
+                                      _want(k_scale, sc, _F32, "k_scale") or None, _want(v_scale, sc, _F32, "v_scale") or None, block,
+                                      _want(prefix_len, (B,), _I32, "prefix_len"), ko, vo, _want(own_len, (N,), _I32, "own_len"), a,
+                                      out.data_ptr(), _want(lse, (N, M, Hq), _F32, "lse"), ws, ws_bytes, _ptr(status), stream),
+           "psd_draft_attention_q8")
+
+
+def psd_confidence_q8_workspace_bytes(n_rows: int, H: int, V: int) -> int:
+    return int(LIB.psd_confidence_q8_workspace_bytes(n_rows, H, V))
+
+
+def psd_confidence_q8(hidden, w_codes, w_scale, out_token, out_conf, out_lse=None, workspace=None, status=None, stream=None):
+    """Token, confidence and lse of every row of ``hidden`` [R, H] (bf16 or fp16) over an LM head in codes [V, H] int8 with a
+    scale [V] per vocabulary row."""
+    R, H = hidden.shape
+    V = w_codes.shape[0]
+    if not hidden.is_contiguous():
+        raise ValueError("psd binding: hidden must be contiguous")
+    stream = _here(stream, hidden, w_codes, w_scale, out_token, out_conf, out_lse, workspace, status)
+    ws, ws_bytes = _space(workspace)
+    _check(LIB.psd_confidence_q8(hidden.data_ptr(), _DTYPES.get(hidden.dtype, -1), _want(w_codes, (V, H), _I8, "w_codes"),
+                                 _want(w_scale, (V,), _F32, "w_scale"), R, H, V, _want_n(out_token, R, _I32, "out_token"),
+                                 _want_n(out_conf, R, _F32, "out_conf"), _want_n(out_lse, R, _F32, "out_lse"), ws, ws_bytes, _ptr(status),
+                                 stream), "psd_confidence_q8")

@@ -453,6 +453,13 @@ const char* draft_attention_kernels(int B, int D, int M, int Hq, int Hkv, int Dh
     return p.fused ? "prefix_attention_kernel" : "prefix_attention_kernel+draft_attention_kernel";
 }
 
+int launch_own_and_join(const void* q, const void* k_own, const void* v_own, const int32_t* own_len, const psd_attention_t& a,
+                        const float* po, const float* pl, int splits, void* out, float* lse, cudaStream_t st) {
+    OwnArgs p = {q, nullptr, nullptr, k_own, v_own, nullptr, own_len, out, lse, a, 0, 1, po, pl, splits, (int64_t)a.B * a.D * a.M * a.Hq};
+    if (a.dtype == PSD_BF16) return a.Dh <= 64 ? launch_dh<__nv_bfloat16, 64>(p, st) : launch_dh<__nv_bfloat16, 128>(p, st);
+    return a.Dh <= 64 ? launch_dh<__half, 64>(p, st) : launch_dh<__half, 128>(p, st);
+}
+
 int launch_draft_attention(const void* q, const void* k_prefix, const void* v_prefix, const int32_t* prefix_len,
                            const void* k_own, const void* v_own, const int32_t* own_len, const psd_attention_t& a,
                            void* out, float* lse, void* workspace, int32_t* status_dev, cudaStream_t st) {

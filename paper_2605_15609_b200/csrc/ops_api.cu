@@ -13,13 +13,6 @@ bool heads_ok(int32_t Hq, int32_t Hkv, int32_t Dh) {
 // Lengths that kernels walk in steps of thousands with 32-bit positions: a step past the end must not overflow.
 constexpr int32_t kMostSteps = 1 << 30;
 
-// Rows (tokens times heads) and head-blocks of the grids are indexed with 32 bits; everything that is
-// multiplied by a stride is computed in 64.
-bool attention_sizes_ok(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P, int32_t S) {
-    if (B < 1 || D < 1 || M < 1 || P < 0 || S < 0 || !heads_ok(Hq, Hkv, Dh)) return false;
-    if ((int64_t)B * D > INT32_MAX || (int64_t)B * D * M > INT32_MAX) return false;
-    return (int64_t)B * D * M * Hq <= INT32_MAX / 2 && P <= INT32_MAX - 1024 && S <= INT32_MAX - 1024;
-}
 bool strides_ok(const psd_kv_strides_t& s) { return s.outer >= 0 && s.token > 0 && s.head >= 0; }
 bool strides_aligned(const psd_kv_strides_t& s) { return s.outer % 8 == 0 && s.token % 8 == 0 && s.head % 8 == 0; }
 // what a tensor map takes: strides below 2^40 bytes
@@ -28,6 +21,15 @@ bool strides_small(const psd_kv_strides_t& s) {
     return s.outer < top && s.token < top && s.head < top;
 }
 
+}  // namespace
+
+// Rows (tokens times heads) and head-blocks of the grids are indexed with 32 bits; everything that is
+// multiplied by a stride is computed in 64.
+bool attention_sizes_ok(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P, int32_t S) {
+    if (B < 1 || D < 1 || M < 1 || P < 0 || S < 0 || !heads_ok(Hq, Hkv, Dh)) return false;
+    if ((int64_t)B * D > INT32_MAX || (int64_t)B * D * M > INT32_MAX) return false;
+    return (int64_t)B * D * M * Hq <= INT32_MAX / 2 && P <= INT32_MAX - 1024 && S <= INT32_MAX - 1024;
+}
 int check_attention(const psd_attention_t& a, bool with_out) {
     if (!attention_sizes_ok(a.B, a.D, a.M, a.Hq, a.Hkv, a.Dh, a.P, a.S)) return PSD_ERR_SHAPE;
     if (!(a.scale > 0.f) || !std::isfinite(a.scale)) return PSD_ERR_SHAPE;
@@ -46,7 +48,6 @@ int check_attention(const psd_attention_t& a, bool with_out) {
     return PSD_OK;
 }
 
-}  // namespace
 }  // namespace psd
 
 using namespace psd;
