@@ -1,7 +1,6 @@
 // extern "C" entry points of the 8-bit step and the rotation: argument checks, then the launches.  See psd.h.
 #include <cmath>
 #include "ops_internal.cuh"
-#include "prefix_attention.cuh"
 #include "prefix_attention_q8.cuh"
 
 namespace psd {
@@ -16,18 +15,6 @@ bool eights(int64_t a, int64_t b, int64_t c) { return a % 8 == 0 && b % 8 == 0 &
 bool head_shape_ok(int32_t n_rows, int32_t H, int32_t V) {
     // sums of products of codes stay below 2^31: 127 * 127 * 131072
     return n_rows >= 1 && n_rows <= kMostSteps && H >= 64 && H % 64 == 0 && H <= 131072 && V >= 1 && V < 2147483647 - 256;
-}
-
-// Partial results of a call and of all calls with smaller B, D, P and S: at most kMaxPrefixSplits per row and no more than the
-// SMs' CTAs hold at once where rows are split (a split form's CTAs fill the SMs once, with up to 256 rows each).
-size_t partials(int64_t rows, int32_t P, int dhp) {
-    constexpr int64_t kOnce = (int64_t)256 * 256;
-    int64_t most = ((int64_t)P + 255) / 256;
-    if (most > kMaxPrefixSplits) most = kMaxPrefixSplits;
-    int64_t n = rows * most;
-    const int64_t cap = rows > kOnce ? rows : kOnce;
-    if (n > cap) n = cap;
-    return round_up((size_t)n * (dhp + 1) * 4);
 }
 
 }  // namespace
@@ -123,8 +110,7 @@ int psd_prefix_quantize(const void* k, const void* v, const int32_t* begin, cons
 
 size_t psd_attention_q8_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P, int32_t S) {
     if (!attention_sizes_ok(B, D, M, Hq, Hkv, Dh, P, S) || Dh % 16) return 0;
-    const size_t n = P == 0 ? 0 : partials((int64_t)B * D * M * Hq, P, Dh <= 64 ? 64 : 128);
-    return n < 256 ? 256 : n;
+    return P == 0 ? 256 : prefix_q8_workspace(B, D, M, Hq, Hkv, Dh, P);
 }
 
 int psd_draft_attention_q8(const void* q, const int8_t* k_codes, const int8_t* v_codes, const float* k_scale,
@@ -145,7 +131,7 @@ int psd_draft_attention_q8(const void* q, const int8_t* k_codes, const int8_t* v
     if (a->P == 0) return launch_draft_attention(q, nullptr, nullptr, nullptr, k_own, v_own, own_len, *a, out, lse, workspace, status_dev, st);
     const PrefixQ8Plan plan = plan_prefix_q8(a->B, a->D, a->M, a->Hq, a->Hkv, a->Dh, a->P);
     const int64_t rows = (int64_t)a->B * a->D * a->M * a->Hq;
-    if (workspace_bytes < (size_t)rows * plan.splits * (plan.dhp + 1) * 4) return PSD_ERR_WORKSPACE;
+    if (workspace_bytes < prefix_q8_needs(a->B, a->D, a->M, a->Hq, a->Hkv, a->Dh, a->P)) return PSD_ERR_WORKSPACE;
     float* po = reinterpret_cast<float*>(workspace);
     float* pl = po + rows * plan.splits * plan.dhp;
     const PrefixQ8 c = {k_codes, v_codes, k_scale, v_scale, block};

@@ -16,7 +16,6 @@
 // Bound for few rows: the cache's bytes, 2 Dh per key; widening takes 3 to 3.5 instructions for two codes, about 40% of the issue
 // slots that the bytes' time offers.
 #include "attn_tc.cuh"
-#include "prefix_attention.cuh"
 #include "prefix_attention_q8.cuh"
 
 namespace psd {
@@ -366,6 +365,13 @@ int launch_r(const CUtensorMap& mk, const CUtensorMap& mv, const Q8Args& a, int6
 PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
     const int64_t rows = (int64_t)D * M * (Hq / Hkv);
     PrefixQ8Plan p = {};
+    p.dhp = Dh <= 64 ? 64 : 128;
+    p.tiles = rows > 32;
+    if (p.tiles) {
+        p.tile = plan_prefix(B, D, M, Hq, Hkv, Dh, P, 0);
+        p.splits = p.tile.splits;
+        return p;
+    }
     p.row_blocks = rows > 16 ? 2 : 1;
     p.units = (int)((rows + 16 * p.row_blocks - 1) / (16 * p.row_blocks));
     const int64_t ctas = (int64_t)B * Hkv * p.units, want = (int64_t)sm_count() * (p.row_blocks == 1 ? 3 : 2);
@@ -374,12 +380,33 @@ PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P)
     if (s > most) s = most;
     if (s > kMaxPrefixSplits) s = kMaxPrefixSplits;
     p.splits = s < 1 ? 1 : (int)s;
-    p.dhp = Dh <= 64 ? 64 : 128;
     return p;
+}
+
+static size_t partial_bytes_q8(int64_t rows, int dhp) { return ((size_t)rows * (dhp + 1) * 4 + 255) / 256 * 256; }
+
+size_t prefix_q8_needs(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
+    const PrefixQ8Plan p = plan_prefix_q8(B, D, M, Hq, Hkv, Dh, P);
+    return partial_bytes_q8((int64_t)B * D * M * Hq * p.splits, p.dhp);
+}
+
+// Rows are split at most while the CTAs fill the SMs once (256 rows each at most), and no further than the prefix allows; a single
+// query tile of the tcgen05 kernel is always split in two.
+size_t prefix_q8_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
+    const int64_t rows = (int64_t)B * D * M * Hq, T = (int64_t)D * M, tq = 128 / (Hq / Hkv);
+    const int64_t pairs = 2 * (int64_t)B * Hq * (T < tq ? T : tq), once = 256 * (int64_t)sm_count();
+    int64_t most = ((int64_t)P + 255) / 256;
+    if (most > kMaxPrefixSplits) most = kMaxPrefixSplits;
+    if (most < 2) most = 2;
+    int64_t n = rows > pairs ? rows : pairs;
+    if (n < once) n = once;
+    if (n > rows * most) n = rows * most;
+    return partial_bytes_q8(n, Dh <= 64 ? 64 : 128);
 }
 
 int launch_prefix_attention_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const psd_attention_t& a, const PrefixQ8Plan& p,
                                float* po, float* pl, int32_t* status_dev, cudaStream_t st) {
+    if (p.tiles) return launch_prefix_tiles_q8(q, c, prefix_len, a, p.tile, po, pl, status_dev, st);
     CUtensorMap mk, mv;
     if (!make_codes_map(&mk, c.k, a.kp, a.B, a.P, a.Hkv, a.Dh, p.dhp, kSlice) || !make_codes_map(&mv, c.v, a.vp, a.B, a.P, a.Hkv, a.Dh, p.dhp, kSlice))
         return PSD_ERR_CUDA;

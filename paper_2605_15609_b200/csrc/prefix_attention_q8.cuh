@@ -1,6 +1,7 @@
 // The prefix part of the drafts' attention over an 8-bit cache, called by ops_q8_api.cu.
 #pragma once
 #include "ops_internal.cuh"
+#include "prefix_attention.cuh"
 
 namespace psd {
 
@@ -10,17 +11,26 @@ struct PrefixQ8 {
     int block;                       // tokens per scale: 16, 32, 64 or 128
 };
 
+// Which kernel takes the prefix, and how its work is cut.
 struct PrefixQ8Plan {
-    int row_blocks;   // 16-row blocks of a warp: 1 or 2
-    int units;        // CTAs along the rows of a key head
-    int splits;       // partial results per row
-    int dhp;          // floats per partial output row: 64 or 128
+    bool tiles;         // prefix_tiles_q8_kernel (tcgen05), cut as `tile` says; else prefix_rows_q8_kernel:
+    int row_blocks;     // 16-row blocks of a warp: 1 or 2
+    int units;          // CTAs along the rows of a key head
+    PrefixPlan tile;
+    int splits;         // partial results per row
+    int dhp;            // floats per partial output row: 64 or 128
 };
 PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P);
+// bytes of the partial results of a call, and of all calls with smaller B, D and P
+size_t prefix_q8_needs(int B, int D, int M, int Hq, int Hkv, int Dh, int P);
+size_t prefix_q8_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P);
 
 // Partial results of every row over its sequence's prefix, as launch_prefix_attention leaves them: po [splits][rows][dhp], pl
 // [splits][rows].
 int launch_prefix_attention_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const psd_attention_t& a, const PrefixQ8Plan& p,
                                float* po, float* pl, int32_t* status_dev, cudaStream_t st);
+// prefix_attention_q8_tc.cu
+int launch_prefix_tiles_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const psd_attention_t& a, const PrefixPlan& p,
+                           float* po, float* pl, int32_t* status_dev, cudaStream_t st);
 
 }  // namespace psd

@@ -1,0 +1,506 @@
+// Attention of many query rows over a prefix in 8-bit codes, on tcgen05: prefix_attention_kernel's two streams (see there: query
+// tiles of up to 128 rows, scores and outputs in tensor memory, weights overwriting scores, a thread per row in the softmax) with
+// a stage in front of the products that widens the codes.
+//
+// TMA brings tiles of 128 keys in codes (16 KB) into a small ring; four warps widen them into a second ring of 16-bit tiles in the
+// swizzled layout that the products read.  Codes are exact in 16 bits, so nothing is rounded there: keys become the queries' type, values
+// fp16.  The keys' scale of each 16 columns is the factor of their scores in the exponent (in place of the one factor of the 16-bit kernel),
+// the values' scale multiplies the weights, which go to the product in fp16, relative to the largest value scale of the CTA's keys and up to 2^15.
+// Keys past the end are masked in the scores; their codes are finite, so their weights of 0 need no further care.
+//
+// Bound: for Dh = 128 products and exponentials as there (2048 cycles each per 256 rows x 128 keys); widening is about 600 issue slots
+// per scheduler of the same round, the values' scales 64 more per warp.
+#include "attn_tc.cuh"
+#include "prefix_attention.cuh"
+#include "prefix_attention_q8.cuh"
+
+namespace psd {
+namespace {
+
+constexpr int kQThreads = 512;              // warps 0-3, 4-7: softmax of stream 0, 1; 8: TMA; 9: MMA; 10, 11 idle; 12-15: widening
+constexpr float kRaise = 8.0f;              // growth of a row's maximum (log2) that triggers a rescale
+constexpr float kHalfRoom = 7.0f;           // how far (log2) the reference is set below the maximum: weights go up to 2^15
+constexpr int kMaxSorted = 128;             // sequences that are put in order of length
+constexpr int kBarBytes = 1024;
+
+template <int SLABS> struct Rings { static constexpr int RAW = SLABS == 2 ? 2 : 4, WIDE = SLABS == 2 ? 4 : 8; };
+
+struct TcArgs {
+    const float *k_scale, *v_scale;
+    const int32_t* prefix_len;
+    float *po, *pl;
+    int32_t* status_dev;
+    int64_t rows;
+    int T, G, Hq, Hkv, Dh, P, nb, shift;
+    int tq, n_qt, units, splits;
+    int k_outer, k_head, v_outer, v_head;
+    int B, longest_first;
+    float c;
+    long long wait_limit;
+    int stall_test;
+};
+
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// The codes in bytes (b, b + 1) of x as two 16-bit numbers (see prefix_attention_q8.cu for the patterns).
+template <bool BF16>
+__device__ __forceinline__ uint32_t widen_pair(uint32_t x, uint32_t sel) {
+    const uint32_t t = __byte_perm(x, 0u, sel);
+    uint32_t r;
+    if (BF16) asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"((t & 0x007f007fu) | 0x43004300u), "r"((t & 0x00800080u) | 0x43004300u));
+    else asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"((t & 0x00ff00ffu) ^ 0x64806480u), "r"(0x64806480u));
+    return r;
+}
+// One tile of 128 keys x SLABS * 64 codes (rows dense) into SLABS swizzled slabs, by 128 threads.
+template <int SLABS, bool BF16>
+__device__ __forceinline__ void widen_tile(const unsigned char* raw, unsigned char* to, int tid) {
+    constexpr int CH = SLABS * 8, N = CH, BATCH = 8;      // pieces of 8 codes per key; pieces per thread
+#pragma unroll 1
+    for (int i0 = 0; i0 < N; i0 += BATCH) {
+        uint2 w[BATCH];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) w[i] = *reinterpret_cast<const uint2*>(raw + ((i0 + i) * 128 + tid) * 8);
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int x = (i0 + i) * 128 + tid, key = x / CH, ch = x % CH;
+            uint4 y;
+            y.x = widen_pair<BF16>(w[i].x, 0x1100);
+            y.y = widen_pair<BF16>(w[i].x, 0x3322);
+            y.z = widen_pair<BF16>(w[i].y, 0x1100);
+            y.w = widen_pair<BF16>(w[i].y, 0x3322);
+            *reinterpret_cast<uint4*>(to + (ch / 8) * kSlabBytes + key * 128 + (((ch % 8) ^ (key & 7)) << 4)) = y;
+        }
+    }
+}
+
+template <int SLABS, bool BF16>
+__global__ void __launch_bounds__(kQThreads, 1)
+prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                       const __grid_constant__ CUtensorMap map_v, const TcArgs a) {
+    extern __shared__ __align__(1024) unsigned char smem[];
+    constexpr int TILE = SLABS * kSlabBytes, RAW = TILE / 2, NR = Rings<SLABS>::RAW, NS = Rings<SLABS>::WIDE, DHP = SLABS * 64;
+    unsigned char* q_tiles = smem;                                   // [2][TILE]
+    unsigned char* ring = smem + 2 * TILE;                           // [NS][TILE]
+    unsigned char* raw = ring + NS * TILE;                           // [NR][RAW]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(raw + NR * RAW);
+    uint64_t *q_full = bars, *raw_full = bars + 1, *raw_empty = raw_full + NR, *full = raw_empty + NR, *empty = full + NS, *s_full = empty + NS /* [2] */,
+             *p_half = s_full + 2, *p_ready = p_half + 2, *o_done = p_ready + 2, *drain = o_done + 2, *never = drain + 1;
+    uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(never + 1);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+    volatile int* sequence = abort_flag + 1;
+
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const bool shared_keys = a.n_qt > 1;
+    const int unit = blockIdx.x % a.units, rest = blockIdx.x / a.units;
+    const int n_cs = shared_keys ? a.splits : a.splits / 2;
+    const int cs = rest % n_cs, bh = rest / n_cs, h = bh % a.Hkv;
+    int b = bh / a.Hkv;
+    const int qt0 = shared_keys ? unit * 2 : 0;
+    const int n_streams = shared_keys ? min(2, a.n_qt - qt0) : 2;
+
+    if (threadIdx.x == 0) {
+        mbar_init(q_full, 1);
+        for (int s = 0; s < NR; ++s) { mbar_init(&raw_full[s], 1); mbar_init(&raw_empty[s], 4); }
+        for (int s = 0; s < NS; ++s) { mbar_init(&full[s], 4); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&s_full[s], 1); mbar_init(&p_half[s], 4); mbar_init(&p_ready[s], 4); mbar_init(&o_done[s], 1); }
+        mbar_init(drain, 1);
+        mbar_init(never, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 8 && lane == 0) { tma_prefetch_desc(&map_q); tma_prefetch_desc(&map_k); tma_prefetch_desc(&map_v); }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_holder)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, *tmem_holder, 0);
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    const WaitCtx wc = {abort_flag, a.status_dev, a.wait_limit, 0u};
+    auto length = [&](int i) { return a.prefix_len ? min(max(a.prefix_len[i], 0), a.P) : a.P; };
+    if (a.longest_first) {
+        // the sequences in order of length, so that the last CTAs to start are short ones
+        const int i = threadIdx.x;
+        if (i < a.B) {
+            const int mine = length(i);
+            int rank = 0;
+            for (int x = 0; x < a.B; ++x) {
+                const int y = length(x);
+                rank += y > mine || (y == mine && x < i);
+            }
+            if (rank == b) *sequence = i;
+        }
+        __syncthreads();
+        b = *sequence;
+    }
+    const int L = length(b), tiles = (L + 127) / 128;
+    auto share = [&](int x) { return (int)((long long)tiles * x / a.splits); };
+    const int sp0 = shared_keys ? cs : cs * 2, sp1 = shared_keys ? cs : cs * 2 + 1;
+    const int t00 = share(sp0), t01 = share(sp1);
+    const int nt0 = share(sp0 + 1) - t00, nt1 = n_streams > 1 ? share(sp1 + 1) - t01 : 0;
+    const int most = max(nt0, nt1);
+    // Tiles in the order: per round j = -1, 0, ..: V of tile j, K of tile j + 1 for stream 0, then for stream 1; with shared keys
+    // they are listed for stream 0 only.
+    const int common = shared_keys ? nt0 : 0;
+    auto listed = [&](int s, int j) { return j >= 0 && j < (s ? nt1 : nt0) && (s == 0 || j >= common); };
+    const int n_q = shared_keys ? n_streams : 1;
+
+    if (warp >= 12) {
+        // -------------------------------------------------------------------- widening
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        const int tid = threadIdx.x - 12 * 32;
+        int item = 0;
+        bool ok = true;
+#pragma unroll 1
+        for (int x = 0; ok && x < 4 * (most + 1); ++x) {
+            const bool is_k = x & 1;
+            const int s = (x >> 1) & 1, j = (x >> 2) - (is_k ? 0 : 1);
+            if (!listed(s, j)) continue;
+            if (!(ok = mbar_wait_warp(&empty[item % NS], ((item / NS) & 1) ^ 1, wc))) break;
+            if (!(ok = mbar_wait_warp(&raw_full[item % NR], (item / NR) & 1, wc))) break;
+            const unsigned char* from = raw + (item % NR) * RAW;
+            unsigned char* to = ring + (item % NS) * TILE;
+            if (BF16 && is_k) widen_tile<SLABS, true>(from, to, tid);
+            else widen_tile<SLABS, false>(from, to, tid);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(&raw_empty[item % NR]);
+                mbar_arrive(&full[item % NS]);
+            }
+            ++item;
+        }
+    } else if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+        if (warp == 8 && most > 0) {
+            // ---------------------------------------------------------------- loader
+            const bool leader = elect_one();
+            if (leader) {
+                mbar_arrive_expect_tx(q_full, (uint32_t)(n_q * SLABS * a.tq * a.G * 128));
+                for (int t = 0; t < n_q; ++t)
+                    for (int c = 0; c < SLABS; ++c)
+                        tma_load_3d(q_tiles + t * TILE + c * kSlabBytes, &map_q, q_full, c * kSlabElems, h * a.G, b * a.T + (qt0 + t) * a.tq);
+            }
+            int item = 0;
+            bool ok = true;
+#pragma unroll 1
+            for (int x = 0; ok && x < 4 * (most + 1); ++x) {
+                const bool is_k = x & 1;
+                const int s = (x >> 1) & 1, j = (x >> 2) - (is_k ? 0 : 1);
+                if (!listed(s, j)) continue;
+                const int slot = item % NR;
+                if (!mbar_wait_warp(&raw_empty[slot], ((item / NR) & 1) ^ 1, wc)) { ok = false; break; }
+                if (leader) {
+                    mbar_arrive_expect_tx(&raw_full[slot], RAW);
+                    tma_load_4d(raw + slot * RAW, is_k ? &map_k : &map_v, &raw_full[slot], 0, h * (is_k ? a.k_head : a.v_head),
+                                ((s ? t01 : t00) + j) * 128, b * (is_k ? a.k_outer : a.v_outer));
+                }
+                ++item;
+                if (a.stall_test && item == 1 && !mbar_wait_warp(never, 0, wc)) ok = false;
+            }
+            if (!ok) {
+                // giving up: no copy may be in flight when the CTA exits
+                long long c0 = clock64();
+                while (!mbar_try_wait(q_full, 0) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
+                for (int i = item > NR ? item - NR : 0; i < item; ++i) {
+                    c0 = clock64();
+                    while (!mbar_try_wait(&raw_full[i % NR], (i / NR) & 1) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
+                }
+            }
+        } else if (warp == 9 && most > 0) {
+            // ---------------------------------------------------------------- products (one warp, both streams in turn)
+            const bool leader = elect_one();
+            const uint32_t id_s = umma_idesc16(128, BF16, false), id_o = umma_idesc16((a.Dh + 15) / 16 * 16, false, true);
+            const int k_steps = (a.Dh + 15) / 16;
+            const uint64_t dq = umma_smem_desc(smem_u32(q_tiles)), dk = umma_smem_desc(smem_u32(ring));
+            const uint64_t dv = umma_smem_desc_mn(smem_u32(ring), kSlabBytes);
+            auto wait_item = [&](int item) { return mbar_wait_warp(&full[item % NS], (item / NS) & 1, wc); };
+            auto scores = [&](int s, int item, bool release) {
+                const uint64_t q = dq + (uint64_t)((shared_keys ? s : 0) * (TILE >> 4)), k = dk + (uint64_t)((item % NS) * (TILE >> 4));
+#pragma unroll
+                for (int i = 0; i < SLABS * 4; ++i)
+                    if (i < k_steps) {
+                        const uint64_t off = (i / 4) * (kSlabBytes >> 4) + (i % 4) * 2;
+                        umma_f16(tmem + s * 128, q + off, k + off, id_s, i != 0);
+                    }
+                umma_commit(&s_full[s]);
+                if (release) umma_commit(&empty[item % NS]);
+            };
+            int next = 0;
+            bool ok = mbar_wait_warp(q_full, 0, wc);
+            int v = 0, k = 0;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (!ok || (s ? nt1 : nt0) == 0) continue;
+                if (listed(s, 0)) {
+                    k = next++;
+                    if (!(ok = wait_item(k))) continue;
+                }
+                tc_fence_after();
+                if (leader) scores(s, k, common == 0 || s == n_streams - 1);
+            }
+#pragma unroll 1
+            for (int j = 0; ok && j < most; ++j) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const int n = s ? nt1 : nt0;
+                    if (!ok || j >= n) continue;
+                    const bool more = j + 1 < n;
+                    if (listed(s, j)) { v = next++; ok = wait_item(v); }
+                    if (ok && listed(s, j + 1)) { k = next++; ok = wait_item(k); }
+                    if (!ok || !(ok = mbar_wait_warp(&p_half[s], j & 1, wc))) continue;
+                    tc_fence_after();
+                    const int left = L - ((s ? t01 : t00) + j) * 128, steps = left >= 128 ? 8 : (left + 15) / 16;
+                    const uint64_t vd = dv + (uint64_t)((v % NS) * (TILE >> 4));
+                    const uint32_t t_s = tmem + s * 128, t_o = t_s + 256;
+                    auto pv = [&](int i) {
+                        if (i < steps) umma_f16_ts(t_o, t_s + i * 8, vd + (uint64_t)(i * (2048 >> 4)), id_o, (j | i) != 0);
+                    };
+                    if (leader) { pv(0); pv(1); pv(2); pv(3); }
+                    if (!(ok = mbar_wait_warp(&p_ready[s], j & 1, wc))) continue;
+                    tc_fence_after();
+                    if (leader) {
+                        pv(4); pv(5); pv(6); pv(7);
+                        // the scores of the next tile overwrite the weights just read; their commit covers PV as well
+                        if (more) scores(s, k, j + 1 >= common || s == n_streams - 1);
+                        else umma_commit(&o_done[s]);
+                        if (j >= common || s == n_streams - 1) umma_commit(&empty[v % NS]);
+                    }
+                }
+            }
+            if (!ok) {
+                if (leader) umma_commit(drain);
+                const long long c0 = clock64();
+                while (!mbar_try_wait(drain, 0) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
+            }
+        }
+        __syncwarp();
+    } else {
+        // -------------------------------------------------------------------- softmax: a row per thread
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        const int s = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const uint32_t t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
+        float m = 0.f, l = 0.f;          // reference (in the exponent's units) and sum relative to it
+        bool fresh = true;               // no score seen yet
+        bool ok = true;
+        const int n = s ? nt1 : nt0, first_tile = s ? t01 : t00;
+        const int my_tok = (qt0 + (shared_keys ? s : 0)) * a.tq + row / a.G;
+        // Scales of a tile: lane i holds the keys' of columns 16 i .., lane 8 + i the values', relative to the largest of this stream's
+        // keys.  They are loaded a round ahead.
+        const float* ks = a.k_scale + ((int64_t)b * a.Hkv + h) * a.nb;
+        const float* vs = a.v_scale + ((int64_t)b * a.Hkv + h) * a.nb;
+        float vref = 1.17549435e-38f;
+        if (n > 0) {
+            const int j1 = min(((first_tile + n) * 128 - 1) >> a.shift, (L - 1) >> a.shift);
+            for (int j = ((first_tile * 128) >> a.shift) + lane; j <= j1; j += 32) vref = fmaxf(vref, vs[j]);
+#pragma unroll
+            for (int x = 16; x; x >>= 1) vref = fmaxf(vref, __shfl_xor_sync(0xffffffffu, vref, x));
+        }
+        const float vinv = 1.f / vref;
+        auto scale_of = [&](int j) {
+            const int key = (first_tile + j) * 128 + (lane & 7) * 16;
+            if (key >= L) return 0.f;                   // (what stands there was never written)
+            const float x = lane & 8 ? vs[key >> a.shift] * vinv : ks[key >> a.shift] * a.c;
+            return lane & 8 || x != 0.f ? x : 1.17549435e-38f;      // masked scores are -inf times this
+        };
+        float next_scale = n > 0 ? scale_of(0) : 0.f;
+        for (int j = 0; j < n; ++j) {
+            const float sc = next_scale;
+            if (j + 1 < n) next_scale = scale_of(j + 1);
+            if (!(ok = mbar_wait_warp(&s_full[s], j & 1, wc))) break;
+            tc_fence_after();
+            const int left = L - (first_tile + j) * 128;   // keys of this tile
+            uint32_t r[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, r[c]);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_wait_ld(r[c]);
+            if (left < 128) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (c * 32 + i >= left) r[c][i] = 0xff800000u;
+            }
+            float high = -INFINITY;
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+                auto x = [&](int i) { return __uint_as_float(r[g >> 1][(g & 1) * 16 + i]); };
+                float u = max3(x(0), x(1), x(2));
+#pragma unroll
+                for (int i = 3; i < 15; i += 2) u = max3(u, x(i), x(i + 1));
+                u = fmaxf(u, x(15));
+                // (columns past the end have the scale 0 where their 16 hold no key: -inf * 0 is no number and drops out)
+                high = fmaxf(high, u * __shfl_sync(0xffffffffu, sc, g));
+            }
+            // the reference that this tile's maximum asks for
+            const float top = high - kHalfRoom;
+            const bool raise = top > (fresh ? -INFINITY : m + kRaise);
+            if (__any_sync(0xffffffffu, raise)) {
+                const bool rescale = raise && !fresh;
+                const float f = rescale ? ex2(m - top) : 1.f;
+                if (raise) { m = top; fresh = false; }
+                l *= f;
+                if (__any_sync(0xffffffffu, rescale))
+#pragma unroll 1
+                for (int c = 0; c < a.Dh; c += 8) {
+                    uint32_t o[8];
+                    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                                 : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7])
+                                 : "r"(t_o + c));
+                    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                                 : "+r"(o[0]), "+r"(o[1]), "+r"(o[2]), "+r"(o[3]), "+r"(o[4]), "+r"(o[5]), "+r"(o[6]), "+r"(o[7]) :: "memory");
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0, %1, %2, %3, %4, %5, %6, %7};"
+                                 ::"r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]), "r"(t_o + c)
+                                 : "memory");
+                }
+            }
+            const f32x2 nm = pack2(-m, -m);
+            f32x2 acc[2] = {0ull, 0ull};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t p[16];
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    float kf = __shfl_sync(0xffffffffu, sc, 2 * c + g);
+                    const float vf = __shfl_sync(0xffffffffu, sc, 8 + 2 * c + g);
+                    if (kf == 0.f) kf = 1.f;               // no key among these 16: their scores are -inf
+                    const f32x2 kk = pack2(kf, kf), vv = pack2(vf, vf);
+#pragma unroll
+                    for (int i = g * 8; i < g * 8 + 8; ++i) {
+                        const f32x2 e = ex2_pair(fma2(pack2(__uint_as_float(r[c][2 * i]), __uint_as_float(r[c][2 * i + 1])), kk, nm));
+                        acc[i & 1] = add2(acc[i & 1], e);
+                        float y, z;
+                        unpack2(mul2(e, vv), y, z);
+                        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p[i]) : "f"(z), "f"(y));
+                    }
+                }
+                tmem_st16(t_s + c * 16, p);
+                if (c == 1 || c == 3) {
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(c == 1 ? &p_half[s] : &p_ready[s]);
+                }
+            }
+            float l0, l1;
+            unpack2(add2(acc[0], acc[1]), l0, l1);
+            l += l0 + l1;
+        }
+        if (s < n_streams) {
+            const bool live = row < a.tq * a.G && my_tok < a.T;
+            if (n > 0 && ok) {
+                ok = mbar_wait_warp(&o_done[s], 0, wc);
+                tc_fence_after();
+            }
+            const float inv = fresh && l == 0.f ? 0.f : vref / l;
+            if (ok) {
+                const int64_t at = (int64_t)(s ? sp1 : sp0) * a.rows + ((int64_t)b * a.T + my_tok) * a.Hq + h * a.G + row % a.G;
+                float* o = a.po + at * DHP;
+#pragma unroll 1
+                for (int c = 0; n > 0 && c < a.Dh; c += 32) {
+                    uint32_t x[32];
+                    tmem_ld32(t_o + c, x);
+                    tmem_wait_ld(x);
+                    if (live) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8)
+                            asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(o + c + i),
+                                         "f"(__uint_as_float(x[i]) * inv), "f"(__uint_as_float(x[i + 1]) * inv),
+                                         "f"(__uint_as_float(x[i + 2]) * inv), "f"(__uint_as_float(x[i + 3]) * inv),
+                                         "f"(__uint_as_float(x[i + 4]) * inv), "f"(__uint_as_float(x[i + 5]) * inv),
+                                         "f"(__uint_as_float(x[i + 6]) * inv), "f"(__uint_as_float(x[i + 7]) * inv) : "memory");
+                    }
+                }
+                if (live) a.pl[at] = n > 0 ? m + log2f(l) : -INFINITY;
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (warp == 9) {
+        __syncwarp();
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+    }
+}
+
+// A cache of codes, boxes of 128 tokens of one head, rows of dhp bytes.
+bool make_tile_map(CUtensorMap* m, const void* base, const psd_kv_strides_t& s, int outer, int tokens, int heads, int Dh, int dhp) {
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dims[4] = {(cuuint64_t)Dh, (cuuint64_t)(s.head ? heads : 1), (cuuint64_t)tokens, (cuuint64_t)(s.outer ? outer : 1)};
+    cuuint64_t strides[3] = {(cuuint64_t)(s.head ? s.head : 16), (cuuint64_t)s.token, (cuuint64_t)(s.outer ? s.outer : 16)};
+    cuuint32_t b[4] = {(cuuint32_t)dhp, 1, 128, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, b, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int SLABS, bool BF16>
+int launch_t(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const TcArgs& a, int64_t grid, cudaStream_t st) {
+    constexpr int TILE = SLABS * kSlabBytes;
+    constexpr int smem = (2 + Rings<SLABS>::WIDE) * TILE + Rings<SLABS>::RAW * (TILE / 2) + kBarBytes;
+    static_assert(smem <= 227 * 1024, "shared memory of the 8-bit tile kernel");
+    static std::atomic<unsigned long long> set{0};
+    if (!ensure_dynamic_smem(prefix_tiles_q8_kernel<SLABS, BF16>, smem, set)) return PSD_ERR_CUDA;
+    static std::atomic<int> regs{0};      // 8 warps of 208 and 8 of 48 registers a thread
+    if (!launched_with(prefix_tiles_q8_kernel<SLABS, BF16>, (256 * 208 + 256 * 48) / kQThreads, regs)) return PSD_ERR_CUDA;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(kQThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, prefix_tiles_q8_kernel<SLABS, BF16>, mq, mk, mv, a);
+    count_launch();
+    return e == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
+}
+
+}  // namespace
+
+int launch_prefix_tiles_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const psd_attention_t& a, const PrefixPlan& p,
+                           float* po, float* pl, int32_t* status_dev, cudaStream_t st) {
+    CUtensorMap mq, mk, mv;
+    if (!make_query_map(&mq, q, a, p.tq) || !make_tile_map(&mk, c.k, a.kp, a.B, a.P, a.Hkv, a.Dh, p.dhp) ||
+        !make_tile_map(&mv, c.v, a.vp, a.B, a.P, a.Hkv, a.Dh, p.dhp))
+        return PSD_ERR_CUDA;
+    const int64_t grid = (int64_t)a.B * a.Hkv * p.units * (p.n_qt > 1 ? p.splits : p.splits / 2);
+    if (grid > INT32_MAX) return PSD_ERR_SHAPE;
+    TcArgs x = {};
+    x.k_scale = c.k_scale; x.v_scale = c.v_scale;
+    x.prefix_len = prefix_len;
+    x.po = po; x.pl = pl;
+    x.status_dev = status_dev;
+    x.rows = (int64_t)a.B * a.D * a.M * a.Hq;
+    x.T = a.D * a.M; x.G = a.Hq / a.Hkv; x.Hq = a.Hq; x.Hkv = a.Hkv; x.Dh = a.Dh; x.P = a.P;
+    x.nb = (a.P + c.block - 1) / c.block;
+    x.shift = c.block == 16 ? 4 : c.block == 32 ? 5 : c.block == 64 ? 6 : 7;
+    x.tq = p.tq; x.n_qt = p.n_qt; x.units = p.units; x.splits = p.splits;
+    x.k_outer = a.kp.outer ? 1 : 0; x.k_head = a.kp.head ? 1 : 0;
+    x.v_outer = a.vp.outer ? 1 : 0; x.v_head = a.vp.head ? 1 : 0;
+    x.B = a.B;
+    x.longest_first = prefix_len && a.B > 1 && a.B <= kMaxSorted && grid > sm_count() ? 1 : 0;
+    x.c = a.scale * kLog2e;
+    x.wait_limit = wait_limit_cycles();
+    x.stall_test = selftest_stall();
+    const bool bf16 = a.dtype == PSD_BF16;
+    if (p.dhp == 64) return bf16 ? launch_t<1, true>(mq, mk, mv, x, grid, st) : launch_t<1, false>(mq, mk, mv, x, grid, st);
+    return bf16 ? launch_t<2, true>(mq, mk, mv, x, grid, st) : launch_t<2, false>(mq, mk, mv, x, grid, st);
+}
+
+}  // namespace psd
