@@ -2,7 +2,7 @@
 // tiles of up to 128 rows, scores and outputs in tensor memory, weights overwriting scores, a thread per row in the softmax) with
 // a stage in front of the products that widens the codes.
 //
-// TMA brings tiles of 128 keys in codes (16 KB) into a small ring; four warps widen them into a second ring of 16-bit tiles in the
+// TMA brings tiles of 128 keys in codes (16 KB) into a small ring; six warps widen them into a second ring of 16-bit tiles in the
 // swizzled layout that the products read.  Codes are exact in 16 bits, so nothing is rounded there: keys become the queries' type, values
 // fp16.  The keys' scale of each 16 columns is the factor of their scores in the exponent (in place of the one factor of the 16-bit kernel),
 // the values' scale multiplies the weights, which go to the product in fp16, relative to the largest value scale of the CTA's keys and up to 2^15.
@@ -17,7 +17,8 @@
 namespace psd {
 namespace {
 
-constexpr int kQThreads = 512;              // warps 0-3, 4-7: softmax of stream 0, 1; 8: TMA; 9: MMA; 10, 11 idle; 12-15: widening
+constexpr int kQThreads = 512;              // warps 0-3, 4-7: softmax of stream 0, 1; 8: TMA; 9: MMA; 10-15: widening
+constexpr int kWideners = 192;
 constexpr float kRaise = 8.0f;              // growth of a row's maximum (log2) that triggers a rescale
 constexpr float kHalfRoom = 7.0f;           // how far (log2) the reference is set below the maximum: weights go up to 2^15
 constexpr int kMaxSorted = 128;             // sequences that are put in order of length
@@ -54,25 +55,30 @@ __device__ __forceinline__ uint32_t widen_pair(uint32_t x, uint32_t sel) {
     else asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"((t & 0x00ff00ffu) ^ 0x64806480u), "r"(0x64806480u));
     return r;
 }
-// One tile of 128 keys x SLABS * 64 codes (rows dense) into SLABS swizzled slabs, by 128 threads.
+// One tile of 128 keys x SLABS * 64 codes (rows dense) into SLABS swizzled slabs, by kWideners threads, 8 codes at a time.  A thread's
+// place in a key's row is the same in every turn; its key moves by 12 (or 24), so the swizzle of its place takes two values: addresses are
+// three registers and constants.
 template <int SLABS, bool BF16>
-__device__ __forceinline__ void widen_tile(const unsigned char* raw, unsigned char* to, int tid) {
-    constexpr int CH = SLABS * 8, N = CH, BATCH = 8;      // pieces of 8 codes per key; pieces per thread
-#pragma unroll 1
-    for (int i0 = 0; i0 < N; i0 += BATCH) {
-        uint2 w[BATCH];
+__device__ __forceinline__ void widen_tile(uint32_t raw, uint32_t to, int tid) {
+    constexpr int CH = SLABS * 8, KEYS = kWideners / CH, TURNS = (128 + KEYS - 1) / KEYS, BATCH = 6;
+    static_assert(KEYS % 4 == 0, "the swizzle of a thread's place");
+    const int key = tid / CH, ch = tid % CH;
+    const uint32_t src = raw + tid * 8, row = to + (ch / 8) * kSlabBytes + key * 128, at = ((ch % 8) ^ (key & 7)) << 4;
+    const uint32_t dst[2] = {row + at, row + (KEYS % 8 ? at ^ 64u : at)};
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) w[i] = *reinterpret_cast<const uint2*>(raw + ((i0 + i) * 128 + tid) * 8);
+    for (int i0 = 0; i0 < TURNS; i0 += BATCH) {
+        uint32_t w[BATCH][2];
 #pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int x = (i0 + i) * 128 + tid, key = x / CH, ch = x % CH;
-            uint4 y;
-            y.x = widen_pair<BF16>(w[i].x, 0x1100);
-            y.y = widen_pair<BF16>(w[i].x, 0x3322);
-            y.z = widen_pair<BF16>(w[i].y, 0x1100);
-            y.w = widen_pair<BF16>(w[i].y, 0x3322);
-            *reinterpret_cast<uint4*>(to + (ch / 8) * kSlabBytes + key * 128 + (((ch % 8) ^ (key & 7)) << 4)) = y;
-        }
+        for (int i = i0; i < i0 + BATCH && i < TURNS; ++i)
+            if ((i + 1) * KEYS <= 128 || i * KEYS + key < 128)
+                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[i - i0][0]), "=r"(w[i - i0][1]) : "r"(src + i * (kWideners * 8)));
+#pragma unroll
+        for (int i = i0; i < i0 + BATCH && i < TURNS; ++i)
+            if ((i + 1) * KEYS <= 128 || i * KEYS + key < 128) {
+                const uint32_t lo = w[i - i0][0], hi = w[i - i0][1];
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst[i & 1] + i * KEYS * 128), "r"(widen_pair<BF16>(lo, 0x1100)),
+                             "r"(widen_pair<BF16>(lo, 0x3322)), "r"(widen_pair<BF16>(hi, 0x1100)), "r"(widen_pair<BF16>(hi, 0x3322)) : "memory");
+            }
     }
 }
 
@@ -103,8 +109,8 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
 
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
-        for (int s = 0; s < NR; ++s) { mbar_init(&raw_full[s], 1); mbar_init(&raw_empty[s], 4); }
-        for (int s = 0; s < NS; ++s) { mbar_init(&full[s], 4); mbar_init(&empty[s], 1); }
+        for (int s = 0; s < NR; ++s) { mbar_init(&raw_full[s], 1); mbar_init(&raw_empty[s], kWideners / 32); }
+        for (int s = 0; s < NS; ++s) { mbar_init(&full[s], kWideners / 32); mbar_init(&empty[s], 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(&s_full[s], 1); mbar_init(&p_half[s], 4); mbar_init(&p_ready[s], 4); mbar_init(&o_done[s], 1); }
         mbar_init(drain, 1);
         mbar_init(never, 1);
@@ -151,10 +157,10 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     auto listed = [&](int s, int j) { return j >= 0 && j < (s ? nt1 : nt0) && (s == 0 || j >= common); };
     const int n_q = shared_keys ? n_streams : 1;
 
-    if (warp >= 12) {
+    if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (warp >= 10) {
         // -------------------------------------------------------------------- widening
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
-        const int tid = threadIdx.x - 12 * 32;
+        const int tid = threadIdx.x - 10 * 32;
         int item = 0;
         bool ok = true;
 #pragma unroll 1
@@ -164,8 +170,7 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             if (!listed(s, j)) continue;
             if (!(ok = mbar_wait_warp(&empty[item % NS], ((item / NS) & 1) ^ 1, wc))) break;
             if (!(ok = mbar_wait_warp(&raw_full[item % NR], (item / NR) & 1, wc))) break;
-            const unsigned char* from = raw + (item % NR) * RAW;
-            unsigned char* to = ring + (item % NS) * TILE;
+            const uint32_t from = smem_u32(raw + (item % NR) * RAW), to = smem_u32(ring + (item % NS) * TILE);
             if (BF16 && is_k) widen_tile<SLABS, true>(from, to, tid);
             else widen_tile<SLABS, false>(from, to, tid);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -177,7 +182,6 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             ++item;
         }
     } else if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
         if (warp == 8 && most > 0) {
             // ---------------------------------------------------------------- loader
             const bool leader = elect_one();
