@@ -129,13 +129,14 @@ int psd_draft_attention_q8(const void* q, const int8_t* k_codes, const int8_t* v
         return PSD_ERR_ALIGN;
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     if (a->P == 0) return launch_draft_attention(q, nullptr, nullptr, nullptr, k_own, v_own, own_len, *a, out, lse, workspace, status_dev, st);
-    const PrefixQ8Plan plan = plan_prefix_q8(a->B, a->D, a->M, a->Hq, a->Hkv, a->Dh, a->P);
+    const PrefixQ8Plan plan = plan_prefix_q8(a->B, a->D, a->M, a->Hq, a->Hkv, a->Dh, a->P, a->S);
     const int64_t rows = (int64_t)a->B * a->D * a->M * a->Hq;
-    if (workspace_bytes < prefix_q8_needs(a->B, a->D, a->M, a->Hq, a->Hkv, a->Dh, a->P)) return PSD_ERR_WORKSPACE;
+    if (workspace_bytes < prefix_q8_needs(a->B, a->D, a->M, a->Hq, a->Hkv, a->Dh, a->P, a->S)) return PSD_ERR_WORKSPACE;
     float* po = reinterpret_cast<float*>(workspace);
     float* pl = po + rows * plan.splits * plan.dhp;
     const PrefixQ8 c = {k_codes, v_codes, k_scale, v_scale, block};
-    if (const int e = launch_prefix_attention_q8(q, c, prefix_len, *a, plan, po, pl, status_dev, st)) return e;
+    const int e = launch_prefix_attention_q8(q, c, prefix_len, k_own, v_own, own_len, *a, plan, po, pl, out, lse, status_dev, st);
+    if (e != PSD_OK || (plan.tiles && plan.tile.fused)) return e;
     return launch_own_and_join(q, k_own, v_own, own_len, *a, po, pl, plan.splits, out, lse, st);
 }
 

@@ -362,13 +362,13 @@ int launch_r(const CUtensorMap& mk, const CUtensorMap& mv, const Q8Args& a, int6
 
 }  // namespace
 
-PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
+PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
     const int64_t rows = (int64_t)D * M * (Hq / Hkv);
     PrefixQ8Plan p = {};
     p.dhp = Dh <= 64 ? 64 : 128;
     p.tiles = rows > 32;
     if (p.tiles) {
-        p.tile = plan_prefix(B, D, M, Hq, Hkv, Dh, P, 0);
+        p.tile = plan_prefix(B, D, M, Hq, Hkv, Dh, P, S);
         p.splits = p.tile.splits;
         return p;
     }
@@ -385,8 +385,9 @@ PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P)
 
 static size_t partial_bytes_q8(int64_t rows, int dhp) { return ((size_t)rows * (dhp + 1) * 4 + 255) / 256 * 256; }
 
-size_t prefix_q8_needs(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
-    const PrefixQ8Plan p = plan_prefix_q8(B, D, M, Hq, Hkv, Dh, P);
+size_t prefix_q8_needs(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
+    const PrefixQ8Plan p = plan_prefix_q8(B, D, M, Hq, Hkv, Dh, P, S);
+    if (p.tiles && p.tile.fused) return 256;
     return partial_bytes_q8((int64_t)B * D * M * Hq * p.splits, p.dhp);
 }
 
@@ -404,9 +405,10 @@ size_t prefix_q8_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P) 
     return partial_bytes_q8(n, Dh <= 64 ? 64 : 128);
 }
 
-int launch_prefix_attention_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const psd_attention_t& a, const PrefixQ8Plan& p,
-                               float* po, float* pl, int32_t* status_dev, cudaStream_t st) {
-    if (p.tiles) return launch_prefix_tiles_q8(q, c, prefix_len, a, p.tile, po, pl, status_dev, st);
+int launch_prefix_attention_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const void* k_own, const void* v_own,
+                               const int32_t* own_len, const psd_attention_t& a, const PrefixQ8Plan& p, float* po, float* pl, void* out,
+                               float* lse, int32_t* status_dev, cudaStream_t st) {
+    if (p.tiles) return launch_prefix_tiles_q8(q, c, prefix_len, k_own, v_own, own_len, a, p.tile, po, pl, out, lse, status_dev, st);
     CUtensorMap mk, mv;
     if (!make_codes_map(&mk, c.k, a.kp, a.B, a.P, a.Hkv, a.Dh, p.dhp, kSlice) || !make_codes_map(&mv, c.v, a.vp, a.B, a.P, a.Hkv, a.Dh, p.dhp, kSlice))
         return PSD_ERR_CUDA;

@@ -20,17 +20,19 @@ struct PrefixQ8Plan {
     int splits;         // partial results per row
     int dhp;            // floats per partial output row: 64 or 128
 };
-PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P);
+PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S);
 // bytes of the partial results of a call, and of all calls with smaller B, D and P
-size_t prefix_q8_needs(int B, int D, int M, int Hq, int Hkv, int Dh, int P);
+size_t prefix_q8_needs(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S);
 size_t prefix_q8_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P);
 
-// Partial results of every row over its sequence's prefix, as launch_prefix_attention leaves them: po [splits][rows][dhp], pl
-// [splits][rows].
-int launch_prefix_attention_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const psd_attention_t& a, const PrefixQ8Plan& p,
-                               float* po, float* pl, int32_t* status_dev, cudaStream_t st);
+// plan.tiles && plan.tile.fused: final outputs into out and lse.  Otherwise partial results of every row over its sequence's prefix, as
+// launch_prefix_attention leaves them: po [splits][rows][dhp], pl [splits][rows].
+int launch_prefix_attention_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const void* k_own, const void* v_own,
+                               const int32_t* own_len, const psd_attention_t& a, const PrefixQ8Plan& p, float* po, float* pl, void* out,
+                               float* lse, int32_t* status_dev, cudaStream_t st);
 // prefix_attention_q8_tc.cu
-int launch_prefix_tiles_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const psd_attention_t& a, const PrefixPlan& p,
-                           float* po, float* pl, int32_t* status_dev, cudaStream_t st);
+int launch_prefix_tiles_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const void* k_own, const void* v_own,
+                           const int32_t* own_len, const psd_attention_t& a, const PrefixPlan& p, float* po, float* pl, void* out, float* lse,
+                           int32_t* status_dev, cudaStream_t st);
 
 }  // namespace psd

@@ -8,6 +8,9 @@
 // the values' scale multiplies the weights, which go to the product in fp16, relative to the largest value scale of the CTA's keys and up to 2^15.
 // Keys past the end are masked in the scores; their codes are finite, so their weights of 0 need no further care.
 //
+// Where the prefix is not split, the drafts' own 16-bit keys follow it as further tiles, as there: TMA brings them into the wide ring
+// directly, and before a stream's first of them its output is multiplied by the reference of the value scales, so that both kinds add up.
+//
 // Bound: for Dh = 128 products and exponentials as there (2048 cycles each per 256 rows x 128 keys); widening is about 600 issue slots
 // per scheduler of the same round, the values' scales 64 more per warp.
 #include "attn_tc.cuh"
@@ -24,6 +27,8 @@ constexpr float kHalfRoom = 7.0f;           // how far (log2) the reference is s
 constexpr int kMaxSorted = 128;             // sequences that are put in order of length
 constexpr int kBarBytes = 1024;
 
+struct OwnTile { int node, key0, len; };    // a tile of own keys: draft of the sequence, first key, the draft's length
+
 template <int SLABS> struct Rings { static constexpr int RAW = SLABS == 2 ? 2 : 4, WIDE = SLABS == 2 ? 4 : 8; };
 
 struct TcArgs {
@@ -36,6 +41,13 @@ struct TcArgs {
     int tq, n_qt, units, splits;
     int k_outer, k_head, v_outer, v_head;
     int B, longest_first;
+    // own keys and final outputs (fused == 1); else partial results
+    int fused, D, M, S, causal, own_box;
+    int ko_outer, ko_head, vo_outer, vo_head;
+    const int32_t* own_len;
+    void* out;
+    float* lse;
+    int64_t out_token, out_head;
     float c;
     long long wait_limit;
     int stall_test;
@@ -60,32 +72,39 @@ __device__ __forceinline__ uint32_t widen_pair(uint32_t x, uint32_t sel) {
 // three registers and constants.
 template <int SLABS, bool BF16>
 __device__ __forceinline__ void widen_tile(uint32_t raw, uint32_t to, int tid) {
-    constexpr int CH = SLABS * 8, KEYS = kWideners / CH, TURNS = (128 + KEYS - 1) / KEYS, BATCH = 6;
-    static_assert(KEYS % 4 == 0, "the swizzle of a thread's place");
+    constexpr int CH = SLABS * 8, KEYS = kWideners / CH, BATCH = 5, TURNS = 128 / KEYS, REST = 128 - TURNS * KEYS;
+    static_assert(KEYS % 4 == 0 && TURNS % BATCH == 0 && REST > 0 && REST < KEYS, "turns of a tile");
+    constexpr uint32_t FLIP = KEYS % 8 ? 64u : 0u;         // what a turn changes in the swizzle of this thread's place
     const int key = tid / CH, ch = tid % CH;
-    const uint32_t src = raw + tid * 8, row = to + (ch / 8) * kSlabBytes + key * 128, at = ((ch % 8) ^ (key & 7)) << 4;
-    const uint32_t dst[2] = {row + at, row + (KEYS % 8 ? at ^ 64u : at)};
-#pragma unroll
+    uint32_t src = raw + tid * 8, row = to + (ch / 8) * kSlabBytes + key * 128, at = ((ch % 8) ^ (key & 7)) << 4;
+    uint32_t w[BATCH][2];
+    auto load = [&](int i) { asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[i][0]), "=r"(w[i][1]) : "r"(src + i * (kWideners * 8))); };
+    auto store = [&](int i) {
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(row + (i & 1 ? at ^ FLIP : at) + i * KEYS * 128), "r"(widen_pair<BF16>(w[i][0], 0x1100)),
+                     "r"(widen_pair<BF16>(w[i][0], 0x3322)), "r"(widen_pair<BF16>(w[i][1], 0x1100)), "r"(widen_pair<BF16>(w[i][1], 0x3322)) : "memory");
+    };
+    // (a loop, not straight code: the kernel's instructions have to stay in the SM's cache beside the softmax)
+#pragma unroll 1
     for (int i0 = 0; i0 < TURNS; i0 += BATCH) {
-        uint32_t w[BATCH][2];
 #pragma unroll
-        for (int i = i0; i < i0 + BATCH && i < TURNS; ++i)
-            if ((i + 1) * KEYS <= 128 || i * KEYS + key < 128)
-                asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[i - i0][0]), "=r"(w[i - i0][1]) : "r"(src + i * (kWideners * 8)));
+        for (int i = 0; i < BATCH; ++i) load(i);
 #pragma unroll
-        for (int i = i0; i < i0 + BATCH && i < TURNS; ++i)
-            if ((i + 1) * KEYS <= 128 || i * KEYS + key < 128) {
-                const uint32_t lo = w[i - i0][0], hi = w[i - i0][1];
-                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dst[i & 1] + i * KEYS * 128), "r"(widen_pair<BF16>(lo, 0x1100)),
-                             "r"(widen_pair<BF16>(lo, 0x3322)), "r"(widen_pair<BF16>(hi, 0x1100)), "r"(widen_pair<BF16>(hi, 0x3322)) : "memory");
-            }
+        for (int i = 0; i < BATCH; ++i) store(i);
+        src += BATCH * kWideners * 8;
+        row += BATCH * KEYS * 128;
+        at ^= BATCH & 1 ? FLIP : 0u;
+    }
+    if (key < REST) {
+        load(0);
+        store(0);
     }
 }
 
 template <int SLABS, bool BF16>
 __global__ void __launch_bounds__(kQThreads, 1)
 prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                       const __grid_constant__ CUtensorMap map_v, const TcArgs a) {
+                       const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_ko,
+                       const __grid_constant__ CUtensorMap map_vo, const TcArgs a) {
     extern __shared__ __align__(1024) unsigned char smem[];
     constexpr int TILE = SLABS * kSlabBytes, RAW = TILE / 2, NR = Rings<SLABS>::RAW, NS = Rings<SLABS>::WIDE, DHP = SLABS * 64;
     unsigned char* q_tiles = smem;                                   // [2][TILE]
@@ -97,6 +116,8 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(never + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
     volatile int* sequence = abort_flag + 1;
+    int* n_own = const_cast<int*>(abort_flag) + 2;                  // [2] own tiles of the streams
+    OwnTile* own = reinterpret_cast<OwnTile*>(n_own + 2);            // [2][kMaxOwnTiles]
 
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const bool shared_keys = a.n_qt > 1;
@@ -146,40 +167,57 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         b = *sequence;
     }
     const int L = length(b), tiles = (L + 127) / 128;
+    if (a.fused) {
+        if (threadIdx.x < 2) {
+            // thread s lists the own tiles of stream s: the drafts whose tokens are in its query tile
+            const int s = threadIdx.x, first = (qt0 + s) * a.tq, last = min(a.T, first + a.tq) - 1;
+            int n = 0;
+            if (s < n_streams && a.S > 0)
+                for (int d = first / a.M; d <= last / a.M; ++d) {
+                    const int len = a.own_len ? min(max(a.own_len[(int64_t)b * a.D + d], 0), a.S) : a.S;
+                    for (int k0 = 0; k0 < len && n < kMaxOwnTiles; k0 += 128) own[s * kMaxOwnTiles + n++] = OwnTile{d, k0, len};
+                }
+            n_own[s] = n;
+        }
+        __syncthreads();
+    }
     auto share = [&](int x) { return (int)((long long)tiles * x / a.splits); };
     const int sp0 = shared_keys ? cs : cs * 2, sp1 = shared_keys ? cs : cs * 2 + 1;
     const int t00 = share(sp0), t01 = share(sp1);
-    const int nt0 = share(sp0 + 1) - t00, nt1 = n_streams > 1 ? share(sp1 + 1) - t01 : 0;
+    const int np0 = share(sp0 + 1) - t00, np1 = n_streams > 1 ? share(sp1 + 1) - t01 : 0;      // tiles of the prefix,
+    const int nt0 = np0 + (a.fused ? n_own[0] : 0), nt1 = np1 + (a.fused ? n_own[1] : 0);      // and with the stream's own
     const int most = max(nt0, nt1);
-    // Tiles in the order: per round j = -1, 0, ..: V of tile j, K of tile j + 1 for stream 0, then for stream 1; with shared keys
-    // they are listed for stream 0 only.
-    const int common = shared_keys ? nt0 : 0;
+    // Tiles in the order: per round j = -1, 0, ..: V of tile j, K of tile j + 1 for stream 0, then for stream 1; those
+    // below `common` are one for both streams and listed for stream 0 only.
+    const int common = shared_keys ? np0 : 0;
     auto listed = [&](int s, int j) { return j >= 0 && j < (s ? nt1 : nt0) && (s == 0 || j >= common); };
     const int n_q = shared_keys ? n_streams : 1;
 
-    if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
+    if (warp >= 8) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp >= 10) {
         // -------------------------------------------------------------------- widening
         const int tid = threadIdx.x - 10 * 32;
-        int item = 0;
+        int item = 0, in = 0;               // ring items, and those that come in codes
         bool ok = true;
 #pragma unroll 1
         for (int x = 0; ok && x < 4 * (most + 1); ++x) {
             const bool is_k = x & 1;
             const int s = (x >> 1) & 1, j = (x >> 2) - (is_k ? 0 : 1);
             if (!listed(s, j)) continue;
+            if (j >= (s ? np1 : np0)) { ++item; continue; }
             if (!(ok = mbar_wait_warp(&empty[item % NS], ((item / NS) & 1) ^ 1, wc))) break;
-            if (!(ok = mbar_wait_warp(&raw_full[item % NR], (item / NR) & 1, wc))) break;
-            const uint32_t from = smem_u32(raw + (item % NR) * RAW), to = smem_u32(ring + (item % NS) * TILE);
+            if (!(ok = mbar_wait_warp(&raw_full[in % NR], (in / NR) & 1, wc))) break;
+            const uint32_t from = smem_u32(raw + (in % NR) * RAW), to = smem_u32(ring + (item % NS) * TILE);
             if (BF16 && is_k) widen_tile<SLABS, true>(from, to, tid);
             else widen_tile<SLABS, false>(from, to, tid);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
-                mbar_arrive(&raw_empty[item % NR]);
+                mbar_arrive(&raw_empty[in % NR]);
                 mbar_arrive(&full[item % NS]);
             }
             ++item;
+            ++in;
         }
     } else if (warp >= 8) {
         if (warp == 8 && most > 0) {
@@ -191,19 +229,37 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     for (int c = 0; c < SLABS; ++c)
                         tma_load_3d(q_tiles + t * TILE + c * kSlabBytes, &map_q, q_full, c * kSlabElems, h * a.G, b * a.T + (qt0 + t) * a.tq);
             }
-            int item = 0;
+            int item = 0, in = 0, first_own = -1;
             bool ok = true;
 #pragma unroll 1
             for (int x = 0; ok && x < 4 * (most + 1); ++x) {
                 const bool is_k = x & 1;
-                const int s = (x >> 1) & 1, j = (x >> 2) - (is_k ? 0 : 1);
+                const int s = (x >> 1) & 1, j = (x >> 2) - (is_k ? 0 : 1), np = s ? np1 : np0;
                 if (!listed(s, j)) continue;
-                const int slot = item % NR;
-                if (!mbar_wait_warp(&raw_empty[slot], ((item / NR) & 1) ^ 1, wc)) { ok = false; break; }
-                if (leader) {
-                    mbar_arrive_expect_tx(&raw_full[slot], RAW);
-                    tma_load_4d(raw + slot * RAW, is_k ? &map_k : &map_v, &raw_full[slot], 0, h * (is_k ? a.k_head : a.v_head),
-                                ((s ? t01 : t00) + j) * 128, b * (is_k ? a.k_outer : a.v_outer));
+                if (j < np) {
+                    const int slot = in % NR;
+                    if (!mbar_wait_warp(&raw_empty[slot], ((in / NR) & 1) ^ 1, wc)) { ok = false; break; }
+                    if (leader) {
+                        mbar_arrive_expect_tx(&raw_full[slot], RAW);
+                        tma_load_4d(raw + slot * RAW, is_k ? &map_k : &map_v, &raw_full[slot], 0, h * (is_k ? a.k_head : a.v_head),
+                                    ((s ? t01 : t00) + j) * 128, b * (is_k ? a.k_outer : a.v_outer));
+                    }
+                    ++in;
+                } else {
+                    const int slot = item % NS;
+                    if (!mbar_wait_warp(&empty[slot], ((item / NS) & 1) ^ 1, wc)) { ok = false; break; }
+                    if (leader) {
+                        const OwnTile o = own[s * kMaxOwnTiles + j - np];
+                        const CUtensorMap* map = is_k ? &map_ko : &map_vo;
+                        // (this warp stands in for the widening ones)
+                        mbar_arrive_expect_tx(&full[slot], (uint32_t)(SLABS * a.own_box * 128));
+                        for (int i = 1; i < kWideners / 32; ++i) mbar_arrive(&full[slot]);
+#pragma unroll
+                        for (int c = 0; c < SLABS; ++c)
+                            tma_load_4d(ring + slot * TILE + c * kSlabBytes, map, &full[slot], c * kSlabElems, h * (is_k ? a.ko_head : a.vo_head),
+                                        o.key0, (b * a.D + o.node) * (is_k ? a.ko_outer : a.vo_outer));
+                    }
+                    if (first_own < 0) first_own = item;
                 }
                 ++item;
                 if (a.stall_test && item == 1 && !mbar_wait_warp(never, 0, wc)) ok = false;
@@ -212,26 +268,32 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 // giving up: no copy may be in flight when the CTA exits
                 long long c0 = clock64();
                 while (!mbar_try_wait(q_full, 0) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
-                for (int i = item > NR ? item - NR : 0; i < item; ++i) {
+                for (int i = in > NR ? in - NR : 0; i < in; ++i) {
                     c0 = clock64();
                     while (!mbar_try_wait(&raw_full[i % NR], (i / NR) & 1) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
+                }
+                for (int i = max(first_own, item - NS); first_own >= 0 && i < item; ++i) {
+                    c0 = clock64();
+                    while (!mbar_try_wait(&full[i % NS], (i / NS) & 1) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
                 }
             }
         } else if (warp == 9 && most > 0) {
             // ---------------------------------------------------------------- products (one warp, both streams in turn)
             const bool leader = elect_one();
             const uint32_t id_s = umma_idesc16(128, BF16, false), id_o = umma_idesc16((a.Dh + 15) / 16 * 16, false, true);
+            const uint32_t id_s_own = umma_idesc16(a.own_box, BF16, false), id_o_own = umma_idesc16((a.Dh + 15) / 16 * 16, BF16, true);
             const int k_steps = (a.Dh + 15) / 16;
             const uint64_t dq = umma_smem_desc(smem_u32(q_tiles)), dk = umma_smem_desc(smem_u32(ring));
             const uint64_t dv = umma_smem_desc_mn(smem_u32(ring), kSlabBytes);
             auto wait_item = [&](int item) { return mbar_wait_warp(&full[item % NS], (item / NS) & 1, wc); };
-            auto scores = [&](int s, int item, bool release) {
+            auto scores = [&](int s, int item, bool own_tile, bool release) {
                 const uint64_t q = dq + (uint64_t)((shared_keys ? s : 0) * (TILE >> 4)), k = dk + (uint64_t)((item % NS) * (TILE >> 4));
+                const uint32_t id = own_tile ? id_s_own : id_s;
 #pragma unroll
                 for (int i = 0; i < SLABS * 4; ++i)
                     if (i < k_steps) {
                         const uint64_t off = (i / 4) * (kSlabBytes >> 4) + (i % 4) * 2;
-                        umma_f16(tmem + s * 128, q + off, k + off, id_s, i != 0);
+                        umma_f16(tmem + s * 128, q + off, k + off, id, i != 0);
                     }
                 umma_commit(&s_full[s]);
                 if (release) umma_commit(&empty[item % NS]);
@@ -247,24 +309,40 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     if (!(ok = wait_item(k))) continue;
                 }
                 tc_fence_after();
-                if (leader) scores(s, k, common == 0 || s == n_streams - 1);
+                if (leader) scores(s, k, (s ? np1 : np0) == 0, common == 0 || s == n_streams - 1);
             }
 #pragma unroll 1
             for (int j = 0; ok && j < most; ++j) {
-#pragma unroll
+#pragma unroll 1
                 for (int s = 0; s < 2; ++s) {
-                    const int n = s ? nt1 : nt0;
+                    const int n = s ? nt1 : nt0, np = s ? np1 : np0;
                     if (!ok || j >= n) continue;
                     const bool more = j + 1 < n;
                     if (listed(s, j)) { v = next++; ok = wait_item(v); }
                     if (ok && listed(s, j + 1)) { k = next++; ok = wait_item(k); }
                     if (!ok || !(ok = mbar_wait_warp(&p_half[s], j & 1, wc))) continue;
                     tc_fence_after();
-                    const int left = L - ((s ? t01 : t00) + j) * 128, steps = left >= 128 ? 8 : (left + 15) / 16;
+                    // keys of this tile in steps of 16 (the last tile of a list may hold fewer); rows of other drafts stay
+                    int left = L - ((s ? t01 : t00) + j) * 128;
+                    uint32_t off[4] = {0u, 0u, 0u, 0u};
+                    if (j >= np) {
+                        const OwnTile o = own[s * kMaxOwnTiles + j - np];
+                        left = o.len - o.key0;
+                        const int lo = (o.node * a.M - (qt0 + s) * a.tq) * a.G, hi = lo + a.M * a.G;
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const int l0 = min(max(lo - w * 32, 0), 32), h0 = min(max(hi - w * 32, 0), 32);     // active rows [l0, h0)
+                            const uint32_t below_h = h0 == 32 ? 0xffffffffu : (1u << h0) - 1u, below_l = l0 == 32 ? 0xffffffffu : (1u << l0) - 1u;
+                            off[w] = ~(below_h & ~below_l);
+                        }
+                    }
+                    const int steps = left >= 128 ? 8 : (left + 15) / 16;
                     const uint64_t vd = dv + (uint64_t)((v % NS) * (TILE >> 4));
                     const uint32_t t_s = tmem + s * 128, t_o = t_s + 256;
                     auto pv = [&](int i) {
-                        if (i < steps) umma_f16_ts(t_o, t_s + i * 8, vd + (uint64_t)(i * (2048 >> 4)), id_o, (j | i) != 0);
+                        if (i >= steps) return;
+                        // (O was set to 0 if np == 0)
+                        umma_f16_ts_rows(t_o, t_s + i * 8, vd + (uint64_t)(i * (2048 >> 4)), j < np ? id_o : id_o_own, off, j >= np || (j | i) != 0);
                     };
                     if (leader) { pv(0); pv(1); pv(2); pv(3); }
                     if (!(ok = mbar_wait_warp(&p_ready[s], j & 1, wc))) continue;
@@ -272,7 +350,7 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     if (leader) {
                         pv(4); pv(5); pv(6); pv(7);
                         // the scores of the next tile overwrite the weights just read; their commit covers PV as well
-                        if (more) scores(s, k, j + 1 >= common || s == n_streams - 1);
+                        if (more) scores(s, k, j + 1 >= np, j + 1 >= common || s == n_streams - 1);
                         else umma_commit(&o_done[s]);
                         if (j >= common || s == n_streams - 1) umma_commit(&empty[v % NS]);
                     }
@@ -287,51 +365,72 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         __syncwarp();
     } else {
         // -------------------------------------------------------------------- softmax: a row per thread
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         const int s = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
         float m = 0.f, l = 0.f;          // reference (in the exponent's units) and sum relative to it
         bool fresh = true;               // no score seen yet
         bool ok = true;
-        const int n = s ? nt1 : nt0, first_tile = s ? t01 : t00;
-        const int my_tok = (qt0 + (shared_keys ? s : 0)) * a.tq + row / a.G;
+        const int n = s ? nt1 : nt0, np = s ? np1 : np0, first_tile = s ? t01 : t00;
+        const int my_tok = (qt0 + (shared_keys ? s : 0)) * a.tq + row / a.G;                     // this row's token of the sequence,
+        const int my_node = a.fused ? my_tok / a.M : 0, my_i = a.fused ? my_tok % a.M : 0;       // its draft and place in it
         // Scales of a tile: lane i holds the keys' of columns 16 i .., lane 8 + i the values', relative to the largest of this stream's
         // keys.  They are loaded a round ahead.
         const float* ks = a.k_scale + ((int64_t)b * a.Hkv + h) * a.nb;
         const float* vs = a.v_scale + ((int64_t)b * a.Hkv + h) * a.nb;
         float vref = 1.17549435e-38f;
-        if (n > 0) {
-            const int j1 = min(((first_tile + n) * 128 - 1) >> a.shift, (L - 1) >> a.shift);
+        if (np > 0) {
+            const int j1 = min(((first_tile + np) * 128 - 1) >> a.shift, (L - 1) >> a.shift);
             for (int j = ((first_tile * 128) >> a.shift) + lane; j <= j1; j += 32) vref = fmaxf(vref, vs[j]);
 #pragma unroll
             for (int x = 16; x; x >>= 1) vref = fmaxf(vref, __shfl_xor_sync(0xffffffffu, vref, x));
         }
         const float vinv = 1.f / vref;
         auto scale_of = [&](int j) {
+            if (j >= np) return lane & 8 ? 1.f : a.c;       // own keys
             const int key = (first_tile + j) * 128 + (lane & 7) * 16;
             if (key >= L) return 0.f;                   // (what stands there was never written)
             const float x = lane & 8 ? vs[key >> a.shift] * vinv : ks[key >> a.shift] * a.c;
             return lane & 8 || x != 0.f ? x : 1.17549435e-38f;      // masked scores are -inf times this
         };
         float next_scale = n > 0 ? scale_of(0) : 0.f;
-        for (int j = 0; j < n; ++j) {
+        if (n > 0 && np == 0) {
+            // only own tiles, each for some of the rows: O begins at 0
+            uint32_t zero[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) zero[i] = 0u;
+            for (int c = 0; c < a.Dh; c += 32) tmem_st32(t_o + c, zero);
+            tmem_wait_st();
+        }
+        int base = listed(0, 0) + listed(1, 0);      // ring items ahead of round j
+        // One tile.  FULL: 128 keys of the prefix, seen by every row; else the prefix's last keys or own ones.  The two are compiled apart:
+        // the walk over full tiles is most of the time, and its instructions have to stay in the SM's cache beside the other warps'.
+        auto tile = [&](int j, auto full_tile) {
+            constexpr bool FULL = decltype(full_tile)::value;
+            const bool own_tile = !FULL && j >= np;
             const float sc = next_scale;
             if (j + 1 < n) next_scale = scale_of(j + 1);
-            if (!(ok = mbar_wait_warp(&s_full[s], j & 1, wc))) break;
+            if (!mbar_wait_warp(&s_full[s], j & 1, wc)) return false;
             tc_fence_after();
-            const int left = L - (first_tile + j) * 128;   // keys of this tile
+            int left = L - (first_tile + j) * 128;   // keys of this tile,
+            int lim = left;                          // and those that this row sees
+            if (own_tile) {
+                const OwnTile o = own[s * kMaxOwnTiles + j - np];
+                left = o.len - o.key0;
+                lim = my_node != o.node ? 0 : a.causal ? min(left, left - a.M + 1 + my_i) : left;
+            }
             uint32_t r[4][32];
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_ld32(t_s + c * 32, r[c]);
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_wait_ld(r[c]);
-            if (left < 128) {
+            if (!FULL) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
                     for (int i = 0; i < 32; ++i)
-                        if (c * 32 + i >= left) r[c][i] = 0xff800000u;
+                        if (c * 32 + i >= lim) r[c][i] = 0xff800000u;
             }
             float high = -INFINITY;
 #pragma unroll
@@ -347,12 +446,14 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             // the reference that this tile's maximum asks for
             const float top = high - kHalfRoom;
             const bool raise = top > (fresh ? -INFINITY : m + kRaise);
-            if (__any_sync(0xffffffffu, raise)) {
+            const bool unit = own_tile && j == np && j > 0;        // from here on outputs are relative to 1, not to vref
+            if (unit || __any_sync(0xffffffffu, raise)) {
                 const bool rescale = raise && !fresh;
-                const float f = rescale ? ex2(m - top) : 1.f;
+                float f = rescale ? ex2(m - top) : 1.f;
                 if (raise) { m = top; fresh = false; }
                 l *= f;
-                if (__any_sync(0xffffffffu, rescale))
+                if (unit) f *= vref;
+                if (unit || __any_sync(0xffffffffu, rescale))
 #pragma unroll 1
                 for (int c = 0; c < a.Dh; c += 8) {
                     uint32_t o[8];
@@ -368,6 +469,18 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                                  : "memory");
                 }
             }
+            if (own_tile && left < 128) {
+                // own values past the end that the product's last step of 16 keys reads: zero, whatever stands there
+                const int item = base + (s && j >= common ? listed(0, j) + listed(0, j + 1) : 0);
+                if (!mbar_wait_warp(&full[item % NS], (item / NS) & 1, wc)) return false;
+                const int stop = (left + 15) / 16 * 16;
+                unsigned char* v = ring + (item % NS) * TILE;
+                for (int x = left * 8 * SLABS + row; x < stop * 8 * SLABS; x += 128) {
+                    const int key = x / (8 * SLABS), ch = x % (8 * SLABS);
+                    *reinterpret_cast<uint4*>(v + (ch / 8) * kSlabBytes + key * 128 + (ch % 8) * 16) = make_uint4(0, 0, 0, 0);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
             const f32x2 nm = pack2(-m, -m);
             f32x2 acc[2] = {0ull, 0ull};
 #pragma unroll
@@ -377,7 +490,7 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 for (int g = 0; g < 2; ++g) {
                     float kf = __shfl_sync(0xffffffffu, sc, 2 * c + g);
                     const float vf = __shfl_sync(0xffffffffu, sc, 8 + 2 * c + g);
-                    if (kf == 0.f) kf = 1.f;               // no key among these 16: their scores are -inf
+                    if (!FULL && kf == 0.f) kf = 1.f;      // no key among these 16: their scores are -inf
                     const f32x2 kk = pack2(kf, kf), vv = pack2(vf, vf);
 #pragma unroll
                     for (int i = g * 8; i < g * 8 + 8; ++i) {
@@ -385,7 +498,9 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                         acc[i & 1] = add2(acc[i & 1], e);
                         float y, z;
                         unpack2(mul2(e, vv), y, z);
-                        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p[i]) : "f"(z), "f"(y));
+                        // (own values are of the queries' type)
+                        if (!FULL && BF16 && own_tile) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(p[i]) : "f"(z), "f"(y));
+                        else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(p[i]) : "f"(z), "f"(y));
                     }
                 }
                 tmem_st16(t_s + c * 16, p);
@@ -399,16 +514,50 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             float l0, l1;
             unpack2(add2(acc[0], acc[1]), l0, l1);
             l += l0 + l1;
-        }
+            base += listed(0, j) + listed(0, j + 1) + listed(1, j) + listed(1, j + 1);
+            return true;
+        };
+        int j = 0;
+#pragma unroll 1
+        for (const int n_full = min(np, L / 128 - first_tile); ok && j < n_full; ++j) ok = tile(j, std::true_type());
+#pragma unroll 1
+        for (; ok && j < n; ++j) ok = tile(j, std::false_type());
         if (s < n_streams) {
             const bool live = row < a.tq * a.G && my_tok < a.T;
             if (n > 0 && ok) {
                 ok = mbar_wait_warp(&o_done[s], 0, wc);
                 tc_fence_after();
             }
-            const float inv = fresh && l == 0.f ? 0.f : vref / l;
-            if (ok) {
-                const int64_t at = (int64_t)(s ? sp1 : sp0) * a.rows + ((int64_t)b * a.T + my_tok) * a.Hq + h * a.G + row % a.G;
+            const bool none = fresh && l == 0.f;             // no key seen
+            const float inv = none ? 0.f : (np < n ? 1.f : vref) / l;
+            const int64_t tok = (int64_t)b * a.T + my_tok;
+            const int head = h * a.G + row % a.G;
+            if (ok && a.fused) {
+                uint16_t* o = reinterpret_cast<uint16_t*>(a.out) + tok * a.out_token + (int64_t)head * a.out_head;
+#pragma unroll 1
+                for (int c = 0; c < a.Dh; c += 32) {
+                    uint32_t x[32];
+                    if (n > 0) {
+                        tmem_ld32(t_o + c, x);
+                        tmem_wait_ld(x);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; i += 8)
+                        if (live && c + i < a.Dh) {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) {
+                                const float lo = __uint_as_float(x[i + 2 * q]) * inv, hi = __uint_as_float(x[i + 2 * q + 1]) * inv;
+                                if (BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y[q]) : "f"(hi), "f"(lo));
+                                else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y[q]) : "f"(hi), "f"(lo));
+                                if (none) y[q] = 0u;
+                            }
+                            *reinterpret_cast<uint4*>(o + c + i) = make_uint4(y[0], y[1], y[2], y[3]);
+                        }
+                }
+                if (live && a.lse) a.lse[tok * a.Hq + head] = none ? -INFINITY : m * kLn2 + logf(l);
+            } else if (ok) {
+                const int64_t at = (int64_t)(s ? sp1 : sp0) * a.rows + tok * a.Hq + head;
                 float* o = a.po + at * DHP;
 #pragma unroll 1
                 for (int c = 0; n > 0 && c < a.Dh; c += 32) {
@@ -452,14 +601,14 @@ bool make_tile_map(CUtensorMap* m, const void* base, const psd_kv_strides_t& s, 
 }
 
 template <int SLABS, bool BF16>
-int launch_t(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const TcArgs& a, int64_t grid, cudaStream_t st) {
+int launch_t(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mko, const CUtensorMap& mvo, const TcArgs& a, int64_t grid, cudaStream_t st) {
     constexpr int TILE = SLABS * kSlabBytes;
     constexpr int smem = (2 + Rings<SLABS>::WIDE) * TILE + Rings<SLABS>::RAW * (TILE / 2) + kBarBytes;
     static_assert(smem <= 227 * 1024, "shared memory of the 8-bit tile kernel");
     static std::atomic<unsigned long long> set{0};
     if (!ensure_dynamic_smem(prefix_tiles_q8_kernel<SLABS, BF16>, smem, set)) return PSD_ERR_CUDA;
-    static std::atomic<int> regs{0};      // 8 warps of 208 and 8 of 48 registers a thread
-    if (!launched_with(prefix_tiles_q8_kernel<SLABS, BF16>, (256 * 208 + 256 * 48) / kQThreads, regs)) return PSD_ERR_CUDA;
+    static std::atomic<int> regs{0};      // 8 warps of 192 and 8 of 64 registers a thread
+    if (!launched_with(prefix_tiles_q8_kernel<SLABS, BF16>, (256 * 192 + 256 * 64) / kQThreads, regs)) return PSD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(kQThreads);
@@ -470,19 +619,29 @@ int launch_t(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv
     attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, prefix_tiles_q8_kernel<SLABS, BF16>, mq, mk, mv, a);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, prefix_tiles_q8_kernel<SLABS, BF16>, mq, mk, mv, mko, mvo, a);
     count_launch();
     return e == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
 }
 
 }  // namespace
 
-int launch_prefix_tiles_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const psd_attention_t& a, const PrefixPlan& p,
-                           float* po, float* pl, int32_t* status_dev, cudaStream_t st) {
-    CUtensorMap mq, mk, mv;
+int launch_prefix_tiles_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const void* k_own, const void* v_own,
+                           const int32_t* own_len, const psd_attention_t& a, const PrefixPlan& p, float* po, float* pl, void* out, float* lse,
+                           int32_t* status_dev, cudaStream_t st) {
+    CUtensorMap mq, mk, mv, mko, mvo;
     if (!make_query_map(&mq, q, a, p.tq) || !make_tile_map(&mk, c.k, a.kp, a.B, a.P, a.Hkv, a.Dh, p.dhp) ||
         !make_tile_map(&mv, c.v, a.vp, a.B, a.P, a.Hkv, a.Dh, p.dhp))
         return PSD_ERR_CUDA;
+    const int own_box = a.S >= 128 ? 128 : (a.S + 15) / 16 * 16;
+    if (p.fused && a.S > 0) {
+        if (!make_cache_map(&mko, k_own, a.dtype, a.ko, a.B * a.D, a.S, a.Hkv, a.Dh, own_box) ||
+            !make_cache_map(&mvo, v_own, a.dtype, a.vo, a.B * a.D, a.S, a.Hkv, a.Dh, own_box))
+            return PSD_ERR_CUDA;
+    } else {
+        mko = mk;
+        mvo = mv;
+    }
     const int64_t grid = (int64_t)a.B * a.Hkv * p.units * (p.n_qt > 1 ? p.splits : p.splits / 2);
     if (grid > INT32_MAX) return PSD_ERR_SHAPE;
     TcArgs x = {};
@@ -499,12 +658,19 @@ int launch_prefix_tiles_q8(const void* q, const PrefixQ8& c, const int32_t* pref
     x.v_outer = a.vp.outer ? 1 : 0; x.v_head = a.vp.head ? 1 : 0;
     x.B = a.B;
     x.longest_first = prefix_len && a.B > 1 && a.B <= kMaxSorted && grid > sm_count() ? 1 : 0;
+    x.fused = p.fused ? 1 : 0;
+    x.D = a.D; x.M = a.M; x.S = a.S; x.causal = a.causal; x.own_box = own_box > 0 ? own_box : 16;
+    x.ko_outer = a.ko.outer ? 1 : 0; x.ko_head = a.ko.head ? 1 : 0;
+    x.vo_outer = a.vo.outer ? 1 : 0; x.vo_head = a.vo.head ? 1 : 0;
+    x.own_len = own_len;
+    x.out = out; x.lse = lse;
+    x.out_token = a.out_token; x.out_head = a.out_head;
     x.c = a.scale * kLog2e;
     x.wait_limit = wait_limit_cycles();
     x.stall_test = selftest_stall();
     const bool bf16 = a.dtype == PSD_BF16;
-    if (p.dhp == 64) return bf16 ? launch_t<1, true>(mq, mk, mv, x, grid, st) : launch_t<1, false>(mq, mk, mv, x, grid, st);
-    return bf16 ? launch_t<2, true>(mq, mk, mv, x, grid, st) : launch_t<2, false>(mq, mk, mv, x, grid, st);
+    if (p.dhp == 64) return bf16 ? launch_t<1, true>(mq, mk, mv, mko, mvo, x, grid, st) : launch_t<1, false>(mq, mk, mv, mko, mvo, x, grid, st);
+    return bf16 ? launch_t<2, true>(mq, mk, mv, mko, mvo, x, grid, st) : launch_t<2, false>(mq, mk, mv, mko, mvo, x, grid, st);
 }
 
 }  // namespace psd
