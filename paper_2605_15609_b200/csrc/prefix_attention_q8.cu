@@ -4,8 +4,8 @@
 //
 // Codes are whole numbers up to 127 and so exact in either 16-bit type: they are widened on the way to the tensor instructions, with
 // nothing rounded, the keys' scale multiplies a score and the values' scale a weight.  Weights go to the product in fp16 whatever
-// the queries' type (their rounding is 2^-11 then), relative to 2^15 of the row's maximum and to the largest value scale of the
-// CTA's keys, so that none is off by more than 2^-40 of the largest beside its rounding.
+// the queries' type (their rounding is 2^-11 then), 2^7 to 2^15 times as large as relative to the row's maximum, and relative to the
+// largest value scale of the CTA's keys, so that none is off by more than 2^-32 of the largest beside its rounding.
 //
 // A CTA takes 16 or 32 rows (query tokens times the heads of one key head) and a range of keys; its four warps go through slices of 32 keys
 // by themselves, each with a ring of its own that TMA fills, a running maximum and sums, and are joined at the end.  No barrier
@@ -24,7 +24,8 @@ namespace {
 constexpr int kThreads = 128;
 constexpr int kSlice = 32;           // keys a warp takes at a time
 constexpr int kStages = 2;           // slices in a warp's ring
-constexpr float kRoom = 15.f;
+constexpr float kRaise = 8.f;        // growth of a row's maximum (log2) that raises its reference
+constexpr float kRoom = 7.f;         // how far (log2) weights are kept above the reference: up to 2^15
 
 struct Q8Args {
     const void* q;
@@ -38,6 +39,7 @@ struct Q8Args {
     float c;                         // scale * log2 e
     long long wait_limit;
     int stall_test;
+    uint32_t f16_codes, bf16_codes;  // kF16Codes, kBf16Codes
 };
 
 __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -48,19 +50,6 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// The codes in bytes 0 and 2 of x as two fp16 numbers: 1024 + (code + 128) is the pattern 0x6400 + (byte ^ 0x80); minus 1152.
-__device__ __forceinline__ uint32_t codes_f16(uint32_t x) {
-    uint32_t r;
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"((x & 0x00ff00ffu) ^ 0x64806480u), "r"(0x64806480u));
-    return r;
-}
-// The same in bf16, whose 7 bits of fraction hold 128 + the code's low 7 bits: minus 128, or 256 where the sign bit is set.
-__device__ __forceinline__ uint32_t codes_bf16(uint32_t x) {
-    uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"((x & 0x007f007fu) | 0x43004300u), "r"((x & 0x00800080u) | 0x43004300u));
-    return r;
-}
-
 template <int DHP, int RB, bool BF16>
 __global__ void __launch_bounds__(kThreads, RB == 1 ? 3 : 2)
 prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const Q8Args a) {
@@ -146,6 +135,7 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
         m[rb][0] = m[rb][1] = -INFINITY;
         l[rb][0] = l[rb][1] = 0.f;
     }
+    const uint32_t f16_codes = a.f16_codes, bf16_codes = a.bf16_codes;
     bool ok = true;
     int i = 0;
 #pragma unroll 1
@@ -168,7 +158,8 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    const uint32_t b0 = BF16 ? codes_bf16(w[x]) : codes_f16(w[x]), b1 = BF16 ? codes_bf16(w[x] >> 8) : codes_f16(w[x] >> 8);
+                    const uint32_t b0 = BF16 ? codes_bf16(w[x], bf16_codes) : codes_f16(w[x], f16_codes);
+                    const uint32_t b1 = BF16 ? codes_bf16(w[x] >> 8, bf16_codes) : codes_f16(w[x] >> 8, f16_codes);
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) {
                         if (BF16) mma_bf16(s[rb][nt], qf[rb][c * 4 + x], b0, b1);
@@ -186,24 +177,31 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[rb][nt][e] *= ks;
-                    if (left < kSlice && nt * 8 + 2 * t + (e & 1) >= left) s[rb][nt][e] = -INFINITY;
-                }
+                for (int e = 0; e < 4; ++e) s[rb][nt][e] *= ks;
         }
+        if (left < kSlice) {
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+                for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (nt * 8 + 2 * t + (e & 1) >= left) s[rb][nt][e] = -INFINITY;
+        }
+        // the reference of a row is raised, and what has been summed rescaled, only when its maximum grew by 2^kRaise
         bool higher = false;
         float top[RB][2];
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                float x = m[rb][u];
+                float x = fmaxf(s[rb][0][2 * u], s[rb][0][2 * u + 1]);
 #pragma unroll
-                for (int nt = 0; nt < 4; ++nt) x = max3(x, s[rb][nt][2 * u], s[rb][nt][2 * u + 1]);
+                for (int nt = 1; nt < 4; ++nt) x = max3(x, s[rb][nt][2 * u], s[rb][nt][2 * u + 1]);
                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
                 x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
                 top[rb][u] = x;
-                higher |= x > m[rb][u];
+                higher |= x > m[rb][u] + kRaise;
             }
         if (__any_sync(0xffffffffu, higher)) {
 #pragma unroll
@@ -211,8 +209,9 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 float f[2];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    f[u] = m[rb][u] == top[rb][u] ? 1.f : ex2(m[rb][u] - top[rb][u]);
-                    m[rb][u] = top[rb][u];
+                    const bool raise = top[rb][u] > m[rb][u] + kRaise;
+                    f[u] = raise ? ex2(m[rb][u] - top[rb][u]) : 1.f;
+                    if (raise) m[rb][u] = top[rb][u];
                     l[rb][u] *= f[u];
                 }
 #pragma unroll
@@ -254,7 +253,8 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
                     const int sel = y | y << 4 | (4 + y) << 8 | (4 + y) << 12;
-                    const uint32_t b0 = codes_f16(__byte_perm(w[0][x], w[1][x], sel)), b1 = codes_f16(__byte_perm(w[2][x], w[3][x], sel));
+                    const uint32_t b0 = codes_f16(__byte_perm(w[0][x], w[1][x], sel), f16_codes);
+                    const uint32_t b1 = codes_f16(__byte_perm(w[2][x], w[3][x], sel), f16_codes);
 #pragma unroll
                     for (int rb = 0; rb < RB; ++rb) mma_f16(o[rb][x * 4 + y], pa[rb][kb], b0, b1);
                 }
@@ -376,6 +376,12 @@ PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P,
     p.units = (int)((rows + 16 * p.row_blocks - 1) / (16 * p.row_blocks));
     const int64_t ctas = (int64_t)B * Hkv * p.units, want = (int64_t)sm_count() * (p.row_blocks == 1 ? 3 : 2);
     int64_t s = want / ctas;
+    if (s < 4) {
+        // few CTAs per slot: several waves of shorter ones, unless they get short
+        int64_t waves = (4 * want + ctas - 1) / ctas;
+        if (waves > P / 1024) waves = P / 1024;
+        if (waves > s) s = waves;
+    }
     const int64_t most = (P + 8 * kSlice - 1) / (8 * kSlice);      // two slices per warp
     if (s > most) s = most;
     if (s > kMaxPrefixSplits) s = kMaxPrefixSplits;
@@ -400,7 +406,7 @@ size_t prefix_q8_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P) 
     if (most > kMaxPrefixSplits) most = kMaxPrefixSplits;
     if (most < 2) most = 2;
     int64_t n = rows > pairs ? rows : pairs;
-    if (n < once) n = once;
+    n += once;
     if (n > rows * most) n = rows * most;
     return partial_bytes_q8(n, Dh <= 64 ? 64 : 128);
 }
@@ -431,6 +437,8 @@ int launch_prefix_attention_q8(const void* q, const PrefixQ8& c, const int32_t* 
     x.c = a.scale * kLog2e;
     x.wait_limit = wait_limit_cycles();
     x.stall_test = selftest_stall();
+    x.f16_codes = kF16Codes;
+    x.bf16_codes = kBf16Codes;
     const bool bf16 = a.dtype == PSD_BF16;
     auto go = [&](auto dhp, auto rb) {
         return bf16 ? launch_r<decltype(dhp)::value, decltype(rb)::value, true>(mk, mv, x, grid, st)

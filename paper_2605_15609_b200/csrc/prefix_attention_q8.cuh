@@ -5,6 +5,25 @@
 
 namespace psd {
 
+// Widening of codes, two at a time.  `pattern` holds kF16Codes or kBf16Codes in a register (it comes with the kernel's arguments): with two
+// constants the compiler makes two instructions of "and, then xor".
+constexpr uint32_t kF16Codes = 0x64806480u, kBf16Codes = 0x43004300u;
+// The codes in bytes 0 and 2 of x as two fp16 numbers: 1024 + (code + 128) is the pattern 0x6400 + (byte ^ 0x80); minus 1152.
+__device__ __forceinline__ uint32_t codes_f16(uint32_t x, uint32_t pattern) {
+    uint32_t t, r;
+    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(t) : "r"(x), "n"(0x00ff00ff), "r"(pattern));      // (x & mask) ^ pattern
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(t), "r"(pattern));
+    return r;
+}
+// The same in bf16, whose 7 bits of fraction hold 128 + the code's low 7 bits: minus 128, or 256 where the sign bit is set.
+__device__ __forceinline__ uint32_t codes_bf16(uint32_t x, uint32_t pattern) {
+    uint32_t t, u, r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(t) : "r"(x), "n"(0x007f007f), "r"(pattern));      // (x & mask) | pattern
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(u) : "r"(x), "n"(0x00800080), "r"(pattern));
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(t), "r"(u));
+    return r;
+}
+
 struct PrefixQ8 {
     const int8_t *k, *v;             // codes
     const float *k_scale, *v_scale;  // [B, Hkv, ceil(P / block)]

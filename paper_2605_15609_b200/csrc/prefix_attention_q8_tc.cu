@@ -51,6 +51,7 @@ struct TcArgs {
     float c;
     long long wait_limit;
     int stall_test;
+    uint32_t f16_codes, bf16_codes;
 };
 
 __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
@@ -58,20 +59,17 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
-// The codes in bytes (b, b + 1) of x as two 16-bit numbers (see prefix_attention_q8.cu for the patterns).
+// The codes in bytes (b, b + 1) of x as two 16-bit numbers; sel spreads them over bytes 0 and 2.
 template <bool BF16>
-__device__ __forceinline__ uint32_t widen_pair(uint32_t x, uint32_t sel) {
+__device__ __forceinline__ uint32_t widen_pair(uint32_t x, uint32_t sel, uint32_t pattern) {
     const uint32_t t = __byte_perm(x, 0u, sel);
-    uint32_t r;
-    if (BF16) asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"((t & 0x007f007fu) | 0x43004300u), "r"((t & 0x00800080u) | 0x43004300u));
-    else asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"((t & 0x00ff00ffu) ^ 0x64806480u), "r"(0x64806480u));
-    return r;
+    return BF16 ? codes_bf16(t, pattern) : codes_f16(t, pattern);
 }
 // One tile of 128 keys x SLABS * 64 codes (rows dense) into SLABS swizzled slabs, by kWideners threads, 8 codes at a time.  A thread's
 // place in a key's row is the same in every turn; its key moves by 12 (or 24), so the swizzle of its place takes two values: addresses are
 // three registers and constants.
 template <int SLABS, bool BF16>
-__device__ __forceinline__ void widen_tile(uint32_t raw, uint32_t to, int tid) {
+__device__ __forceinline__ void widen_tile(uint32_t raw, uint32_t to, int tid, uint32_t pattern) {
     constexpr int CH = SLABS * 8, KEYS = kWideners / CH, BATCH = 5, TURNS = 128 / KEYS, REST = 128 - TURNS * KEYS;
     static_assert(KEYS % 4 == 0 && TURNS % BATCH == 0 && REST > 0 && REST < KEYS, "turns of a tile");
     constexpr uint32_t FLIP = KEYS % 8 ? 64u : 0u;         // what a turn changes in the swizzle of this thread's place
@@ -80,8 +78,8 @@ __device__ __forceinline__ void widen_tile(uint32_t raw, uint32_t to, int tid) {
     uint32_t w[BATCH][2];
     auto load = [&](int i) { asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[i][0]), "=r"(w[i][1]) : "r"(src + i * (kWideners * 8))); };
     auto store = [&](int i) {
-        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(row + (i & 1 ? at ^ FLIP : at) + i * KEYS * 128), "r"(widen_pair<BF16>(w[i][0], 0x1100)),
-                     "r"(widen_pair<BF16>(w[i][0], 0x3322)), "r"(widen_pair<BF16>(w[i][1], 0x1100)), "r"(widen_pair<BF16>(w[i][1], 0x3322)) : "memory");
+        asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(row + (i & 1 ? at ^ FLIP : at) + i * KEYS * 128), "r"(widen_pair<BF16>(w[i][0], 0x1100, pattern)),
+                     "r"(widen_pair<BF16>(w[i][0], 0x3322, pattern)), "r"(widen_pair<BF16>(w[i][1], 0x1100, pattern)), "r"(widen_pair<BF16>(w[i][1], 0x3322, pattern)) : "memory");
     };
     // (a loop, not straight code: the kernel's instructions have to stay in the SM's cache beside the softmax)
 #pragma unroll 1
@@ -208,8 +206,8 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             if (!(ok = mbar_wait_warp(&empty[item % NS], ((item / NS) & 1) ^ 1, wc))) break;
             if (!(ok = mbar_wait_warp(&raw_full[in % NR], (in / NR) & 1, wc))) break;
             const uint32_t from = smem_u32(raw + (in % NR) * RAW), to = smem_u32(ring + (item % NS) * TILE);
-            if (BF16 && is_k) widen_tile<SLABS, true>(from, to, tid);
-            else widen_tile<SLABS, false>(from, to, tid);
+            if (BF16 && is_k) widen_tile<SLABS, true>(from, to, tid, a.bf16_codes);
+            else widen_tile<SLABS, false>(from, to, tid, a.f16_codes);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
@@ -668,6 +666,8 @@ int launch_prefix_tiles_q8(const void* q, const PrefixQ8& c, const int32_t* pref
     x.c = a.scale * kLog2e;
     x.wait_limit = wait_limit_cycles();
     x.stall_test = selftest_stall();
+    x.f16_codes = kF16Codes;
+    x.bf16_codes = kBf16Codes;
     const bool bf16 = a.dtype == PSD_BF16;
     if (p.dhp == 64) return bf16 ? launch_t<1, true>(mq, mk, mv, mko, mvo, x, grid, st) : launch_t<1, false>(mq, mk, mv, mko, mvo, x, grid, st);
     return bf16 ? launch_t<2, true>(mq, mk, mv, mko, mvo, x, grid, st) : launch_t<2, false>(mq, mk, mv, mko, mvo, x, grid, st);
