@@ -667,7 +667,7 @@ int psd_rope_frequencies(int32_t rotary, double base, int32_t kind, double facto
 /* Shapes of psd_rotate_qk. */
 typedef struct psd_rotate_t {
     int32_t n_tokens;     /* T >= 1                                                                          */
-    int32_t Hq, Hkv, Dh;  /* heads, >= 0, not both 0 (0: q, or k and v, are not read); 8 <= Dh <= 128, Dh % 8 == 0 */
+    int32_t Hq, Hkv, Dh;  /* heads, 0 .. 16384, not both 0 (0: q, or k and v, are not read); 8 <= Dh <= 128, Dh % 8 == 0 */
     int32_t dtype;        /* PSD_BF16 or PSD_FP16: q, k, v, weights and outputs                               */
     int32_t rotary;       /* the first `rotary` numbers of a head are rotated: even, 0 .. Dh                  */
     int32_t interleaved;  /* pairs: 0 (j, j + rotary/2), 1 (2j, 2j + 1)                                       */

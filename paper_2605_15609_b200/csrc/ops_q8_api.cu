@@ -53,7 +53,7 @@ int psd_rotate_qk(const void* q, const void* k, const void* v, const int32_t* po
                   void* v_out, void* cuda_stream) {
     if (!r) return PSD_ERR_NULL;
     if (r->n_tokens < 1 || r->n_tokens > kMostSteps || r->Hq < 0 || r->Hkv < 0 || r->Hq + (int64_t)r->Hkv < 1 ||
-        r->Hq > 65536 || r->Hkv > 65536 || !head_ok(r->Dh) || r->rotary < 0 || r->rotary > r->Dh || r->rotary % 2)
+        r->Hq > 16384 || r->Hkv > 16384 || !head_ok(r->Dh) || r->rotary < 0 || r->rotary > r->Dh || r->rotary % 2)
         return PSD_ERR_SHAPE;
     if ((r->interleaved != 0 && r->interleaved != 1) || !(r->eps > 0.f) || !std::isfinite(r->eps) || !(r->gain > 0.f) ||
         !std::isfinite(r->gain) || (slot && r->n_slots < 0))

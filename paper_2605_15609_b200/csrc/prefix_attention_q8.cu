@@ -15,6 +15,7 @@
 //
 // Bound for few rows: the cache's bytes, 2 Dh per key; widening takes 3 to 3.5 instructions for two codes, about 40% of the issue
 // slots that the bytes' time offers.
+#include <cmath>
 #include "attn_tc.cuh"
 #include "prefix_attention_q8.cuh"
 
@@ -36,6 +37,7 @@ struct Q8Args {
     int64_t rows, q_token, q_head;   // rows: B * D * M * Hq
     int T, G, Hq, Hkv, Dh, P, nb, shift, units, splits;
     int k_outer, k_head, v_outer, v_head;
+    int B, longest_first;            // longest_first: CTAs take the sequences by falling length
     float c;                         // scale * log2 e
     long long wait_limit;
     int stall_test;
@@ -56,7 +58,7 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     extern __shared__ __align__(1024) unsigned char smem[];
     constexpr int SLICE = kSlice * DHP, STAGE = 2 * SLICE, KS = DHP / 16, NO = DHP / 8;
     __shared__ uint64_t bars[4 * kStages + 1];
-    __shared__ int abort_word;
+    __shared__ int abort_word, sequence;
     volatile int* abort_flag = &abort_word;
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     unsigned char* ring = smem + warp * kStages * STAGE;
@@ -72,7 +74,22 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     const int unit = blockIdx.x % a.units, rest = blockIdx.x / a.units, cs = rest % a.splits, bh = rest / a.splits;
-    const int h = bh % a.Hkv, b = bh / a.Hkv;
+    const int h = bh % a.Hkv;
+    int b = bh / a.Hkv;
+    if (a.longest_first) {
+        // the sequences in order of length, so that the last CTAs to start are short ones
+        if (threadIdx.x < a.B) {
+            const int mine = a.prefix_len[threadIdx.x];
+            int rank = 0;
+            for (int x = 0; x < a.B; ++x) {
+                const int y = a.prefix_len[x];
+                rank += y > mine || (y == mine && x < (int)threadIdx.x);
+            }
+            if (rank == b) sequence = threadIdx.x;
+        }
+        __syncthreads();
+        b = sequence;
+    }
     const WaitCtx wc = {abort_flag, a.status_dev, a.wait_limit, 0u};
     const int L = a.prefix_len ? min(max(a.prefix_len[b], 0), a.P) : a.P;
     const int slices = (L + kSlice - 1) / kSlice;
@@ -362,6 +379,14 @@ int launch_r(const CUtensorMap& mk, const CUtensorMap& mv, const Q8Args& a, int6
 
 }  // namespace
 
+// How the keys of the few-rows kernel are split.  At least what fills the SMs (a partial wave of CTAs else); beyond that, a CTA costs about as
+// much as kCost keys beside its own: split into s, all CTAs' costs take ctas * kCost * s / slots of the time, and the last one to finish P / s
+// keys, least together at s = sqrt(P * slots / (ctas * kCost)).  Measured, single tokens, 32 heads of 128 over 8: 64 sequences of up to 16384
+// keys: 2 waves of CTAs 241 us, s = 4 or 5 234, 8 waves 245; 16 sequences: s = 3 104, 7 74, 14 85.  No fewer than kLeast keys: one sequence of 16384
+// keys in 55 splits 22.8, in 32 19.5 (the join reads less).
+constexpr double kCost = 1500;
+constexpr int kLeast = 512;
+
 PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
     const int64_t rows = (int64_t)D * M * (Hq / Hkv);
     PrefixQ8Plan p = {};
@@ -374,16 +399,10 @@ PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P,
     }
     p.row_blocks = rows > 16 ? 2 : 1;
     p.units = (int)((rows + 16 * p.row_blocks - 1) / (16 * p.row_blocks));
-    const int64_t ctas = (int64_t)B * Hkv * p.units, want = (int64_t)sm_count() * (p.row_blocks == 1 ? 3 : 2);
-    int64_t s = want / ctas;
-    if (s < 4) {
-        // few CTAs per slot: several waves of shorter ones, unless they get short
-        int64_t waves = (4 * want + ctas - 1) / ctas;
-        if (waves > P / 1024) waves = P / 1024;
-        if (waves > s) s = waves;
-    }
-    const int64_t most = (P + 8 * kSlice - 1) / (8 * kSlice);      // two slices per warp
-    if (s > most) s = most;
+    const int64_t ctas = (int64_t)B * Hkv * p.units, slots = (int64_t)sm_count() * (p.row_blocks == 1 ? 3 : 2);
+    int64_t s = (int64_t)(std::sqrt((double)P * slots / (ctas * kCost)) + 0.5);
+    if (s < slots / ctas) s = slots / ctas;
+    if (s > (P + kLeast - 1) / kLeast) s = (P + kLeast - 1) / kLeast;
     if (s > kMaxPrefixSplits) s = kMaxPrefixSplits;
     p.splits = s < 1 ? 1 : (int)s;
     return p;
@@ -397,16 +416,17 @@ size_t prefix_q8_needs(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int 
     return partial_bytes_q8((int64_t)B * D * M * Hq * p.splits, p.dhp);
 }
 
-// Rows are split at most while the CTAs fill the SMs once (256 rows each at most), and no further than the prefix allows; a single
-// query tile of the tcgen05 kernel is always split in two.
+// An upper bound of what this call and all with smaller B, D and P need.  Rows are split while their CTAs fill the SMs once (256 rows each at
+// most), in the few-rows kernel as plan_prefix_q8 says (32 rows each at most), and no further than the prefix allows; a single query tile of
+// the tcgen05 kernel is always split in two.
 size_t prefix_q8_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
-    const int64_t rows = (int64_t)B * D * M * Hq, T = (int64_t)D * M, tq = 128 / (Hq / Hkv);
-    const int64_t pairs = 2 * (int64_t)B * Hq * (T < tq ? T : tq), once = 256 * (int64_t)sm_count();
+    const int64_t rows = (int64_t)B * D * M * Hq, T = (int64_t)D * M, G = Hq / Hkv, tq = 128 / G, sms = sm_count();
+    const int64_t pairs = 2 * (int64_t)B * Hq * (T < tq ? T : tq);
+    const double few = 2.0 * B * Hkv;                               // CTAs of the few-rows kernel along rows, at most
+    int64_t n = (rows > pairs ? rows : pairs) + 256 * sms + (int64_t)(32.0 * (std::sqrt(3.0 * sms * few * P / kCost) + few));
     int64_t most = ((int64_t)P + 255) / 256;
     if (most > kMaxPrefixSplits) most = kMaxPrefixSplits;
     if (most < 2) most = 2;
-    int64_t n = rows > pairs ? rows : pairs;
-    n += once;
     if (n > rows * most) n = rows * most;
     return partial_bytes_q8(n, Dh <= 64 ? 64 : 128);
 }
@@ -434,6 +454,8 @@ int launch_prefix_attention_q8(const void* q, const PrefixQ8& c, const int32_t* 
     x.units = p.units; x.splits = p.splits;
     x.k_outer = a.kp.outer ? 1 : 0; x.k_head = a.kp.head ? 1 : 0;
     x.v_outer = a.vp.outer ? 1 : 0; x.v_head = a.vp.head ? 1 : 0;
+    x.B = a.B;
+    x.longest_first = prefix_len && a.B > 1 && a.B <= kThreads && grid > 3 * (int64_t)sm_count() ? 1 : 0;
     x.c = a.scale * kLog2e;
     x.wait_limit = wait_limit_cycles();
     x.stall_test = selftest_stall();

@@ -54,11 +54,6 @@ struct TcArgs {
     uint32_t f16_codes, bf16_codes;
 };
 
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-    f32x2 d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
 // The codes in bytes (b, b + 1) of x as two 16-bit numbers; sel spreads them over bytes 0 and 2.
 template <bool BF16>
 __device__ __forceinline__ uint32_t widen_pair(uint32_t x, uint32_t sel, uint32_t pattern) {
