@@ -23,6 +23,7 @@ struct RotateArgs {
     const int32_t *position, *slot;
     const double* frequency;
     psd_rotate_t a;
+    int per;              // heads that a warp takes
     int parts_q, parts_k; // CTAs along the heads of q, and of k (the rest: of v)
 };
 
@@ -117,12 +118,13 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs p) {
     constexpr int HPW = 32 / LANES;                                 // heads a warp takes at a time
     constexpr bool PAIRED = MODE != kAnyHalves, INTER = MODE == kInterleaved;
     __shared__ float row[PAIRED ? 1 : kThreads / 32][PAIRED ? 1 : HPW][PAIRED ? 1 : LANES * 16 + 1];
+    __shared__ float2 turns[PAIRED ? 1 : kThreads / 32][PAIRED ? 1 : 64];
     const psd_rotate_t& a = p.a;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    // blockIdx.x: four tokens, one per warp; blockIdx.y: up to N * HPW heads of q, of k or of v
+    // blockIdx.x: four tokens, one per warp; blockIdx.y: up to `per` heads of q, of k or of v
     const int t = blockIdx.x * (kThreads / 32) + warp;
     const int kind = (int)blockIdx.y < p.parts_q ? 0 : (int)blockIdx.y < p.parts_q + p.parts_k ? 1 : 2;
-    const int h0 = ((int)blockIdx.y - (kind == 0 ? 0 : kind == 1 ? p.parts_q : p.parts_q + p.parts_k)) * N * HPW, H = kind == 0 ? a.Hq : a.Hkv;
+    const int h0 = ((int)blockIdx.y - (kind == 0 ? 0 : kind == 1 ? p.parts_q : p.parts_q + p.parts_k)) * p.per, H = min(kind == 0 ? a.Hq : a.Hkv, h0 + p.per);
     asm volatile("griddepcontrol.wait;" ::: "memory");
     if (t >= a.n_tokens) return;
     const int l = lane % LANES, grp = lane / LANES, R = a.rotary, half = R / 2, pieces = a.Dh / 8;
@@ -138,23 +140,35 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs p) {
                           t * (kind == 0 ? a.q_token : kind == 1 ? a.k_token : a.v_token) + (h0 + grp) * in_head;
     uint16_t* dst = reinterpret_cast<uint16_t*>(kind == 0 ? p.q_out : kind == 1 ? p.k_out : p.v_out) +
                     at * (kind == 0 ? a.q_out_token : kind == 1 ? a.k_out_token : a.v_out_token) + (h0 + grp) * out_head;
+    // N groups of heads are in flight: each is loaded again as soon as it has been stored
+    const int64_t in_step = HPW * in_head, out_step = HPW * out_head;
     uint4 x0[N], x1[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
+    auto load = [&](int i, int h) {
         x0[i] = x1[i] = make_uint4(0, 0, 0, 0);
-        if (h0 + i * HPW + grp < H) {
-            if (has0) x0[i] = *reinterpret_cast<const uint4*>(src + i * HPW * in_head + c0 * 8);
-            if (has1) x1[i] = *reinterpret_cast<const uint4*>(src + i * HPW * in_head + c1 * 8);
+        if (h + grp < H) {
+            if (has0) x0[i] = *reinterpret_cast<const uint4*>(src + c0 * 8);
+            if (has1) x1[i] = *reinterpret_cast<const uint4*>(src + c1 * 8);
         }
-    }
-    auto store = [&](int i, const uint4& u, const uint4& v) {
-        if (!filed || h0 + i * HPW + grp >= H) return;
-        if (has0) *reinterpret_cast<uint4*>(dst + i * HPW * out_head + c0 * 8) = u;
-        if (has1) *reinterpret_cast<uint4*>(dst + i * HPW * out_head + c1 * 8) = v;
+        src += in_step;
     };
-    if (kind == 2) {
+    auto store = [&](int h, const uint4& u, const uint4& v) {
+        if (filed && h + grp < H) {
+            if (has0) *reinterpret_cast<uint4*>(dst + c0 * 8) = u;
+            if (has1) *reinterpret_cast<uint4*>(dst + c1 * 8) = v;
+        }
+        dst += out_step;
+    };
 #pragma unroll
-        for (int i = 0; i < N; ++i) store(i, x0[i], x1[i]);
+    for (int i = 0; i < N; ++i) load(i, h0 + i * HPW);
+    if (kind == 2) {
+#pragma unroll 1
+        for (int h = h0; h < H; h += N * HPW) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                store(h + i * HPW, x0[i], x1[i]);
+                load(i, h + (N + i) * HPW);
+            }
+        }
         return;
     }
     // sines and cosines of this lane's 8 pairs (first of them: pair j0 of the head); kAnyHalves: of its 16 numbers
@@ -176,10 +190,12 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs p) {
             sn[j] = __shfl_sync(0xffffffffu, mine[j % EACH].y, (j / EACH) * LANES + l);
         }
     } else {
+        for (int j = lane; j < half; j += 32) turns[warp][j] = turn(pos, p.frequency[j], a.gain);
+        __syncwarp();
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             const int d = 16 * l + j;
-            const float2 z = d < R ? turn(pos, p.frequency[d % half], a.gain) : make_float2(1.f, 0.f);
+            const float2 z = d < R ? turns[warp][d < half ? d : d - half] : make_float2(1.f, 0.f);
             cs[j] = z.x;
             sn[j] = d < half ? -z.y : z.y;
         }
@@ -215,9 +231,11 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs p) {
         }
     }
     const float per = 1.f / (float)a.Dh;
+#pragma unroll 1
+    for (int h = h0; h < H; h += N * HPW)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        if (h0 + i * HPW >= H) break;
+        if (h + i * HPW >= H) break;
         uint4 y0 = x0[i], y1 = x1[i];
         f32x2 x[4], y[4];
         split_pairs<BF16, INTER>(x0[i], x1[i], x, y);
@@ -284,14 +302,14 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateArgs p) {
             y0 = make_uint4(o[0], o[1], o[2], o[3]);
             y1 = make_uint4(o[4], o[5], o[6], o[7]);
         }
-        store(i, y0, y1);
+        store(h + i * HPW, y0, y1);
+        load(i, h + (N + i) * HPW);
     }
 }
 
 template <bool BF16, int LANES, int N, int MODE>
 int launch_n(RotateArgs& p, cudaStream_t st) {
-    constexpr int HPW = 32 / LANES;
-    auto parts = [](int heads) { return (heads + HPW * N - 1) / (HPW * N); };
+    auto parts = [&](int heads) { return (heads + p.per - 1) / p.per; };
     p.parts_q = parts(p.a.Hq);
     p.parts_k = parts(p.a.Hkv);
     cudaLaunchConfig_t cfg = {};
@@ -309,10 +327,14 @@ int launch_n(RotateArgs& p, cudaStream_t st) {
 }
 template <bool BF16, int LANES, int MODE>
 int launch_l(RotateArgs& p, cudaStream_t st) {
-    // several groups of heads per warp once the warps fill the SMs anyway
+    // A warp takes all heads of a token's queries (keys, values) once the tokens alone fill the SMs, one group at a time of few tokens.
     constexpr int HPW = 32 / LANES;
-    const int64_t groups = (int64_t)p.a.n_tokens * ((p.a.Hq + 2 * (int64_t)p.a.Hkv + HPW - 1) / HPW);
-    return groups >= 4 * 64 * (int64_t)sm_count() ? launch_n<BF16, LANES, 4, MODE>(p, st) : launch_n<BF16, LANES, 1, MODE>(p, st);
+    if (p.a.n_tokens >= 8 * sm_count()) {
+        p.per = 16 * HPW;
+        return launch_n<BF16, LANES, 2, MODE>(p, st);
+    }
+    p.per = HPW;
+    return launch_n<BF16, LANES, 1, MODE>(p, st);
 }
 template <bool BF16, int LANES>
 int launch_m(RotateArgs& p, cudaStream_t st) {
@@ -328,7 +350,7 @@ int launch_t(RotateArgs& p, cudaStream_t st) {
 
 int launch_rotate(const void* q, const void* k, const void* v, const int32_t* position, const double* frequency, const void* q_norm,
                   const void* k_norm, const int32_t* slot, const psd_rotate_t& a, void* q_out, void* k_out, void* v_out, cudaStream_t st) {
-    RotateArgs p = {q, k, v, q_norm, k_norm, q_out, k_out, v_out, position, slot, frequency, a, 0, 0};
+    RotateArgs p = {q, k, v, q_norm, k_norm, q_out, k_out, v_out, position, slot, frequency, a, 0, 0, 0};
     return a.dtype == PSD_BF16 ? launch_t<true>(p, st) : launch_t<false>(p, st);
 }
 
