@@ -789,16 +789,17 @@ def psd_rope_frequencies(rotary, base=10000.0, kind=PSD_ROPE_PLAIN, factor=1.0, 
 
 
 def _heads_strides(t, name):
-    """(tokens, heads, token stride, head stride) of [T, H, Dh], or of [N, M, H, Dh] whose first two dimensions are one run."""
-    if t.dim() == 4:
-        N, M, H, Dh = t.shape
-        token, head = _tokens_strides(t, N, M, H, Dh, name)
-        return N * M, H, Dh, token, head
-    T, H, Dh = t.shape
-    st, sh, sd = t.stride()
-    if sd != 1 and Dh > 1:
-        raise ValueError(f"psd binding: {name} needs a dense last dimension")
-    return T, H, Dh, st if T > 1 else H * Dh, sh if H > 1 else Dh
+    """(tokens, heads, head size, token stride, head stride) of [T, H, Dh], or of [N, M, H, Dh] whose first two dimensions are
+    one run."""
+    shape = t.shape
+    if len(shape) == 3:
+        T, H, Dh = shape
+        st, sh, sd = t.stride()
+        if sd != 1 and Dh > 1:
+            raise ValueError(f"psd binding: {name} needs a dense last dimension")
+        return T, H, Dh, st if T > 1 else H * Dh, sh if H > 1 else Dh
+    N, M, H, Dh = shape
+    return N * M, H, Dh, *_tokens_strides(t, N, M, H, Dh, name)
 
 
 def psd_rotate_qk(q, k, q_out, k_out, position, frequency, v=None, v_out=None, slot=None, q_norm=None, k_norm=None, eps=1e-6,
@@ -806,45 +807,40 @@ def psd_rotate_qk(q, k, q_out, k_out, position, frequency, v=None, v_out=None, s
     """Norms and position rotation of q [T, Hq, Dh] and k [T, Hkv, Dh] (or [N, M, H, Dh]; either may be None with its output)
     into q_out and k_out, v into v_out; with ``slot`` [T] int32, token t of k and v goes to row slot[t].  ``frequency``
     [rotary/2] float64 says how much of a head is rotated (None: nothing)."""
-    some = q if q is not None else k
-    T, Hq, Hkv, Dh, qs, ks, vs = 0, 0, 0, some.shape[-1], (8, 8, 8, 8), (8, 8, 8, 8), (8, 8, 8, 8)
-    n_slots = 0
-    if (q is None) != (q_out is None) or (k is None) != (k_out is None) or (v is None) != (v_out is None):
-        raise ValueError("psd binding: q, k and v come with their outputs")
+    T = Hq = Hkv = n_slots = 0
+    qa = qb = qc = qd = ka = kb = kc = kd = va = vb = vc = vd = 8
+    pq = pk = pv = oq = ok = ov = None
     if q is not None:
-        T, Hq, _, a, b = _heads_strides(q, "q")
-        To, Ho, Do, c, d = _heads_strides(q_out, "q_out")
-        if (To, Ho, Do) != (T, Hq, Dh):
-            raise ValueError("psd binding: q_out has q's tokens and heads")
-        qs = (a, b, c, d)
-    for name, x, y in (("k", k, k_out), ("v", v, v_out)):
-        if x is None:
-            continue
-        Tx, H, Dx, a, b = _heads_strides(x, name)
-        To, Ho, Do, c, d = _heads_strides(y, name + "_out")
-        if name == "v" and (k is None or H != Hkv) or Dx != Dh or (q is not None or name == "v") and Tx != T or (Ho, Do) != (H, Dh):
-            raise ValueError("psd binding: q, k, v are [T, heads, Dh] of the same tokens; k and v, and their outputs, have the same heads")
-        T, Hkv = Tx, H
-        if slot is None and To != T:
-            raise ValueError(f"psd binding: {name}_out has {name}'s tokens where there are no slots")
-        if slot is not None:
-            if name == "v" and To != n_slots:
-                raise ValueError("psd binding: k_out and v_out have one number of slots")
-            n_slots = To
-        if name == "k":
-            ks = (a, b, c, d)
-        else:
-            vs = (a, b, c, d)
-    rotary = 0 if frequency is None else 2 * frequency.numel()
-    r = _pack_rotate(T, Hq, Hkv, Dh, _one_type(some.dtype, q, k, v, q_out, k_out, v_out, q_norm, k_norm), rotary,
-                     1 if interleaved else 0, n_slots, eps, gain, qs[0], qs[1], ks[0], ks[1], vs[0], vs[1], qs[2], qs[3], ks[2], ks[3],
-                     vs[2], vs[3])
-    stream = _here(stream, some, q, k, v, q_out, k_out, v_out, position, frequency, slot, q_norm, k_norm)
-    _check(LIB.psd_rotate_qk(None if q is None else q.data_ptr(), None if k is None else k.data_ptr(), None if v is None else v.data_ptr(),
-                             _want_n(position, T, _I32, "position"), _want_n(frequency, rotary // 2, _F64, "frequency"),
+        T, Hq, Dh, qa, qb = _heads_strides(q, "q")
+        To, Ho, Do, qc, qd = _heads_strides(q_out, "q_out")
+        if To != T or Ho != Hq or Do != Dh:
+            raise ValueError("psd binding: q_out has q's tokens, heads and head size")
+        pq, oq = q.data_ptr(), q_out.data_ptr()
+    if k is not None:
+        Tk, Hkv, Dk, ka, kb = _heads_strides(k, "k")
+        n_slots, Ho, Do, kc, kd = _heads_strides(k_out, "k_out")
+        if q is None:
+            T, Dh = Tk, Dk
+        if Tk != T or Dk != Dh or Ho != Hkv or Do != Dh or (slot is None and n_slots != T):
+            raise ValueError("psd binding: k has q's tokens and head size, k_out k's heads (and, without slots, its tokens)")
+        pk, ok = k.data_ptr(), k_out.data_ptr()
+        if v is not None:
+            Tv, Hv, Dv, va, vb = _heads_strides(v, "v")
+            To, Ho, Do, vc, vd = _heads_strides(v_out, "v_out")
+            if Tv != T or Hv != Hkv or Dv != Dh or To != n_slots or Ho != Hkv or Do != Dh:
+                raise ValueError("psd binding: v has k's shape, v_out k_out's")
+            pv, ov = v.data_ptr(), v_out.data_ptr()
+    some = q if q is not None else k
+    if some is None or (q is None) != (q_out is None) or (k is None) != (k_out is None) or (v is None) != (v_out is None) or \
+            (v is not None and k is None):
+        raise ValueError("psd binding: q, k and v come with their outputs, v with k")
+    pairs = 0 if frequency is None else frequency.numel()
+    r = _pack_rotate(T, Hq, Hkv, Dh, _one_type(some.dtype, q, k, v, q_out, k_out, v_out), 2 * pairs, 1 if interleaved else 0, n_slots, eps,
+                     gain, qa, qb, ka, kb, va, vb, qc, qd, kc, kd, vc, vd)
+    stream = _here(stream, some, k, v, q_out, k_out, v_out, position, frequency, slot, q_norm, k_norm)
+    _check(LIB.psd_rotate_qk(pq, pk, pv, _want_n(position, T, _I32, "position"), _want_n(frequency, pairs, _F64, "frequency"),
                              _want(q_norm, (Dh,), some.dtype, "q_norm"), _want(k_norm, (Dh,), some.dtype, "k_norm"),
-                             _want_n(slot, T, _I32, "slot"), r, None if q is None else q_out.data_ptr(),
-                             None if k is None else k_out.data_ptr(), None if v is None else v_out.data_ptr(), stream), "psd_rotate_qk")
+                             _want_n(slot, T, _I32, "slot"), r, oq, ok, ov, stream), "psd_rotate_qk")
 
 
 def psd_quantize_rows(x, codes, scale, stream=None):
