@@ -28,7 +28,8 @@ struct QuantArgs {
     int64_t n_units;
     int64_t outer[2], token[2], head[2], code_outer[2], code_token[2], code_head[2];
     int pieces;                      // per unit
-    int per_token;                   // pieces of one token (caches), or `pieces`
+    int per_token;                   // pieces of one token (caches), 1 .. 16
+    int magic;                       // p / per_token = p * magic >> 16 for p < 2048: ceil(65536 / per_token)
     int P, Hkv, T, nb, nb_call;      // caches: capacity, heads, tokens per block, blocks, blocks per sequence of this call
     int span;
 };
@@ -93,7 +94,8 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantArgs a) {
             const int p = p0 + i * LANES + lane_u;
             v[i] = make_uint4(0, 0, 0, 0);
             if (p < pieces) {
-                const uint16_t* at = CACHE ? x + (p / a.per_token) * step_in + (p % a.per_token) * 8 : x + (int64_t)p * 8;
+                const int tok = CACHE ? p * a.magic >> 16 : 0;
+                const uint16_t* at = CACHE ? x + tok * step_in + (p - tok * a.per_token) * 8 : x + (int64_t)p * 8;
                 v[i] = __ldcs(reinterpret_cast<const uint4*>(at));
             }
         }
@@ -144,7 +146,8 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantArgs a) {
             o.x = __byte_perm(__byte_perm(n[0], n[1], 0x0040), __byte_perm(n[2], n[3], 0x0040), 0x5410);
             o.y = __byte_perm(__byte_perm(n[4], n[5], 0x0040), __byte_perm(n[6], n[7], 0x0040), 0x5410);
             if (!fine) o = make_uint2(0, 0);
-            int8_t* at = CACHE ? codes + (p / a.per_token) * step_out + (p % a.per_token) * 8 : codes + (int64_t)p * 8;
+            const int tok = CACHE ? p * a.magic >> 16 : 0;
+            int8_t* at = CACHE ? codes + tok * step_out + (p - tok * a.per_token) * 8 : codes + (int64_t)p * 8;
             *reinterpret_cast<uint2*>(at) = o;
         }
     }
@@ -190,7 +193,7 @@ int launch_quantize_rows(const void* x, int dtype, int64_t row_stride, int64_t n
     a.n_units = n_rows;
     a.outer[0] = row_stride;
     a.code_outer[0] = code_stride;
-    a.pieces = a.per_token = H / 8;
+    a.pieces = H / 8;
     return launch_q<false>(a, dtype == PSD_BF16, st);
 }
 
@@ -214,6 +217,7 @@ int launch_prefix_quantize(const void* k, const void* v, const int32_t* begin, c
     a.nb_call = most < a.nb ? most : a.nb;
     a.n_units = (int64_t)q.B * a.nb_call * q.Hkv * 2;
     a.per_token = q.Dh / 8;
+    a.magic = (65536 + a.per_token - 1) / a.per_token;
     a.pieces = q.block * a.per_token;
     return launch_q<true>(a, q.dtype == PSD_BF16, st);
 }
