@@ -17,6 +17,6 @@ from .binding import (ACCEPT_AGREE_AND_CONF, ACCEPT_AGREE_AND_POLICY, ACCEPT_AGR
                       psd_attention_workspace_bytes, psd_attention_kernel_names, psd_draft_attention, psd_weights_workspace_bytes, psd_prefix_weights,
                       psd_prefix_evict, psd_logits_workspace_bytes, psd_confidence_logits, PSD_ROPE_PLAIN, PSD_ROPE_LINEAR, PSD_ROPE_STRETCHED,
                       PSD_ROPE_BY_PARTS, PsdRotate, PsdQuantize, psd_rope_frequencies, psd_rotate_qk, psd_quantize_rows, psd_prefix_quantize,
-                      psd_attention_q8_workspace_bytes, psd_draft_attention_q8, psd_confidence_q8_workspace_bytes, psd_confidence_q8)
+                      psd_attention_q8_workspace_bytes, psd_attention_q8_kernel_names, psd_draft_attention_q8, psd_confidence_q8_workspace_bytes, psd_confidence_q8)
 
 __all__ = [n for n in dir() if not n.startswith("_")]

@@ -192,6 +192,8 @@ def _load() -> ctypes.CDLL:
     lib.psd_prefix_quantize.argtypes = [_vp] * 10
     lib.psd_attention_q8_workspace_bytes.restype = _sz
     lib.psd_attention_q8_workspace_bytes.argtypes = [_i32] * 8
+    lib.psd_attention_q8_kernel_names.restype = ctypes.c_char_p
+    lib.psd_attention_q8_kernel_names.argtypes = [_i32] * 8 + [_vp]
     lib.psd_draft_attention_q8.restype = ctypes.c_int
     lib.psd_draft_attention_q8.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp, _vp]
     lib.psd_confidence_q8_workspace_bytes.restype = _sz
@@ -807,6 +809,10 @@ def psd_rotate_qk(q, k, q_out, k_out, position, frequency, v=None, v_out=None, s
     """Norms and position rotation of q [T, Hq, Dh] and k [T, Hkv, Dh] (or [N, M, H, Dh]; either may be None with its output)
     into q_out and k_out, v into v_out; with ``slot`` [T] int32, token t of k and v goes to row slot[t].  ``frequency``
     [rotary/2] float64 says how much of a head is rotated (None: nothing)."""
+    some = q if q is not None else k
+    if some is None or (q is None) != (q_out is None) or (k is None) != (k_out is None) or (v is None) != (v_out is None) or \
+            (v is not None and k is None):
+        raise ValueError("psd binding: q, k and v come with their outputs, v with k")
     T = Hq = Hkv = n_slots = 0
     qa = qb = qc = qd = ka = kb = kc = kd = va = vb = vc = vd = 8
     pq = pk = pv = oq = ok = ov = None
@@ -830,10 +836,6 @@ def psd_rotate_qk(q, k, q_out, k_out, position, frequency, v=None, v_out=None, s
             if Tv != T or Hv != Hkv or Dv != Dh or To != n_slots or Ho != Hkv or Do != Dh:
                 raise ValueError("psd binding: v has k's shape, v_out k_out's")
             pv, ov = v.data_ptr(), v_out.data_ptr()
-    some = q if q is not None else k
-    if some is None or (q is None) != (q_out is None) or (k is None) != (k_out is None) or (v is None) != (v_out is None) or \
-            (v is not None and k is None):
-        raise ValueError("psd binding: q, k and v come with their outputs, v with k")
     pairs = 0 if frequency is None else frequency.numel()
     r = _pack_rotate(T, Hq, Hkv, Dh, _one_type(some.dtype, q, k, v, q_out, k_out, v_out), 2 * pairs, 1 if interleaved else 0, n_slots, eps,
                      gain, qa, qb, ka, kb, va, vb, qc, qd, kc, kd, vc, vd)
@@ -873,6 +875,13 @@ def psd_prefix_quantize(k, v, k_codes, v_codes, k_scale, v_scale, block=32, begi
 
 def psd_attention_q8_workspace_bytes(B, D, M, Hq, Hkv, Dh, P, S) -> int:
     return int(LIB.psd_attention_q8_workspace_bytes(B, D, M, Hq, Hkv, Dh, P, S))
+
+
+def psd_attention_q8_kernel_names(B, D, M, Hq, Hkv, Dh, P, S):
+    """(names of the kernels that psd_draft_attention_q8 launches at these sizes, partial results per row), or None."""
+    splits = _i32(0)
+    names = LIB.psd_attention_q8_kernel_names(B, D, M, Hq, Hkv, Dh, P, S, ctypes.byref(splits))
+    return None if names is None else (names.decode(), splits.value)
 
 
 def _codes_strides(strides, no, nt, nh, nd, name):

@@ -113,6 +113,16 @@ size_t psd_attention_q8_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t
     return P == 0 ? 256 : prefix_q8_workspace(B, D, M, Hq, Hkv, Dh, P);
 }
 
+const char* psd_attention_q8_kernel_names(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P, int32_t S,
+                                          int32_t* splits) {
+    if (!attention_sizes_ok(B, D, M, Hq, Hkv, Dh, P, S) || Dh % 16) return nullptr;
+    if (P == 0) return draft_attention_kernels(B, D, M, Hq, Hkv, Dh, P, S, splits);
+    const PrefixQ8Plan p = plan_prefix_q8(B, D, M, Hq, Hkv, Dh, P, S);
+    if (splits) *splits = p.splits;
+    return !p.tiles ? "prefix_rows_q8_kernel+draft_attention_kernel"
+                    : p.tile.fused ? "prefix_tiles_q8_kernel" : "prefix_tiles_q8_kernel+draft_attention_kernel";
+}
+
 int psd_draft_attention_q8(const void* q, const int8_t* k_codes, const int8_t* v_codes, const float* k_scale,
                            const float* v_scale, int32_t block, const int32_t* prefix_len, const void* k_own,
                            const void* v_own, const int32_t* own_len, const psd_attention_t* a, void* out, float* lse,
