@@ -29,7 +29,9 @@ constexpr int kBarBytes = 1024;
 
 struct OwnTile { int node, key0, len; };    // a tile of own keys: draft of the sequence, first key, the draft's length
 
-template <int SLABS> struct Rings { static constexpr int RAW = SLABS == 2 ? 2 : 4, WIDE = SLABS == 2 ? 4 : 8; };
+// Tiles in flight: codes (RAW; with a single query tile the other's memory holds as many again, since a cache that is read for few rows comes from
+// HBM at the rate that the copies in flight allow) and widened ones.
+template <int SLABS> struct Rings { static constexpr int RAW = SLABS == 2 ? 2 : 8, MOST = SLABS == 2 ? 4 : 8, WIDE = SLABS == 2 ? 4 : 8; };
 
 struct TcArgs {
     const float *k_scale, *v_scale;
@@ -99,12 +101,12 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                        const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_ko,
                        const __grid_constant__ CUtensorMap map_vo, const TcArgs a) {
     extern __shared__ __align__(1024) unsigned char smem[];
-    constexpr int TILE = SLABS * kSlabBytes, RAW = TILE / 2, NR = Rings<SLABS>::RAW, NS = Rings<SLABS>::WIDE, DHP = SLABS * 64;
+    constexpr int TILE = SLABS * kSlabBytes, RAW = TILE / 2, MOST = Rings<SLABS>::MOST, NS = Rings<SLABS>::WIDE, DHP = SLABS * 64;
     unsigned char* q_tiles = smem;                                   // [2][TILE]
     unsigned char* ring = smem + 2 * TILE;                           // [NS][TILE]
-    unsigned char* raw = ring + NS * TILE;                           // [NR][RAW]
-    uint64_t* bars = reinterpret_cast<uint64_t*>(raw + NR * RAW);
-    uint64_t *q_full = bars, *raw_full = bars + 1, *raw_empty = raw_full + NR, *full = raw_empty + NR, *empty = full + NS, *s_full = empty + NS /* [2] */,
+    unsigned char* raw = ring + NS * TILE;                           // [Rings::RAW][RAW]
+    uint64_t* bars = reinterpret_cast<uint64_t*>(raw + Rings<SLABS>::RAW * RAW);
+    uint64_t *q_full = bars, *raw_full = bars + 1, *raw_empty = raw_full + MOST, *full = raw_empty + MOST, *empty = full + NS, *s_full = empty + NS /* [2] */,
              *p_half = s_full + 2, *p_ready = p_half + 2, *o_done = p_ready + 2, *drain = o_done + 2, *never = drain + 1;
     uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(never + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
@@ -114,6 +116,13 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
 
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const bool shared_keys = a.n_qt > 1;
+    const uint32_t NR = shared_keys ? Rings<SLABS>::RAW : MOST;      // (powers of 2)
+    auto raw_slot = [&](int in) {
+        const uint32_t slot = (uint32_t)in & (NR - 1);
+        return slot < Rings<SLABS>::RAW ? raw + slot * RAW : q_tiles + TILE + (slot - Rings<SLABS>::RAW) * RAW;
+    };
+    auto raw_bar = [&](uint64_t* b, int in) { return b + ((uint32_t)in & (NR - 1)); };
+    auto raw_turn = [&](int in) { return (uint32_t)in / NR & 1u; };
     const int unit = blockIdx.x % a.units, rest = blockIdx.x / a.units;
     const int n_cs = shared_keys ? a.splits : a.splits / 2;
     const int cs = rest % n_cs, bh = rest / n_cs, h = bh % a.Hkv;
@@ -123,7 +132,7 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
 
     if (threadIdx.x == 0) {
         mbar_init(q_full, 1);
-        for (int s = 0; s < NR; ++s) { mbar_init(&raw_full[s], 1); mbar_init(&raw_empty[s], kWideners / 32); }
+        for (int s = 0; s < MOST; ++s) { mbar_init(&raw_full[s], 1); mbar_init(&raw_empty[s], kWideners / 32); }
         for (int s = 0; s < NS; ++s) { mbar_init(&full[s], kWideners / 32); mbar_init(&empty[s], 1); }
         for (int s = 0; s < 2; ++s) { mbar_init(&s_full[s], 1); mbar_init(&p_half[s], 4); mbar_init(&p_ready[s], 4); mbar_init(&o_done[s], 1); }
         mbar_init(drain, 1);
@@ -199,14 +208,14 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             if (!listed(s, j)) continue;
             if (j >= (s ? np1 : np0)) { ++item; continue; }
             if (!(ok = mbar_wait_warp(&empty[item % NS], ((item / NS) & 1) ^ 1, wc))) break;
-            if (!(ok = mbar_wait_warp(&raw_full[in % NR], (in / NR) & 1, wc))) break;
-            const uint32_t from = smem_u32(raw + (in % NR) * RAW), to = smem_u32(ring + (item % NS) * TILE);
+            if (!(ok = mbar_wait_warp(raw_bar(raw_full, in), raw_turn(in), wc))) break;
+            const uint32_t from = smem_u32(raw_slot(in)), to = smem_u32(ring + (item % NS) * TILE);
             if (BF16 && is_k) widen_tile<SLABS, true>(from, to, tid, a.bf16_codes);
             else widen_tile<SLABS, false>(from, to, tid, a.f16_codes);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) {
-                mbar_arrive(&raw_empty[in % NR]);
+                mbar_arrive(raw_bar(raw_empty, in));
                 mbar_arrive(&full[item % NS]);
             }
             ++item;
@@ -230,11 +239,10 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 const int s = (x >> 1) & 1, j = (x >> 2) - (is_k ? 0 : 1), np = s ? np1 : np0;
                 if (!listed(s, j)) continue;
                 if (j < np) {
-                    const int slot = in % NR;
-                    if (!mbar_wait_warp(&raw_empty[slot], ((in / NR) & 1) ^ 1, wc)) { ok = false; break; }
+                    if (!mbar_wait_warp(raw_bar(raw_empty, in), raw_turn(in) ^ 1, wc)) { ok = false; break; }
                     if (leader) {
-                        mbar_arrive_expect_tx(&raw_full[slot], RAW);
-                        tma_load_4d(raw + slot * RAW, is_k ? &map_k : &map_v, &raw_full[slot], 0, h * (is_k ? a.k_head : a.v_head),
+                        mbar_arrive_expect_tx(raw_bar(raw_full, in), RAW);
+                        tma_load_4d(raw_slot(in), is_k ? &map_k : &map_v, raw_bar(raw_full, in), 0, h * (is_k ? a.k_head : a.v_head),
                                     ((s ? t01 : t00) + j) * 128, b * (is_k ? a.k_outer : a.v_outer));
                     }
                     ++in;
@@ -261,9 +269,9 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 // giving up: no copy may be in flight when the CTA exits
                 long long c0 = clock64();
                 while (!mbar_try_wait(q_full, 0) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
-                for (int i = in > NR ? in - NR : 0; i < in; ++i) {
+                for (int i = max(in - (int)NR, 0); i < in; ++i) {
                     c0 = clock64();
-                    while (!mbar_try_wait(&raw_full[i % NR], (i / NR) & 1) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
+                    while (!mbar_try_wait(raw_bar(raw_full, i), raw_turn(i)) && clock64() - c0 < WAIT_LIMIT_CYCLES) {}
                 }
                 for (int i = max(first_own, item - NS); first_own >= 0 && i < item; ++i) {
                     c0 = clock64();
