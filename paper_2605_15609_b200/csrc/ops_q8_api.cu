@@ -120,7 +120,7 @@ const char* psd_attention_q8_kernel_names(int32_t B, int32_t D, int32_t M, int32
     const PrefixQ8Plan p = plan_prefix_q8(B, D, M, Hq, Hkv, Dh, P, S);
     if (splits) *splits = p.splits;
     return !p.tiles ? "prefix_rows_q8_kernel+draft_attention_kernel"
-                    : p.tile.fused ? "prefix_tiles_q8_kernel" : "prefix_tiles_q8_kernel+draft_attention_kernel";
+                    : p.final ? "prefix_tiles_q8_kernel" : "prefix_tiles_q8_kernel+draft_attention_kernel";
 }
 
 int psd_draft_attention_q8(const void* q, const int8_t* k_codes, const int8_t* v_codes, const float* k_scale,
@@ -146,7 +146,7 @@ int psd_draft_attention_q8(const void* q, const int8_t* k_codes, const int8_t* v
     float* pl = po + rows * plan.splits * plan.dhp;
     const PrefixQ8 c = {k_codes, v_codes, k_scale, v_scale, block};
     const int e = launch_prefix_attention_q8(q, c, prefix_len, k_own, v_own, own_len, *a, plan, po, pl, out, lse, status_dev, st);
-    if (e != PSD_OK || (plan.tiles && plan.tile.fused)) return e;
+    if (e != PSD_OK || plan.final) return e;
     return launch_own_and_join(q, k_own, v_own, own_len, *a, po, pl, plan.splits, out, lse, st);
 }
 

@@ -32,7 +32,9 @@ struct PrefixQ8 {
 
 // Which kernel takes the prefix, and how its work is cut.
 struct PrefixQ8Plan {
-    bool tiles;         // prefix_tiles_q8_kernel (tcgen05), cut as `tile` says; else prefix_rows_q8_kernel:
+    bool tiles;         // prefix_tiles_q8_kernel (tcgen05), cut as `tile` says; else prefix_rows_q8_kernel: row_blocks, units
+    bool joined;        // ..with splits that a cluster joins
+    bool final;         // the kernel takes the own keys too and writes final outputs; else partial results
     int row_blocks;     // 16-row blocks of a warp: 1 or 2
     int units;          // CTAs along the rows of a key head
     PrefixPlan tile;
@@ -44,14 +46,15 @@ PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P,
 size_t prefix_q8_needs(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S);
 size_t prefix_q8_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P);
 
-// plan.tiles && plan.tile.fused: final outputs into out and lse.  Otherwise partial results of every row over its sequence's prefix, as
+// plan.final: final outputs into out and lse.  Otherwise partial results of every row over its sequence's prefix, as
 // launch_prefix_attention leaves them: po [splits][rows][dhp], pl [splits][rows].
 int launch_prefix_attention_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const void* k_own, const void* v_own,
                                const int32_t* own_len, const psd_attention_t& a, const PrefixQ8Plan& p, float* po, float* pl, void* out,
                                float* lse, int32_t* status_dev, cudaStream_t st);
 // prefix_attention_q8_tc.cu
+int q8_clusters(int n);      // clusters of n CTAs of the tcgen05 kernel that the device holds at once
 int launch_prefix_tiles_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const void* k_own, const void* v_own,
-                           const int32_t* own_len, const psd_attention_t& a, const PrefixPlan& p, float* po, float* pl, void* out, float* lse,
-                           int32_t* status_dev, cudaStream_t st);
+                           const int32_t* own_len, const psd_attention_t& a, const PrefixPlan& p, bool joined, float* po, float* pl, void* out,
+                           float* lse, int32_t* status_dev, cudaStream_t st);
 
 }  // namespace psd

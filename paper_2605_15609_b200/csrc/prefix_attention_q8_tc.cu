@@ -11,6 +11,10 @@
 // Where the prefix is not split, the drafts' own 16-bit keys follow it as further tiles, as there: TMA brings them into the wide ring
 // directly, and before a stream's first of them its output is multiplied by the reference of the value scales, so that both kinds add up.
 //
+// Where the keys are split over up to eight CTAs, these are a cluster and join their results themselves: the own tiles are dealt out to
+// them, each leaves its outputs, maxima and sums in its shared memory, and each reads and writes a share of the rows.  Nothing goes through
+// memory, and no second kernel starts.
+//
 // Bound: for Dh = 128 products and exponentials as there (2048 cycles each per 256 rows x 128 keys); widening is about 600 issue slots
 // per scheduler of the same round, the values' scales 64 more per warp.
 #include "attn_tc.cuh"
@@ -26,6 +30,7 @@ constexpr float kRaise = 8.0f;              // growth of a row's maximum (log2) 
 constexpr float kHalfRoom = 7.0f;           // how far (log2) the reference is set below the maximum: weights go up to 2^15
 constexpr int kMaxSorted = 128;             // sequences that are put in order of length
 constexpr int kBarBytes = 1024;
+constexpr int kParts = 16;                  // results of a row that a cluster joins, at most
 
 struct OwnTile { int node, key0, len; };    // a tile of own keys: draft of the sequence, first key, the draft's length
 
@@ -43,8 +48,8 @@ struct TcArgs {
     int tq, n_qt, units, splits;
     int k_outer, k_head, v_outer, v_head;
     int B, longest_first;
-    // own keys and final outputs (fused == 1); else partial results
-    int fused, D, M, S, causal, own_box;
+    // own keys and final outputs (fused == 1: one CTA has all keys of a row; 2: a cluster of n_cs joins); else partial results
+    int fused, n_cs, D, M, S, causal, own_box;
     int ko_outer, ko_head, vo_outer, vo_head;
     const int32_t* own_len;
     void* out;
@@ -55,6 +60,15 @@ struct TcArgs {
     int stall_test;
     uint32_t f16_codes, bf16_codes;
 };
+
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release;\n\tbarrier.cluster.wait.acquire;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t peer(uint32_t addr, int rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
 
 // The codes in bytes (b, b + 1) of x as two 16-bit numbers; sel spreads them over bytes 0 and 2.
 template <bool BF16>
@@ -95,7 +109,7 @@ __device__ __forceinline__ void widen_tile(uint32_t raw, uint32_t to, int tid, u
     }
 }
 
-template <int SLABS, bool BF16>
+template <int SLABS, bool BF16, bool JOINED>
 __global__ void __launch_bounds__(kQThreads, 1)
 prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                        const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_ko,
@@ -123,9 +137,10 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     };
     auto raw_bar = [&](uint64_t* b, int in) { return b + ((uint32_t)in & (NR - 1)); };
     auto raw_turn = [&](int in) { return (uint32_t)in / NR & 1u; };
-    const int unit = blockIdx.x % a.units, rest = blockIdx.x / a.units;
-    const int n_cs = shared_keys ? a.splits : a.splits / 2;
-    const int cs = rest % n_cs, bh = rest / n_cs, h = bh % a.Hkv;
+    const int n_cs = a.n_cs;                      // CTAs along the keys; joined: neighbours (a cluster)
+    constexpr bool joined = JOINED;               // (compiled apart: the other form is a few percent faster without this one's code)
+    const int rest = joined ? blockIdx.x / n_cs : blockIdx.x / a.units, unit = joined ? rest % a.units : blockIdx.x % a.units;
+    const int cs = joined ? blockIdx.x % n_cs : rest % n_cs, bh = rest / (joined ? a.units : n_cs), h = bh % a.Hkv;
     int b = bh / a.Hkv;
     const int qt0 = shared_keys ? unit * 2 : 0;
     const int n_streams = shared_keys ? min(2, a.n_qt - qt0) : 2;
@@ -170,16 +185,30 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     }
     const int L = length(b), tiles = (L + 127) / 128;
     if (a.fused) {
-        if (threadIdx.x < 2) {
-            // thread s lists the own tiles of stream s: the drafts whose tokens are in its query tile
-            const int s = threadIdx.x, first = (qt0 + s) * a.tq, last = min(a.T, first + a.tq) - 1;
-            int n = 0;
+        if (warp < 2) {
+            // warp s lists the own tiles of stream s, the drafts whose tokens are in its query tile, a lane per draft (joined: every n_cs-th tile, or with
+            // one query tile every 2 n_cs-th)
+            const int s = warp, first = (qt0 + (shared_keys ? s : 0)) * a.tq, last = min(a.T, first + a.tq) - 1;
+            const int deal = !joined ? 1 : shared_keys ? n_cs : 2 * n_cs, mine = !joined ? 0 : shared_keys ? cs : 2 * cs + s;
+            int before = 0;
             if (s < n_streams && a.S > 0)
-                for (int d = first / a.M; d <= last / a.M; ++d) {
-                    const int len = a.own_len ? min(max(a.own_len[(int64_t)b * a.D + d], 0), a.S) : a.S;
-                    for (int k0 = 0; k0 < len && n < kMaxOwnTiles; k0 += 128) own[s * kMaxOwnTiles + n++] = OwnTile{d, k0, len};
+                for (int d0 = first / a.M; d0 <= last / a.M; d0 += 32) {
+                    const int d = d0 + lane;
+                    const int len = d > last / a.M ? 0 : a.own_len ? min(max(a.own_len[(int64_t)b * a.D + d], 0), a.S) : a.S;
+                    int upto = (len + 127) / 128;
+                    const int n = upto;
+#pragma unroll
+                    for (int x = 1; x < 32; x *= 2) {
+                        const int y = __shfl_up_sync(0xffffffffu, upto, x);
+                        if (lane >= x) upto += y;
+                    }
+                    for (int k = 0; k < n; ++k) {
+                        const int i = before + upto - n + k;
+                        if (i % deal == mine && i / deal < kMaxOwnTiles) own[s * kMaxOwnTiles + i / deal] = OwnTile{d, k * 128, len};
+                    }
+                    before += __shfl_sync(0xffffffffu, upto, 31);
                 }
-            n_own[s] = n;
+            if (lane == 0) n_own[s] = min(before > mine ? (before - mine + deal - 1) / deal : 0, kMaxOwnTiles);
         }
         __syncthreads();
     }
@@ -329,7 +358,7 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     if (j >= np) {
                         const OwnTile o = own[s * kMaxOwnTiles + j - np];
                         left = o.len - o.key0;
-                        const int lo = (o.node * a.M - (qt0 + s) * a.tq) * a.G, hi = lo + a.M * a.G;
+                        const int lo = (o.node * a.M - (qt0 + (shared_keys ? s : 0)) * a.tq) * a.G, hi = lo + a.M * a.G;
 #pragma unroll
                         for (int w = 0; w < 4; ++w) {
                             const int l0 = min(max(lo - w * 32, 0), 32), h0 = min(max(hi - w * 32, 0), 32);     // active rows [l0, h0)
@@ -523,7 +552,26 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         for (const int n_full = min(np, L / 128 - first_tile); ok && j < n_full; ++j) ok = tile(j, std::true_type());
 #pragma unroll 1
         for (; ok && j < n; ++j) ok = tile(j, std::false_type());
-        if (s < n_streams) {
+        if (joined) {
+            // outputs (of a row: 16-byte pieces, rotated by the row so that a quarter of a warp writes all banks) and (reference, sum)
+            // into the ring, which is free once both streams' products are done
+            for (int x = 0; ok && x < 2; ++x)
+                if ((x ? nt1 : nt0) > 0) ok = mbar_wait_warp(&o_done[x], 0, wc);
+            tc_fence_after();
+            const float u = np < n ? 1.f : vref;
+            const uint32_t to = smem_u32(ring) + (s * 128 + row) * DHP * 4;
+#pragma unroll 1
+            for (int c = 0; ok && n > 0 && c < a.Dh; c += 32) {
+                uint32_t x[32];
+                tmem_ld32(t_o + c, x);
+                tmem_wait_ld(x);
+#pragma unroll
+                for (int i = 0; i < 32; i += 4)
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((((c + i) / 4) ^ (row & 7)) << 4)), "f"(__uint_as_float(x[i]) * u),
+                                 "f"(__uint_as_float(x[i + 1]) * u), "f"(__uint_as_float(x[i + 2]) * u), "f"(__uint_as_float(x[i + 3]) * u) : "memory");
+            }
+            reinterpret_cast<float2*>(raw)[s * 128 + row] = n == 0 || (fresh && l == 0.f) ? make_float2(-INFINITY, 0.f) : make_float2(m, l);
+        } else if (s < n_streams) {
             const bool live = row < a.tq * a.G && my_tok < a.T;
             if (n > 0 && ok) {
                 ok = mbar_wait_warp(&o_done[s], 0, wc);
@@ -579,8 +627,92 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             }
         }
     }
+    __syncwarp();
     tc_fence_before();
-    __syncthreads();
+    if (joined) {
+        cluster_sync();
+        if (warp < 8 && !*abort_flag) {
+            // A share of the rows; part p of a row is CTA p's (one query tile: stream p % 2 of CTA p / 2).  First the parts' weights, a thread per row,
+            // then the outputs, a thread per row and four columns.
+            const int n_rows = shared_keys ? n_streams * 128 : 128, parts = shared_keys ? n_cs : 2 * n_cs;
+            const int lo = n_rows * cs / n_cs, n_mine = n_rows * (cs + 1) / n_cs - lo;
+            const uint32_t so = smem_u32(ring), stats = smem_u32(raw);
+            float* weights = reinterpret_cast<float*>(raw + 2048);               // [128][kParts]
+            auto place = [&](int x, int q) { return shared_keys ? x : (q & 1) * 128 + x; };        // of row x in part q
+            auto owner = [&](int q) { return shared_keys ? q : q / 2; };
+            auto token = [&](int x) {                                              // -1: no row
+                const int r = x & 127, t = (qt0 + (x >> 7)) * a.tq + r / a.G;
+                return r < a.tq * a.G && t < a.T ? t : -1;
+            };
+            if ((int)threadIdx.x < n_mine) {
+                const int x = lo + threadIdx.x, t = token(x);
+                float mm[kParts], ll[kParts], top = -INFINITY, sum = 0.f;
+#pragma unroll
+                for (int q = 0; q < kParts; ++q) {
+                    mm[q] = -INFINITY;
+                    ll[q] = 0.f;
+                    if (q < parts && t >= 0)
+                        asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(mm[q]), "=f"(ll[q]) : "r"(peer(stats + place(x, q) * 8, owner(q))) : "memory");
+                }
+#pragma unroll
+                for (int q = 0; q < kParts; ++q) top = fmaxf(top, mm[q]);
+                const float base = top == -INFINITY ? 0.f : top;
+                bool some = false;
+#pragma unroll
+                for (int q = 0; q < kParts; ++q)
+                    if (mm[q] != -INFINITY) {                                    // (others hold no outputs)
+                        some = true;
+                        mm[q] = ex2(mm[q] - base);
+                        sum = fmaf(mm[q], ll[q], sum);
+                    } else {
+                        mm[q] = 0.f;
+                    }
+                const float inv = some ? 1.f / sum : 0.f;
+#pragma unroll
+                for (int q = 0; q < kParts; ++q) weights[threadIdx.x * kParts + q] = mm[q] * inv;
+                if (a.lse && t >= 0) a.lse[((int64_t)b * a.T + t) * a.Hq + h * a.G + (x & 127) % a.G] = some ? top * kLn2 + logf(sum) : -INFINITY;
+            }
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+#pragma unroll 1
+            for (int i = threadIdx.x; i < n_mine * (DHP / 4); i += 256) {
+                const int y = i / (DHP / 4), col = i % (DHP / 4) * 4, x = lo + y, r = x & 127, t = token(x);
+                if (t < 0 || col >= a.Dh) continue;
+                const float* w = weights + y * kParts;
+                float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+                for (int q0 = 0; q0 < parts; q0 += 8) {
+                    float4 z[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        z[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (q0 + q < parts && w[q0 + q] != 0.f)
+                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(z[q].x), "=f"(z[q].y), "=f"(z[q].z), "=f"(z[q].w)
+                                         : "r"(peer(so + place(x, q0 + q) * DHP * 4 + (((col >> 2) ^ (r & 7)) << 4), owner(q0 + q))) : "memory");
+                    }
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const float f = q0 + q < parts ? w[q0 + q] : 0.f;
+                        acc[0] = fmaf(f, z[q].x, acc[0]); acc[1] = fmaf(f, z[q].y, acc[1]);
+                        acc[2] = fmaf(f, z[q].z, acc[2]); acc[3] = fmaf(f, z[q].w, acc[3]);
+                    }
+                }
+                uint32_t y0, y1;
+                if (BF16) {
+                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y0) : "f"(acc[1]), "f"(acc[0]));
+                    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y1) : "f"(acc[3]), "f"(acc[2]));
+                } else {
+                    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y0) : "f"(acc[1]), "f"(acc[0]));
+                    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(y1) : "f"(acc[3]), "f"(acc[2]));
+                }
+                *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(a.out) + ((int64_t)b * a.T + t) * a.out_token + (int64_t)(h * a.G + r % a.G) * a.out_head + col) =
+                    make_uint2(y0, y1);
+            }
+        }
+        __syncwarp();
+        cluster_sync();                                  // no CTA leaves while another reads its shared memory
+    } else {
+        __syncthreads();
+    }
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == 9) {
         __syncwarp();
@@ -601,41 +733,80 @@ bool make_tile_map(CUtensorMap* m, const void* base, const psd_kv_strides_t& s, 
               CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int SLABS, bool BF16>
-int launch_t(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mko, const CUtensorMap& mvo, const TcArgs& a, int64_t grid, cudaStream_t st) {
+template <int SLABS, bool BF16, bool JOINED>
+int launch_j(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mko, const CUtensorMap& mvo, const TcArgs& a, int64_t grid,
+             cudaStream_t st) {
     constexpr int TILE = SLABS * kSlabBytes;
     constexpr int smem = (2 + Rings<SLABS>::WIDE) * TILE + Rings<SLABS>::RAW * (TILE / 2) + kBarBytes;
     static_assert(smem <= 227 * 1024, "shared memory of the 8-bit tile kernel");
+    static_assert(Rings<SLABS>::WIDE * TILE >= 2 * 128 * SLABS * 64 * 4 && Rings<SLABS>::RAW * (TILE / 2) >= 2 * 128 * 8 + 128 * kParts * 4, "outputs and sums that a cluster joins");
     static std::atomic<unsigned long long> set{0};
-    if (!ensure_dynamic_smem(prefix_tiles_q8_kernel<SLABS, BF16>, smem, set)) return PSD_ERR_CUDA;
+    if (!ensure_dynamic_smem(prefix_tiles_q8_kernel<SLABS, BF16, JOINED>, smem, set)) return PSD_ERR_CUDA;
     static std::atomic<int> regs{0};      // 8 warps of 192 and 8 of 64 registers a thread
-    if (!launched_with(prefix_tiles_q8_kernel<SLABS, BF16>, (256 * 192 + 256 * 64) / kQThreads, regs)) return PSD_ERR_CUDA;
+    if (!launched_with(prefix_tiles_q8_kernel<SLABS, BF16, JOINED>, (256 * 192 + 256 * 64) / kQThreads, regs)) return PSD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(kQThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {JOINED ? (unsigned)a.n_cs : 1u, 1u, 1u};
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, prefix_tiles_q8_kernel<SLABS, BF16>, mq, mk, mv, mko, mvo, a);
+    cfg.numAttrs = JOINED ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, prefix_tiles_q8_kernel<SLABS, BF16, JOINED>, mq, mk, mv, mko, mvo, a);
     count_launch();
     return e == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
 }
 
+template <int SLABS, bool BF16>
+int launch_t(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const CUtensorMap& mko, const CUtensorMap& mvo, const TcArgs& a, int64_t grid,
+             cudaStream_t st) {
+    return a.fused == 2 ? launch_j<SLABS, BF16, true>(mq, mk, mv, mko, mvo, a, grid, st) : launch_j<SLABS, BF16, false>(mq, mk, mv, mko, mvo, a, grid, st);
+}
+
 }  // namespace
 
+// Clusters of n CTAs of this kernel that the device holds at once (asked once per device; without a device: a B200 whose processor clusters leave
+// 15 clusters of 8).
+int q8_clusters(int n) {
+    static const int usual[9] = {0, 148, 74, 45, 33, 26, 22, 15, 15};
+    static std::atomic<int> seen[64][9];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return usual[n];
+    int v = seen[dev][n].load(std::memory_order_relaxed);
+    if (v > 0) return v;
+    constexpr int smem = (2 + Rings<2>::WIDE) * 2 * kSlabBytes + Rings<2>::RAW * kSlabBytes + kBarBytes;
+    static std::atomic<unsigned long long> set{0};
+    if (!ensure_dynamic_smem(prefix_tiles_q8_kernel<2, true, true>, smem, set)) return usual[n];
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)n * 64);
+    cfg.blockDim = dim3(kQThreads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim = {(unsigned)n, 1u, 1u};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&v, prefix_tiles_q8_kernel<2, true, true>, &cfg) != cudaSuccess || v < 1) {
+        cudaGetLastError();
+        v = usual[n];
+    }
+    seen[dev][n].store(v, std::memory_order_relaxed);
+    return v;
+}
+
 int launch_prefix_tiles_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const void* k_own, const void* v_own,
-                           const int32_t* own_len, const psd_attention_t& a, const PrefixPlan& p, float* po, float* pl, void* out, float* lse,
-                           int32_t* status_dev, cudaStream_t st) {
+                           const int32_t* own_len, const psd_attention_t& a, const PrefixPlan& p, bool joined, float* po, float* pl, void* out,
+                           float* lse, int32_t* status_dev, cudaStream_t st) {
     CUtensorMap mq, mk, mv, mko, mvo;
     if (!make_query_map(&mq, q, a, p.tq) || !make_tile_map(&mk, c.k, a.kp, a.B, a.P, a.Hkv, a.Dh, p.dhp) ||
         !make_tile_map(&mv, c.v, a.vp, a.B, a.P, a.Hkv, a.Dh, p.dhp))
         return PSD_ERR_CUDA;
     const int own_box = a.S >= 128 ? 128 : (a.S + 15) / 16 * 16;
-    if (p.fused && a.S > 0) {
+    if ((p.fused || joined) && a.S > 0) {
         if (!make_cache_map(&mko, k_own, a.dtype, a.ko, a.B * a.D, a.S, a.Hkv, a.Dh, own_box) ||
             !make_cache_map(&mvo, v_own, a.dtype, a.vo, a.B * a.D, a.S, a.Hkv, a.Dh, own_box))
             return PSD_ERR_CUDA;
@@ -659,7 +830,8 @@ int launch_prefix_tiles_q8(const void* q, const PrefixQ8& c, const int32_t* pref
     x.v_outer = a.vp.outer ? 1 : 0; x.v_head = a.vp.head ? 1 : 0;
     x.B = a.B;
     x.longest_first = prefix_len && a.B > 1 && a.B <= kMaxSorted && grid > sm_count() ? 1 : 0;
-    x.fused = p.fused ? 1 : 0;
+    x.fused = joined ? 2 : p.fused ? 1 : 0;
+    x.n_cs = p.n_qt > 1 ? p.splits : p.splits / 2;
     x.D = a.D; x.M = a.M; x.S = a.S; x.causal = a.causal; x.own_box = own_box > 0 ? own_box : 16;
     x.ko_outer = a.ko.outer ? 1 : 0; x.ko_head = a.ko.head ? 1 : 0;
     x.vo_outer = a.vo.outer ? 1 : 0; x.vo_head = a.vo.head ? 1 : 0;

@@ -13,11 +13,13 @@ from test_gpu_q8 import _cache, _check, _f64, _head_inputs, _i32, _rnd, _run_hea
 pytestmark = pytest.mark.gpu
 
 ROWS = (3, 1, 1, 8, 2, 128, 700, 6)           # few rows per key head
-PARTIAL = (1, 4, 32, 8, 2, 128, 700, 32)      # query tiles, keys split
+PARTIAL = (1, 16, 2, 8, 2, 128, 700, 2)       # a query tile, keys split, a second kernel joins
+JOINED = (1, 4, 32, 8, 2, 128, 700, 32)       # query tiles, keys split over a cluster that joins
+JOINED_ONE = (1, 1, 32, 8, 2, 64, 900, 32)    # the same with one query tile
 FUSED = (16, 4, 64, 32, 8, 128, 300, 64)      # query tiles, own keys in the same kernel
 SMALL = (40, 4, 33, 16, 4, 64, 200, 33)       # the same with heads of 64, two drafts to a tile
 FORMS = {ROWS: "prefix_rows_q8_kernel+draft_attention_kernel", PARTIAL: "prefix_tiles_q8_kernel+draft_attention_kernel",
-         FUSED: "prefix_tiles_q8_kernel", SMALL: "prefix_tiles_q8_kernel"}
+         JOINED: "prefix_tiles_q8_kernel", JOINED_ONE: "prefix_tiles_q8_kernel", FUSED: "prefix_tiles_q8_kernel", SMALL: "prefix_tiles_q8_kernel"}
 
 
 def _space(n):
@@ -47,7 +49,26 @@ def _attend(t, ws=None, block=32, status=None, **kw):
 
 @pytest.mark.parametrize("shape", list(FORMS))
 def test_shapes_reach_their_form(shape):
-    assert psd.psd_attention_q8_kernel_names(*shape)[0] == FORMS[shape]
+    names, splits = psd.psd_attention_q8_kernel_names(*shape)
+    assert names == FORMS[shape] and (splits > 1) == (shape in (PARTIAL, JOINED, JOINED_ONE, ROWS))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", [(1, 4, 32, 8, 2, 128, 700, 32), (1, 1, 32, 8, 2, 64, 900, 32), (1, 2, 16, 8, 2, 64, 900, 40), (2, 4, 33, 14, 2, 96, 1500, 33), (1, 1, 300, 2, 2, 128, 1025, 300),
+                                   (3, 2, 40, 4, 2, 80, 600, 129), (1, 4, 32, 16, 4, 128, 2000, 32)])
+def test_keys_split_over_a_cluster(shape, causal, dtype):
+    """Sequences shorter than the splits, without a prefix, own keys of several tiles dealt out to the cluster."""
+    B, D, M, Hq, Hkv, Dh, P, S = shape
+    names, splits = psd.psd_attention_q8_kernel_names(*shape)
+    assert names == "prefix_tiles_q8_kernel" and splits > 1
+    for plen in ([P] * B, [P // 3 + 1] * B, [[100, 0, P][b % 3] for b in range(B)], [0] * B):
+        for olen in ([S] * (B * D), [[0, S, 1][n % 3] for n in range(B * D)]):
+            t, kp, vp = _inputs(shape, 4, {"bf16": torch.bfloat16, "fp16": torch.float16}[dtype], 32, plen, olen)
+            past = torch.arange(S, device="cuda")[None] >= t["own_len"][:, None]
+            t["k_own"][past], t["v_own"][past] = math.nan, math.inf
+            out, lse = _attend(t, causal=causal)
+            _check(out, lse, t["q"], kp, vp, np.nan_to_num(_f64(t["k_own"])), np.nan_to_num(_f64(t["v_own"]), posinf=0), plen, olen, Dh ** -0.5, causal, dtype)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
@@ -131,7 +152,7 @@ def test_scales(shape):
     assert bool((l - math.log(P)).abs().max() <= 1e-5)
 
 
-@pytest.mark.parametrize("shape", [PARTIAL, FUSED, SMALL])
+@pytest.mark.parametrize("shape", [PARTIAL, JOINED, FUSED, SMALL])
 def test_a_draft_does_not_reach_another(shape):
     """NaN and infinities in one draft's own keys and values leave all other drafts' bits as they were."""
     B, D, M, Hq, Hkv, Dh, P, S = shape
@@ -145,7 +166,7 @@ def test_a_draft_does_not_reach_another(shape):
     assert bool((~torch.isfinite(o[n].float())).all())
 
 
-@pytest.mark.parametrize("shape", [ROWS, PARTIAL])
+@pytest.mark.parametrize("shape", [ROWS, PARTIAL, JOINED])
 def test_a_cache_shared_by_all_heads_and_sequences(shape):
     """Stride 0 of the outer dimension and of the heads."""
     B, D, M, Hq, Hkv, Dh, P, S = shape
@@ -379,7 +400,7 @@ def test_a_workspace_for_the_largest_batch_serves_smaller_ones():
         assert torch.equal(o, out) and torch.equal(l, lse)
 
 
-@pytest.mark.parametrize("what", [ROWS, PARTIAL, FUSED, "head"])
+@pytest.mark.parametrize("what", [ROWS, PARTIAL, JOINED, JOINED_ONE, FUSED, "head"])
 def test_a_wait_that_runs_out(what):
     """With the loaders told to wait on a barrier that nothing arrives on, the call and its kernels return and the status word says so; the next call is
     as ever."""

@@ -188,7 +188,9 @@ def test_attention_kernel_names():
     """Few rows per key head, query tiles with and without partial results, no prefix; the splits of the partial results."""
     names = lambda *a: psd.psd_attention_q8_kernel_names(*a)  # noqa: E731
     assert names(64, 1, 1, 32, 8, 128, 16384, 64)[0] == "prefix_rows_q8_kernel+draft_attention_kernel"
-    assert names(1, 4, 32, 32, 8, 128, 2000, 32) == ("prefix_tiles_q8_kernel+draft_attention_kernel", 8)
+    assert names(1, 16, 1, 32, 8, 128, 4000, 8) == ("prefix_tiles_q8_kernel+draft_attention_kernel", 16)
+    which, splits = names(1, 4, 32, 32, 8, 128, 2000, 32)
+    assert which == "prefix_tiles_q8_kernel" and 2 <= splits <= 8                        # joined by a cluster
     assert names(16, 8, 64, 32, 8, 128, 8192, 64) == ("prefix_tiles_q8_kernel", 1)
     assert names(16, 8, 64, 32, 8, 128, 0, 64)[0] == "draft_attention_kernel"
     assert names(1, 1, 1, 3, 2, 128, 100, 1) is None and names(1, 1, 1, 2, 2, 72, 100, 1) is None
