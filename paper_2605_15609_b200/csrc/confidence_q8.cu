@@ -15,6 +15,7 @@
 // there, 94 bytes per clock and SM from L2 are what the products need.
 #include <algorithm>
 #include "attn_tc.cuh"
+#include "combine.cuh"
 
 namespace psd {
 namespace {
@@ -229,6 +230,61 @@ confidence_q8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     }
 }
 
+// Joins the triples of few rows, a warp per row and lanes along the splits, all loads issued together: combine_kernel's 8 threads per row
+// would walk 19 of 148 splits each, one after the other (10 us for 128 rows, against 5).  Equal maxima keep the lower index, sums that hold a NaN stay NaN.
+constexpr int kJoinRows = 2048;
+__global__ void __launch_bounds__(128) join_triples_kernel(const float* __restrict__ pm, const float* __restrict__ ps, const int32_t* __restrict__ pa,
+                                                           const SplitPlan plan, int n_rows, int32_t* __restrict__ out_token, float* __restrict__ out_conf,
+                                                           float* __restrict__ out_lse, int32_t* status_dev) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (row >= n_rows) return;
+    const int n = plan.uniform > 0 ? plan.uniform : carried_splits(plan.G, plan.hb, (n_rows + plan.tile_rows - 1) / plan.tile_rows, row / plan.tile_rows);
+    constexpr int kBatch = 5;
+    float m = -INFINITY, s = 0.f;
+    int32_t a = INT32_MAX;
+    for (int j0 = lane; j0 < n; j0 += 32 * kBatch) {
+        float bm[kBatch], bs[kBatch];
+        int32_t ba[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int j = j0 + 32 * u;
+            const size_t o = (size_t)j * n_rows + row;
+            bm[u] = j < n ? pm[o] : -INFINITY;
+            bs[u] = j < n ? ps[o] : 0.f;
+            ba[u] = j < n ? pa[o] : INT32_MAX;
+        }
+        float top = m;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) top = fmaxf(top, bm[u]);
+        const float base = top == -INFINITY ? 0.f : top;
+        s *= expf(m - base);
+        if (m != top) a = INT32_MAX;
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            s = fmaf(bs[u], expf(bm[u] - base), s);
+            if (bm[u] == top) a = min(a, ba[u]);
+        }
+        m = top;
+    }
+    float top = m;
+#pragma unroll
+    for (int x = 16; x; x >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+    s *= expf(m - (top == -INFINITY ? 0.f : top));
+    if (m != top) a = INT32_MAX;
+#pragma unroll
+    for (int x = 16; x; x >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, x);
+        a = min(a, __shfl_xor_sync(0xffffffffu, a, x));
+    }
+    if (lane == 0) {
+        out_token[row] = a;
+        out_conf[row] = 1.0f / s;
+        if (out_lse) out_lse[row] = top + logf(s);
+        if (status_dev && !(isfinite(top) && isfinite(s))) count_nonfinite_row(status_dev);
+    }
+}
+
 // A [rows, H] matrix of codes, boxes of 128 x box_rows, 128-byte swizzle, zeros outside.
 bool make_codes_map(CUtensorMap* m, const void* base, int rows, int H, int box_rows) {
     EncodeTiledFn fn = encode_fn();
@@ -280,6 +336,24 @@ int launch_confidence_q8(const int8_t* x, const float* x_scale, const int8_t* w,
     cfg.numAttrs = 1;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, confidence_q8_kernel, map_a, map_bw, map_bn, g, n_rows, H, V, x_scale, w_scale, part.m,
                                              part.s, part.a, status_dev, part.cap);
+    count_launch();
+    return e == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
+}
+
+int launch_join_triples(Partials part, const SplitPlan& plan, int n_rows, int32_t* out_token, float* out_conf, float* out_lse, int32_t* status_dev,
+                        cudaStream_t st) {
+    if (n_rows > kJoinRows) return launch_combine(part, plan, n_rows, out_token, out_conf, out_lse, st, nullptr, nullptr, 0, status_dev);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((n_rows + 3) / 4);
+    cfg.blockDim = dim3(128);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, join_triples_kernel, (const float*)part.m, (const float*)part.s, (const int32_t*)part.a, plan, n_rows,
+                                             out_token, out_conf, out_lse, status_dev);
     count_launch();
     return e == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
 }

@@ -55,5 +55,7 @@ int launch_rotate(const void* q, const void* k, const void* v, const int32_t* po
 // confidence_q8.cu
 int launch_confidence_q8(const int8_t* x, const float* x_scale, const int8_t* w, const float* w_scale, int n_rows, int H, int V,
                          Partials part, int32_t* status_dev, cudaStream_t st, SplitPlan* plan);
+int launch_join_triples(Partials part, const SplitPlan& plan, int n_rows, int32_t* out_token, float* out_conf, float* out_lse, int32_t* status_dev,
+                        cudaStream_t st);
 
 }  // namespace psd

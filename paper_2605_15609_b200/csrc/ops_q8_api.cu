@@ -172,7 +172,7 @@ int psd_confidence_q8(const void* hidden, int32_t dtype, const int8_t* w_codes, 
     if (const int e = launch_quantize_rows(hidden, dtype, H, n_rows, H, codes, H, scale, st)) return e;
     SplitPlan plan;
     if (const int e = launch_confidence_q8(codes, scale, w_codes, w_scale, n_rows, H, V, part, status_dev, st, &plan)) return e;
-    return launch_combine(part, plan, n_rows, out_token, out_conf, out_lse, st, nullptr, nullptr, 0, status_dev);
+    return launch_join_triples(part, plan, n_rows, out_token, out_conf, out_lse, status_dev, st);
 }
 
 }  // extern "C"
