@@ -52,7 +52,7 @@ int launch_prefix_quantize(const void* k, const void* v, const int32_t* begin, c
 int launch_rotate(const void* q, const void* k, const void* v, const int32_t* position, const double* frequency, const void* q_norm,
                   const void* k_norm, const int32_t* slot, const psd_rotate_t& a, void* q_out, void* k_out, void* v_out, cudaStream_t st);
 
-// confidence_q8.cu
+// confidence_q8.cu (x: memory for n_rows rounded up to 128 rows)
 int launch_confidence_q8(const int8_t* x, const float* x_scale, const int8_t* w, const float* w_scale, int n_rows, int H, int V,
                          Partials part, int32_t* status_dev, cudaStream_t st, SplitPlan* plan);
 int launch_join_triples(Partials part, const SplitPlan& plan, int n_rows, int32_t* out_token, float* out_conf, float* out_lse, int32_t* status_dev,

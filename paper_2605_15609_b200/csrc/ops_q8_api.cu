@@ -12,6 +12,8 @@ bool head_ok(int32_t Dh) { return Dh >= 8 && Dh <= 128 && Dh % 8 == 0; }
 bool block_ok(int32_t n) { return n == 16 || n == 32 || n == 64 || n == 128; }
 constexpr int32_t kMostSteps = 1 << 30;
 bool eights(int64_t a, int64_t b, int64_t c) { return a % 8 == 0 && b % 8 == 0 && c % 8 == 0; }
+// codes of the hidden rows: whole tiles of 128 rows (launch_confidence_q8)
+size_t codes_bytes(int32_t n_rows, int32_t H) { return round_up((size_t)((n_rows + 127) / 128) * 128 * H); }
 bool head_shape_ok(int32_t n_rows, int32_t H, int32_t V) {
     // sums of products of codes stay below 2^31: 127 * 127 * 131072
     return n_rows >= 1 && n_rows <= kMostSteps && H >= 64 && H % 64 == 0 && H <= 131072 && V >= 1 && V < 2147483647 - 256;
@@ -152,7 +154,7 @@ int psd_draft_attention_q8(const void* q, const int8_t* k_codes, const int8_t* v
 
 size_t psd_confidence_q8_workspace_bytes(int32_t n_rows, int32_t H, int32_t V) {
     if (!head_shape_ok(n_rows, H, V)) return 0;
-    return partial_bytes(n_rows, V) + round_up((size_t)n_rows * H) + round_up((size_t)n_rows * 4);
+    return partial_bytes(n_rows, V) + codes_bytes(n_rows, H) + round_up((size_t)n_rows * 4);
 }
 
 int psd_confidence_q8(const void* hidden, int32_t dtype, const int8_t* w_codes, const float* w_scale, int32_t n_rows, int32_t H,
@@ -168,7 +170,7 @@ int psd_confidence_q8(const void* hidden, int32_t dtype, const int8_t* w_codes, 
     cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
     const Partials part = carve_partials(workspace, n_rows, V);
     int8_t* codes = reinterpret_cast<int8_t*>(workspace) + partial_bytes(n_rows, V);
-    float* scale = reinterpret_cast<float*>(codes + round_up((size_t)n_rows * H));
+    float* scale = reinterpret_cast<float*>(codes + codes_bytes(n_rows, H));
     if (const int e = launch_quantize_rows(hidden, dtype, H, n_rows, H, codes, H, scale, st)) return e;
     SplitPlan plan;
     if (const int e = launch_confidence_q8(codes, scale, w_codes, w_scale, n_rows, H, V, part, status_dev, st, &plan)) return e;
