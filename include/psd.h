@@ -731,7 +731,8 @@ int psd_prefix_quantize(const void* k, const void* v, const int32_t* begin, cons
 size_t psd_attention_q8_workspace_bytes(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P, int32_t S);
 
 /* Names of the kernels that psd_draft_attention_q8 launches at these sizes, as psd_attention_kernel_names tells them: "prefix_rows_q8_kernel"
- * (few rows per key head) or "prefix_tiles_q8_kernel", and "+draft_attention_kernel" where partial results are joined. */
+ * (few rows per key head) or "prefix_tiles_q8_kernel", and "+draft_attention_kernel" where partial results are joined; "draft_attention_kernel"
+ * alone: a short prefix, or none. */
 const char* psd_attention_q8_kernel_names(int32_t B, int32_t D, int32_t M, int32_t Hq, int32_t Hkv, int32_t Dh, int32_t P,
                                           int32_t S, int32_t* splits);
 

@@ -7,11 +7,16 @@
 // V tiles are double-buffered by asynchronous copies that fill what lies past a length (or past Dh) with zeros, so nothing
 // that was never written is multiplied.
 //
+// CODES: the prefix is a cache of 8-bit codes (prefix_attention_q8.cu), short enough to be walked here.  Its tiles are widened on their way to
+// shared memory (keys to T, values to fp16; registers hold the next tile's codes meanwhile), scores are multiplied by their key's scale, weights, in fp16,
+// by the value's, relative to the largest of the sequence; outputs are relative to that until the first own tile.
+//
 // What the warps of a row block hold and the partial results over the prefix are then joined row by row, a warp per row
 // and all lanes along Dh: the kernel's time is the traffic of those partial results (4 bytes per output element and split
 // against 2 written), and this order reads and writes whole lines.
 #include "attn_tc.cuh"
 #include "prefix_attention.cuh"
+#include "prefix_attention_q8.cuh"
 
 namespace psd {
 namespace {
@@ -23,6 +28,7 @@ constexpr int kThreads = 128;
 // that far below a maximum count together; with the largest weight at 2^15 nothing above 2^-40 of it is lost.
 template <typename T> struct Mma;
 template <> struct Mma<__nv_bfloat16> {
+    static constexpr bool BF16 = true;
     static constexpr float ROOM = 0.f;
     static __device__ __forceinline__ void run(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -36,6 +42,7 @@ template <> struct Mma<__nv_bfloat16> {
     }
 };
 template <> struct Mma<__half> {
+    static constexpr bool BF16 = false;
     static constexpr float ROOM = 15.f;
     static __device__ __forceinline__ void run(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -73,6 +80,9 @@ struct OwnArgs {
     const float *po, *pl;
     int splits;          // <= kMaxPrefixSplits
     int64_t rows;
+    PrefixQ8 q8;         // CODES: the prefix
+    int nb, shift;
+    uint32_t f16_codes, bf16_codes;
 };
 
 // Joins the rows warp, warp + 4, .. of a CTA: WK warps' results in shared memory and the splits' in global memory, RB rows
@@ -162,8 +172,10 @@ __device__ __forceinline__ void join_rows(const OwnArgs& p, const float* so, con
     }
 }
 
-template <typename T, int DHP, int WM>
-__global__ void __launch_bounds__(kThreads, WM == 1 ? 4 : 3) draft_attention_kernel(const OwnArgs p) {
+template <typename T, int DHP, int WM, bool CODES>
+__global__ void __launch_bounds__(kThreads, WM == 1 && !CODES ? 4 : 3) draft_attention_kernel(const OwnArgs p) {
+    constexpr bool BF16 = Mma<T>::BF16;
+    constexpr float ROOM = CODES ? 15.f : Mma<T>::ROOM;         // (weights over codes are fp16)
     constexpr int WK = 4 / WM, KPW = kKeys / WK;      // warps per row block, keys per warp and tile
     constexpr int LD = DHP + 8;                        // padded row of a tile (bank-conflict-free ldmatrix)
     constexpr int NQ = DHP / 16, NO = DHP / 8, NS = KPW / 8;
@@ -233,10 +245,64 @@ __global__ void __launch_bounds__(kThreads, WM == 1 ? 4 : 3) draft_attention_ker
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     const bool ahead = p.stages == 2;
-    if (ahead && tiles_n > 0) fetch(0, 0);
+    if (ahead && tiles_n > 0 && (!CODES || tp == 0)) fetch(0, 0);
+    // CODES: a tile's codes and scales, between memory and shared memory
+    constexpr int PIECES = kKeys * (DHP / 8) / kThreads;                      // of 8 codes, a thread's, of keys and as many of values
+    __shared__ float key_scale[CODES ? kKeys : 1], value_scale[CODES ? kKeys : 1];
+    uint2 codes[CODES ? 2 * PIECES : 1];
+    float scale_kv = 0.f, vref = 1.17549435e-38f, vinv = 0.f;
+    const float *ks = nullptr, *vs = nullptr;
+    auto load_codes = [&](int t) {
+        const int8_t* kb = p.q8.k + b * a.kp.outer + h * a.kp.head;
+        const int8_t* vb = p.q8.v + b * a.vp.outer + h * a.vp.head;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int x = threadIdx.x + i * kThreads, c = x % (DHP / 8) * 8, j = t * kKeys + x / (DHP / 8);
+            const bool ok = j < Lp && c < a.Dh;
+            codes[i] = ok ? *reinterpret_cast<const uint2*>(kb + j * a.kp.token + c) : make_uint2(0u, 0u);
+            codes[PIECES + i] = ok ? *reinterpret_cast<const uint2*>(vb + j * a.vp.token + c) : make_uint2(0u, 0u);
+        }
+        // threads 0 .. 63: the keys' scales, 64 .. 127: the values'; those of keys past the end were never written
+        const int j = t * kKeys + threadIdx.x % kKeys;
+        scale_kv = 0.f;
+        if (j < Lp) {
+            scale_kv = (int)threadIdx.x < kKeys ? ks[j >> p.shift] * scale2 : vs[j >> p.shift] * vinv;
+            if ((int)threadIdx.x < kKeys && scale_kv == 0.f) scale_kv = 1.17549435e-38f;
+        }
+    };
+    auto store_codes = [&](int stage) {
+        T* dk = tiles + stage * 2 * kKeys * LD;
+        auto pair = [&](uint32_t w, uint32_t sel, bool bf16) {
+            const uint32_t x = __byte_perm(w, 0u, sel);
+            return bf16 ? codes_bf16(x, p.bf16_codes) : codes_f16(x, p.f16_codes);
+        };
+#pragma unroll
+        for (int i = 0; i < 2 * PIECES; ++i) {
+            const int x = threadIdx.x + i % PIECES * kThreads, c = x % (DHP / 8) * 8, r = x / (DHP / 8) + (i < PIECES ? 0 : kKeys);
+            const bool bf16 = BF16 && i < PIECES;
+            *reinterpret_cast<uint4*>(dk + r * LD + c) = make_uint4(pair(codes[i].x, 0x1100, bf16), pair(codes[i].x, 0x3322, bf16),
+                                                                     pair(codes[i].y, 0x1100, bf16), pair(codes[i].y, 0x3322, bf16));
+        }
+        ((int)threadIdx.x < kKeys ? key_scale : value_scale)[threadIdx.x % kKeys] = scale_kv;
+    };
+    if (CODES && Lp > 0) {
+        ks = p.q8.k_scale + ((int64_t)b * a.Hkv + h) * p.nb;
+        vs = p.q8.v_scale + ((int64_t)b * a.Hkv + h) * p.nb;
+        for (int j = lane; j <= (Lp - 1) >> p.shift; j += 32) vref = fmaxf(vref, vs[j]);
+#pragma unroll
+        for (int x = 16; x; x >>= 1) vref = fmaxf(vref, __shfl_xor_sync(0xffffffffu, vref, x));
+        vinv = 1.f / vref;
+        load_codes(0);
+    }
     for (int t = 0; t < tiles_n; ++t) {
-        if (!ahead) fetch(t, 0);
-        if (ahead && t + 1 < tiles_n) {
+        const bool coded = CODES && t < tp;
+        if (coded) {
+            store_codes(ahead ? t & 1 : 0);
+            if (t + 1 < tp) load_codes(t + 1);
+        } else if (!ahead) {
+            fetch(t, 0);
+        }
+        if (ahead && t + 1 < tiles_n && !(CODES && t + 1 < tp)) {
             fetch(t + 1, (t + 1) & 1);
             asm volatile("cp.async.wait_group 1;" ::: "memory");
         } else {
@@ -266,7 +332,8 @@ __global__ void __launch_bounds__(kThreads, WM == 1 ? 4 : 3) draft_attention_ker
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int j = j0 + n * 8 + (e & 1);
-                s[n][e] = j < (own ? own_seen[e >> 1] : Lp) ? s[n][e] * scale2 : -INFINITY;
+                const float by = coded ? key_scale[(wk * KPW + n * 8 + (lane & 3) * 2 + (e & 1)) % (CODES ? kKeys : 1)] : scale2;
+                s[n][e] = j < (own ? own_seen[e >> 1] : Lp) ? s[n][e] * by : -INFINITY;
                 mx[e >> 1] = fmaxf(mx[e >> 1], s[n][e]);
             }
         float f[2], base[2];
@@ -275,9 +342,10 @@ __global__ void __launch_bounds__(kThreads, WM == 1 ? 4 : 3) draft_attention_ker
             mx[u] = fmaxf(mx[u], __shfl_xor_sync(0xffffffffu, mx[u], 1));
             mx[u] = fmaxf(mx[u], __shfl_xor_sync(0xffffffffu, mx[u], 2));
             f[u] = m[u] == mx[u] ? 1.f : ex2(m[u] - mx[u]);
-            base[u] = mx[u] == -INFINITY ? 0.f : mx[u] - Mma<T>::ROOM;
+            base[u] = mx[u] == -INFINITY ? 0.f : mx[u] - ROOM;
             m[u] = mx[u];
             l[u] *= f[u];
+            if (CODES && t == tp && t > 0) f[u] *= vref;          // the first own tile: from here on outputs are relative to 1
         }
 #pragma unroll
         for (int n = 0; n < NO; ++n) {
@@ -289,9 +357,22 @@ __global__ void __launch_bounds__(kThreads, WM == 1 ? 4 : 3) draft_attention_ker
             for (int e = 0; e < 4; ++e) {
                 s[n][e] = ex2(s[n][e] - base[e >> 1]);
                 l[e >> 1] += s[n][e];
+                if (coded) s[n][e] *= value_scale[(wk * KPW + n * 8 + (lane & 3) * 2 + (e & 1)) % (CODES ? kKeys : 1)];
             }
 #pragma unroll
         for (int kb = 0; kb < KPW / 16; ++kb) {
+            if (coded) {
+                const uint32_t pa[4] = {Mma<__half>::pack(s[2 * kb][0], s[2 * kb][1]), Mma<__half>::pack(s[2 * kb][2], s[2 * kb][3]),
+                                        Mma<__half>::pack(s[2 * kb + 1][0], s[2 * kb + 1][1]), Mma<__half>::pack(s[2 * kb + 1][2], s[2 * kb + 1][3])};
+#pragma unroll
+                for (int n = 0; n < NO; n += 2) {
+                    uint32_t r[4];
+                    ldsm4_t(r, smem_u32(vt + (kb * 16 + (lane & 15)) * LD + n * 8 + (lane >> 4) * 8));
+                    Mma<__half>::run(o[n], pa, r[0], r[1]);
+                    Mma<__half>::run(o[n + 1], pa, r[2], r[3]);
+                }
+                continue;
+            }
             const uint32_t pa[4] = {Mma<T>::pack(s[2 * kb][0], s[2 * kb][1]), Mma<T>::pack(s[2 * kb][2], s[2 * kb][3]),
                                     Mma<T>::pack(s[2 * kb + 1][0], s[2 * kb + 1][1]), Mma<T>::pack(s[2 * kb + 1][2], s[2 * kb + 1][3])};
 #pragma unroll
@@ -309,6 +390,12 @@ __global__ void __launch_bounds__(kThreads, WM == 1 ? 4 : 3) draft_attention_ker
         l[u] += __shfl_xor_sync(0xffffffffu, l[u], 1);
         l[u] += __shfl_xor_sync(0xffffffffu, l[u], 2);
     }
+    if (CODES && tiles_n == tp) {                            // no own tile came
+#pragma unroll
+        for (int n = 0; n < NO; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[n][e] *= vref;
+    }
     // every warp's rows to shared memory (the tiles are no longer needed: the loop ends with a barrier)
     constexpr int OLD = DHP + 8;                             // padded row: the float2 stores of 8 rows hit different banks
     float* so = reinterpret_cast<float*>(smem);              // [4 warps][16][OLD]
@@ -320,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, WM == 1 ? 4 : 3) draft_attention_ker
         for (int n = 0; n < NO; ++n)
             *reinterpret_cast<float2*>(&so[r * OLD + n * 8 + (lane & 3) * 2]) = make_float2(o[n][2 * u], o[n][2 * u + 1]);
         if ((lane & 3) == 0) {
-            sm[r] = m[u] - Mma<T>::ROOM;      // what outputs and sums are relative to
+            sm[r] = m[u] - ROOM;      // what outputs and sums are relative to
             sm[64 + r] = l[u];
         }
     }
@@ -334,7 +421,7 @@ __global__ void __launch_bounds__(kThreads, WM == 1 ? 4 : 3) draft_attention_ker
     else join_rows<T, DHP, WK, 1, 8>(p, so, sm, rb * 16 * WM, row_end, node, h, warp, lane);
 }
 
-template <typename T, int DHP, int WM>
+template <typename T, int DHP, int WM, bool CODES>
 int launch_rows(OwnArgs& p, cudaStream_t st) {
     const psd_attention_t& a = p.a;
     const int rows = a.M * (a.Hq / a.Hkv);
@@ -347,7 +434,7 @@ int launch_rows(OwnArgs& p, cudaStream_t st) {
     constexpr int tile_bytes = 2 * kKeys * (DHP + 8) * 2, join_bytes = (4 * 16 * (DHP + 8) + 4 * 16 * 2) * 4;
     const int smem = p.stages * tile_bytes > join_bytes ? p.stages * tile_bytes : join_bytes;
     static std::atomic<unsigned long long> set{0};
-    if (!ensure_dynamic_smem(draft_attention_kernel<T, DHP, WM>, 2 * tile_bytes, set)) return PSD_ERR_CUDA;
+    if (!ensure_dynamic_smem(draft_attention_kernel<T, DHP, WM, CODES>, 2 * tile_bytes, set)) return PSD_ERR_CUDA;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(kThreads);
@@ -358,7 +445,7 @@ int launch_rows(OwnArgs& p, cudaStream_t st) {
     attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled() ? 1 : 0;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, draft_attention_kernel<T, DHP, WM>, (const OwnArgs)p);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, draft_attention_kernel<T, DHP, WM, CODES>, (const OwnArgs)p);
     count_launch();
     return e == cudaSuccess ? PSD_OK : PSD_ERR_CUDA;
 }
@@ -396,12 +483,12 @@ bool one_launch(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
     return waves * ((P + kKeys - 1) / kKeys) <= one_launch_tiles(Dh);
 }
 
-template <typename T, int DHP>
+template <typename T, int DHP, bool CODES = false>
 int launch_dh(OwnArgs& p, cudaStream_t st) {
     switch (row_blocks_per_cta((int64_t)p.a.B * p.a.D * p.a.Hkv, p.a.M * (p.a.Hq / p.a.Hkv))) {
-        case 4: return launch_rows<T, DHP, 4>(p, st);
-        case 2: return launch_rows<T, DHP, 2>(p, st);
-        default: return launch_rows<T, DHP, 1>(p, st);
+        case 4: return launch_rows<T, DHP, 4, CODES>(p, st);
+        case 2: return launch_rows<T, DHP, 2, CODES>(p, st);
+        default: return launch_rows<T, DHP, 1, CODES>(p, st);
     }
 }
 
@@ -453,9 +540,36 @@ const char* draft_attention_kernels(int B, int D, int M, int Hq, int Hkv, int Dh
     return p.fused ? "prefix_attention_kernel" : "prefix_attention_kernel+draft_attention_kernel";
 }
 
+// Whether this kernel walks a prefix in codes too: while it is short (a tile takes 1.6 us of a CTA, 0.8 with heads of 64, and more the more CTAs share an
+// SM), against what else there is: two launches for few rows of a key head, else the tcgen05 kernel.  Measured in us, this against that, 32 heads of 128 over
+// 8 where nothing else is said.  One token, prefix 64: 6.3, 8.4; 128: 7.9, 8.6; 257: 12.4, 10.6; 16 tokens, 128: 8.4, 10.2; 257: 13.0, 12.3; 64 tokens, 64:
+// 13.6, 18.1.  4 drafts of 32 tokens, 64: 9.4, 13.0; 257: 17.0, 17.2; 768: 31.1, 22.5; the same of 4 heads of 64, 257: 9.1, 15.3; 512: 11.5, 14.9; 1024:
+// 18.1, 17.2.  8 x 8 drafts of 4 tokens, 16 heads over 2, 64: 9.2, 20.4; 257: 17.0, 24.5; 512: 22.8, 20.2.  16 x 2 drafts of 8 tokens, 28 heads over 4, 64:
+// 16.9, 19.6; 128: 20.9, 17.9.  32 heads of 64 over 8, 16 x one token, 257: 7.9, 9.3; 512: 10.4, 10.0; 64 x one token, 64: 9.8, 9.6; 128: 12.0, 10.5.
+bool one_launch_codes(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
+    const PrefixPlan plan = plan_prefix(B, D, M, Hq, Hkv, Dh, P, S);
+    if (plan.fused && 3 * (int64_t)B * Hkv * plan.units >= sm_count() && (P > (Dh <= 64 ? 320 : 128) || drafts_per_tile(M, plan.tq) < 4)) return false;
+    const int rows = M * (Hq / Hkv), sms = sm_count();
+    const int64_t nh = (int64_t)B * D * Hkv;
+    const int r = 16 * row_blocks_per_cta(nh, rows);
+    const int64_t ctas = nh * ((rows + r - 1) / r);
+    if (ctas > 4 * sms) return false;
+    const int crowd = ctas <= 2 * sms ? 1 : ctas <= 3 * sms ? 2 : 4;
+    const bool few = (int64_t)D * rows <= 32;
+    return (int64_t)crowd * ((P + kKeys - 1) / kKeys) <= (Dh <= 64 ? few ? 6 : 8 : few ? 4 : 5);
+}
+
+int launch_codes_and_own(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const void* k_own, const void* v_own, const int32_t* own_len,
+                         const psd_attention_t& a, void* out, float* lse, cudaStream_t st) {
+    OwnArgs p = {q, nullptr, nullptr, k_own, v_own, prefix_len, own_len, out, lse, a, 0, 1, nullptr, nullptr, 0, 0, c, (a.P + c.block - 1) / c.block,
+                 c.block == 16 ? 4 : c.block == 32 ? 5 : c.block == 64 ? 6 : 7, kF16Codes, kBf16Codes};
+    if (a.dtype == PSD_BF16) return a.Dh <= 64 ? launch_dh<__nv_bfloat16, 64, true>(p, st) : launch_dh<__nv_bfloat16, 128, true>(p, st);
+    return a.Dh <= 64 ? launch_dh<__half, 64, true>(p, st) : launch_dh<__half, 128, true>(p, st);
+}
+
 int launch_own_and_join(const void* q, const void* k_own, const void* v_own, const int32_t* own_len, const psd_attention_t& a,
                         const float* po, const float* pl, int splits, void* out, float* lse, cudaStream_t st) {
-    OwnArgs p = {q, nullptr, nullptr, k_own, v_own, nullptr, own_len, out, lse, a, 0, 1, po, pl, splits, (int64_t)a.B * a.D * a.M * a.Hq};
+    OwnArgs p = {q, nullptr, nullptr, k_own, v_own, nullptr, own_len, out, lse, a, 0, 1, po, pl, splits, (int64_t)a.B * a.D * a.M * a.Hq, {}, 0, 0, 0, 0};
     if (a.dtype == PSD_BF16) return a.Dh <= 64 ? launch_dh<__nv_bfloat16, 64>(p, st) : launch_dh<__nv_bfloat16, 128>(p, st);
     return a.Dh <= 64 ? launch_dh<__half, 64>(p, st) : launch_dh<__half, 128>(p, st);
 }
@@ -463,7 +577,7 @@ int launch_own_and_join(const void* q, const void* k_own, const void* v_own, con
 int launch_draft_attention(const void* q, const void* k_prefix, const void* v_prefix, const int32_t* prefix_len,
                            const void* k_own, const void* v_own, const int32_t* own_len, const psd_attention_t& a,
                            void* out, float* lse, void* workspace, int32_t* status_dev, cudaStream_t st) {
-    OwnArgs p = {q, k_prefix, v_prefix, k_own, v_own, prefix_len, own_len, out, lse, a, 0, 1, nullptr, nullptr, 0, 0};
+    OwnArgs p = {q, k_prefix, v_prefix, k_own, v_own, prefix_len, own_len, out, lse, a, 0, 1, nullptr, nullptr, 0, 0, {}, 0, 0, 0, 0};
     if (!one_launch(a.B, a.D, a.M, a.Hq, a.Hkv, a.Dh, a.P, a.S)) {
         const PrefixPlan plan = plan_prefix(a.B, a.D, a.M, a.Hq, a.Hkv, a.Dh, a.P, a.S);
         p.rows = (int64_t)a.B * a.D * a.M * a.Hq;

@@ -120,7 +120,8 @@ const char* psd_attention_q8_kernel_names(int32_t B, int32_t D, int32_t M, int32
     if (!attention_sizes_ok(B, D, M, Hq, Hkv, Dh, P, S) || Dh % 16) return nullptr;
     if (P == 0) return draft_attention_kernels(B, D, M, Hq, Hkv, Dh, P, S, splits);
     const PrefixQ8Plan p = plan_prefix_q8(B, D, M, Hq, Hkv, Dh, P, S);
-    if (splits) *splits = p.splits;
+    if (splits) *splits = p.one ? 0 : p.splits;
+    if (p.one) return "draft_attention_kernel";
     return !p.tiles ? "prefix_rows_q8_kernel+draft_attention_kernel"
                     : p.final ? "prefix_tiles_q8_kernel" : "prefix_tiles_q8_kernel+draft_attention_kernel";
 }

@@ -392,6 +392,11 @@ PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P,
     const int64_t rows = (int64_t)D * M * (Hq / Hkv);
     PrefixQ8Plan p = {};
     p.dhp = Dh <= 64 ? 64 : 128;
+    if (one_launch_codes(B, D, M, Hq, Hkv, Dh, P, S)) {
+        p.one = p.final = true;
+        p.splits = 1;
+        return p;
+    }
     p.tiles = rows > 32;
     if (p.tiles) {
         p.tile = plan_prefix(B, D, M, Hq, Hkv, Dh, P, S);
@@ -450,6 +455,7 @@ size_t prefix_q8_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P) 
 int launch_prefix_attention_q8(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const void* k_own, const void* v_own,
                                const int32_t* own_len, const psd_attention_t& a, const PrefixQ8Plan& p, float* po, float* pl, void* out,
                                float* lse, int32_t* status_dev, cudaStream_t st) {
+    if (p.one) return launch_codes_and_own(q, c, prefix_len, k_own, v_own, own_len, a, out, lse, st);
     if (p.tiles) return launch_prefix_tiles_q8(q, c, prefix_len, k_own, v_own, own_len, a, p.tile, p.joined, po, pl, out, lse, status_dev, st);
     CUtensorMap mk, mv;
     if (!make_codes_map(&mk, c.k, a.kp, a.B, a.P, a.Hkv, a.Dh, p.dhp, kSlice) || !make_codes_map(&mv, c.v, a.vp, a.B, a.P, a.Hkv, a.Dh, p.dhp, kSlice))

@@ -30,8 +30,14 @@ struct PrefixQ8 {
     int block;                       // tokens per scale: 16, 32, 64 or 128
 };
 
+// draft_attention.cu: the prefix in codes and the own keys in one launch, and whether that is the form of these sizes
+int launch_codes_and_own(const void* q, const PrefixQ8& c, const int32_t* prefix_len, const void* k_own, const void* v_own, const int32_t* own_len,
+                         const psd_attention_t& a, void* out, float* lse, cudaStream_t st);
+bool one_launch_codes(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S);
+
 // Which kernel takes the prefix, and how its work is cut.
 struct PrefixQ8Plan {
+    bool one;           // draft_attention_kernel walks it (final outputs); else:
     bool tiles;         // prefix_tiles_q8_kernel (tcgen05), cut as `tile` says; else prefix_rows_q8_kernel: row_blocks, units
     bool joined;        // ..with splits that a cluster joins
     bool final;         // the kernel takes the own keys too and writes final outputs; else partial results

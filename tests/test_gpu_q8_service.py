@@ -18,8 +18,11 @@ JOINED = (1, 4, 32, 8, 2, 128, 700, 32)       # query tiles, keys split over a c
 JOINED_ONE = (1, 1, 32, 8, 2, 64, 900, 32)    # the same with one query tile
 FUSED = (16, 4, 64, 32, 8, 128, 300, 64)      # query tiles, own keys in the same kernel
 SMALL = (40, 4, 33, 16, 4, 64, 200, 33)       # the same with heads of 64, two drafts to a tile
+SHORT = (2, 2, 21, 8, 2, 96, 150, 40)         # a short prefix and the own keys, no query tiles
+SHORT_ONE = (3, 1, 1, 4, 4, 64, 300, 6)       # the same of single tokens
 FORMS = {ROWS: "prefix_rows_q8_kernel+draft_attention_kernel", PARTIAL: "prefix_tiles_q8_kernel+draft_attention_kernel",
-         JOINED: "prefix_tiles_q8_kernel", JOINED_ONE: "prefix_tiles_q8_kernel", FUSED: "prefix_tiles_q8_kernel", SMALL: "prefix_tiles_q8_kernel"}
+         JOINED: "prefix_tiles_q8_kernel", JOINED_ONE: "prefix_tiles_q8_kernel", FUSED: "prefix_tiles_q8_kernel", SMALL: "prefix_tiles_q8_kernel",
+         SHORT: "draft_attention_kernel", SHORT_ONE: "draft_attention_kernel"}
 
 
 def _space(n):
@@ -152,7 +155,7 @@ def test_scales(shape):
     assert bool((l - math.log(P)).abs().max() <= 1e-5)
 
 
-@pytest.mark.parametrize("shape", [PARTIAL, JOINED, FUSED, SMALL])
+@pytest.mark.parametrize("shape", [PARTIAL, JOINED, FUSED, SMALL, SHORT])
 def test_a_draft_does_not_reach_another(shape):
     """NaN and infinities in one draft's own keys and values leave all other drafts' bits as they were."""
     B, D, M, Hq, Hkv, Dh, P, S = shape
@@ -184,9 +187,9 @@ def test_strides_past_32_bits():
     """Caches, rows and tokens more than 2^32 bytes apart."""
     far = (1 << 32) + 64
     mem = torch.empty(far + (1 << 20), dtype=torch.int8, device="cuda")
-    B, P, Hkv, Dh = 2, 100, 2, 64
-    spread = mem.as_strided((B, P, Hkv, Dh), (far, Hkv * Dh, Dh, 1))
-    for shape in ((B, 1, 1, 4, Hkv, Dh, P, 3), (B, 4, 32, 4, Hkv, Dh, P, 3)):
+    for P, M, D in ((1000, 1, 1), (1000, 32, 4), (100, 1, 1), (100, 32, 4)):
+        B, Hkv, Dh = 2, 2, 64
+        shape, spread = (B, D, M, 4, Hkv, Dh, P, 3), mem.as_strided((B, P, Hkv, Dh), (far, Hkv * Dh, Dh, 1))
         t, _, _ = _inputs(shape, 9)
         out, lse = _attend(t)
         spread.copy_(t["k_codes"])

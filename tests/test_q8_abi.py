@@ -193,6 +193,7 @@ def test_attention_kernel_names():
     assert which == "prefix_tiles_q8_kernel" and 2 <= splits <= 8                        # joined by a cluster
     assert names(16, 8, 64, 32, 8, 128, 8192, 64) == ("prefix_tiles_q8_kernel", 1)
     assert names(16, 8, 64, 32, 8, 128, 0, 64)[0] == "draft_attention_kernel"
+    assert names(1, 1, 1, 32, 8, 128, 100, 8) == ("draft_attention_kernel", 0) and names(1, 4, 32, 4, 4, 64, 500, 32) == ("draft_attention_kernel", 0)
     assert names(1, 1, 1, 3, 2, 128, 100, 1) is None and names(1, 1, 1, 2, 2, 72, 100, 1) is None
 
 
