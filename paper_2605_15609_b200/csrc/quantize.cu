@@ -8,7 +8,7 @@
 // NaN or an infinity gets the scale NaN and codes 0: all of it stands for NaN.
 //
 // Bound: memory, 2 bytes read and 1 written per element.  A UNIT (one row, or the tokens of a block of one head) is read once
-// into registers by 1, 2 or 4 warps, 8 pieces of 8 numbers per lane at most (all loads in flight together: 4 KB a warp; with 16
+// into registers by 1, 2, 4 or 8 warps, 8 pieces of 8 numbers per lane at most (all loads in flight together: 4 KB a warp; with 16
 // pieces fewer warps fit: 16 tokens a block 169 against 110 us, 64 a block 109 against 104, with 4 129 us),
 // reduced, and written from the registers; longer rows are read twice.  Absolute values are compared as 16-bit integers, two
 // at a time, which also finds NaN and infinity (the largest patterns).
@@ -18,8 +18,8 @@
 namespace psd {
 namespace {
 
-constexpr int kThreads = 128;
 constexpr int kPieces = 8;           // pieces of 8 numbers that a lane holds
+template <int WPU> constexpr int kWarps = WPU < 4 ? 4 : WPU;         // of a CTA
 
 struct QuantArgs {
     const void* x[2];                // rows: x[0]; caches: keys, values
@@ -49,10 +49,10 @@ __device__ __forceinline__ void widen(uint32_t w, float& lo, float& hi) {
 
 // CACHE: units are (sequence, block, head, keys or values); else rows.  WPU warps share a unit.
 template <bool CACHE, bool BF16, int WPU>
-__global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantArgs a) {
-    __shared__ uint32_t top[kThreads / 32];
+__global__ void __launch_bounds__(kWarps<WPU> * 32) quantize_kernel(const QuantArgs a) {
+    __shared__ uint32_t top[kWarps<WPU>];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t unit = (int64_t)blockIdx.x * (4 / WPU) + warp / WPU;
+    const int64_t unit = (int64_t)blockIdx.x * (kWarps<WPU> / WPU) + warp / WPU;
     const int lane_u = (warp % WPU) * 32 + lane;                  // lane among the unit's
     constexpr int LANES = WPU * 32;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -158,12 +158,12 @@ __global__ void __launch_bounds__(kThreads) quantize_kernel(const QuantArgs a) {
 
 template <bool CACHE, bool BF16, int WPU>
 int launch_w(const QuantArgs& a, cudaStream_t st) {
-    constexpr int per_cta = 4 / WPU;
+    constexpr int per_cta = kWarps<WPU> / WPU;
     const int64_t grid = (a.n_units + per_cta - 1) / per_cta;
     if (grid > INT32_MAX) return PSD_ERR_SHAPE;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(kWarps<WPU> * 32);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -177,12 +177,14 @@ int launch_w(const QuantArgs& a, cudaStream_t st) {
 
 template <bool CACHE>
 int launch_q(const QuantArgs& a, bool bf16, cudaStream_t st) {
-    // Warps per unit: what holds it in registers; four where the units alone leave most warps of the SMs without work.
-    int w = a.pieces <= kPieces * 32 ? 1 : a.pieces <= kPieces * 64 ? 2 : 4;
-    if (a.n_units * w < 16 * (int64_t)sm_count() && a.pieces > 64) w = 4;
+    // Warps per unit: what holds it in registers; four where the units alone leave most warps of the SMs without work.  Eight against four that
+    // read twice: 128 tokens a block of 128, 140 against 201 us for 8 x 16384 tokens; 4096 rows of 16384, 37 against 54, of 20000 (read twice either way) 62 against 69.
+    int w = a.pieces <= kPieces * 32 ? 1 : a.pieces <= kPieces * 64 ? 2 : a.pieces <= kPieces * 128 ? 4 : 8;
+    if (w < 4 && a.n_units * w < 16 * (int64_t)sm_count() && a.pieces > 64) w = 4;
     if (w == 1) return bf16 ? launch_w<CACHE, true, 1>(a, st) : launch_w<CACHE, false, 1>(a, st);
     if (w == 2) return bf16 ? launch_w<CACHE, true, 2>(a, st) : launch_w<CACHE, false, 2>(a, st);
-    return bf16 ? launch_w<CACHE, true, 4>(a, st) : launch_w<CACHE, false, 4>(a, st);
+    if (w == 4) return bf16 ? launch_w<CACHE, true, 4>(a, st) : launch_w<CACHE, false, 4>(a, st);
+    return bf16 ? launch_w<CACHE, true, 8>(a, st) : launch_w<CACHE, false, 8>(a, st);
 }
 
 }  // namespace
