@@ -8,8 +8,10 @@
 // The kernel is built as the 16-bit one is (one CTA per SM over a list of tiles of 128 rows x up to 256 vocabulary rows, TMA
 // ring, one issuing thread, epilogue out of tensor memory, carried triples); a K-slice is again one 128-byte swizzle row, which
 // here is 128 codes, and the product is kind::i8 (M 128, N the tile's width, K 32, 32-bit integer accumulators).  The epilogue
-// converts a sum, multiplies it by the column's and the row's scale and folds it as there; each epilogue warp keeps the
-// columns' scales of its tile in shared memory.
+// converts a sum, multiplies it by the column's and the row's scale and folds it; each epilogue warp keeps the columns' scales of its
+// tile in shared memory, loaded a tile ahead.  A tile's columns are shared by two groups of four warps: the products of a tile of 128 x 256 take 0.25 us
+// for every 128 of H, and the epilogue, a chain of latencies, 7 us with four warps, 2.9 with eight and 2.8 with sixteen, which slow the
+// products down (8192 rows, H = 1024: 1.47 ms, 0.79, 0.85; 3537 rows, H = 256: 652 us, 283, 269; 512 rows, H = 4096: 200, 196, 200).
 //
 // Bound: one pass over W for few rows (half the bytes of a 16-bit head), the tensor cores (twice the 16-bit rate) for many; as
 // there, 94 bytes per clock and SM from L2 are what the products need.  Measured (V = 126464, H = 4096): 128 rows 85.8 us, 6.1 TB/s
@@ -24,8 +26,12 @@ namespace {
 constexpr int kSlice = 128;                                    // codes per K-slice
 constexpr int kBarriers = 256;
 constexpr int kCarry = kCarryEntries * BLOCK_M * 12;
-constexpr int kScales = 4 * BLOCK_N * 4;                       // the columns' scales, a copy per epilogue warp
-constexpr int kSmem = STAGES * STAGE_BYTES + 1024 + kBarriers + kCarry + kScales;
+constexpr int kGroups = 2;                                     // of four epilogue warps, each with a share of a tile's columns
+constexpr int kThreads = 64 + kGroups * 128;                   // warp 0: TMA, warp 1: MMA and tensor memory
+constexpr int kShare = BLOCK_N / kGroups;
+constexpr int kScales = 4 * BLOCK_N * 4;                       // the columns' scales, each epilogue warp's
+constexpr int kHanded = (kGroups - 1) * BLOCK_M * 12;          // triples of the other groups' shares
+constexpr int kSmem = STAGES * STAGE_BYTES + 1024 + kBarriers + kCarry + kScales + kHanded;
 static_assert(kSmem <= 227 * 1024, "shared memory of the 8-bit kernel");
 
 // kind::i8: signed 8-bit A and B, 32-bit integer accumulator, both K-major, M = 128, N = n
@@ -38,7 +44,88 @@ __device__ __forceinline__ void umma_i8(uint32_t tmem_d, uint64_t desc_a, uint64
                  ::"r"(tmem_d), "l"(desc_a), "l"(desc_b), "r"(idesc), "r"(accumulate) : "memory");
 }
 
-__global__ void __launch_bounds__(NUM_THREADS, 1)
+// A CTA's tiles in the order of TileCursor.  Within a band the next one is found without a division, which each of the epilogue's warps would else wait for
+// between tiles (`entry`: which of the band's row tiles that the CTA meets).
+struct TileWalk : TileCursor {
+    int entry, v, m, e, step_v, step_m, step_e, entries;
+    __device__ __forceinline__ void band_begins() {
+        if (h <= 0) return;
+        v = c / h; m = c - v * h; e = m / gcd;
+        step_v = G / h; step_m = G - step_v * h; step_e = step_m / gcd;
+        entries = h / gcd;
+    }
+    __device__ __forceinline__ void begin(const TileGeometry& g, int c_, int G_, int n_mt_) {
+        TileCursor::begin(g, c_, G_, n_mt_);
+        entry = 0;
+        if (g.carry) band_begins();
+    }
+    __device__ __forceinline__ int next(const TileGeometry& g) {
+        if (!g.carry || m0 >= n_mt) return TileCursor::next(g);
+        if (v < g.n_vt) {
+            v_tile = v; m_tile = m0 + m; entry = e;
+            tile_columns(g, v_tile, v0, ncols);
+            v += step_v; m += step_m; e += step_e;
+            if (m >= h) { m -= h; e -= entries; ++v; }
+            return TILE;
+        }
+        r = h * g.n_vt;
+        const int ev = TileCursor::next(g);
+        band_begins();
+        return ev;
+    }
+};
+
+// 32 sums of a row, columns col0 .. col0 + n - 1 of them, to logits and into the running triple.  The column of a maximum is not looked for if it is
+// no larger than `known`.
+__device__ __forceinline__ void fold_sums(const uint32_t (&r)[32], const float* ws, float xs, int col0, int n, float known, float& run_m, float& run_s,
+                                          int& run_a) {
+    constexpr float LOG2E = 1.4426950408889634f;
+    float x[32];
+    const f32x2 xs2 = pack2(xs, xs);
+#pragma unroll
+    for (int j = 0; j < 32; j += 4) {
+        const float4 w = *reinterpret_cast<const float4*>(ws + j);
+        unpack2(mul2(mul2(pack2(__int2float_rn((int)r[j]), __int2float_rn((int)r[j + 1])), pack2(w.x, w.y)), xs2), x[j], x[j + 1]);
+        unpack2(mul2(mul2(pack2(__int2float_rn((int)r[j + 2]), __int2float_rn((int)r[j + 3])), pack2(w.z, w.w)), xs2), x[j + 2], x[j + 3]);
+    }
+    if (n < 32) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (j >= n) x[j] = -INFINITY;                          // no logits
+    }
+    float top[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        top[u] = max3(x[8 * u], x[8 * u + 1], x[8 * u + 2]);
+        top[u] = max3(top[u], x[8 * u + 3], x[8 * u + 4]);
+        top[u] = max3(top[u], x[8 * u + 5], x[8 * u + 6]);
+        top[u] = fmaxf(top[u], x[8 * u + 7]);
+    }
+    const float cm = fmaxf(max3(top[0], top[1], top[2]), top[3]);
+    if (cm > run_m) {
+        if (cm > known) {
+            int at[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                at[u] = 32;
+#pragma unroll
+                for (int j = 7; j >= 0; --j) at[u] = x[8 * u + j] == cm ? 8 * u + j : at[u];
+            }
+            run_a = col0 + min(min(at[0], at[1]), min(at[2], at[3]));
+        }
+        run_s *= ex2((run_m - cm) * LOG2E);
+        run_m = cm;
+    }
+    const f32x2 neg = pack2(-run_m * LOG2E, -run_m * LOG2E), log2e = pack2(LOG2E, LOG2E);
+    f32x2 acc[2] = {0ull, 0ull};
+#pragma unroll
+    for (int j = 0; j < 32; j += 2) acc[j / 2 & 1] = add2(acc[j / 2 & 1], ex2_pair(fma2(pack2(x[j], x[j + 1]), log2e, neg)));
+    float a, b;
+    unpack2(add2(acc[0], acc[1]), a, b);
+    run_s += a + b;
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
 confidence_q8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b_wide,
                      const __grid_constant__ CUtensorMap map_b_narrow, const TileGeometry geo, int n_rows, int H, int V,
                      const float* __restrict__ x_scale, const float* __restrict__ w_scale, float* __restrict__ pm,
@@ -47,19 +134,23 @@ confidence_q8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * STAGE_BYTES);
     uint64_t *full_bar = bars, *empty_bar = bars + STAGES, *acc_full_bar = bars + 2 * STAGES, *acc_empty_bar = acc_full_bar + 2,
-             *drain_bar = acc_empty_bar + 2, *never_bar = drain_bar + 1;
-    uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(never_bar + 1);
+             *drain_bar = acc_empty_bar + 2, *never_bar = drain_bar + 1, *handed_bar = never_bar + 1, *taken_bar = handed_bar + 4;      // [4]: a quarter of the rows each
+    uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(taken_bar + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
     float* carry_m = reinterpret_cast<float*>(smem + STAGES * STAGE_BYTES + kBarriers);
     float* carry_s = carry_m + kCarryEntries * BLOCK_M;
     int32_t* carry_a = reinterpret_cast<int32_t*>(carry_s + kCarryEntries * BLOCK_M);
-    float* scales = reinterpret_cast<float*>(carry_a + kCarryEntries * BLOCK_M);     // [4][BLOCK_N]
+    float* scales = reinterpret_cast<float*>(carry_a + kCarryEntries * BLOCK_M);     // [kGroups][4][kShare]
+    float* handed_m = scales + 4 * BLOCK_N;                                          // [kGroups - 1][BLOCK_M]
+    float* handed_s = handed_m + (kGroups - 1) * BLOCK_M;
+    int32_t* handed_a = reinterpret_cast<int32_t*>(handed_s + (kGroups - 1) * BLOCK_M);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int k_blocks = (H + kSlice - 1) / kSlice;          // (the last slice may be half: TMA fills zeros)
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(&acc_full_bar[a], 1); mbar_init(&acc_empty_bar[a], 4); }
+        for (int a = 0; a < 2; ++a) { mbar_init(&acc_full_bar[a], 1); mbar_init(&acc_empty_bar[a], 4 * kGroups); }
+        for (int a = 0; a < 4; ++a) { mbar_init(&handed_bar[a], kGroups - 1); mbar_init(&taken_bar[a], 1); }
         mbar_init(drain_bar, 1);
         mbar_init(never_bar, 1);
         *abort_flag = 0;
@@ -78,7 +169,7 @@ confidence_q8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
 
     const int n_mt = geo.n_mt;
     const WaitCtx wc = {abort_flag, status_dev, geo.wait_limit, 0u};
-    TileCursor cur;
+    TileWalk cur;
     cur.begin(geo, blockIdx.x, gridDim.x, n_mt);
 
     if (warp == 0) {
@@ -143,8 +234,10 @@ confidence_q8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
             }
         }
     } else {
-        const int quarter = warp & 3, row_in_tile = quarter * 32 + lane;
-        float* ws = scales + quarter * BLOCK_N;
+        // Group g takes the columns from g * share(ncols) on.  Group 0 carries what was before; the others start anew with every tile and hand
+        // their triples to group 0.
+        const int quarter = warp & 3, row_in_tile = quarter * 32 + lane, group = (warp - 2) >> 2;
+        float* ws = scales + (warp - 2) * kShare;
         int it = 0;
         bool ok = true;
         auto reset_carry = [&]() {
@@ -155,69 +248,108 @@ confidence_q8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
                 carry_a[e * BLOCK_M + row_in_tile] = 0;
             }
         };
-        if (geo.carry) reset_carry();
-        for (int ev; ok && (ev = cur.next(geo)) != TileCursor::DONE;) {
+        if (geo.carry && group == 0) reset_carry();
+        // the next tile's scales come while this one is folded
+        auto share = [](int ncols) { return (ncols / kGroups + 31) / 32 * 32; };
+        float next_w[kShare / 32], next_x = 0.f;
+        auto load_scales = [&]() {
+            const int v = cur.v0 + group * share(cur.ncols) + lane, row = cur.m_tile * BLOCK_M + row_in_tile;
+#pragma unroll
+            for (int u = 0; u < kShare / 32; ++u) next_w[u] = v + u * 32 < V ? w_scale[v + u * 32] : 0.f;
+            next_x = row < n_rows ? x_scale[row] : 0.f;
+        };
+        int in_band = 0;                                  // tiles of this band so far
+        int ev = cur.next(geo);
+        bool loaded = false;
+        while (ev != TileCursor::DONE) {
             if (ev == TileCursor::BAND_END) {
-                const int entries = cur.end_h / cur.end_gcd;
-                const int slot = (int)blockIdx.x / cur.end_gcd, base = (int)blockIdx.x % cur.end_gcd;
-                for (int e = 0; e < entries; ++e) {
-                    const int row = (cur.end_m0 + base + e * cur.end_gcd) * BLOCK_M + row_in_tile;
-                    if (row < n_rows && PSD_DEBUG_OK((size_t)slot * n_rows + row < part_cap && e < kCarryEntries, status_dev)) {
-                        const size_t o = (size_t)slot * n_rows + row;
-                        pm[o] = carry_m[e * BLOCK_M + row_in_tile];
-                        ps[o] = carry_s[e * BLOCK_M + row_in_tile];
-                        pa[o] = carry_a[e * BLOCK_M + row_in_tile];
+                if (group == 0) {
+                    const int entries = cur.end_h / cur.end_gcd;
+                    const int slot = (int)blockIdx.x / cur.end_gcd, base = (int)blockIdx.x % cur.end_gcd;
+                    for (int e = 0; e < entries; ++e) {
+                        const int row = (cur.end_m0 + base + e * cur.end_gcd) * BLOCK_M + row_in_tile;
+                        if (row < n_rows && PSD_DEBUG_OK((size_t)slot * n_rows + row < part_cap && e < kCarryEntries, status_dev)) {
+                            const size_t o = (size_t)slot * n_rows + row;
+                            pm[o] = carry_m[e * BLOCK_M + row_in_tile];
+                            ps[o] = carry_s[e * BLOCK_M + row_in_tile];
+                            pa[o] = carry_a[e * BLOCK_M + row_in_tile];
+                        }
                     }
+                    reset_carry();
                 }
-                reset_carry();
+                in_band = 0;
+                ev = cur.next(geo);
                 continue;
             }
-            const int v0 = cur.v0, ncols = cur.ncols, acc = it & 1, row = cur.m_tile * BLOCK_M + row_in_tile;
+            if (!loaded) load_scales();
+            const int v0 = cur.v0, ncols = cur.ncols, acc = it & 1, v_tile = cur.v_tile, row = cur.m_tile * BLOCK_M + row_in_tile;
+            const int limit = min(ncols, V - v0), c0 = group * share(ncols), c1 = min(c0 + share(ncols), limit);
+            const int entry = cur.entry * BLOCK_M + row_in_tile;
+            if (!PSD_DEBUG_OK(cur.m_tile >= 0 && cur.m_tile < n_mt && v0 >= 0 && v0 < V && ncols > 0 && ncols <= BLOCK_N && c1 - c0 <= kShare &&
+                                  entry >= 0 && entry < kCarryEntries * BLOCK_M, status_dev)) { ok = false; break; }
             __syncwarp();                                 // the warp is done with the last tile's scales
-            for (int c = lane; c < ncols; c += 32) ws[c] = v0 + c < V ? w_scale[v0 + c] : 0.f;
-            const float xs = row < n_rows ? x_scale[row] : 0.f;
+#pragma unroll
+            for (int u = 0; u < kShare / 32; ++u) ws[u * 32 + lane] = next_w[u];
+            const float xs = next_x;
             __syncwarp();
+            ev = cur.next(geo);
+            if ((loaded = ev == TileCursor::TILE)) load_scales();
             if (!mbar_wait(&acc_full_bar[acc], (it >> 1) & 1, wc)) ok = false;
             if (!(ok = __all_sync(0xffffffffu, ok))) break;
             tc_fence_after();
             const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BLOCK_N);
-            const int entry = geo.carry ? ((cur.m_tile - cur.m0) / cur.gcd) * BLOCK_M + row_in_tile : 0;
-            if (!PSD_DEBUG_OK(cur.m_tile >= 0 && cur.m_tile < n_mt && v0 >= 0 && v0 < V && ncols > 0 && ncols <= BLOCK_N &&
-                                  entry >= 0 && entry < kCarryEntries * BLOCK_M, status_dev)) { ok = false; break; }
             float run_m = -INFINITY, run_s = 0.f;
             int run_a = 0;
-            if (geo.carry) { run_m = carry_m[entry]; run_s = carry_s[entry]; run_a = carry_a[entry]; }
-            const bool ragged = v0 + ncols > V;
-            for (int c = 0; c < ncols; c += 32) {
+            if (geo.carry && group == 0) { run_m = carry_m[entry]; run_s = carry_s[entry]; run_a = carry_a[entry]; }
+            // What group 0 has carried by now only spares the search for the column of a maximum that will not be one.  It may be as it was two tiles ago, which
+            // this accumulator's round trip bears out, and must be of this band.
+            const float known = geo.carry && group && in_band >= 2 ? reinterpret_cast<volatile float*>(carry_m)[entry] : -INFINITY;
+            ++in_band;
+            // (a chunk of 32 columns stays inside the accumulator; what lies behind the tile's columns is masked)
+            for (int c = c0; c < c1; c += 32) {
                 uint32_t r[32];
-                float x[32];
-                const bool whole = ncols - c >= 32;
-                if (whole) {
-                    tmem_ld32(taddr + c, r);
-                    tmem_wait_ld(r);
-                } else {
-                    uint32_t h[16];
-                    tmem_ld16(taddr + c, h);
-                    tmem_wait_ld16(h);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) { r[j] = h[j]; r[16 + j] = 0; }
-                }
-#pragma unroll
-                for (int j = 0; j < 32; ++j) x[j] = __fmul_rn(__fmul_rn(__int2float_rn((int)r[j]), ws[(c + j) & (BLOCK_N - 1)]), xs);
-                if (ragged || !whole) {
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (v0 + c + j >= V || c + j >= ncols) x[j] = -INFINITY;     // no logits
-                }
-                fold_chunk(x, v0 + c, run_m, run_s, run_a);
+                tmem_ld32(taddr + c, r);
+                tmem_wait_ld(r);
+                fold_sums(r, ws + c - c0, xs, v0 + c, limit - c, known, run_m, run_s, run_a);
             }
             tc_fence_before();
+            if (group) {
+                const int hand = (group - 1) * BLOCK_M + row_in_tile;
+                if (!mbar_wait(&taken_bar[quarter], (it & 1) ^ 1, wc)) ok = false;
+                if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                handed_m[hand] = run_m; handed_s[hand] = run_s; handed_a[hand] = run_a;
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(&handed_bar[quarter]);
+                    mbar_arrive(&acc_empty_bar[acc]);
+                }
+                ++it;
+                continue;
+            }
+            if (!mbar_wait(&handed_bar[quarter], it & 1, wc)) ok = false;
+            if (!(ok = __all_sync(0xffffffffu, ok))) break;
+            float other[kGroups - 1], top = run_m;
+#pragma unroll
+            for (int u = 0; u < kGroups - 1; ++u) {
+                other[u] = handed_m[u * BLOCK_M + row_in_tile];
+                if (other[u] > top) {                     // (equal maxima: the lower column)
+                    top = other[u];
+                    run_a = handed_a[u * BLOCK_M + row_in_tile];
+                }
+            }
+            if (run_m != top) run_s *= ex2((run_m - top) * kLog2e);
+#pragma unroll
+            for (int u = 0; u < kGroups - 1; ++u)
+                run_s = fmaf(handed_s[u * BLOCK_M + row_in_tile], other[u] == top ? 1.f : ex2((other[u] - top) * kLog2e), run_s);
+            run_m = top;
+            if (geo.carry) { carry_m[entry] = run_m; carry_s[entry] = run_s; carry_a[entry] = run_a; }
             __syncwarp();
-            if (lane == 0) mbar_arrive(&acc_empty_bar[acc]);
-            if (geo.carry) {
-                carry_m[entry] = run_m; carry_s[entry] = run_s; carry_a[entry] = run_a;
-            } else if (row < n_rows && PSD_DEBUG_OK((size_t)cur.v_tile * n_rows + row < part_cap, status_dev)) {
-                const size_t o = (size_t)cur.v_tile * n_rows + row;
+            if (lane == 0) {
+                mbar_arrive(&taken_bar[quarter]);
+                mbar_arrive(&acc_empty_bar[acc]);
+            }
+            if (!geo.carry && row < n_rows && PSD_DEBUG_OK((size_t)v_tile * n_rows + row < part_cap, status_dev)) {
+                const size_t o = (size_t)v_tile * n_rows + row;
                 pm[o] = run_m;
                 ps[o] = run_s;
                 pa[o] = run_a;
@@ -311,7 +443,8 @@ int launch_confidence_q8(const int8_t* x, const float* x_scale, const int8_t* w,
     const int sms = sm_count();
     TileGeometry g = choose_geometry(n_rows, V, sms, max_splits(V), BLOCK_M, 16);
     choose_order(g, n_rows, (H + 1) / 2, V, BLOCK_M, band_bytes(), tile_order());     // (rows of H bytes)
-    if (g.n_mt == 1) { g.row_bands = 1; g.band = 1; }
+    // Rows that fit a band are read once in either order; in this one they are carried over the vocabulary.
+    if (g.n_mt == 1 || (tile_order() == 0 && (long long)g.n_mt * BLOCK_M * H <= band_bytes())) { g.row_bands = 1; g.band = g.n_mt; }
     const int wide_rows = (g.rem ? g.base_units + 1 : g.base_units) * 16;
     const int narrow_rows = g.base_units > 0 ? g.base_units * 16 : wide_rows;
     CUtensorMap map_a, map_bw, map_bn;
@@ -333,7 +466,7 @@ int launch_confidence_q8(const int8_t* x, const float* x_scale, const int8_t* w,
     else *plan = uniform_splits(g.n_vt);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(grid);
-    cfg.blockDim = dim3(NUM_THREADS);
+    cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kSmem;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
