@@ -297,7 +297,8 @@ def test_attention_past_the_short_prefixes(shape, dtype):
 @pytest.mark.parametrize("block", [16, 32, 64, 128])
 @pytest.mark.parametrize("layout", ["dense", "heads_first", "padded"])
 @pytest.mark.parametrize("shape", [(3, 1, 1, 8, 2, 128, 500, 3), (2, 4, 32, 8, 2, 64, 400, 32), (2, 3, 30, 16, 4, 128, 333, 30), (3, 1, 1, 8, 2, 128, 950, 3),
-                                   (2, 4, 32, 8, 2, 64, 1100, 32), (3, 2, 9, 6, 2, 112, 201, 9), (2, 1, 1, 5, 5, 32, 140, 2)])
+                                   (2, 4, 32, 8, 2, 64, 1100, 32), (3, 2, 9, 6, 2, 112, 201, 9), (2, 1, 1, 5, 5, 32, 140, 2),
+                                   (40, 3, 9, 16, 8, 64, 20, 9), (30, 2, 10, 32, 32, 96, 70, 10)])
 def test_attention_blocks_and_layouts(shape, layout, block):
     _attention(shape, block, "bf16", layout)
     _attention(shape, block, "fp16", layout, causal=True, seed=9)

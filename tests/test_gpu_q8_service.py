@@ -20,9 +20,10 @@ FUSED = (16, 4, 64, 32, 8, 128, 300, 64)      # query tiles, own keys in the sam
 SMALL = (40, 4, 33, 16, 4, 64, 200, 33)       # the same with heads of 64, two drafts to a tile
 SHORT = (2, 2, 21, 8, 2, 96, 150, 40)         # a short prefix and the own keys, no query tiles
 SHORT_ONE = (3, 1, 1, 4, 4, 64, 300, 6)       # the same of single tokens
+SHORT_MANY = (40, 3, 9, 16, 8, 64, 80, 9)     # the same with several waves of CTAs
 FORMS = {ROWS: "prefix_rows_q8_kernel+draft_attention_kernel", PARTIAL: "prefix_tiles_q8_kernel+draft_attention_kernel",
          JOINED: "prefix_tiles_q8_kernel", JOINED_ONE: "prefix_tiles_q8_kernel", FUSED: "prefix_tiles_q8_kernel", SMALL: "prefix_tiles_q8_kernel",
-         SHORT: "draft_attention_kernel", SHORT_ONE: "draft_attention_kernel"}
+         SHORT: "draft_attention_kernel", SHORT_ONE: "draft_attention_kernel", SHORT_MANY: "draft_attention_kernel"}
 
 
 def _space(n):
