@@ -15,7 +15,7 @@
 //
 // Bound: one pass over W for few rows (half the bytes of a 16-bit head), the tensor cores (twice the 16-bit rate) for many; as
 // there, 94 bytes per clock and SM from L2 are what the products need.  Measured (V = 126464, H = 4096): 128 rows 85.8 us, 6.1 TB/s
-// (the whole call 89), 8192 rows 3.07-3.1 ms, 2.77 POP/s at the board's power limit (the 16-bit head: 176 us, 6.2 ms).
+// (the whole call 89), 8192 rows 3.07-3.15 ms, 2.77 POP/s at the board's power limit (the 16-bit head: 176 us, 6.2 ms).
 #include <algorithm>
 #include "attn_tc.cuh"
 #include "combine.cuh"
