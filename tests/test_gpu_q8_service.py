@@ -77,6 +77,27 @@ def test_keys_split_over_a_cluster(shape, causal, dtype):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", [(1, 1, 700, 2, 1, 64, 33, 700), (2, 1, 3, 4, 2, 128, 64, 1500), (1, 2, 70, 4, 4, 32, 129, 90), (45, 3, 9, 16, 8, 64, 5, 9), (3, 1, 1, 128, 1, 112, 1, 1)])
+def test_short_prefixes_in_one_launch(shape, causal, dtype):
+    """Many query rows or own keys beside a few prefix keys, ragged and empty lengths, strided queries, outputs and own keys."""
+    B, D, M, Hq, Hkv, Dh, P, S = shape
+    assert psd.psd_attention_q8_kernel_names(*shape) == ("draft_attention_kernel", 0)
+    plen, olen = [(P * (b % 4) + 2) // 3 for b in range(B)], [[S, 0, S // 2, 1][n % 4] for n in range(B * D)]
+    t, kp, vp = _inputs(shape, 13, {"bf16": torch.bfloat16, "fp16": torch.float16}[dtype], 32, plen, olen)
+    for n in ("q", "k_own", "v_own"):
+        x = t[n]
+        wide = torch.full((x.shape[0], x.shape[1], x.shape[2] + 2, x.shape[3] + 16), math.nan, dtype=x.dtype, device="cuda")
+        wide[:, :, 1:-1, 8:-8] = x
+        t[n] = wide[:, :, 1:-1, 8:-8]
+    past = torch.arange(S, device="cuda")[None] >= t["own_len"][:, None]
+    t["k_own"][past], t["v_own"][past] = math.nan, math.inf
+    out, lse = _attend(t, causal=causal)
+    plen = [min(p, P) for p in plen]
+    _check(out, lse, t["q"], kp, vp, np.nan_to_num(_f64(t["k_own"])), np.nan_to_num(_f64(t["v_own"]), posinf=0), plen, olen, Dh ** -0.5, causal, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("causal", [False, True])
 @pytest.mark.parametrize("shape", [(16, 4, 32, 16, 8, 128, 130, 32), (20, 3, 33, 16, 8, 64, 300, 33), (17, 3, 70, 8, 4, 80, 129, 70), (40, 8, 32, 8, 2, 128, 1, 32),
                                    (19, 4, 40, 16, 8, 128, 257, 40), (12, 6, 32, 28, 4, 128, 200, 32), (10, 2, 150, 8, 4, 96, 200, 170)])
 def test_own_keys_behind_an_unsplit_prefix(shape, causal, dtype):
@@ -235,6 +256,32 @@ def test_head_at_larger_sizes(R, H, V):
     assert status == 0 and torch.equal(tok.long(), first)
     want = torch.exp(m.double() - z)
     assert bool(((conf.double() - want).abs() <= 6e-5 * want).all()) and bool(((lse.double() - z).abs() <= 6e-5 + 2.0 ** -22 * z.abs()).all())
+
+
+@pytest.mark.parametrize("R, H, V", [(128 * 37 + 5, 128, 2500), (128 * 74, 64, 1999), (128 * 111 - 1, 64, 777), (200001, 64, 33), (60000, 64, 300), (20000, 64, 1), (641, 64, 16),
+                                     (2, 64, 100003), (700, 576, 4000), (50000, 768, 1000), (9000, 4608, 1200)])
+def test_head_row_tiles_and_bands(R, H, V):
+    """Counts of row tiles that share different factors with the number of SMs (bands are cut shorter), fewer tiles than SMs, rows larger than a band;
+    equal logits in all parts of a tile and in several tiles: the lowest token."""
+    rnd = _rnd(R + V)
+    hidden, w, ws = rnd(R, H).bfloat16(), (rnd(V, H) * 40).clamp(-127, 127).round().to(torch.int8), (rnd(V).abs() + 0.1) * 2e-2 / H
+    for v in range(V // 3, V, max(1, V // 7)):
+        w[v], ws[v] = w[0], ws[0]
+    hidden[::2] = w[0].to(torch.bfloat16)
+    tok, conf, lse, status = _run_head(hidden, w, ws)
+    c, s = torch.empty(R, H, dtype=torch.int8, device="cuda"), torch.empty(R, device="cuda")
+    psd.psd_quantize_rows(hidden, c, s)
+    assert status == 0
+    for r in range(0, R, 1 << 13):
+        n = c[r:r + (1 << 13)].double() @ w.double().t()                    # exact
+        l = (n.float() * ws) * s[r:r + (1 << 13), None]
+        m = l.amax(1)
+        first = torch.where(l == m[:, None], torch.arange(V, device="cuda"), V).amin(1)
+        z = torch.logsumexp(l.double(), 1)
+        want = torch.exp(m.double() - z)
+        got = slice(r, r + (1 << 13))
+        assert torch.equal(tok[got].long(), first)
+        assert bool(((conf[got].double() - want).abs() <= 6e-5 * want).all()) and bool(((lse[got].double() - z).abs() <= 6e-5 + 2.0 ** -22 * z.abs()).all())
 
 
 def test_head_special_rows():
