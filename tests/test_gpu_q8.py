@@ -143,6 +143,7 @@ ROTATE = [  # T, Hq, Hkv, Dh, rotary, interleaved, norm, values
     (33, 3, 3, 128, 64, True, True, False), (33, 5, 1, 96, 32, False, False, True), (9, 6, 2, 80, 20, False, True, True), (9, 6, 2, 80, 20, True, True, True),
     (4, 2, 2, 72, 72, False, True, True), (4, 2, 2, 72, 10, True, True, False), (2, 3, 1, 24, 2, False, False, True), (6, 4, 4, 128, 0, False, True, True),
     (900, 40, 8, 128, 128, False, True, True), (2500, 32, 8, 64, 32, True, True, True), (1200, 40, 8, 120, 60, False, False, True), (1, 128, 1, 128, 128, True, True, True),
+    (1300, 4, 4, 80, 40, False, True, True), (2000, 3, 1, 64, 64, True, True, True), (1500, 2, 5, 128, 96, False, False, True),
 ]
 
 
