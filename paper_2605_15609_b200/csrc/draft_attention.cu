@@ -547,7 +547,7 @@ const char* draft_attention_kernels(int B, int D, int M, int Hq, int Hkv, int Dh
 // 18.1, 17.2.  8 x 8 drafts of 4 tokens, 16 heads over 2, 64: 9.2, 20.4; 257: 17.0, 24.5; 512: 22.8, 20.2.  16 x 2 drafts of 8 tokens, 28 heads over 4, 64:
 // 16.9, 19.6; 128: 20.9, 17.9.  32 heads of 64 over 8, 16 x one token, 257: 7.9, 9.3; 512: 10.4, 10.0; 64 x one token, 64: 9.8, 9.6; 128: 12.0, 10.5.
 // Beyond four CTAs per SM (drafts in the hundreds over a few keys) the forms' times follow their waves of CTAs, and the lower estimate wins: fitted to
-// 150 drawn shapes of up to 700 keys, 16 to 160 us, which each estimate meets within 15%; by it 23.9 us on average (geometric), always the better form 23.5.
+// 240 drawn shapes of up to 700 keys, 5 to 250 us, which each estimate meets within 15%; by it 25.1 us on average (geometric), always the better form 24.8.
 bool one_launch_codes(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
     const PrefixPlan plan = plan_prefix(B, D, M, Hq, Hkv, Dh, P, S);
     const int rows = M * (Hq / Hkv), sms = sm_count(), steps = (P + kKeys - 1) / kKeys, own = (S + kKeys - 1) / kKeys;
@@ -557,11 +557,14 @@ bool one_launch_codes(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S
     const int64_t ctas = nh * ((rows + r - 1) / r);
     if (ctas > 4 * sms) {
         const double half = Dh <= 64 ? 0.5 : 1, x = half * ctas * blocks / sms, y = half * ctas / sms;      // (blocks of rows, CTAs) per SM
-        const double one = 3.8 + 0.7 * y + x * (0.55 + 0.6 * (steps + own)) + 0.37 * half * (steps + own), joins = 0.8 * x * (1 + own);
-        if (few) return one < 7.9 + 0.62 * half * B * Hkv / sms * steps + joins;
+        const double one = 3.8 + 0.7 * y + x * (0.55 + 0.6 * (steps + own)) + 0.37 * half * (steps + own);
+        if (few) {
+            const double z = (double)B * Hkv / sms;
+            return one < 6.8 + z * (D * rows > 16 ? 1.36 + 2 * half * (1.9 + 0.26 * steps) : half * (1.9 + 0.26 * steps)) + 0.6 * x * (1 + own);
+        }
         const double waves = (double)(((int64_t)B * Hkv * plan.units + sms - 1) / sms), tiles = (P + 127) / 128;
         const int met = plan.tq / M < 1 ? 1 : plan.tq / M < D ? plan.tq / M : D;
-        return one < (plan.fused ? 1.5 + waves * (9 + 2.3 * tiles + 1.6 * met * ((S + 127) / 128)) : 5.1 + waves * (6.5 + 1.55 * tiles) + joins);
+        return one < (plan.fused ? 1.5 + waves * (9 + 2.3 * tiles + 1.6 * met * ((S + 127) / 128)) : 5.1 + waves * (6.5 + 1.55 * tiles) + 0.8 * x * (1 + own));
     }
     if (plan.fused && 3 * (int64_t)B * Hkv * plan.units >= sms && (P > (Dh <= 64 ? 320 : 128) || drafts_per_tile(M, plan.tq) < 4)) return false;
     const int crowd = ctas <= 2 * sms ? 1 : ctas <= 3 * sms ? 2 : 4;
