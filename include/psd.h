@@ -646,7 +646,7 @@ int psd_confidence_logits(const void* logits, int32_t dtype, int64_t row_stride,
  * CODES are int8 numbers from -127 to 127 that stand for code * scale.  One scale serves a row of a matrix, or the
  * tokens of a block of one key head in a cache.  Over a unit x of numbers, in fp32, each operation rounded on its own:
  *   scale = max(max |x| * fp32(1/127), 2^-126),   r = 1 / scale,   code = rint(x * r)      (ties to even).
- * A unit that holds a NaN or an infinity gets the scale NaN and codes 0.  Scales made elsewhere are >= 0 (or NaN).
+ * A unit that holds a NaN or an infinity gets the scale NaN and codes 0.  Scales made elsewhere are finite and >= 0, or NaN.
  */
 
 /* How psd_rope_frequencies scales a context of `original` tokens by `factor`. */
@@ -741,8 +741,11 @@ const char* psd_attention_q8_kernel_names(int32_t B, int32_t D, int32_t M, int32
  * k_scale[b, h, j / block], and so are the values; the drafts' own keys and values are 16-bit as there.
  *   block 16, 32, 64 or 128;  Dh % 16 == 0;  a->kp, a->vp are in bytes, multiples of 16;  codes 16-byte aligned
  *   k_scale, v_scale [B, Hkv, ceil(P / block)] fp32; neither codes nor scales past a length are used.  A scale NaN makes
- *   the outputs that draw on its block NaN.  Scores, statistics and sums are fp32, weights over the prefix are rounded to
- *   fp16 (none is off by more than 2^-30 of the row's largest beside that), the codes enter exactly.
+ *   the outputs that draw on its block NaN.  Scores, statistics and sums are fp32, the codes enter exactly.  Weights over the
+ *   prefix are rounded to fp16 after they are multiplied by their value's scale: none is off by more than 2^-32 of the row's
+ *   largest such product beside that, however far the scales of a sequence and head lie apart (up to 2^110, and for weights
+ *   above 2^-110 of the row's largest; smaller ones may add nothing to out).  Weights over own keys are rounded to the inputs'
+ *   type, as there.
  *   Other arguments as for psd_draft_attention.
  */
 int psd_draft_attention_q8(const void* q, const int8_t* k_codes, const int8_t* v_codes, const float* k_scale,

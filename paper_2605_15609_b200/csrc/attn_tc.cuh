@@ -176,6 +176,16 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
     return d;
 }
 
+__device__ __forceinline__ float lg2(float x) {
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// x * 2^e where 2^e alone may leave fp32's range
+__device__ __forceinline__ float times_ex2(float x, float e) {
+    const float h = ex2(0.5f * e);
+    return x * h * h;
+}
 // (2^x stays with ex2: a polynomial on the fp32 pipes takes 10 cycles of a scheduler per 32 results, ex2 takes 8.)
 __device__ __forceinline__ f32x2 ex2_pair(f32x2 x) {
     float a, b;

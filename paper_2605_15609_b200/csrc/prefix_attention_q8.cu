@@ -3,9 +3,10 @@
 //   s_j = scale * k_scale[block of j] * (q . kc_j),   out = sum_j p_j * v_scale[block of j] * vc_j / sum_j p_j,  p_j = 2^(s_j log2 e - m)
 //
 // Codes are whole numbers up to 127 and so exact in either 16-bit type: they are widened on the way to the tensor instructions, with
-// nothing rounded, the keys' scale multiplies a score and the values' scale a weight.  Weights go to the product in fp16 whatever
-// the queries' type (their rounding is 2^-11 then), 2^7 to 2^15 times as large as relative to the row's maximum, and relative to the
-// largest value scale of the CTA's keys, so that none is off by more than 2^-32 of the largest beside its rounding.
+// nothing rounded, the keys' scale multiplies a score and the values' scale a weight.  Weights times value scale go to the product in fp16 whatever
+// the queries' type (their rounding is 2^-11 then), 2^7 to 2^15 times as large as relative to the row's largest such product, so that none is off by
+// more than 2^-32 of that beside its rounding: a row keeps two references, one of its weights for their sum and one of these products for its outputs.
+// (With one reference and the largest value scale a row lost what it attends to beside a block of larger values that it does not.)
 //
 // A CTA takes 16 or 32 rows (query tokens times the heads of one key head) and a range of keys; its four warps go through slices of 32 keys
 // by themselves, each with a ring of its own that TMA fills, a running maximum and sums, and are joined at the end.  No barrier
@@ -106,8 +107,8 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     if (lane == 0)
         for (int i = 0; i < issued; ++i) load(first + 4 * i, i);
 
-    // scales: lane nt holds what scores of the slice's keys 8 nt .. 8 nt + 7 are multiplied by, lane 4 + nt the same for weights
-    const float* scales = (lane & 4 ? a.v_scale : a.k_scale) + ((int64_t)b * a.Hkv + h) * a.nb;
+    // scales: lane i holds what scores of the slice's keys 16 i .. 16 i + 15 are multiplied by, lane 2 + i the same for weights, lane 4 + i its logarithm
+    const float* scales = (lane & 6 ? a.v_scale : a.k_scale) + ((int64_t)b * a.Hkv + h) * a.nb;
     float vref = 1.17549435e-38f;                       // one for the CTA: its warps are joined
     if (s1 > s0) {
         const float* vs = a.v_scale + ((int64_t)b * a.Hkv + h) * a.nb;
@@ -118,10 +119,11 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     }
     const float vinv = 1.f / vref;
     auto scale_of = [&](int slice) {
-        const int key = slice * kSlice + (lane & 3) * 8;
+        const int key = slice * kSlice + (lane & 1) * 16;
         if (key >= L) return 0.f;                       // (what stands there was never written)
-        const float x = scales[key >> a.shift] * (lane & 4 ? vinv : a.c);
-        return lane & 4 || x != 0.f ? x : 1.17549435e-38f;      // masked scores are -inf times this
+        const float x = scales[key >> a.shift] * (lane & 6 ? vinv : a.c);
+        if (lane & 4) return lg2(x);
+        return lane & 2 || x != 0.f ? x : 1.17549435e-38f;      // masked scores are -inf times this
     };
     float next_scale = mine > 0 ? scale_of(first) : 0.f;
 
@@ -145,12 +147,13 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 qf[rb][s][2 + u] = __byte_perm(w.x, w.y, 0x7632);
             }
         }
-    float o[RB][NO][4], m[RB][2], l[RB][2];
+    // m: the scores' reference, which l is relative to; w: that of scores plus log2 of their value's scale, which o is relative to
+    float o[RB][NO][4], m[RB][2], w[RB][2], l[RB][2];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
 #pragma unroll
         for (int n = 0; n < NO; ++n) o[rb][n][0] = o[rb][n][1] = o[rb][n][2] = o[rb][n][3] = 0.f;
-        m[rb][0] = m[rb][1] = -INFINITY;
+        m[rb][0] = m[rb][1] = w[rb][0] = w[rb][1] = -INFINITY;
         l[rb][0] = l[rb][1] = 0.f;
     }
     const uint32_t f16_codes = a.f16_codes, bf16_codes = a.bf16_codes;
@@ -187,15 +190,16 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             }
         }
         const int left = L - slice * kSlice;
-        float vn[4];
+        float vn[2], vlog[2];
 #pragma unroll
-        for (int nt = 0; nt < 4; ++nt) {
-            const float ks = __shfl_sync(0xffffffffu, sc, nt);
-            vn[nt] = __shfl_sync(0xffffffffu, sc, 4 + nt);
+        for (int i = 0; i < 2; ++i) {
+            const float ks = __shfl_sync(0xffffffffu, sc, i);
+            vn[i] = __shfl_sync(0xffffffffu, sc, 2 + i);
+            vlog[i] = __shfl_sync(0xffffffffu, sc, 4 + i);
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[rb][nt][e] *= ks;
+                for (int e = 0; e < 8; ++e) s[rb][2 * i + e / 4][e % 4] *= ks;
         }
         if (left < kSlice) {
 #pragma unroll
@@ -206,20 +210,21 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                     for (int e = 0; e < 4; ++e)
                         if (nt * 8 + 2 * t + (e & 1) >= left) s[rb][nt][e] = -INFINITY;
         }
-        // the reference of a row is raised, and what has been summed rescaled, only when its maximum grew by 2^kRaise
+        // a reference of a row is raised, and what has been summed rescaled, only when its maximum grew by 2^kRaise (which one of the row's lanes sees)
         bool higher = false;
-        float top[RB][2];
+        auto maxima = [&](int rb, int u, float& x, float& y) {
+            auto of16 = [&](int i) { return fmaxf(max3(s[rb][2 * i][2 * u], s[rb][2 * i][2 * u + 1], s[rb][2 * i + 1][2 * u]), s[rb][2 * i + 1][2 * u + 1]); };
+            const float x0 = of16(0), x1 = of16(1);
+            x = fmaxf(x0, x1);
+            y = fmaxf(x0 + vlog[0], x1 + vlog[1]);
+        };
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                float x = fmaxf(s[rb][0][2 * u], s[rb][0][2 * u + 1]);
-#pragma unroll
-                for (int nt = 1; nt < 4; ++nt) x = max3(x, s[rb][nt][2 * u], s[rb][nt][2 * u + 1]);
-                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-                x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-                top[rb][u] = x;
-                higher |= x > m[rb][u] + kRaise;
+                float x, y;
+                maxima(rb, u, x, y);
+                higher |= x > m[rb][u] + kRaise || y > w[rb][u] + kRaise;
             }
         if (__any_sync(0xffffffffu, higher)) {
 #pragma unroll
@@ -227,10 +232,20 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                 float f[2];
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const bool raise = top[rb][u] > m[rb][u] + kRaise;
-                    f[u] = raise ? ex2(m[rb][u] - top[rb][u]) : 1.f;
-                    if (raise) m[rb][u] = top[rb][u];
-                    l[rb][u] *= f[u];
+                    float x, y;
+                    maxima(rb, u, x, y);
+#pragma unroll
+                    for (int i = 1; i < 4; i *= 2) {
+                        x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, i));
+                        y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, i));
+                    }
+                    if (x > m[rb][u] + kRaise) {
+                        l[rb][u] *= ex2(m[rb][u] - x);
+                        m[rb][u] = x;
+                    }
+                    y = fmaxf(y > w[rb][u] + kRaise ? y : w[rb][u], m[rb][u] - kFar);
+                    f[u] = y == w[rb][u] ? 1.f : ex2(w[rb][u] - y);
+                    w[rb][u] = y;
                 }
 #pragma unroll
                 for (int n = 0; n < NO; ++n) { o[rb][n][0] *= f[0]; o[rb][n][1] *= f[0]; o[rb][n][2] *= f[1]; o[rb][n][3] *= f[1]; }
@@ -240,13 +255,20 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
 #pragma unroll
         for (int rb = 0; rb < RB; ++rb) {
             const float base[2] = {m[rb][0] == -INFINITY ? 0.f : m[rb][0] - kRoom, m[rb][1] == -INFINITY ? 0.f : m[rb][1] - kRoom};
+            float vg[2][2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const float gain = ex2(fminf(m[rb][u] - w[rb][u], kFar));
+                vg[u][0] = vn[0] * gain;
+                vg[u][1] = vn[1] * gain;
+            }
 #pragma unroll
             for (int nt = 0; nt < 4; ++nt) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float p = ex2(s[rb][nt][e] - base[e >> 1]);
                     l[rb][e >> 1] += p;
-                    s[rb][nt][e] = p * vn[nt];
+                    s[rb][nt][e] = p * vg[e >> 1][nt >> 1];
                 }
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
@@ -302,6 +324,7 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
             sum += __shfl_xor_sync(0xffffffffu, sum, 1);
             sum += __shfl_xor_sync(0xffffffffu, sum, 2);
             const int r = warp * 16 + g + 8 * u;
+            const float by = m[rb][u] == -INFINITY ? 1.f : ex2(w[rb][u] - m[rb][u]);      // outputs relative to m and vref, as the other warps'
             if (t == 0) { sm[r] = m[rb][u]; sl[r] = sum; }
             // column 2 t + e of tile n is dimension (2 t + e) * NO + n
 #pragma unroll
@@ -309,7 +332,7 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
 #pragma unroll
                 for (int n = 0; n < NO; n += 4)
                     *reinterpret_cast<float4*>(&so[r * OLD + (2 * t + e) * NO + n]) =
-                        make_float4(o[rb][n][2 * u + e], o[rb][n + 1][2 * u + e], o[rb][n + 2][2 * u + e], o[rb][n + 3][2 * u + e]);
+                        make_float4(o[rb][n][2 * u + e] * by, o[rb][n + 1][2 * u + e] * by, o[rb][n + 2][2 * u + e] * by, o[rb][n + 3][2 * u + e] * by);
         }
         __syncthreads();
         const int x = threadIdx.x >> 3, part = threadIdx.x & 7, r = r0 + rb * 16 + x;

@@ -24,6 +24,12 @@ __device__ __forceinline__ uint32_t codes_bf16(uint32_t x, uint32_t pattern) {
     return r;
 }
 
+// Kernels whose time is instructions keep one reference for a row while no value scale at hand is below kNear of the largest.
+constexpr float kNear = 1.f / 16.f;
+// How far (log2) a row's reference of weight times value scale (relative to the largest scale at hand) may lie below that of its weights: the factor between
+// the two, and weights times it, stay inside fp32's range.
+constexpr float kFar = 110.f;
+
 struct PrefixQ8 {
     const int8_t *k, *v;             // codes
     const float *k_scale, *v_scale;  // [B, Hkv, ceil(P / block)]

@@ -5,11 +5,14 @@
 // TMA brings tiles of 128 keys in codes (16 KB) into a small ring; six warps widen them into a second ring of 16-bit tiles in the
 // swizzled layout that the products read.  Codes are exact in 16 bits, so nothing is rounded there: keys become the queries' type, values
 // fp16.  The keys' scale of each 16 columns is the factor of their scores in the exponent (in place of the one factor of the 16-bit kernel),
-// the values' scale multiplies the weights, which go to the product in fp16, relative to the largest value scale of the CTA's keys and up to 2^15.
+// the values' scale multiplies the weights, and these products go to tensor memory in fp16, up to 2^15 relative to a reference of the row's own (w) beside
+// the one of its weights (m): a row may attend to none of the blocks whose values are large.  That is a product's maximum per 16 columns and 8 factors more
+// a tile, 1.4% of the time below.
 // Keys past the end are masked in the scores; their codes are finite, so their weights of 0 need no further care.
 //
 // Where the prefix is not split, the drafts' own 16-bit keys follow it as further tiles, as there: TMA brings them into the wide ring
-// directly, and before a stream's first of them its output is multiplied by the reference of the value scales, so that both kinds add up.
+// directly, and before a stream's first of them its output is multiplied by the reference of the value scales, so that both kinds add up.  The own
+// weights of bf16 are kept below 1 (kOwnRoom), or sums of large values would leave fp32's range where their mean does not.
 //
 // Where the keys are split over up to eight CTAs, these are a cluster and join their results themselves: the own tiles are dealt out to
 // them, each leaves its outputs, maxima and sums in its shared memory, and each reads and writes a share of the rows.  Nothing goes through
@@ -31,6 +34,7 @@ constexpr int kQThreads = 512;              // warps 0-3, 4-7: softmax of stream
 constexpr int kWideners = 192;
 constexpr float kRaise = 8.0f;              // growth of a row's maximum (log2) that triggers a rescale
 constexpr float kHalfRoom = 7.0f;           // how far (log2) the reference is set below the maximum: weights go up to 2^15
+constexpr float kOwnRoom = -8.0f;           // the same for the own keys of bf16: weights up to 1
 constexpr int kMaxSorted = 128;             // sequences that are put in order of length
 constexpr int kBarBytes = 1024;
 constexpr int kParts = 16;                  // results of a row that a cluster joins, at most
@@ -403,13 +407,14 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         const uint32_t t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
         float m = 0.f, l = 0.f;          // reference (in the exponent's units) and sum relative to it
+        float w = -INFINITY;             // reference of weight times value scale, which the output is relative to (own keys: m)
         bool fresh = true;               // no score seen yet
         bool ok = true;
         const int n = s ? nt1 : nt0, np = s ? np1 : np0, first_tile = s ? t01 : t00;
         const int my_tok = (qt0 + (shared_keys ? s : 0)) * a.tq + row / a.G;                     // this row's token of the sequence,
         const int my_node = a.fused ? my_tok / a.M : 0, my_i = a.fused ? my_tok % a.M : 0;       // its draft and place in it
         // Scales of a tile: lane i holds the keys' of columns 16 i .., lane 8 + i the values', relative to the largest of this stream's
-        // keys.  They are loaded a round ahead.
+        // keys, lane 16 + i their logarithms.  They are loaded a round ahead.
         const float* ks = a.k_scale + ((int64_t)b * a.Hkv + h) * a.nb;
         const float* vs = a.v_scale + ((int64_t)b * a.Hkv + h) * a.nb;
         float vref = 1.17549435e-38f;
@@ -424,7 +429,8 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
             if (j >= np) return lane & 8 ? 1.f : a.c;       // own keys
             const int key = (first_tile + j) * 128 + (lane & 7) * 16;
             if (key >= L) return 0.f;                   // (what stands there was never written)
-            const float x = lane & 8 ? vs[key >> a.shift] * vinv : ks[key >> a.shift] * a.c;
+            const float x = lane & 24 ? vs[key >> a.shift] * vinv : ks[key >> a.shift] * a.c;
+            if (lane & 16) return lg2(x);
             return lane & 8 || x != 0.f ? x : 1.17549435e-38f;      // masked scores are -inf times this
         };
         float next_scale = n > 0 ? scale_of(0) : 0.f;
@@ -465,7 +471,7 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     for (int i = 0; i < 32; ++i)
                         if (c * 32 + i >= lim) r[c][i] = 0xff800000u;
             }
-            float high = -INFINITY;
+            float high = -INFINITY, high_w = -INFINITY;
 #pragma unroll
             for (int g = 0; g < 8; ++g) {
                 auto x = [&](int i) { return __uint_as_float(r[g >> 1][(g & 1) * 16 + i]); };
@@ -474,19 +480,28 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 for (int i = 3; i < 15; i += 2) u = max3(u, x(i), x(i + 1));
                 u = fmaxf(u, x(15));
                 // (columns past the end have the scale 0 where their 16 hold no key: -inf * 0 is no number and drops out)
-                high = fmaxf(high, u * __shfl_sync(0xffffffffu, sc, g));
+                u *= __shfl_sync(0xffffffffu, sc, g);
+                high = fmaxf(high, u);
+                high_w = fmaxf(high_w, u + __shfl_sync(0xffffffffu, sc, 16 + g));
             }
-            // the reference that this tile's maximum asks for
-            const float top = high - kHalfRoom;
+            // the references that this tile's maxima ask for
+            const float top = high - (BF16 && own_tile ? kOwnRoom : kHalfRoom);
             const bool raise = top > (fresh ? -INFINITY : m + kRaise);
+            const float top_w = high_w - kHalfRoom;
+            const bool raise_w = !own_tile && top_w > w + kRaise;
             const bool unit = own_tile && j == np && j > 0;        // from here on outputs are relative to 1, not to vref
-            if (unit || __any_sync(0xffffffffu, raise)) {
-                const bool rescale = raise && !fresh;
-                float f = rescale ? ex2(m - top) : 1.f;
-                if (raise) { m = top; fresh = false; }
-                l *= f;
-                if (unit) f *= vref;
-                if (unit || __any_sync(0xffffffffu, rescale))
+            if (unit || __any_sync(0xffffffffu, raise || raise_w)) {
+                const float m0 = m, w0 = w;
+                float f = 1.f;
+                if (raise) m = top;
+                if (unit && BF16 && !fresh) m = fmaxf(m, m0 + (kHalfRoom - kOwnRoom));
+                w = own_tile ? m : fmaxf(raise_w ? top_w : w, m - kFar);
+                if (!fresh) {
+                    l *= ex2(m0 - m);
+                    f = unit ? times_ex2(vref, w0 - w) : ex2(w0 - w);
+                }
+                fresh = fresh && !raise;
+                if (__any_sync(0xffffffffu, f != 1.f))
 #pragma unroll 1
                 for (int c = 0; c < a.Dh; c += 8) {
                     uint32_t o[8];
@@ -515,6 +530,7 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             }
             const f32x2 nm = pack2(-m, -m);
+            const float gain = ex2(fminf(m - w, kFar));
             f32x2 acc[2] = {0ull, 0ull};
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
@@ -522,7 +538,7 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
                     float kf = __shfl_sync(0xffffffffu, sc, 2 * c + g);
-                    const float vf = __shfl_sync(0xffffffffu, sc, 8 + 2 * c + g);
+                    const float vf = __shfl_sync(0xffffffffu, sc, 8 + 2 * c + g) * gain;
                     if (!FULL && kf == 0.f) kf = 1.f;      // no key among these 16: their scores are -inf
                     const f32x2 kk = pack2(kf, kf), vv = pack2(vf, vf);
 #pragma unroll
@@ -555,13 +571,15 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         for (const int n_full = min(np, L / 128 - first_tile); ok && j < n_full; ++j) ok = tile(j, std::true_type());
 #pragma unroll 1
         for (; ok && j < n; ++j) ok = tile(j, std::false_type());
+        const float out_unit = np < n ? 1.f : times_ex2(vref, w - m);       // of the outputs
         if (joined) {
-            // outputs (of a row: 16-byte pieces, rotated by the row so that a quarter of a warp writes all banks) and (reference, sum)
+            // outputs by the sum of weights (of a row: 16-byte pieces, rotated by the row so that a quarter of a warp writes all banks) and (reference, sum)
             // into the ring, which is free once both streams' products are done
             for (int x = 0; ok && x < 2; ++x)
                 if ((x ? nt1 : nt0) > 0) ok = mbar_wait_warp(&o_done[x], 0, wc);
             tc_fence_after();
-            const float u = np < n ? 1.f : vref;
+            const bool none = n == 0 || (fresh && l == 0.f);
+            const float u = none ? 0.f : out_unit / l;
             const uint32_t to = smem_u32(ring) + (s * 128 + row) * DHP * 4;
 #pragma unroll 1
             for (int c = 0; ok && n > 0 && c < a.Dh; c += 32) {
@@ -573,7 +591,7 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + ((((c + i) / 4) ^ (row & 7)) << 4)), "f"(__uint_as_float(x[i]) * u),
                                  "f"(__uint_as_float(x[i + 1]) * u), "f"(__uint_as_float(x[i + 2]) * u), "f"(__uint_as_float(x[i + 3]) * u) : "memory");
             }
-            reinterpret_cast<float2*>(raw)[s * 128 + row] = n == 0 || (fresh && l == 0.f) ? make_float2(-INFINITY, 0.f) : make_float2(m, l);
+            reinterpret_cast<float2*>(raw)[s * 128 + row] = none ? make_float2(-INFINITY, 0.f) : make_float2(m, l);
         } else if (s < n_streams) {
             const bool live = row < a.tq * a.G && my_tok < a.T;
             if (n > 0 && ok) {
@@ -581,7 +599,7 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 tc_fence_after();
             }
             const bool none = fresh && l == 0.f;             // no key seen
-            const float inv = none ? 0.f : (np < n ? 1.f : vref) / l;
+            const float inv = none ? 0.f : out_unit / l;
             const int64_t tok = (int64_t)b * a.T + my_tok;
             const int head = h * a.G + row % a.G;
             if (ok && a.fused) {
@@ -665,8 +683,8 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                 for (int q = 0; q < kParts; ++q)
                     if (mm[q] != -INFINITY) {                                    // (others hold no outputs)
                         some = true;
-                        mm[q] = ex2(mm[q] - base);
-                        sum = fmaf(mm[q], ll[q], sum);
+                        mm[q] = ex2(mm[q] - base) * ll[q];
+                        sum += mm[q];
                     } else {
                         mm[q] = 0.f;
                     }
