@@ -43,7 +43,10 @@ struct OwnTile { int node, key0, len; };    // a tile of own keys: draft of the 
 
 // Tiles in flight: codes (RAW; with a single query tile the other's memory holds as many again, since a cache that is read for few rows comes from
 // HBM at the rate that the copies in flight allow) and widened ones.
-template <int SLABS> struct Rings { static constexpr int RAW = SLABS == 2 ? 2 : 8, MOST = SLABS == 2 ? 4 : 8, WIDE = SLABS == 2 ? 4 : 8; };
+template <int SLABS> struct Rings {
+    static constexpr int RAW = SLABS == 2 ? 2 : 8, MOST = SLABS == 2 ? 4 : 8, WIDE = SLABS == 2 ? 4 : 8;
+    static_assert(MOST < 2 * WIDE, "the loader is less than two items of a wide slot ahead of the widening");
+};
 
 struct TcArgs {
     const float *k_scale, *v_scale;
@@ -284,6 +287,9 @@ prefix_tiles_q8_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
                     ++in;
                 } else {
                     const int slot = item % NS;
+                    // The slot's last item must have come and gone.  Up to here this warp has only seen the codes' ring, which lets it be two items of a
+                    // slot ahead of the widening; a wait by parity tells one from the other only once the slot's last item is known to be there.
+                    if (item >= NS && !mbar_wait_warp(&full[slot], ((item / NS) & 1) ^ 1, wc)) { ok = false; break; }
                     if (!mbar_wait_warp(&empty[slot], ((item / NS) & 1) ^ 1, wc)) { ok = false; break; }
                     if (leader) {
                         const OwnTile o = own[s * kMaxOwnTiles + j - np];
