@@ -782,8 +782,16 @@ _pack_rotate = struct.Struct("=8i2f12q").pack
 _pack_quantize = struct.Struct("=8i12q").pack
 
 
+def _fits(*sizes):
+    """Sizes that go to the library as 32-bit arguments: ctypes would pass on their low bits."""
+    for n in sizes:
+        if not -2 ** 31 <= n < 2 ** 31:
+            raise ValueError(f"psd binding: {n} does not fit into 32 bits")
+
+
 def psd_rope_frequencies(rotary, base=10000.0, kind=PSD_ROPE_PLAIN, factor=1.0, original=0.0, low=1.0, high=32.0):
     """(frequencies [rotary/2] float64 on the CPU, the gain that goes with them) for psd_rotate_qk."""
+    _fits(int(rotary), int(kind))
     table, gain = torch.empty(max(int(rotary) // 2, 1), dtype=_F64), _f32(1.0)
     _check(LIB.psd_rope_frequencies(int(rotary), float(base), int(kind), float(factor), float(original), float(low), float(high),
                                     table.data_ptr(), ctypes.byref(gain)), "psd_rope_frequencies")
@@ -850,6 +858,7 @@ def psd_quantize_rows(x, codes, scale, stream=None):
     R, H = x.shape
     if codes.shape != x.shape or codes.dtype is not _I8 or (x.stride(1) != 1 or codes.stride(1) != 1) and H > 1:
         raise ValueError("psd binding: x [R, H] and codes [R, H] int8 need a dense last dimension")
+    _fits(H)
     stream = _here(stream, x, codes, scale)
     _check(LIB.psd_quantize_rows(x.data_ptr(), _DTYPES.get(x.dtype, -1), x.stride(0) if R > 1 else H, R, H, codes.data_ptr(),
                                  codes.stride(0) if R > 1 else H, _want(scale, (R,), _F32, "scale"), stream), "psd_quantize_rows")
@@ -874,11 +883,13 @@ def psd_prefix_quantize(k, v, k_codes, v_codes, k_scale, v_scale, block=32, begi
 
 
 def psd_attention_q8_workspace_bytes(B, D, M, Hq, Hkv, Dh, P, S) -> int:
+    _fits(B, D, M, Hq, Hkv, Dh, P, S)
     return int(LIB.psd_attention_q8_workspace_bytes(B, D, M, Hq, Hkv, Dh, P, S))
 
 
 def psd_attention_q8_kernel_names(B, D, M, Hq, Hkv, Dh, P, S):
     """(names of the kernels that psd_draft_attention_q8 launches at these sizes, partial results per row), or None."""
+    _fits(B, D, M, Hq, Hkv, Dh, P, S)
     splits = _i32(0)
     names = LIB.psd_attention_q8_kernel_names(B, D, M, Hq, Hkv, Dh, P, S, ctypes.byref(splits))
     return None if names is None else (names.decode(), splits.value)
@@ -904,6 +915,7 @@ def psd_draft_attention_q8(q, k_codes, v_codes, k_scale, v_scale, out, lse=None,
         raise ValueError("psd binding: k_codes and v_codes are int8 of one shape")
     if out.shape != rows or (k_own is None) != (v_own is None) or block < 1:
         raise ValueError("psd binding: out and q have one shape, k_own and v_own come together, block is positive")
+    _fits(block)
     S, ko, vo, own = 0, None, None, _NO_CACHE
     if k_own is not None:
         shape = k_own.shape
@@ -927,6 +939,7 @@ def psd_draft_attention_q8(q, k_codes, v_codes, k_scale, v_scale, out, lse=None,
 
 
 def psd_confidence_q8_workspace_bytes(n_rows: int, H: int, V: int) -> int:
+    _fits(n_rows, H, V)
     return int(LIB.psd_confidence_q8_workspace_bytes(n_rows, H, V))
 
 
@@ -937,6 +950,7 @@ def psd_confidence_q8(hidden, w_codes, w_scale, out_token, out_conf, out_lse=Non
     V = w_codes.shape[0]
     if not hidden.is_contiguous():
         raise ValueError("psd binding: hidden must be contiguous")
+    _fits(R, H, V)
     stream = _here(stream, hidden, w_codes, w_scale, out_token, out_conf, out_lse, workspace, status)
     ws, ws_bytes = _space(workspace)
     _check(LIB.psd_confidence_q8(hidden.data_ptr(), _DTYPES.get(hidden.dtype, -1), _want(w_codes, (V, H), _I8, "w_codes"),
