@@ -445,6 +445,9 @@ int launch_confidence_q8(const int8_t* x, const float* x_scale, const int8_t* w,
     choose_order(g, n_rows, (H + 1) / 2, V, BLOCK_M, band_bytes(), tile_order());     // (rows of H bytes)
     // Rows that fit a band are read once in either order; in this one they are carried over the vocabulary.
     if (g.n_mt == 1 || (tile_order() == 0 && (long long)g.n_mt * BLOCK_M * H <= band_bytes())) { g.row_bands = 1; g.band = g.n_mt; }
+    const int n_tiles = g.n_mt * g.n_vt, grid = n_tiles < sms ? n_tiles : sms;
+    // (the height that such bands get: looked for once here, it is at hand for each thread that asks)
+    if (g.row_bands) g.band = band_height(grid, g.band, g.band);
     const int wide_rows = (g.rem ? g.base_units + 1 : g.base_units) * 16;
     const int narrow_rows = g.base_units > 0 ? g.base_units * 16 : wide_rows;
     CUtensorMap map_a, map_bw, map_bn;
@@ -453,7 +456,6 @@ int launch_confidence_q8(const int8_t* x, const float* x_scale, const int8_t* w,
     if (!make_codes_map(&map_a, x, (n_rows + BLOCK_M - 1) / BLOCK_M * BLOCK_M, H, BLOCK_M) || !make_codes_map(&map_bw, w, V, H, wide_rows) ||
         !make_codes_map(&map_bn, w, V, H, narrow_rows))
         return PSD_ERR_CUDA;
-    const int n_tiles = g.n_mt * g.n_vt, grid = n_tiles < sms ? n_tiles : sms;
     int most_splits = 0;
     for (int m0 = 0; m0 < g.n_mt;) {
         const int h = band_height(grid, g.band, g.n_mt - m0);
