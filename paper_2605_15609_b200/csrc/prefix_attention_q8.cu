@@ -37,7 +37,7 @@ struct Q8Args {
     float *po, *pl;
     int32_t* status_dev;
     int64_t rows, q_token, q_head;   // rows: B * D * M * Hq
-    int T, G, Hq, Hkv, Dh, P, nb, shift, units, splits;
+    int T, G, Hq, Hkv, Dh, P, nb, shift, splits;
     int k_outer, k_head, v_outer, v_head;
     int B, longest_first;            // longest_first: CTAs take the sequences by falling length
     float c;                         // scale * log2 e
@@ -75,7 +75,7 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    const int unit = blockIdx.x % a.units, rest = blockIdx.x / a.units, cs = rest % a.splits, bh = rest / a.splits;
+    const int cs = blockIdx.x % a.splits, bh = blockIdx.x / a.splits;
     const int h = bh % a.Hkv;
     int b = bh / a.Hkv;
     if (a.longest_first) {
@@ -128,13 +128,13 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
     float next_scale = mine > 0 ? scale_of(first) : 0.f;
 
     // queries: in step s of the product over dimensions this thread's share is 4 neighbouring ones from `base(s)`
-    const int rows = a.T * a.G, r0 = unit * 16 * RB;
+    const int rows = a.T * a.G;                          // 16 RB at most
     uint32_t qf[RB][KS][4];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int r = r0 + rb * 16 + g + 8 * u;
+            const int r = rb * 16 + g + 8 * u;
             const bool live = r < rows;
             const int64_t tok = (int64_t)b * a.T + (live ? r / a.G : 0);
             const uint16_t* q = reinterpret_cast<const uint16_t*>(a.q) + tok * a.q_token + (int64_t)(h * a.G + (live ? r % a.G : 0)) * a.q_head;
@@ -335,7 +335,7 @@ prefix_rows_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_co
                         make_float4(o[rb][n][2 * u + e] * by, o[rb][n + 1][2 * u + e] * by, o[rb][n + 2][2 * u + e] * by, o[rb][n + 3][2 * u + e] * by);
         }
         __syncthreads();
-        const int x = threadIdx.x >> 3, part = threadIdx.x & 7, r = r0 + rb * 16 + x;
+        const int x = threadIdx.x >> 3, part = threadIdx.x & 7, r = rb * 16 + x;
         if (r < rows && ok) {
             float top = -INFINITY, sum = 0.f, f[4];
 #pragma unroll
@@ -442,8 +442,7 @@ PrefixQ8Plan plan_prefix_q8(int B, int D, int M, int Hq, int Hkv, int Dh, int P,
         return p;
     }
     p.row_blocks = rows > 16 ? 2 : 1;
-    p.units = (int)((rows + 16 * p.row_blocks - 1) / (16 * p.row_blocks));
-    const int64_t ctas = (int64_t)B * Hkv * p.units, slots = (int64_t)sm_count() * (p.row_blocks == 1 ? 3 : 2);
+    const int64_t ctas = (int64_t)B * Hkv, slots = (int64_t)sm_count() * (p.row_blocks == 1 ? 3 : 2);
     int64_t s = (int64_t)(std::sqrt((double)P * slots / (ctas * kCost)) + 0.5);
     if (s < slots / ctas) s = slots / ctas;
     if (s > (P + kLeast - 1) / kLeast) s = (P + kLeast - 1) / kLeast;
@@ -466,7 +465,7 @@ size_t prefix_q8_needs(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int 
 size_t prefix_q8_workspace(int B, int D, int M, int Hq, int Hkv, int Dh, int P) {
     const int64_t rows = (int64_t)B * D * M * Hq, T = (int64_t)D * M, G = Hq / Hkv, tq = 128 / G, sms = sm_count();
     const int64_t pairs = 2 * (int64_t)B * Hq * (T < tq ? T : tq);
-    const double few = 2.0 * B * Hkv;                               // CTAs of the few-rows kernel along rows, at most
+    const double few = 2.0 * B * Hkv;                               // the few-rows kernel's CTAs ahead of the splits, twice over
     int64_t n = (rows > pairs ? rows : pairs) + 256 * sms + (int64_t)(32.0 * (std::sqrt(3.0 * sms * few * P / kCost) + few));
     int64_t most = ((int64_t)P + 255) / 256;
     if (most > kMaxPrefixSplits) most = kMaxPrefixSplits;
@@ -483,7 +482,7 @@ int launch_prefix_attention_q8(const void* q, const PrefixQ8& c, const int32_t* 
     CUtensorMap mk, mv;
     if (!make_codes_map(&mk, c.k, a.kp, a.B, a.P, a.Hkv, a.Dh, p.dhp, kSlice) || !make_codes_map(&mv, c.v, a.vp, a.B, a.P, a.Hkv, a.Dh, p.dhp, kSlice))
         return PSD_ERR_CUDA;
-    const int64_t grid = (int64_t)a.B * a.Hkv * p.units * p.splits;
+    const int64_t grid = (int64_t)a.B * a.Hkv * p.splits;
     if (grid > INT32_MAX) return PSD_ERR_SHAPE;
     Q8Args x = {};
     x.q = q;
@@ -496,7 +495,7 @@ int launch_prefix_attention_q8(const void* q, const PrefixQ8& c, const int32_t* 
     x.T = a.D * a.M; x.G = a.Hq / a.Hkv; x.Hq = a.Hq; x.Hkv = a.Hkv; x.Dh = a.Dh; x.P = a.P;
     x.nb = (a.P + c.block - 1) / c.block;
     x.shift = c.block == 16 ? 4 : c.block == 32 ? 5 : c.block == 64 ? 6 : 7;
-    x.units = p.units; x.splits = p.splits;
+    x.splits = p.splits;
     x.k_outer = a.kp.outer ? 1 : 0; x.k_head = a.kp.head ? 1 : 0;
     x.v_outer = a.vp.outer ? 1 : 0; x.v_head = a.vp.head ? 1 : 0;
     x.B = a.B;

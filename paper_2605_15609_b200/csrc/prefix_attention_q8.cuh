@@ -44,11 +44,10 @@ bool one_launch_codes(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S
 // Which kernel takes the prefix, and how its work is cut.
 struct PrefixQ8Plan {
     bool one;           // draft_attention_kernel walks it (final outputs); else:
-    bool tiles;         // prefix_tiles_q8_kernel (tcgen05), cut as `tile` says; else prefix_rows_q8_kernel: row_blocks, units
+    bool tiles;         // prefix_tiles_q8_kernel (tcgen05), cut as `tile` says; else prefix_rows_q8_kernel: row_blocks
     bool joined;        // ..with splits that a cluster joins
     bool final;         // the kernel takes the own keys too and writes final outputs; else partial results
     int row_blocks;     // 16-row blocks of a warp: 1 or 2
-    int units;          // CTAs along the rows of a key head
     PrefixPlan tile;
     int splits;         // partial results per row
     int dhp;            // floats per partial output row: 64 or 128
