@@ -654,7 +654,9 @@ int psd_confidence_logits(const void* logits, int32_t dtype, int64_t row_stride,
 #define PSD_ROPE_LINEAR 1    /* f[j] / factor                                                                         */
 #define PSD_ROPE_STRETCHED 2 /* base * factor^(rotary / (rotary - 2)) in place of base (rotary > 2)                   */
 #define PSD_ROPE_BY_PARTS 3  /* with n = original * f[j] / 2 pi turns over the original context and
-                                w = clamp((n - low) / (high - low), 0, 1):  w * f[j] + (1 - w) * f[j] / factor        */
+                                w = clamp((n - low) / (high - low), 0, 1):  w * f[j] + (1 - w) * f[j] / factor
+                                (the ramp is linear in the turns n, not in the index j, and comes with a gain above 1:
+                                a model whose ramp or gain differ needs a table or a gain of its own)                 */
 
 /*
  * psd_rope_frequencies — the table that psd_rotate_qk reads, computed on the host in 64 bits.

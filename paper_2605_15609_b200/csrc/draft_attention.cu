@@ -577,13 +577,11 @@ const char* draft_attention_kernels(int B, int D, int M, int Hq, int Hkv, int Dh
 }
 
 // Whether this kernel walks a prefix in codes too: while it is short (a tile takes 1.6 us of a CTA, 0.8 with heads of 64, and more the more CTAs share an
-// SM), against what else there is: two launches for few rows of a key head, else the tcgen05 kernel.  Measured in us, this against that, 32 heads of 128 over
-// 8 where nothing else is said.  One token, prefix 64: 6.3, 8.4; 128: 7.9, 8.6; 257: 12.4, 10.6; 16 tokens, 128: 8.4, 10.2; 257: 13.0, 12.3; 64 tokens, 64:
-// 13.6, 18.1.  4 drafts of 32 tokens, 64: 9.4, 13.0; 257: 17.0, 17.2; 768: 31.1, 22.5; the same of 4 heads of 64, 257: 9.1, 15.3; 512: 11.5, 14.9; 1024:
-// 18.1, 17.2.  8 x 8 drafts of 4 tokens, 16 heads over 2, 64: 9.2, 20.4; 257: 17.0, 24.5; 512: 22.8, 20.2.  16 x 2 drafts of 8 tokens, 28 heads over 4, 64:
-// 16.9, 19.6; 128: 20.9, 17.9.  32 heads of 64 over 8, 16 x one token, 257: 7.9, 9.3; 512: 10.4, 10.0; 64 x one token, 64: 9.8, 9.6; 128: 12.0, 10.5.
+// SM), against what else there is: two launches for few rows of a key head, else the tcgen05 kernel.  Measured in us, this against that, 32 heads of 128 over 8:
+// one token, prefix 128: 8.1, 8.4; 257: 13.0, 10.7; 4 drafts of 32 tokens, 64: 9.7, 13.1; 257: 17.7, 17.5; 768: 32.2, 23.0.
 // Beyond four CTAs per SM (drafts in the hundreds over a few keys) the forms' times follow their waves of CTAs, and the lower estimate wins: fitted to
-// 240 drawn shapes of up to 700 keys, 5 to 250 us, which each estimate meets within 15%; by it 25.1 us on average (geometric), always the better form 24.8.
+// 240 drawn shapes of up to 700 keys, 5 to 250 us, which each estimate meets within 15%.  Over 81 other shapes the rule takes 12.8 us on average (geometric),
+// always the better form 12.7.
 bool one_launch_codes(int B, int D, int M, int Hq, int Hkv, int Dh, int P, int S) {
     const PrefixPlan plan = plan_prefix(B, D, M, Hq, Hkv, Dh, P, S);
     const int rows = M * (Hq / Hkv), sms = sm_count(), steps = (P + kKeys - 1) / kKeys, own = (S + kKeys - 1) / kKeys;

@@ -15,8 +15,9 @@
 // laid out to match), and for the values the bytes of four keys at 16 neighbouring dimensions, which are paired key by key.
 //
 // Bound for few rows: the cache's bytes, 2 Dh per key; widening takes 3 to 4 instructions for two codes, about 40% of the issue
-// slots that the bytes' time offers.  Measured, single tokens of 32 heads of 128 over 8: 64 sequences of 16384 keys 343-359 us, 6.0-6.3 TB/s of
-// codes and scales; of 3300 to 16384 keys 234-240 us, 5.6-5.7 TB/s; 32 sequences x 5 tokens (20 rows) 201-207 us, 3.0 TB/s (issue slots).
+// slots that the bytes' time offers.  Measured, single tokens of 32 heads of 128 over 8: 64 sequences of 16384 keys 363-381 us, 5.9 TB/s of
+// codes and scales; of 3300 to 16384 keys 233-244 us, 5.6-5.7 TB/s; 32 sequences x 5 tokens (20 rows) 197-211 us, 2.7 TB/s (two CTAs per SM, whose
+// warps' chains use 38% of the issue slots).
 #include <cmath>
 #include "attn_tc.cuh"
 #include "prefix_attention_q8.cuh"

@@ -7,7 +7,7 @@
 // fp16.  The keys' scale of each 16 columns is the factor of their scores in the exponent (in place of the one factor of the 16-bit kernel),
 // the values' scale multiplies the weights, and these products go to tensor memory in fp16, up to 2^15 relative to a reference of the row's own (w) beside
 // the one of its weights (m): a row may attend to none of the blocks whose values are large.  That is a product's maximum per 16 columns and 8 factors more
-// a tile, 1.4% of the time below.
+// a tile, 2% of the time below.
 // Keys past the end are masked in the scores; their codes are finite, so their weights of 0 need no further care.
 //
 // Where the prefix is not split, the drafts' own 16-bit keys follow it as further tiles, as there: TMA brings them into the wide ring
@@ -20,7 +20,7 @@
 //
 // Bound: for Dh = 128 products and exponentials as there (2048 cycles each per 256 rows x 128 keys), in the latency chain of scores, softmax
 // and products; widening takes about 650 issue slots per scheduler of the same round, the values' scales 64 more per warp.  Measured: 16 sequences x 8 key
-// heads x 2048 rows over up to 8192 keys (the seed's 667 GFLOP) 757-770 us, 0.87 PFLOP/s (16-bit cache: 665 us; without widening 690).  The
+// heads x 2048 rows over up to 8192 keys (the seed's 667 GFLOP) 759-790 us, 0.85-0.88 PFLOP/s (16-bit cache: 665 us; without widening, and with one reference a row, 690).  The
 // instruction cache is the next bound: with full and last tiles in one piece of straight code beside unrolled widening and issuing
 // the same call took 1064 us.
 #include "attn_tc.cuh"
